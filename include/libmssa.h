@@ -455,6 +455,144 @@ mssa_status mssa_forward_head_ring(mssa_plan plan, const void* q_win, const void
  * (spare + F) mod ring_frames. */
 mssa_status mssa_head_ring_roll(mssa_plan plan, int32_t ring_frames, int32_t* ring_count, int32_t* ring_spare);
 
+/* ------------------------------------------------------- low-bit layers
+ * The steps of a transformer layer around and inside its attention with
+ * activations in 8 bits and weights and K/V history in 4 bits: the
+ * residual's addition with the root-mean-square norm (and its backward),
+ * quantisation to MXFP4, the product with MXFP4 weights, and the attention
+ * over an MXFP4 cache.  They need no plan; the conventions above hold
+ * (caller-owned device memory, caller's stream, no synchronisation, fixed
+ * reduction orders), with these formats besides:
+ *   - MXFP4: a row of `cols` values is cut into blocks of 32; block b holds
+ *     one scale byte E (the power of two 2^(E - 127); E = 255 makes the block
+ *     NaN) and 32 e2m1 codes (bit 3 the sign, magnitudes 0, 0.5, 1, 1.5, 2,
+ *     3, 4, 6).  With NB = ceil(cols / 32) a row's codes are 16 NB bytes,
+ *     value 2 i in the low half of byte i, and its scales NB bytes; the
+ *     codes past `cols` in the last block are zeros.  Rows follow one another
+ *     without gaps.  Code and scale arrays are 16-byte aligned.
+ *   - 8-bit rows: OCP e4m3 codes, 32 NB bytes a row (zeros past `cols`),
+ *     with one fp32 scale a row that multiplies them. */
+typedef enum {
+  MSSA_E4M3 = 2, /* 8-bit rows, one fp32 scale each */
+  MSSA_MXFP4 = 3 /* 4-bit values, one power-of-two scale per 32 */
+} mssa_lowbit_format;
+
+/* Rows of the norm.  Strides are in elements between rows, 0 = cols; x and
+ * the residual need element alignment only (rows cut out of a wider tensor),
+ * every other tensor is contiguous. */
+typedef struct {
+  int64_t rows;            /* >= 0 */
+  int32_t cols;            /* 1..32768 */
+  int32_t dtype;           /* mssa_dtype of x, residual, weight, sum and the gradients */
+  int32_t out_dtype;       /* of y: dtype, or MSSA_E4M3 */
+  float eps;               /* finite, >= 0 */
+  int64_t x_stride, residual_stride, sum_stride;
+} mssa_norm_desc;
+
+/* s = x + residual, rounded once to dtype; y = s * weight / sqrt(mean(s^2) +
+ * eps) per row, the mean and the product in fp32 on the rounded s (what the
+ * residual stream keeps and the backward sees), y rounded once.
+ *   residual   may be NULL: s = x, and sum must be NULL too
+ *   sum        s; may be x or residual itself (same stride)
+ *   weight     [cols]
+ *   y          [rows, cols] in dtype, or 8-bit rows with y_scale[row] =
+ *              max(max |y|, 2^-100) / 448: the row's largest value becomes
+ *              +-448, codes rounded to nearest even from the fp32 product.  A
+ *              NaN or an infinity in a row makes its scale NaN or infinite.
+ *   y_scale    [rows] fp32 for MSSA_E4M3, else NULL
+ *   rstd       [rows] fp32, 1 / sqrt(mean(s^2) + eps), or NULL */
+mssa_status mssa_add_rms_norm(const mssa_norm_desc* desc, const void* x, const void* residual, const void* weight,
+                              void* sum, void* y, float* y_scale, float* rstd, void* stream);
+
+/* Device workspace bytes of mssa_add_rms_norm_backward. */
+mssa_status mssa_add_rms_norm_workspace_size(const mssa_norm_desc* desc, int64_t* bytes);
+
+/* Gradients of mssa_add_rms_norm, with s the forward's sum (its x where there
+ * was no residual; rows sum_stride apart), rstd its rstd, dy the gradient of y
+ * (an 8-bit y passes it straight through) and dsum the gradient that reaches s
+ * along the residual stream (or NULL):
+ *   dx = dsum + rstd (w dy - s rstd^2 mean(w dy s)), the gradient of x and of
+ *        the residual alike; [rows, cols], may be dy or dsum itself
+ *   dweight = sum over rows of dy s rstd, fp32 [cols] (zeros for no rows)
+ * desc->out_dtype, x_stride and residual_stride are not used. */
+mssa_status mssa_add_rms_norm_backward(const mssa_norm_desc* desc, const void* sum, const void* weight,
+                                       const float* rstd, const void* dy, const void* dsum, void* workspace,
+                                       int64_t workspace_bytes, void* dx, float* dweight, void* stream);
+
+/* Rows of values (dtype MSSA_BF16 or MSSA_F32, x_stride elements apart, 0 =
+ * cols, element aligned) to MXFP4.  A block's exponent is floor(log2 max|x|)
+ * - 2, at least -127, so that its largest value lands in [4, 8) and saturates
+ * at 6; values round to nearest, ties to the even code.  A block of zeros has
+ * scale byte 0; a block that holds an infinity or a NaN has 255 and zero
+ * codes.  Rows of K or V are (token, head) pairs with cols = head_dim. */
+mssa_status mssa_mx_quantize(int64_t rows, int32_t cols, int32_t dtype, const void* x, int64_t x_stride, void* codes,
+                             void* scales, void* stream);
+
+/* The values that MXFP4 rows stand for, in dtype (bf16 holds them exactly
+ * down to its smallest normal power of two; a product past the type's range
+ * is infinite). */
+mssa_status mssa_mx_dequantize(int64_t rows, int32_t cols, int32_t dtype, const void* codes, const void* scales,
+                               void* y, int64_t y_stride, void* stream);
+
+/* Y = X W^T + bias with MXFP4 weights. */
+typedef struct {
+  int64_t rows;           /* tokens, 0..2^30 */
+  int32_t in_features;    /* 1..2^20 */
+  int32_t out_features;   /* 1..2^20, a multiple of parts */
+  int32_t parts;          /* 1..8: the features' columns are split evenly over so many outputs (3: q, k, v) */
+  int32_t x_format;       /* MSSA_E4M3 or MSSA_MXFP4 */
+  int32_t out_dtype;      /* mssa_dtype of bias and outputs */
+  float part0_scale;      /* finite; multiplies part 0 (bias included), 1 to leave it */
+} mssa_mx_project_desc;
+
+/* y[p][row, n] = sum_k x[row, k] w[p * N + n, k] + bias, N = out_features /
+ * parts, fp32 accumulation, rounded once.
+ *   x, x_scales  tokens as 8-bit rows with fp32 scales [rows], or as MXFP4
+ *                with scale bytes [rows, ceil(in_features / 32)]
+ *   w, w_scales  MXFP4 rows, one per output feature
+ *   bias         [out_features], or NULL
+ *   y            host array of `parts` device pointers, each [rows, N]
+ * With part0_scale = softmax_scale * log2(e) part 0 is the queries of a
+ * MSSA_PLAN_Q_PRESCALED plan.  Outputs must not alias the inputs. */
+mssa_status mssa_mx_project(const mssa_mx_project_desc* desc, const void* x, const void* x_scales, const void* w,
+                            const void* w_scales, const void* bias, void* const* y, void* stream);
+
+/* Attention over K/V caches held in MXFP4. */
+typedef struct {
+  int32_t batch;          /* >= 1 */
+  int32_t n_q;            /* queries per sequence, >= 1 */
+  int32_t q_heads;        /* a multiple of kv_heads: query head h reads key head h / (q_heads / kv_heads) */
+  int32_t kv_heads;       /* >= 1 */
+  int32_t head_dim;       /* 64 or 128 */
+  int64_t cache_tokens;   /* capacity of each sequence's cache, 1..2^31 - 1 */
+  int64_t lse_stride;     /* floats between the heads of lse, 0 = n_q */
+  float softmax_scale;    /* <= 0 selects 1/sqrt(head_dim) */
+} mssa_mx_attention_desc;
+
+/* Device workspace bytes of mssa_mx_attention. */
+mssa_status mssa_mx_attention_workspace_size(const mssa_mx_attention_desc* desc, int64_t* bytes);
+
+/* out = softmax(scale q k^T) v over the first kv_len[b] tokens of sequence
+ * b's cache, joined with an earlier result over other keys of the same
+ * queries if one is given.
+ *   q, out       [batch, n_q, q_heads, head_dim] bf16
+ *   k/v_codes    [batch, cache_tokens, kv_heads, head_dim / 2] bytes
+ *   k/v_scales   [batch, cache_tokens, kv_heads, head_dim / 32] bytes
+ *   kv_len       [batch] int32 on the device, clamped to [0, cache_tokens];
+ *                NULL: the whole cache.  Tokens past it are not used, whatever
+ *                they hold.
+ *   prior_out, prior_lse  an attention output over other keys and its log
+ *                sum of exponentials (mssa_forward_lse's, or this function's):
+ *                the result is the softmax over both sets of keys.  Both or
+ *                neither; they may be out and lse themselves.
+ *   lse          [batch, q_heads, n_q] (lse_stride) natural log of the sum of
+ *                exp(scale q k) over all keys, or NULL
+ * A query with no keys at all has out = 0 and lse = -inf. */
+mssa_status mssa_mx_attention(const mssa_mx_attention_desc* desc, const void* q, const void* k_codes,
+                              const void* k_scales, const void* v_codes, const void* v_scales, const int32_t* kv_len,
+                              const void* prior_out, const float* prior_lse, void* workspace,
+                              int64_t workspace_bytes, void* out, float* lse, void* stream);
+
 /* Name of a status code (static string). */
 const char* mssa_status_string(mssa_status s);
 

@@ -14,6 +14,7 @@
 #include <vector>
 
 #include "../../include/libmssa.h"
+#include "abi_status.hpp"
 #include "kernels.hpp"
 #include "noalloc.hpp"
 #include "plan.hpp"
@@ -28,6 +29,10 @@ namespace {
 // failure never allocates, so it cannot throw.
 thread_local char g_last_error[512] = "";
 
+}  // namespace
+
+namespace mssa {
+
 mssa_status fail(mssa_status s, const char* msg) noexcept {
   std::snprintf(g_last_error, sizeof g_last_error, "%s", msg);
   return s;
@@ -38,20 +43,14 @@ mssa_status fail(mssa_status s, const char* what, const char* detail) noexcept {
   return s;
 }
 
-// Body of an entry point: no C++ exception leaves the library.  A failed
-// host allocation is MSSA_ERR_NO_MEMORY, anything else MSSA_ERR_INVALID_ARG.
-template <class Body>
-mssa_status guarded(const char* where, Body&& body) noexcept {
-  try {
-    return body();
-  } catch (const std::bad_alloc&) {
-    return fail(MSSA_ERR_NO_MEMORY, where, "host allocation failed");
-  } catch (...) {
-    return fail(MSSA_ERR_INVALID_ARG, where, "unexpected internal error");
-  }
-}
+}  // namespace mssa
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+namespace {
+
+using mssa::aligned16;
+using mssa::check_device;
+using mssa::fail;
+using mssa::guarded;
 
 // Attention blocks resident at once on the current device (CUs x blocks per
 // CU), or 0 when there is no usable device (the plan then assumes 512).
@@ -64,11 +63,6 @@ int resident_attention_blocks(int head_dim) {
   }
   const int per_cu = mssa::forward_blocks_per_cu(head_dim);
   return per_cu > 0 ? cus * per_cu : 0;
-}
-
-mssa_status check_device(hipError_t e, const char* what) {
-  if (e == hipSuccess) return MSSA_OK;
-  return fail(MSSA_ERR_DEVICE, what, hipGetErrorString(e));
 }
 
 // Launch pool jobs (source and destination pointers filled in), at most

@@ -1,0 +1,90 @@
+// Kernel arguments and launchers of the low-bit layers (norm, MXFP4
+// quantisation, product with MXFP4 weights, attention over an MXFP4 cache).
+#pragma once
+
+#include <hip/hip_runtime_api.h>
+
+#include <cstdint>
+
+namespace mssa {
+
+constexpr int kMxBlock = 32;  // values under one MXFP4 scale
+
+inline int64_t mx_blocks(int64_t cols) { return (cols + kMxBlock - 1) / kMxBlock; }
+
+// ------------------------------------------------------------------- norm
+constexpr int kNormMaxCols = 32768;
+
+struct NormArgs {
+  const void *x, *residual, *weight;
+  void *sum, *y;
+  float *y_scale, *rstd;
+  int64_t rows, x_stride, residual_stride, sum_stride;
+  int32_t cols, y_pitch;  // y_pitch: elements between rows of y
+  float eps, inv_cols;
+};
+
+struct NormBwdArgs {
+  const void *sum, *weight, *dy, *dsum;
+  const float* rstd;
+  void* dx;
+  float *dweight, *partial;  // partial: [blocks, cols], null with one block
+  int64_t rows, sum_stride;
+  int32_t cols, blocks;
+  float inv_cols;
+};
+
+hipError_t launch_norm(const NormArgs& a, bool bf16, bool e4m3, hipStream_t stream);
+// Blocks of the backward's first launch: a static rule on the sizes.
+int32_t norm_bwd_blocks(int64_t rows, int32_t cols);
+hipError_t launch_norm_bwd(const NormBwdArgs& a, bool bf16, hipStream_t stream);
+
+// ------------------------------------------------------------- conversion
+struct MxArgs {
+  const void* in;
+  void *codes, *scales, *out;
+  int64_t rows, stride;  // stride: elements between rows of the values
+  int32_t cols, blocks;  // blocks of 32 a row
+};
+
+hipError_t launch_mx_quantize(const MxArgs& a, bool bf16, hipStream_t stream);    // in -> codes, scales
+hipError_t launch_mx_dequantize(const MxArgs& a, bool bf16, hipStream_t stream);  // codes, scales -> out
+
+// ---------------------------------------------------------------- product
+constexpr int kMaxParts = 8;
+
+struct ProjectArgs {
+  const void *x, *xs, *w, *ws, *bias;
+  void* y[kMaxParts];
+  int32_t M, N, NB;  // tokens, features, blocks of 32 along the contraction
+  int32_t split;     // features of a part
+  float part0_scale;
+};
+
+hipError_t launch_mx_project(const ProjectArgs& a, bool x_fp4, bool out_bf16, hipStream_t stream);
+
+// -------------------------------------------------------------- attention
+struct MxAttnArgs {
+  const void *q, *kc, *ks, *vc, *vs, *prior_out;
+  const int32_t* kv_len;
+  const float* prior_lse;
+  void* out;
+  float *lse, *partial;
+  int64_t cache_tokens, lse_stride;
+  int32_t batch, n_q, q_heads, kv_heads, group;  // group = q_heads / kv_heads
+  int32_t rows;    // n_q * group: query rows that share a key head
+  int32_t splits;  // pieces of the context, each a block
+  float scale_log2e;
+};
+
+// How a call is cut: rows of a block and pieces of the context.
+struct MxAttnPlan {
+  int32_t waves, splits;
+  int64_t items;           // blocks per piece of the context
+  int64_t workspace_bytes;
+};
+MxAttnPlan plan_mx_attention(int32_t batch, int32_t n_q, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
+                             int64_t cache_tokens);
+hipError_t launch_mx_attention(const MxAttnArgs& a, const MxAttnPlan& plan, int head_dim, hipStream_t stream);
+
+}  // namespace mssa

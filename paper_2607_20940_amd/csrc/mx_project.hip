@@ -1,0 +1,458 @@
+// Y = X W^T + b with MXFP4 weights (mssa_mx_project): tokens in 8 bits with
+// one fp32 scale each (applied to the fp32 sum), or in MXFP4.
+//
+// The block-scaled matrix instructions take both operands as they lie in
+// memory: a lane holds the 32 values of one MXFP4 block (16 bytes) and the
+// block's scale byte; e4m3 operands are 16-byte pieces of two such blocks.  The contraction runs over blocks in
+// any order as long as both operands take the same one, so the two lane
+// halves take the first and the second half of a stage's blocks and each
+// lane's scales of a stage are consecutive bytes.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "lds_stage.hpp"
+#include "lowbit_args.hpp"
+#include "xcd.hpp"
+
+namespace mssa {
+namespace {
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr int kFmtE4M3 = 0, kFmtE2M1 = 4;  // operand formats of the f8f6f4 instructions
+constexpr uint32_t kPastEnd = 0xfffffff0u;  // a buffer offset outside every range
+
+// bf16 outputs take the f8f6f4 instructions for 8-bit tokens too.  Inside one
+// of those steps the matrix core aligns e4m3 products to the largest of them
+// with fewer bits than fp32 has: up to 2^-12 of the sum of magnitudes was
+// measured on codes of every size, 6e-6 of the result's norm on ordinary
+// tokens, far below the output's own rounding.  fp32 outputs of 8-bit tokens
+// are asked for to be more exact than that: both operands are expanded to
+// bf16, which holds them exactly, and multiplied with fp32 sums, at less than
+// half the rate.  (e2m1 by e2m1 steps add exactly enough for both.)
+template <bool XF4, class T>
+constexpr bool kWide = !XF4 && std::is_same_v<T, float>;
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+// Eight consecutive values of an MXFP4 block, or of e4m3, in bf16.
+__device__ inline bf16x8 expand4(uint32_t codes, float scale) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0);
+  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2);
+  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+__device__ inline bf16x8 expand8(uint32_t lo, uint32_t hi) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false);
+  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false);
+  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+__device__ inline float mx_scale(uint32_t e) {
+  return __builtin_bit_cast(float, e == 255 ? 0x7fc00000u : e == 0 ? 0x00400000u : e << 23);
+}
+
+__device__ inline i32x8 widen(i32x4 v) { return i32x8{v[0], v[1], v[2], v[3], 0, 0, 0, 0}; }
+
+// n consecutive features' outputs of one token, from feature col on.
+template <class T, int N>
+__device__ inline void store_features(const ProjectArgs& a, int64_t row, int col, const float (&v)[N]) {
+  const T* bias = static_cast<const T*>(a.bias);
+  const int part = col / a.split, pc = col - part * a.split;
+  if ((a.split & 3) == 0 && col + N <= a.N) {
+    typedef T vec __attribute__((ext_vector_type(N)));
+    vec u;
+    const float f = part == 0 ? a.part0_scale : 1.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) u[i] = static_cast<T>((v[i] + (bias ? static_cast<float>(bias[col + i]) : 0.f)) * f);
+    *reinterpret_cast<vec*>(static_cast<T*>(a.y[part]) + row * a.split + pc) = u;
+    return;
+  }
+  for (int i = 0; i < N && col + i < a.N; ++i) {
+    const int p = (col + i) / a.split, c = col + i - p * a.split;
+    static_cast<T*>(a.y[p])[row * a.split + c] =
+        static_cast<T>((v[i] + (bias ? static_cast<float>(bias[col + i]) : 0.f)) * (p == 0 ? a.part0_scale : 1.f));
+  }
+}
+
+// Tiles.  A block of WM x WN waves owns BM tokens x BN features; the matrix
+// instruction computes the transposed tile (A = W rows, B = X rows), so a
+// lane holds one token and runs of four features.  A stage is 128 bytes of
+// every token (four blocks of e4m3, eight of MXFP4) and as many blocks of
+// every feature, moved by direct global -> LDS transfers into the buffer that
+// is not being multiplied.
+template <bool XF4, int BM, int BN, int WM, int WN>
+struct TileShape {
+  static constexpr int kThreads = WM * WN * 64;
+  static constexpr int NBK = XF4 ? 8 : 4;          // blocks a stage
+  static constexpr int NS = NBK / 2;               // matrix steps a stage
+  static constexpr int XB = 128, WB = NBK * 16;    // bytes of a row a stage
+  static constexpr int kXBytes = BM * XB, kWBytes = BN * WB;
+  static constexpr int kSRows = (XF4 ? BM : 0) + BN;
+  static constexpr int kStage = kXBytes + kWBytes + kSRows * NBK;
+};
+
+template <bool XF4, class T, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(WM* WN * 64) void tile_kernel(ProjectArgs a) {
+  using S = TileShape<XF4, BM, BN, WM, WN>;
+  constexpr int NBK = S::NBK, NS = S::NS, XB = S::XB, WB = S::WB;
+  constexpr int TM = BM / WM / 32, TN = BN / WN / 32, kWaves = WM * WN;
+  constexpr int NX = S::kXBytes / 1024 / kWaves, NW = S::kWBytes / 1024 / kWaves;
+  static_assert(NX * 1024 * kWaves == S::kXBytes && NW * 1024 * kWaves == S::kWBytes, "whole transfers");
+  __shared__ __attribute__((aligned(16))) char lds[2][S::kStage];
+
+  const int tiles_m = (a.M + BM - 1) / BM;
+  const int L = xcd_remap(blockIdx.x, gridDim.x);
+  const int tm = L % tiles_m, tn = L / tiles_m;
+  const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, hh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave % WM, wn = wave / WM;
+  const int mrows = min(BM, a.M - tm * BM), nrows = min(BN, a.N - tn * BN);
+  const uint32_t xp = static_cast<uint32_t>(a.NB) * (XF4 ? 16 : 32), wp = static_cast<uint32_t>(a.NB) * 16;
+  const char* X = static_cast<const char*>(a.x) + static_cast<int64_t>(tm) * BM * xp;
+  const char* W = static_cast<const char*>(a.w) + static_cast<int64_t>(tn) * BN * wp;
+  const uint8_t* XS = XF4 ? static_cast<const uint8_t*>(a.xs) + static_cast<int64_t>(tm) * BM * a.NB : nullptr;
+  const uint8_t* WS = static_cast<const uint8_t*>(a.ws) + static_cast<int64_t>(tn) * BN * a.NB;
+
+  // Transfer i of a wave fills 1 KB of consecutive LDS: 128-byte rows hold
+  // eight 16-byte chunks, 64-byte rows four, swizzled so that sixteen rows
+  // read at one chunk hit distinct banks.
+  uint32_t xo[NX], wo[NW];
+  int xb[NX], wb[NW];  // the block a lane's chunk belongs to, within the stage
+#pragma unroll
+  for (int i = 0; i < NX; ++i) {
+    const int p = (wave * NX + i) * 1024 + 16 * lane, row = p / XB, lc = unswz128(row, (p / 16) & 7);
+    xo[i] = row * xp + lc * 16;
+    xb[i] = XF4 ? lc : lc / 2;
+  }
+#pragma unroll
+  for (int i = 0; i < NW; ++i) {
+    const int p = (wave * NW + i) * 1024 + 16 * lane, row = p / WB;
+    const int lc = XF4 ? unswz128(row, (p / 16) & 7) : ((p / 16) & 3) ^ ((row >> 2) & 3);
+    wo[i] = row * wp + lc * 16;
+    wb[i] = lc;
+  }
+  const i32x4 rx = rsrc_of(X, static_cast<uint32_t>(mrows) * xp);
+  const i32x4 rw = rsrc_of(W, static_cast<uint32_t>(nrows) * wp);
+  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(&lds[0][0]));
+  auto issue = [&](int st, int s) {
+    const uint32_t base = lds0 + s * S::kStage;
+    const int left = a.NB - st * NBK;
+#pragma unroll
+    for (int i = 0; i < NX; ++i)
+      dma16(rx, xb[i] < left ? xo[i] + st * XB : kPastEnd, __builtin_amdgcn_readfirstlane(base + (wave * NX + i) * 1024));
+#pragma unroll
+    for (int i = 0; i < NW; ++i)
+      dma16(rw, wb[i] < left ? wo[i] + st * WB : kPastEnd,
+            __builtin_amdgcn_readfirstlane(base + S::kXBytes + (wave * NW + i) * 1024));
+  };
+  // Scale bytes of a stage, one row per thread and pass, through registers:
+  // rows past the tile and blocks past the row are zeros (their codes are).
+  constexpr int NSC = (S::kSRows + S::kThreads - 1) / S::kThreads;
+  uint64_t sc[NSC];
+  auto load_scales = [&](int st) {
+    const int left = a.NB - st * NBK;
+#pragma unroll
+    for (int i = 0; i < NSC; ++i) {
+      const int r = tid + i * S::kThreads;
+      const bool is_x = XF4 && r < BM;
+      const int rr = XF4 && !is_x ? r - BM : r;
+      const uint8_t* p = (is_x ? XS : WS) + static_cast<int64_t>(rr) * a.NB + st * NBK;
+      sc[i] = 0;
+      if (r < S::kSRows && rr < (is_x ? mrows : nrows)) {
+        if (left >= NBK) {
+          if constexpr (NBK == 8) {
+            typedef uint64_t u64_u __attribute__((aligned(1)));
+            sc[i] = *reinterpret_cast<const u64_u*>(p);
+          } else {
+            typedef uint32_t u32_u __attribute__((aligned(1)));
+            sc[i] = *reinterpret_cast<const u32_u*>(p);
+          }
+        } else {
+          for (int b = 0; b < left; ++b) sc[i] |= static_cast<uint64_t>(p[b]) << (8 * b);
+        }
+      }
+    }
+  };
+  auto store_scales = [&](int s) {
+    char* p = lds[s] + S::kXBytes + S::kWBytes;
+#pragma unroll
+    for (int i = 0; i < NSC; ++i) {
+      const int r = tid + i * S::kThreads;
+      if (r >= S::kSRows) continue;
+      if constexpr (NBK == 8)
+        *reinterpret_cast<uint64_t*>(p + r * 8) = sc[i];
+      else
+        *reinterpret_cast<uint32_t*>(p + r * 4) = static_cast<uint32_t>(sc[i]);
+    }
+  };
+  // The scales of one row's blocks hh * NS ..: byte j is matrix step j's.
+  auto scale_of = [&](const char* st, int r) -> int {
+    const char* p = st + S::kXBytes + S::kWBytes + r * NBK;
+    if constexpr (NBK == 8)
+      return *reinterpret_cast<const int*>(p + 4 * hh);
+    else
+      return *reinterpret_cast<const uint16_t*>(p + 2 * hh);
+  };
+
+  f32x16 acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j) acc[i][j] = f32x16{};
+
+  const int nst = (a.NB + NBK - 1) / NBK;
+  load_scales(0);
+  store_scales(0);
+  issue(0, 0);
+  wait_vmcnt<0>();
+  __syncthreads();
+  for (int st = 0; st < nst; ++st) {
+    const char* B = lds[st & 1];
+    const bool more = st + 1 < nst;
+    if (more) {
+      load_scales(st + 1);
+      issue(st + 1, (st + 1) & 1);
+    }
+    int sx[TM], sw[TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i) sx[i] = XF4 ? scale_of(B, (wm * TM + i) * 32 + n32) : 0x7f7f7f7f;
+#pragma unroll
+    for (int j = 0; j < TN; ++j) sw[j] = scale_of(B, (XF4 ? BM : 0) + (wn * TN + j) * 32 + n32);
+    auto step = [&](auto js) {
+      constexpr int J = decltype(js)::value;
+      if constexpr (kWide<XF4, T>) {
+        // lane half hh's block hh * NS + J, eight values at a time
+        const int c = hh * NS + J;
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+          bf16x8 xw[TM], ww[TN];
+#pragma unroll
+          for (int i = 0; i < TM; ++i) {
+            const int row = (wm * TM + i) * 32 + n32;
+            const uint2 v = *reinterpret_cast<const uint2*>(B + row * XB + (((2 * c + (p >> 1)) ^ ((row >> 1) & 7)) << 4) + (p & 1) * 8);
+            xw[i] = expand8(v.x, v.y);
+          }
+#pragma unroll
+          for (int j = 0; j < TN; ++j) {
+            const int row = (wn * TN + j) * 32 + n32;
+            const uint32_t v = *reinterpret_cast<const uint32_t*>(B + S::kXBytes + row * WB + ((c ^ ((row >> 2) & 3)) << 4) + p * 4);
+            ww[j] = expand4(v, mx_scale((static_cast<uint32_t>(sw[j]) >> (8 * J)) & 255u));
+          }
+#pragma unroll
+          for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ww[j], xw[i], acc[i][j], 0, 0, 0);
+        }
+        return;
+      }
+      i32x8 xv[TM], wv[TN];
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        const int row = (wm * TM + i) * 32 + n32, s = (row >> 1) & 7;
+        if constexpr (XF4) {
+          xv[i] = widen(*reinterpret_cast<const i32x4*>(B + row * XB + (((hh * NS + J) ^ s) << 4)));
+        } else {
+          // e4m3: a lane's first 16 bytes are its half's piece of the first
+          // lane half's block, its last 16 bytes of the second's
+          const i32x4 lo = *reinterpret_cast<const i32x4*>(B + row * XB + (((2 * J + hh) ^ s) << 4));
+          const i32x4 hi = *reinterpret_cast<const i32x4*>(B + row * XB + (((2 * (NS + J) + hh) ^ s) << 4));
+          xv[i] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < TN; ++j) {
+        const int row = (wn * TN + j) * 32 + n32, c = hh * NS + J;
+        const int ch = XF4 ? c ^ ((row >> 1) & 7) : c ^ ((row >> 2) & 3);
+        wv[j] = widen(*reinterpret_cast<const i32x4*>(B + S::kXBytes + row * WB + (ch << 4)));
+      }
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wv[j], xv[i], acc[i][j], kFmtE2M1,
+                                                                     XF4 ? kFmtE2M1 : kFmtE4M3, J, sw[j], XF4 ? J : 0, sx[i]);
+    };
+    step(std::integral_constant<int, 0>{});
+    step(std::integral_constant<int, 1>{});
+    if constexpr (NS > 2) {
+      step(std::integral_constant<int, 2>{});
+      step(std::integral_constant<int, 3>{});
+    }
+    if (more) store_scales((st + 1) & 1);
+    wait_vmcnt<0>();
+    __syncthreads();
+  }
+
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const int64_t row = static_cast<int64_t>(tm) * BM + (wm * TM + i) * 32 + n32;
+    if (row >= a.M) continue;
+    const float xs = XF4 ? 1.f : static_cast<const float*>(a.xs)[row];
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int jj = 0; jj < 4; ++jj) {
+        const int col = tn * BN + (wn * TN + j) * 32 + 8 * jj + 4 * hh;
+        if (col >= a.N) continue;
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * jj + e] * xs;
+        store_features<T, 4>(a, row, col, v);
+      }
+  }
+}
+
+// Few tokens: the weights are read once, from memory straight into the
+// matrix instruction's operand (16 features x 128 values, A = W rows); the
+// tokens are the 16 columns of B.  Sixteen features a block, whose waves take
+// pieces of the contraction and join their sums in LDS.  A lane group (lane /
+// 16) takes blocks 4 g .. 4 g + 3 of sixteen, one per matrix step, so its
+// codes are 64 consecutive bytes and its scales four.
+constexpr int kFewWaves = 4;
+
+template <bool XF4, class T, int TT>
+__global__ __launch_bounds__(kFewWaves * 64) void few_kernel(ProjectArgs a) {
+  __shared__ float red[kFewWaves - 1][TT][4][64];
+  const int tid = threadIdx.x, lane = tid & 63, m = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n0 = blockIdx.x * 16;
+  const int64_t xp = static_cast<int64_t>(a.NB) * (XF4 ? 16 : 32);
+  const int feature = min(n0 + m, a.N - 1);
+  const char* W = static_cast<const char*>(a.w) + static_cast<int64_t>(feature) * a.NB * 16;
+  const uint8_t* WS = static_cast<const uint8_t*>(a.ws) + static_cast<int64_t>(feature) * a.NB;
+  f32x4 acc[TT];
+#pragma unroll
+  for (int t = 0; t < TT; ++t) acc[t] = f32x4{};
+
+  const int nsb = (a.NB + 15) / 16;
+  for (int sb = wave; sb < nsb; sb += kFewWaves) {
+    const int b0 = sb * 16 + g * 4, left = a.NB - b0;
+    i32x4 wv[4], xv[TT][4][XF4 ? 1 : 2];
+    uint32_t sw = 0, sx[TT];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) wv[j] = j < left ? *reinterpret_cast<const i32x4*>(W + (b0 + j) * 16) : i32x4{};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sw |= j < left ? static_cast<uint32_t>(WS[b0 + j]) << (8 * j) : 0u;
+#pragma unroll
+    for (int t = 0; t < TT; ++t) {
+      const int64_t tok = t * 16 + m;
+      const bool ok = tok < a.M;
+      const char* X = static_cast<const char*>(a.x) + (ok ? tok : 0) * xp;
+      const uint8_t* XS = static_cast<const uint8_t*>(a.xs) + (ok ? tok : 0) * a.NB;
+      sx[t] = XF4 ? 0u : 0x7f7f7f7fu;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if constexpr (XF4) {
+          const bool in = ok && j < left;
+          xv[t][j][0] = in ? *reinterpret_cast<const i32x4*>(X + (b0 + j) * 16) : i32x4{};
+          sx[t] |= in ? static_cast<uint32_t>(XS[b0 + j]) << (8 * j) : 0u;
+        } else if constexpr (kWide<XF4, T>) {
+          xv[t][j][0] = ok && j < left ? *reinterpret_cast<const i32x4*>(X + (b0 + j) * 32) : i32x4{};
+          xv[t][j][1] = ok && j < left ? *reinterpret_cast<const i32x4*>(X + (b0 + j) * 32 + 16) : i32x4{};
+        } else {
+          // e4m3: 16 bytes of the block of group g / 2, 16 of group 2 + g / 2's
+          const int c0 = sb * 16 + (g >> 1) * 4 + j, c1 = c0 + 8;
+          xv[t][j][0] = ok && c0 < a.NB ? *reinterpret_cast<const i32x4*>(X + c0 * 32 + (g & 1) * 16) : i32x4{};
+          xv[t][j][1] = ok && c1 < a.NB ? *reinterpret_cast<const i32x4*>(X + c1 * 32 + (g & 1) * 16) : i32x4{};
+        }
+      }
+    }
+    auto step = [&](auto js) {
+      constexpr int J = decltype(js)::value;
+      if constexpr (kWide<XF4, T>) {
+        const float f = mx_scale((sw >> (8 * J)) & 255u);
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+          const bf16x8 wa = expand4(static_cast<uint32_t>(wv[J][p]), f);
+#pragma unroll
+          for (int t = 0; t < TT; ++t) {
+            const i32x4 v = xv[t][J][p >> 1];
+            const bf16x8 xw = expand8(static_cast<uint32_t>(v[2 * (p & 1)]), static_cast<uint32_t>(v[2 * (p & 1) + 1]));
+            acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wa, xw, acc[t], 0, 0, 0);
+          }
+        }
+        return;
+      }
+#pragma unroll
+      for (int t = 0; t < TT; ++t) {
+        i32x8 b;
+        if constexpr (XF4)
+          b = widen(xv[t][J][0]);
+        else
+          b = __builtin_shufflevector(xv[t][J][0], xv[t][J][1], 0, 1, 2, 3, 4, 5, 6, 7);
+        acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(widen(wv[J]), b, acc[t], kFmtE2M1, XF4 ? kFmtE2M1 : kFmtE4M3,
+                                                                  J, sw, XF4 ? J : 0, sx[t]);
+      }
+    };
+    step(std::integral_constant<int, 0>{});
+    step(std::integral_constant<int, 1>{});
+    step(std::integral_constant<int, 2>{});
+    step(std::integral_constant<int, 3>{});
+  }
+  if (wave > 0) {
+#pragma unroll
+    for (int t = 0; t < TT; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) red[wave - 1][t][e][lane] = acc[t][e];
+  }
+  __syncthreads();
+  if (wave > 0) return;
+#pragma unroll
+  for (int t = 0; t < TT; ++t) {
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[e] = acc[t][e];
+#pragma unroll
+      for (int w = 0; w < kFewWaves - 1; ++w) v[e] += red[w][t][e][lane];
+    }
+    const int64_t tok = t * 16 + m;
+    const int col = n0 + 4 * g;
+    if (tok >= a.M || col >= a.N) continue;
+    if constexpr (!XF4) {
+      const float xs = static_cast<const float*>(a.xs)[tok];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] *= xs;
+    }
+    store_features<T, 4>(a, tok, col, v);
+  }
+}
+
+template <bool XF4, class T, int TT>
+hipError_t few_go(const ProjectArgs& a, hipStream_t stream) {
+  hipLaunchKernelGGL((few_kernel<XF4, T, TT>), dim3((a.N + 15) / 16), dim3(kFewWaves * 64), 0, stream, a);
+  return hipGetLastError();
+}
+
+template <bool XF4, class T, int BM, int BN, int WM, int WN>
+hipError_t tile_go(const ProjectArgs& a, hipStream_t stream) {
+  const int64_t tiles = static_cast<int64_t>((a.M + BM - 1) / BM) * ((a.N + BN - 1) / BN);
+  if (tiles > 0x7fffffff) return hipErrorInvalidValue;
+  hipLaunchKernelGGL((tile_kernel<XF4, T, BM, BN, WM, WN>), dim3(static_cast<uint32_t>(tiles)), dim3(WM * WN * 64), 0, stream, a);
+  return hipGetLastError();
+}
+
+template <bool XF4, class T>
+hipError_t project(const ProjectArgs& a, hipStream_t stream) {
+  if (a.M <= 16) return few_go<XF4, T, 1>(a, stream);
+  if (a.M <= 32) return few_go<XF4, T, 2>(a, stream);
+  if (static_cast<int64_t>((a.M + 255) / 256) * ((a.N + 255) / 256) >= 256) return tile_go<XF4, T, 256, 256, 2, 4>(a, stream);
+  return tile_go<XF4, T, 128, 128, 2, 2>(a, stream);
+}
+
+}  // namespace
+
+hipError_t launch_mx_project(const ProjectArgs& a, bool x_fp4, bool out_bf16, hipStream_t stream) {
+  if (x_fp4) return out_bf16 ? project<true, __bf16>(a, stream) : project<true, float>(a, stream);
+  return out_bf16 ? project<false, __bf16>(a, stream) : project<false, float>(a, stream);
+}
+
+}  // namespace mssa

@@ -18,6 +18,7 @@ MSSA_MAX_STATES = 8
 MSSA_OK, MSSA_ERR_INVALID_ARG, MSSA_ERR_UNSUPPORTED = 0, 1, 2
 MSSA_ERR_WORKSPACE, MSSA_ERR_DEVICE, MSSA_ERR_NO_MEMORY = 3, 4, 5
 MSSA_BF16, MSSA_F32 = 0, 1
+MSSA_E4M3, MSSA_MXFP4 = 2, 3
 MSSA_PLAN_POOLED_HIST_RING = 1
 MSSA_PLAN_STRIDED_SUBSAMPLE = 2
 MSSA_PLAN_HEAD_IN_RING = 4
@@ -29,13 +30,33 @@ EXPORTS = ("mssa_plan_create", "mssa_plan_create_ex", "mssa_plan_destroy", "mssa
            "mssa_forward_ring", "mssa_hist_append_ring", "mssa_forward_lse", "mssa_backward_workspace_size",
            "mssa_backward", "mssa_tier_workspace_size", "mssa_patch_embed", "mssa_patch_unembed",
            "mssa_qkv_project", "mssa_qkv_project_scaled", "mssa_attention_noalloc", "mssa_pool_kv_head_ring", "mssa_forward_head_ring",
-           "mssa_head_ring_roll", "mssa_status_string", "mssa_last_error")
+           "mssa_head_ring_roll", "mssa_add_rms_norm", "mssa_add_rms_norm_workspace_size",
+           "mssa_add_rms_norm_backward", "mssa_mx_quantize", "mssa_mx_dequantize", "mssa_mx_project",
+           "mssa_mx_attention_workspace_size", "mssa_mx_attention", "mssa_status_string", "mssa_last_error")
 
 MSSA_NOALLOC_SCRATCH_BYTES = 256 << 20
 
 
 class mssa_tier_desc(ctypes.Structure):
     _fields_ = [("latent_channels", ctypes.c_int32), ("patch", ctypes.c_int32), ("hidden", ctypes.c_int32)]
+
+
+class mssa_norm_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("out_dtype", ctypes.c_int32), ("eps", ctypes.c_float), ("x_stride", ctypes.c_int64),
+                ("residual_stride", ctypes.c_int64), ("sum_stride", ctypes.c_int64)]
+
+
+class mssa_mx_project_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("in_features", ctypes.c_int32), ("out_features", ctypes.c_int32),
+                ("parts", ctypes.c_int32), ("x_format", ctypes.c_int32), ("out_dtype", ctypes.c_int32),
+                ("part0_scale", ctypes.c_float)]
+
+
+class mssa_mx_attention_desc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("n_q", ctypes.c_int32), ("q_heads", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("cache_tokens", ctypes.c_int64),
+                ("lse_stride", ctypes.c_int64), ("softmax_scale", ctypes.c_float)]
 
 
 class mssa_plan_desc(ctypes.Structure):
@@ -100,6 +121,15 @@ def _load():
     lib.mssa_patch_unembed.argtypes = [P, TD, V, PP, PP, V, I64, V, V]
     lib.mssa_qkv_project.argtypes = [I64, ctypes.c_int32, V, V, V, V, V, V, V]
     lib.mssa_qkv_project_scaled.argtypes = [I64, ctypes.c_int32, V, V, V, ctypes.c_float, V, V, V, V]
+    ND, PD, AD = (ctypes.POINTER(t) for t in (mssa_norm_desc, mssa_mx_project_desc, mssa_mx_attention_desc))
+    lib.mssa_add_rms_norm.argtypes = [ND, V, V, V, V, V, V, V, V]
+    lib.mssa_add_rms_norm_workspace_size.argtypes = [ND, ctypes.POINTER(I64)]
+    lib.mssa_add_rms_norm_backward.argtypes = [ND, V, V, V, V, V, V, I64, V, V, V]
+    lib.mssa_mx_quantize.argtypes = [I64, I32, I32, V, I64, V, V, V]
+    lib.mssa_mx_dequantize.argtypes = [I64, I32, I32, V, V, V, I64, V]
+    lib.mssa_mx_project.argtypes = [PD, V, V, V, V, V, PP, V]
+    lib.mssa_mx_attention_workspace_size.argtypes = [AD, ctypes.POINTER(I64)]
+    lib.mssa_mx_attention.argtypes = [AD, V, V, V, V, V, V, V, V, V, I64, V, V, V]
     lib.mssa_status_string.argtypes = [ctypes.c_int]
     lib.mssa_status_string.restype = ctypes.c_char_p
     lib.mssa_last_error.argtypes = []
@@ -339,6 +369,93 @@ def mssa_qkv_project_scaled(n_tokens, hidden, x, w_qkv, b_qkv, q_scale, q, k, v,
     _check(lib.mssa_qkv_project_scaled(int(n_tokens), int(hidden), _ptr(x), _ptr(w_qkv), _ptr(b_qkv),
                                        float(q_scale), _ptr(q), _ptr(k), _ptr(v), _stream(stream)),
            "mssa_qkv_project_scaled")
+
+
+_DTYPES = {"bf16": MSSA_BF16, "f32": MSSA_F32, "e4m3": MSSA_E4M3, "mxfp4": MSSA_MXFP4}
+
+
+def _dtype(name):
+    if name in _DTYPES:
+        return _DTYPES[name]
+    if isinstance(name, int):
+        return name
+    raise ValueError(f"unknown type {name!r}: one of {sorted(_DTYPES)}")
+
+
+def norm_desc(rows, cols, dtype="bf16", out=None, eps=1e-6, x_stride=0, residual_stride=0, sum_stride=0):
+    """Descriptor of mssa_add_rms_norm and its backward (out: the type of y,
+    dtype or "e4m3"; strides in elements between rows, 0 = cols)."""
+    return mssa_norm_desc(int(rows), int(cols), _dtype(dtype), _dtype(dtype if out is None else out), float(eps),
+                          int(x_stride), int(residual_stride), int(sum_stride))
+
+
+def mx_project_desc(rows, in_features, out_features, parts=1, x_format="e4m3", out="bf16", part0_scale=1.0):
+    return mssa_mx_project_desc(int(rows), int(in_features), int(out_features), int(parts), _dtype(x_format),
+                                _dtype(out), float(part0_scale))
+
+
+def mx_attention_desc(batch, n_q, q_heads, kv_heads, head_dim, cache_tokens, softmax_scale=0.0, lse_stride=0):
+    return mssa_mx_attention_desc(int(batch), int(n_q), int(q_heads), int(kv_heads), int(head_dim),
+                                  int(cache_tokens), int(lse_stride), float(softmax_scale))
+
+
+def mx_shapes(rows, cols):
+    """Shapes (in bytes) of the codes and scales of `rows` MXFP4 rows of `cols` values."""
+    blocks = -(-int(cols) // 32)
+    return (int(rows), 16 * blocks), (int(rows), blocks)
+
+
+def mssa_add_rms_norm(desc, x, residual, weight, sum_out, y, y_scale=None, rstd=None, stream=None):
+    _check(lib.mssa_add_rms_norm(ctypes.byref(desc), _ptr(x), _ptr(residual), _ptr(weight), _ptr(sum_out), _ptr(y),
+                                 _ptr(y_scale), _ptr(rstd), _stream(stream)), "mssa_add_rms_norm")
+
+
+def mssa_add_rms_norm_workspace_size(desc):
+    n = ctypes.c_int64()
+    _check(lib.mssa_add_rms_norm_workspace_size(ctypes.byref(desc), ctypes.byref(n)),
+           "mssa_add_rms_norm_workspace_size")
+    return n.value
+
+
+def mssa_add_rms_norm_backward(desc, sum_in, weight, rstd, dy, dsum, workspace, dx, dweight, workspace_bytes=None,
+                               stream=None):
+    wb = _nbytes(workspace) if workspace_bytes is None else int(workspace_bytes)
+    _check(lib.mssa_add_rms_norm_backward(ctypes.byref(desc), _ptr(sum_in), _ptr(weight), _ptr(rstd), _ptr(dy),
+                                          _ptr(dsum), _ptr(workspace), wb, _ptr(dx), _ptr(dweight), _stream(stream)),
+           "mssa_add_rms_norm_backward")
+
+
+def mssa_mx_quantize(rows, cols, dtype, x, codes, scales, x_stride=0, stream=None):
+    _check(lib.mssa_mx_quantize(int(rows), int(cols), _dtype(dtype), _ptr(x), int(x_stride), _ptr(codes),
+                                _ptr(scales), _stream(stream)), "mssa_mx_quantize")
+
+
+def mssa_mx_dequantize(rows, cols, dtype, codes, scales, y, y_stride=0, stream=None):
+    _check(lib.mssa_mx_dequantize(int(rows), int(cols), _dtype(dtype), _ptr(codes), _ptr(scales), _ptr(y),
+                                  int(y_stride), _stream(stream)), "mssa_mx_dequantize")
+
+
+def mssa_mx_project(desc, x, x_scales, w, w_scales, bias, y, stream=None):
+    """y: the desc.parts outputs."""
+    if len(y) != desc.parts:
+        raise ValueError("one output per part")
+    _check(lib.mssa_mx_project(ctypes.byref(desc), _ptr(x), _ptr(x_scales), _ptr(w), _ptr(w_scales), _ptr(bias),
+                               _ptr_array(y), _stream(stream)), "mssa_mx_project")
+
+
+def mssa_mx_attention_workspace_size(desc):
+    n = ctypes.c_int64()
+    _check(lib.mssa_mx_attention_workspace_size(ctypes.byref(desc), ctypes.byref(n)),
+           "mssa_mx_attention_workspace_size")
+    return n.value
+
+
+def mssa_mx_attention(desc, q, k_codes, k_scales, v_codes, v_scales, kv_len, prior_out, prior_lse, workspace, out,
+                      lse=None, workspace_bytes=None, stream=None):
+    wb = _nbytes(workspace) if workspace_bytes is None else int(workspace_bytes)
+    _check(lib.mssa_mx_attention(ctypes.byref(desc), _ptr(q), _ptr(k_codes), _ptr(k_scales), _ptr(v_codes),
+                                 _ptr(v_scales), _ptr(kv_len), _ptr(prior_out), _ptr(prior_lse), _ptr(workspace), wb,
+                                 _ptr(out), _ptr(lse), _stream(stream)), "mssa_mx_attention")
 
 
 class HeadRing:
