@@ -92,8 +92,10 @@ mssa_status attention_check(const mssa_mx_attention_desc* d) {
   return MSSA_OK;
 }
 
-mssa::MxAttnPlan plan_of(const mssa_mx_attention_desc* d) {
-  return mssa::plan_mx_attention(d->batch, d->n_q, d->q_heads, d->kv_heads, d->head_dim, d->cache_tokens);
+mssa_status plan_of(const mssa_mx_attention_desc* d, mssa::MxAttnPlan* plan) {
+  if (mssa::plan_mx_attention(d->batch, d->n_q, d->q_heads, d->kv_heads, d->head_dim, d->cache_tokens, plan) != hipSuccess)
+    return fail(MSSA_ERR_UNSUPPORTED, "too many query rows or heads");
+  return MSSA_OK;
 }
 
 }  // namespace
@@ -246,8 +248,10 @@ mssa_status mssa_mx_attention_workspace_size(const mssa_mx_attention_desc* desc,
     const mssa_status s = attention_check(desc);
     if (s != MSSA_OK) return s;
     if (!bytes) return fail(MSSA_ERR_INVALID_ARG, "null argument");
-    *bytes = plan_of(desc).workspace_bytes;
-    return MSSA_OK;
+    mssa::MxAttnPlan plan;
+    const mssa_status planned = plan_of(desc, &plan);
+    if (planned == MSSA_OK) *bytes = plan.workspace_bytes;
+    return planned;
   });
 }
 
@@ -266,7 +270,8 @@ mssa_status mssa_mx_attention(const mssa_mx_attention_desc* desc, const void* q,
     for (const void* t : {static_cast<const void*>(kv_len), static_cast<const void*>(prior_lse), static_cast<const void*>(lse)})
       if (!aligned_to(t, 4)) return fail(MSSA_ERR_INVALID_ARG, "kv_len and lse must be aligned to 4 bytes");
     if (out == q) return fail(MSSA_ERR_INVALID_ARG, "out must not alias q");
-    const mssa::MxAttnPlan plan = plan_of(desc);
+    mssa::MxAttnPlan plan;
+    if (const mssa_status planned = plan_of(desc, &plan); planned != MSSA_OK) return planned;
     if (plan.workspace_bytes > 0) {
       if (!workspace || workspace_bytes < plan.workspace_bytes)
         return fail(MSSA_ERR_WORKSPACE, "workspace smaller than mssa_mx_attention_workspace_size");
@@ -292,7 +297,10 @@ mssa_status mssa_mx_attention(const mssa_mx_attention_desc* desc, const void* q,
     a.kv_heads = desc->kv_heads;
     a.group = desc->q_heads / desc->kv_heads;
     a.rows = desc->n_q * a.group;
-    a.splits = plan.splits;
+    a.items = plan.items;
+    a.workers = plan.workers;
+    a.slot_rows = plan.slot_rows;
+    a.head_waves = plan.head_waves;
     const double scale = desc->softmax_scale > 0.f ? static_cast<double>(desc->softmax_scale)
                                                    : 1.0 / std::sqrt(static_cast<double>(desc->head_dim));
     a.scale_log2e = static_cast<float>(scale * 1.4426950408889634);

@@ -72,19 +72,22 @@ struct MxAttnArgs {
   float *lse, *partial;
   int64_t cache_tokens, lse_stride;
   int32_t batch, n_q, q_heads, kv_heads, group;  // group = q_heads / kv_heads
-  int32_t rows;    // n_q * group: query rows that share a key head
-  int32_t splits;  // pieces of the context, each a block
+  int32_t rows;                                  // n_q * group: query rows that share a key head
+  int32_t items, workers, slot_rows, head_waves;  // of the plan
   float scale_log2e;
 };
 
-// How a call is cut: rows of a block and pieces of the context.
+// How a call is cut (a static rule on the sizes).
 struct MxAttnPlan {
-  int32_t waves, splits;
-  int64_t items;           // blocks per piece of the context
-  int64_t workspace_bytes;
+  int32_t waves;       // 32 rows each in a block; 0: the kernel for few rows
+  int32_t items;       // pieces of work of a sequence that one block at a time takes
+  int32_t workers;     // shares of all items' contexts, 0: a block per item and no joining launch
+  int32_t slot_rows;   // query rows of an item
+  int32_t head_waves;  // few rows: waves of a block on neighbouring key heads
+  int64_t blocks, workspace_bytes;
 };
-MxAttnPlan plan_mx_attention(int32_t batch, int32_t n_q, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
-                             int64_t cache_tokens);
+hipError_t plan_mx_attention(int32_t batch, int32_t n_q, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
+                             int64_t cache_tokens, MxAttnPlan* plan);
 hipError_t launch_mx_attention(const MxAttnArgs& a, const MxAttnPlan& plan, int head_dim, hipStream_t stream);
 
 }  // namespace mssa

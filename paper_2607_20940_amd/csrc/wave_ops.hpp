@@ -38,6 +38,12 @@ __device__ inline float wave_sum(float v) {
   }));
 }
 
+__device__ inline float wave_fmax(float v) {
+  return __builtin_bit_cast(float, wave_reduce(__builtin_bit_cast(uint32_t, v), [](uint32_t a, uint32_t b) {
+    return __builtin_bit_cast(uint32_t, fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b)));
+  }));
+}
+
 __device__ inline uint32_t wave_umax(uint32_t v) {
   return wave_reduce(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
 }
