@@ -84,33 +84,46 @@ __device__ inline void store_features(const ProjectArgs& a, int64_t row, int col
 
 // Tiles.  A block of WM x WN waves owns BM tokens x BN features; the matrix
 // instruction computes the transposed tile (A = W rows, B = X rows), so a
-// lane holds one token and runs of four features.  A stage is 128 bytes of
-// every token (four blocks of e4m3, eight of MXFP4) and as many blocks of
-// every feature, moved by direct global -> LDS transfers into the buffer that
-// is not being multiplied.
+// lane holds one token and runs of four features.  A stage is four blocks (128
+// values) of every token and feature, moved by direct global -> LDS transfers.
+// kBufs - 1 stages are on their way or in LDS ahead of the one that is
+// multiplied: a stage takes the matrix cores half a microsecond, a transfer
+// up to two.  Scale bytes come sixteen to a row, for four stages at once.
 template <bool XF4, int BM, int BN, int WM, int WN>
 struct TileShape {
-  static constexpr int kThreads = WM * WN * 64;
-  static constexpr int NBK = XF4 ? 8 : 4;          // blocks a stage
-  static constexpr int NS = NBK / 2;               // matrix steps a stage
-  static constexpr int XB = 128, WB = NBK * 16;    // bytes of a row a stage
-  static constexpr int kXBytes = BM * XB, kWBytes = BN * WB;
-  static constexpr int kSRows = (XF4 ? BM : 0) + BN;
-  static constexpr int kStage = kXBytes + kWBytes + kSRows * NBK;
+  static constexpr int kThreads = WM * WN * 64, kWaves = WM * WN;
+  static constexpr int NBK = 4, NS = 2;            // blocks and matrix steps a stage
+  static constexpr int kSuper = 4;                 // stages that share a load of scales
+  static constexpr int XB = XF4 ? 64 : 128, WB = 64;  // bytes of a row a stage
+  static constexpr int kBufs = XF4 ? 4 : 3;
+  static constexpr int kXBytes = BM * XB, kWBytes = BN * WB, kStage = kXBytes + kWBytes;
+  static constexpr int kSRows = (XF4 ? BM : 0) + BN, kScales = kSRows * NBK * kSuper;
+  static constexpr int NX = kXBytes / 1024 / kWaves, NW = kWBytes / 1024 / kWaves;  // transfers of a wave a stage
+  static_assert(NX * 1024 * kWaves == kXBytes && NW * 1024 * kWaves == kWBytes, "whole transfers");
+  static_assert(kSRows <= kThreads && kSRows % 64 == 0, "a scale row per thread, whole waves");
+  static_assert(kBufs * kStage + 2 * kScales <= 160 * 1024, "LDS of a CU");
 };
 
-template <bool XF4, class T, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(WM* WN * 64) void tile_kernel(ProjectArgs a) {
-  using S = TileShape<XF4, BM, BN, WM, WN>;
-  constexpr int NBK = S::NBK, NS = S::NS, XB = S::XB, WB = S::WB;
-  constexpr int TM = BM / WM / 32, TN = BN / WN / 32, kWaves = WM * WN;
-  constexpr int NX = S::kXBytes / 1024 / kWaves, NW = S::kWBytes / 1024 / kWaves;
-  static_assert(NX * 1024 * kWaves == S::kXBytes && NW * 1024 * kWaves == S::kWBytes, "whole transfers");
-  __shared__ __attribute__((aligned(16))) char lds[2][S::kStage];
+// Chunk (16 bytes) c of row r lies at chunk c ^ swizzle(r): sixteen rows read
+// at one chunk hit distinct banks.
+template <int ROW>
+__device__ inline int chunk_swizzle(int row) {
+  return ROW == 128 ? (row >> 1) & 7 : (row >> 2) & 3;
+}
 
-  const int tiles_m = (a.M + BM - 1) / BM;
+template <bool XF4, class T, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(WM* WN * 64) __attribute__((amdgpu_waves_per_eu(2))) void tile_kernel(ProjectArgs a) {
+  using S = TileShape<XF4, BM, BN, WM, WN>;
+  constexpr int NBK = S::NBK, NS = S::NS, XB = S::XB, WB = S::WB, NX = S::NX, NW = S::NW;
+  constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
+  __shared__ __attribute__((aligned(16))) char lds[S::kBufs * S::kStage + 2 * S::kScales];
+
+  // Tiles in panels of four feature tiles: the blocks of an XCD, a run of
+  // them, share rows of both operands in its L2.
+  const int tiles_m = (a.M + BM - 1) / BM, tiles_n = (a.N + BN - 1) / BN;
   const int L = xcd_remap(blockIdx.x, gridDim.x);
-  const int tm = L % tiles_m, tn = L / tiles_m;
+  const int panel = L / (tiles_m * 4), in = L - panel * tiles_m * 4, wide = min(4, tiles_n - panel * 4);
+  const int tm = in / wide, tn = panel * 4 + in - tm * wide;
   const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, hh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave % WM, wn = wave / WM;
@@ -118,33 +131,58 @@ __global__ __launch_bounds__(WM* WN * 64) void tile_kernel(ProjectArgs a) {
   const uint32_t xp = static_cast<uint32_t>(a.NB) * (XF4 ? 16 : 32), wp = static_cast<uint32_t>(a.NB) * 16;
   const char* X = static_cast<const char*>(a.x) + static_cast<int64_t>(tm) * BM * xp;
   const char* W = static_cast<const char*>(a.w) + static_cast<int64_t>(tn) * BN * wp;
-  const uint8_t* XS = XF4 ? static_cast<const uint8_t*>(a.xs) + static_cast<int64_t>(tm) * BM * a.NB : nullptr;
-  const uint8_t* WS = static_cast<const uint8_t*>(a.ws) + static_cast<int64_t>(tn) * BN * a.NB;
+  // this thread's (and this wave's) row of scales: X rows first for MXFP4 tokens
+  const bool s_x = XF4 && wave * 64 < BM;
+  const int s_row = XF4 && !s_x ? tid - BM : tid, s_rows = s_x ? mrows : nrows;
+  const uint8_t* SC = s_x ? static_cast<const uint8_t*>(a.xs) + static_cast<int64_t>(tm) * BM * a.NB
+                          : static_cast<const uint8_t*>(a.ws) + static_cast<int64_t>(tn) * BN * a.NB;
+  // Scales go straight to LDS too where sixteen bytes of a row are whole
+  // dwords of it; else through registers.
+  const bool direct = a.NB % 4 == 0 && a.NB >= 16;
 
-  // Transfer i of a wave fills 1 KB of consecutive LDS: 128-byte rows hold
-  // eight 16-byte chunks, 64-byte rows four, swizzled so that sixteen rows
-  // read at one chunk hit distinct banks.
+  // Transfer i of a wave fills 1 KB of consecutive LDS; a lane's 16 bytes are
+  // its physical chunk's.  xb, wb: the block that chunk belongs to in a stage.
   uint32_t xo[NX], wo[NW];
-  int xb[NX], wb[NW];  // the block a lane's chunk belongs to, within the stage
+  int xb[NX], wb[NW];
 #pragma unroll
   for (int i = 0; i < NX; ++i) {
-    const int p = (wave * NX + i) * 1024 + 16 * lane, row = p / XB, lc = unswz128(row, (p / 16) & 7);
+    const int p = (wave * NX + i) * 1024 + 16 * lane, row = p / XB, lc = (p / 16) % (XB / 16) ^ chunk_swizzle<XB>(row);
     xo[i] = row * xp + lc * 16;
     xb[i] = XF4 ? lc : lc / 2;
   }
 #pragma unroll
   for (int i = 0; i < NW; ++i) {
-    const int p = (wave * NW + i) * 1024 + 16 * lane, row = p / WB;
-    const int lc = XF4 ? unswz128(row, (p / 16) & 7) : ((p / 16) & 3) ^ ((row >> 2) & 3);
+    const int p = (wave * NW + i) * 1024 + 16 * lane, row = p / WB, lc = (p / 16) % (WB / 16) ^ chunk_swizzle<WB>(row);
     wo[i] = row * wp + lc * 16;
     wb[i] = lc;
   }
   const i32x4 rx = rsrc_of(X, static_cast<uint32_t>(mrows) * xp);
   const i32x4 rw = rsrc_of(W, static_cast<uint32_t>(nrows) * wp);
-  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(&lds[0][0]));
-  auto issue = [&](int st, int s) {
-    const uint32_t base = lds0 + s * S::kStage;
+  const i32x4 rs = rsrc_of(SC, static_cast<uint32_t>(s_rows) * a.NB);
+  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(&lds[0]));
+  // First block of a group's sixteen scales: the last group ends at the row's end.
+  auto scale_base = [&](int st) { return direct ? min(st / S::kSuper * 16, a.NB - 16) : st / S::kSuper * 16; };
+  // Stage st into its buffer (stages past the last: zeros, which keep the
+  // count of transfers in flight the same).
+  auto issue = [&](int st) {
     const int left = a.NB - st * NBK;
+    if (st % S::kSuper == 0 && left > 0 && wave * 64 < S::kSRows) {
+      const uint32_t dst = S::kBufs * S::kStage + (st / S::kSuper & 1) * S::kScales;
+      const int first = scale_base(st);
+      if (direct) {
+        dma16(rs, s_row < s_rows ? s_row * static_cast<uint32_t>(a.NB) + first : kPastEnd,
+              __builtin_amdgcn_readfirstlane(lds0 + dst + wave * 1024));
+      } else {
+        // rows past the tile and blocks past the row: zeros (their codes are)
+        uint32_t v[4] = {};
+        if (s_row < s_rows) {
+          const uint8_t* p = SC + static_cast<int64_t>(s_row) * a.NB + first;
+          for (int i = 0; i < 16 && first + i < a.NB; ++i) v[i >> 2] |= static_cast<uint32_t>(p[i]) << (8 * (i & 3));
+        }
+        *reinterpret_cast<uint4*>(lds + dst + tid * 16) = make_uint4(v[0], v[1], v[2], v[3]);
+      }
+    }
+    const uint32_t base = lds0 + st % S::kBufs * S::kStage;
 #pragma unroll
     for (int i = 0; i < NX; ++i)
       dma16(rx, xb[i] < left ? xo[i] + st * XB : kPastEnd, __builtin_amdgcn_readfirstlane(base + (wave * NX + i) * 1024));
@@ -152,54 +190,6 @@ __global__ __launch_bounds__(WM* WN * 64) void tile_kernel(ProjectArgs a) {
     for (int i = 0; i < NW; ++i)
       dma16(rw, wb[i] < left ? wo[i] + st * WB : kPastEnd,
             __builtin_amdgcn_readfirstlane(base + S::kXBytes + (wave * NW + i) * 1024));
-  };
-  // Scale bytes of a stage, one row per thread and pass, through registers:
-  // rows past the tile and blocks past the row are zeros (their codes are).
-  constexpr int NSC = (S::kSRows + S::kThreads - 1) / S::kThreads;
-  uint64_t sc[NSC];
-  auto load_scales = [&](int st) {
-    const int left = a.NB - st * NBK;
-#pragma unroll
-    for (int i = 0; i < NSC; ++i) {
-      const int r = tid + i * S::kThreads;
-      const bool is_x = XF4 && r < BM;
-      const int rr = XF4 && !is_x ? r - BM : r;
-      const uint8_t* p = (is_x ? XS : WS) + static_cast<int64_t>(rr) * a.NB + st * NBK;
-      sc[i] = 0;
-      if (r < S::kSRows && rr < (is_x ? mrows : nrows)) {
-        if (left >= NBK) {
-          if constexpr (NBK == 8) {
-            typedef uint64_t u64_u __attribute__((aligned(1)));
-            sc[i] = *reinterpret_cast<const u64_u*>(p);
-          } else {
-            typedef uint32_t u32_u __attribute__((aligned(1)));
-            sc[i] = *reinterpret_cast<const u32_u*>(p);
-          }
-        } else {
-          for (int b = 0; b < left; ++b) sc[i] |= static_cast<uint64_t>(p[b]) << (8 * b);
-        }
-      }
-    }
-  };
-  auto store_scales = [&](int s) {
-    char* p = lds[s] + S::kXBytes + S::kWBytes;
-#pragma unroll
-    for (int i = 0; i < NSC; ++i) {
-      const int r = tid + i * S::kThreads;
-      if (r >= S::kSRows) continue;
-      if constexpr (NBK == 8)
-        *reinterpret_cast<uint64_t*>(p + r * 8) = sc[i];
-      else
-        *reinterpret_cast<uint32_t*>(p + r * 4) = static_cast<uint32_t>(sc[i]);
-    }
-  };
-  // The scales of one row's blocks hh * NS ..: byte j is matrix step j's.
-  auto scale_of = [&](const char* st, int r) -> int {
-    const char* p = st + S::kXBytes + S::kWBytes + r * NBK;
-    if constexpr (NBK == 8)
-      return *reinterpret_cast<const int*>(p + 4 * hh);
-    else
-      return *reinterpret_cast<const uint16_t*>(p + 2 * hh);
   };
 
   f32x16 acc[TM][TN];
@@ -209,23 +199,26 @@ __global__ __launch_bounds__(WM* WN * 64) void tile_kernel(ProjectArgs a) {
     for (int j = 0; j < TN; ++j) acc[i][j] = f32x16{};
 
   const int nst = (a.NB + NBK - 1) / NBK;
-  load_scales(0);
-  store_scales(0);
-  issue(0, 0);
-  wait_vmcnt<0>();
-  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < S::kBufs - 1; ++i) issue(i);
   for (int st = 0; st < nst; ++st) {
-    const char* B = lds[st & 1];
-    const bool more = st + 1 < nst;
-    if (more) {
-      load_scales(st + 1);
-      issue(st + 1, (st + 1) & 1);
-    }
+    // this wave's part of stage st has arrived; then everybody's has, and
+    // everybody is done with the buffer that the next transfers fill
+    wait_vmcnt<(S::kBufs - 2) * (NX + NW)>();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    issue(st + S::kBufs - 1);
+    const char* B = lds + st % S::kBufs * S::kStage;
+    // The scales of a row's blocks 2 hh, 2 hh + 1 of the stage: byte j is step j's.
+    const char* SB = lds + S::kBufs * S::kStage + (st / S::kSuper & 1) * S::kScales + (st * NBK - scale_base(st)) + 2 * hh;
     int sx[TM], sw[TN];
 #pragma unroll
-    for (int i = 0; i < TM; ++i) sx[i] = XF4 ? scale_of(B, (wm * TM + i) * 32 + n32) : 0x7f7f7f7f;
+    for (int i = 0; i < TM; ++i)
+      sx[i] = XF4 ? *reinterpret_cast<const uint16_t*>(SB + ((wm * TM + i) * 32 + n32) * 16) : 0x7f7f;
 #pragma unroll
-    for (int j = 0; j < TN; ++j) sw[j] = scale_of(B, (XF4 ? BM : 0) + (wn * TN + j) * 32 + n32);
+    for (int j = 0; j < TN; ++j)
+      sw[j] = *reinterpret_cast<const uint16_t*>(SB + ((XF4 ? BM : 0) + (wn * TN + j) * 32 + n32) * 16);
     auto step = [&](auto js) {
       constexpr int J = decltype(js)::value;
       if constexpr (kWide<XF4, T>) {
@@ -237,13 +230,13 @@ __global__ __launch_bounds__(WM* WN * 64) void tile_kernel(ProjectArgs a) {
 #pragma unroll
           for (int i = 0; i < TM; ++i) {
             const int row = (wm * TM + i) * 32 + n32;
-            const uint2 v = *reinterpret_cast<const uint2*>(B + row * XB + (((2 * c + (p >> 1)) ^ ((row >> 1) & 7)) << 4) + (p & 1) * 8);
+            const uint2 v = *reinterpret_cast<const uint2*>(B + row * XB + (((2 * c + (p >> 1)) ^ chunk_swizzle<XB>(row)) << 4) + (p & 1) * 8);
             xw[i] = expand8(v.x, v.y);
           }
 #pragma unroll
           for (int j = 0; j < TN; ++j) {
             const int row = (wn * TN + j) * 32 + n32;
-            const uint32_t v = *reinterpret_cast<const uint32_t*>(B + S::kXBytes + row * WB + ((c ^ ((row >> 2) & 3)) << 4) + p * 4);
+            const uint32_t v = *reinterpret_cast<const uint32_t*>(B + S::kXBytes + row * WB + ((c ^ chunk_swizzle<WB>(row)) << 4) + p * 4);
             ww[j] = expand4(v, mx_scale((static_cast<uint32_t>(sw[j]) >> (8 * J)) & 255u));
           }
 #pragma unroll
@@ -256,7 +249,7 @@ __global__ __launch_bounds__(WM* WN * 64) void tile_kernel(ProjectArgs a) {
       i32x8 xv[TM], wv[TN];
 #pragma unroll
       for (int i = 0; i < TM; ++i) {
-        const int row = (wm * TM + i) * 32 + n32, s = (row >> 1) & 7;
+        const int row = (wm * TM + i) * 32 + n32, s = chunk_swizzle<XB>(row);
         if constexpr (XF4) {
           xv[i] = widen(*reinterpret_cast<const i32x4*>(B + row * XB + (((hh * NS + J) ^ s) << 4)));
         } else {
@@ -269,9 +262,8 @@ __global__ __launch_bounds__(WM* WN * 64) void tile_kernel(ProjectArgs a) {
       }
 #pragma unroll
       for (int j = 0; j < TN; ++j) {
-        const int row = (wn * TN + j) * 32 + n32, c = hh * NS + J;
-        const int ch = XF4 ? c ^ ((row >> 1) & 7) : c ^ ((row >> 2) & 3);
-        wv[j] = widen(*reinterpret_cast<const i32x4*>(B + S::kXBytes + row * WB + (ch << 4)));
+        const int row = (wn * TN + j) * 32 + n32;
+        wv[j] = widen(*reinterpret_cast<const i32x4*>(B + S::kXBytes + row * WB + (((hh * NS + J) ^ chunk_swizzle<WB>(row)) << 4)));
       }
 #pragma unroll
       for (int i = 0; i < TM; ++i)
@@ -282,31 +274,53 @@ __global__ __launch_bounds__(WM* WN * 64) void tile_kernel(ProjectArgs a) {
     };
     step(std::integral_constant<int, 0>{});
     step(std::integral_constant<int, 1>{});
-    if constexpr (NS > 2) {
-      step(std::integral_constant<int, 2>{});
-      step(std::integral_constant<int, 3>{});
-    }
-    if (more) store_scales((st + 1) & 1);
-    wait_vmcnt<0>();
-    __syncthreads();
   }
-
+  // Outputs leave through LDS, 32 rows of every wave at a time, as whole rows
+  // of the tile: a lane's own runs of four features would be 8-byte stores
+  // into 32 rows at once (half of the time of a short contraction).
+  constexpr int kPitch = BN * static_cast<int>(sizeof(T)) + 16, kOut = WM * 32 * kPitch, kVec = 16 / sizeof(T);
+  static_assert(2 * kOut <= static_cast<int>(sizeof(lds)), "two groups of rows fit the stages' place");
+  const T* bias = static_cast<const T*>(a.bias);
+  const bool vectors = a.split % kVec == 0;
+  wait_vmcnt<0>();  // the transfers past the last stage
+  __syncthreads();
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
-    const int64_t row = static_cast<int64_t>(tm) * BM + (wm * TM + i) * 32 + n32;
-    if (row >= a.M) continue;
-    const float xs = XF4 ? 1.f : static_cast<const float*>(a.xs)[row];
+    char* E = lds + (i & 1) * kOut;
+    const int r_in = (wm * TM + i) * 32 + n32;
+    const float xs = XF4 || r_in >= mrows ? 1.f : static_cast<const float*>(a.xs)[static_cast<int64_t>(tm) * BM + r_in];
 #pragma unroll
     for (int j = 0; j < TN; ++j)
 #pragma unroll
       for (int jj = 0; jj < 4; ++jj) {
-        const int col = tn * BN + (wn * TN + j) * 32 + 8 * jj + 4 * hh;
-        if (col >= a.N) continue;
-        float v[4];
+        const int ct = (wn * TN + j) * 32 + 8 * jj + 4 * hh, col = tn * BN + ct;
+        typedef T vec4 __attribute__((ext_vector_type(4)));
+        vec4 u;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * jj + e] * xs;
-        store_features<T, 4>(a, row, col, v);
+        for (int e = 0; e < 4; ++e) {
+          const float add = bias && col + e < a.N ? static_cast<float>(bias[col + e]) : 0.f;
+          u[e] = static_cast<T>((acc[i][j][4 * jj + e] * xs + add) * (col + e < a.split ? a.part0_scale : 1.f));
+        }
+        *reinterpret_cast<vec4*>(E + (wm * 32 + n32) * kPitch + ct * sizeof(T)) = u;
       }
+    __syncthreads();
+    for (int p = tid; p < WM * 32 * (BN / kVec); p += S::kThreads) {
+      const int er = p / (BN / kVec), ct = p % (BN / kVec) * kVec, col = tn * BN + ct;
+      const int row_in = (er / 32 * TM + i) * 32 + er % 32;
+      if (row_in >= mrows || col >= a.N) continue;
+      const int64_t row = static_cast<int64_t>(tm) * BM + row_in;
+      const char* src = E + er * kPitch + ct * sizeof(T);
+      if (vectors) {
+        const int part = col / a.split;
+        *reinterpret_cast<uint4*>(static_cast<T*>(a.y[part]) + row * a.split + (col - part * a.split)) =
+            *reinterpret_cast<const uint4*>(src);
+      } else {
+        for (int e = 0; e < kVec && col + e < a.N; ++e) {
+          const int part = (col + e) / a.split;
+          static_cast<T*>(a.y[part])[row * a.split + (col + e - part * a.split)] = reinterpret_cast<const T*>(src)[e];
+        }
+      }
+    }
   }
 }
 
