@@ -89,18 +89,19 @@ __device__ inline void store_features(const ProjectArgs& a, int64_t row, int col
 // kBufs - 1 stages are on their way or in LDS ahead of the one that is
 // multiplied: a stage takes the matrix cores half a microsecond, a transfer
 // up to two.  Scale bytes come sixteen to a row, for four stages at once.
-template <bool XF4, int BM, int BN, int WM, int WN>
+template <bool XF4, int BM, int BN, int WM, int WN, int BUFS>
 struct TileShape {
   static constexpr int kThreads = WM * WN * 64, kWaves = WM * WN;
   static constexpr int NBK = 4, NS = 2;            // blocks and matrix steps a stage
   static constexpr int kSuper = 4;                 // stages that share a load of scales
   static constexpr int XB = XF4 ? 64 : 128, WB = 64;  // bytes of a row a stage
-  static constexpr int kBufs = XF4 ? 4 : 3;
+  static constexpr int kBufs = BUFS;
   static constexpr int kXBytes = BM * XB, kWBytes = BN * WB, kStage = kXBytes + kWBytes;
   static constexpr int kSRows = (XF4 ? BM : 0) + BN, kScales = kSRows * NBK * kSuper;
   static constexpr int NX = kXBytes / 1024 / kWaves, NW = kWBytes / 1024 / kWaves;  // transfers of a wave a stage
   static_assert(NX * 1024 * kWaves == kXBytes && NW * 1024 * kWaves == kWBytes, "whole transfers");
-  static_assert(kSRows <= kThreads && kSRows % 64 == 0, "a scale row per thread, whole waves");
+  static constexpr int NSG = (kSRows / 64 + kWaves - 1) / kWaves;  // groups of 64 scale rows of a wave
+  static_assert(kSRows % 64 == 0 && BM % 64 == 0, "whole groups of scale rows");
   static_assert(kBufs * kStage + 2 * kScales <= 160 * 1024, "LDS of a CU");
 };
 
@@ -111,12 +112,16 @@ __device__ inline int chunk_swizzle(int row) {
   return ROW == 128 ? (row >> 1) & 7 : (row >> 2) & 3;
 }
 
-template <bool XF4, class T, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(WM* WN * 64) __attribute__((amdgpu_waves_per_eu(2))) void tile_kernel(ProjectArgs a) {
-  using S = TileShape<XF4, BM, BN, WM, WN>;
+template <bool XF4, class T, int BM, int BN, int WM, int WN, int BUFS>
+__global__ __launch_bounds__(WM* WN * 64) __attribute__((amdgpu_waves_per_eu(BM / WM * BN / WN > 128 * 64 ? 1 : 2)))
+void tile_kernel(ProjectArgs a) {
+  using S = TileShape<XF4, BM, BN, WM, WN, BUFS>;
   constexpr int NBK = S::NBK, NS = S::NS, XB = S::XB, WB = S::WB, NX = S::NX, NW = S::NW;
   constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
-  __shared__ __attribute__((aligned(16))) char lds[S::kBufs * S::kStage + 2 * S::kScales];
+  // The output's rows, 32 of every wave, take the stages' place at the end.
+  constexpr int kPitch = BN * static_cast<int>(sizeof(T)) + 16, kOut = WM * 32 * kPitch, kVec = 16 / sizeof(T);
+  constexpr int kIn = S::kBufs * S::kStage + 2 * S::kScales, kOutBufs = 2 * kOut <= kIn ? 2 : 1;
+  __shared__ __attribute__((aligned(16))) char lds[kIn > kOut ? kIn : kOut];
 
   // Tiles in panels of four feature tiles: the blocks of an XCD, a run of
   // them, share rows of both operands in its L2.
@@ -131,11 +136,8 @@ __global__ __launch_bounds__(WM* WN * 64) __attribute__((amdgpu_waves_per_eu(2))
   const uint32_t xp = static_cast<uint32_t>(a.NB) * (XF4 ? 16 : 32), wp = static_cast<uint32_t>(a.NB) * 16;
   const char* X = static_cast<const char*>(a.x) + static_cast<int64_t>(tm) * BM * xp;
   const char* W = static_cast<const char*>(a.w) + static_cast<int64_t>(tn) * BN * wp;
-  // this thread's (and this wave's) row of scales: X rows first for MXFP4 tokens
-  const bool s_x = XF4 && wave * 64 < BM;
-  const int s_row = XF4 && !s_x ? tid - BM : tid, s_rows = s_x ? mrows : nrows;
-  const uint8_t* SC = s_x ? static_cast<const uint8_t*>(a.xs) + static_cast<int64_t>(tm) * BM * a.NB
-                          : static_cast<const uint8_t*>(a.ws) + static_cast<int64_t>(tn) * BN * a.NB;
+  const uint8_t* XS = static_cast<const uint8_t*>(a.xs) + static_cast<int64_t>(tm) * BM * a.NB;
+  const uint8_t* WS = static_cast<const uint8_t*>(a.ws) + static_cast<int64_t>(tn) * BN * a.NB;
   // Scales go straight to LDS too where sixteen bytes of a row are whole
   // dwords of it; else through registers.
   const bool direct = a.NB % 4 == 0 && a.NB >= 16;
@@ -158,7 +160,6 @@ __global__ __launch_bounds__(WM* WN * 64) __attribute__((amdgpu_waves_per_eu(2))
   }
   const i32x4 rx = rsrc_of(X, static_cast<uint32_t>(mrows) * xp);
   const i32x4 rw = rsrc_of(W, static_cast<uint32_t>(nrows) * wp);
-  const i32x4 rs = rsrc_of(SC, static_cast<uint32_t>(s_rows) * a.NB);
   const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(&lds[0]));
   // First block of a group's sixteen scales: the last group ends at the row's end.
   auto scale_base = [&](int st) { return direct ? min(st / S::kSuper * 16, a.NB - 16) : st / S::kSuper * 16; };
@@ -166,20 +167,29 @@ __global__ __launch_bounds__(WM* WN * 64) __attribute__((amdgpu_waves_per_eu(2))
   // count of transfers in flight the same).
   auto issue = [&](int st) {
     const int left = a.NB - st * NBK;
-    if (st % S::kSuper == 0 && left > 0 && wave * 64 < S::kSRows) {
+    if (st % S::kSuper == 0 && left > 0) {
       const uint32_t dst = S::kBufs * S::kStage + (st / S::kSuper & 1) * S::kScales;
       const int first = scale_base(st);
-      if (direct) {
-        dma16(rs, s_row < s_rows ? s_row * static_cast<uint32_t>(a.NB) + first : kPastEnd,
-              __builtin_amdgcn_readfirstlane(lds0 + dst + wave * 1024));
-      } else {
-        // rows past the tile and blocks past the row: zeros (their codes are)
-        uint32_t v[4] = {};
-        if (s_row < s_rows) {
-          const uint8_t* p = SC + static_cast<int64_t>(s_row) * a.NB + first;
-          for (int i = 0; i < 16 && first + i < a.NB; ++i) v[i >> 2] |= static_cast<uint32_t>(p[i]) << (8 * (i & 3));
+#pragma unroll
+      for (int i = 0; i < S::NSG; ++i) {
+        const int group = wave + i * S::kWaves;  // 64 rows, those of X first for MXFP4 tokens
+        if (group * 64 >= S::kSRows) continue;
+        const bool of_x = XF4 && group * 64 < BM;
+        const int row = group * 64 + lane - (XF4 && !of_x ? BM : 0), rows = of_x ? mrows : nrows;
+        const uint8_t* base = of_x ? XS : WS;
+        if (direct) {
+          dma16(rsrc_of(base, static_cast<uint32_t>(rows) * a.NB),
+                row < rows ? row * static_cast<uint32_t>(a.NB) + first : kPastEnd,
+                __builtin_amdgcn_readfirstlane(lds0 + dst + group * 1024));
+        } else {
+          // rows past the tile and blocks past the row: zeros (their codes are)
+          uint32_t v[4] = {};
+          if (row < rows) {
+            const uint8_t* p = base + static_cast<int64_t>(row) * a.NB + first;
+            for (int k = 0; k < 16 && first + k < a.NB; ++k) v[k >> 2] |= static_cast<uint32_t>(p[k]) << (8 * (k & 3));
+          }
+          *reinterpret_cast<uint4*>(lds + dst + group * 1024 + lane * 16) = make_uint4(v[0], v[1], v[2], v[3]);
         }
-        *reinterpret_cast<uint4*>(lds + dst + tid * 16) = make_uint4(v[0], v[1], v[2], v[3]);
       }
     }
     const uint32_t base = lds0 + st % S::kBufs * S::kStage;
@@ -278,29 +288,36 @@ __global__ __launch_bounds__(WM* WN * 64) __attribute__((amdgpu_waves_per_eu(2))
   // Outputs leave through LDS, 32 rows of every wave at a time, as whole rows
   // of the tile: a lane's own runs of four features would be 8-byte stores
   // into 32 rows at once (half of the time of a short contraction).
-  constexpr int kPitch = BN * static_cast<int>(sizeof(T)) + 16, kOut = WM * 32 * kPitch, kVec = 16 / sizeof(T);
-  static_assert(2 * kOut <= static_cast<int>(sizeof(lds)), "two groups of rows fit the stages' place");
   const T* bias = static_cast<const T*>(a.bias);
   const bool vectors = a.split % kVec == 0;
+  // this lane's features: bias and factor, 4 jj + e of feature block j
+  float add[TN][16], factor[TN][16];
+#pragma unroll
+  for (int j = 0; j < TN; ++j)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int col = tn * BN + (wn * TN + j) * 32 + 8 * (e >> 2) + 4 * hh + (e & 3);
+      add[j][e] = bias && col < a.N ? static_cast<float>(bias[col]) : 0.f;
+      factor[j][e] = col < a.split ? a.part0_scale : 1.f;
+    }
   wait_vmcnt<0>();  // the transfers past the last stage
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
-    char* E = lds + (i & 1) * kOut;
+    char* E = lds + i % kOutBufs * kOut;
+    if (kOutBufs == 1 && i > 0) __syncthreads();
     const int r_in = (wm * TM + i) * 32 + n32;
     const float xs = XF4 || r_in >= mrows ? 1.f : static_cast<const float*>(a.xs)[static_cast<int64_t>(tm) * BM + r_in];
 #pragma unroll
     for (int j = 0; j < TN; ++j)
 #pragma unroll
       for (int jj = 0; jj < 4; ++jj) {
-        const int ct = (wn * TN + j) * 32 + 8 * jj + 4 * hh, col = tn * BN + ct;
+        const int ct = (wn * TN + j) * 32 + 8 * jj + 4 * hh;
         typedef T vec4 __attribute__((ext_vector_type(4)));
         vec4 u;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float add = bias && col + e < a.N ? static_cast<float>(bias[col + e]) : 0.f;
-          u[e] = static_cast<T>((acc[i][j][4 * jj + e] * xs + add) * (col + e < a.split ? a.part0_scale : 1.f));
-        }
+        for (int e = 0; e < 4; ++e)
+          u[e] = static_cast<T>((acc[i][j][4 * jj + e] * xs + add[j][4 * jj + e]) * factor[j][4 * jj + e]);
         *reinterpret_cast<vec4*>(E + (wm * 32 + n32) * kPitch + ct * sizeof(T)) = u;
       }
     __syncthreads();
@@ -312,8 +329,9 @@ __global__ __launch_bounds__(WM* WN * 64) __attribute__((amdgpu_waves_per_eu(2))
       const char* src = E + er * kPitch + ct * sizeof(T);
       if (vectors) {
         const int part = col / a.split;
-        *reinterpret_cast<uint4*>(static_cast<T*>(a.y[part]) + row * a.split + (col - part * a.split)) =
-            *reinterpret_cast<const uint4*>(src);
+        // streamed: the outputs are not to push the operands out of L2
+        __builtin_nontemporal_store(*reinterpret_cast<const i32x4*>(src),
+                                    reinterpret_cast<i32x4*>(static_cast<T*>(a.y[part]) + row * a.split + (col - part * a.split)));
       } else {
         for (int e = 0; e < kVec && col + e < a.N; ++e) {
           const int part = (col + e) / a.split;
@@ -446,11 +464,11 @@ hipError_t few_go(const ProjectArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-template <bool XF4, class T, int BM, int BN, int WM, int WN>
+template <bool XF4, class T, int BM, int BN, int WM, int WN, int BUFS>
 hipError_t tile_go(const ProjectArgs& a, hipStream_t stream) {
   const int64_t tiles = static_cast<int64_t>((a.M + BM - 1) / BM) * ((a.N + BN - 1) / BN);
   if (tiles > 0x7fffffff) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((tile_kernel<XF4, T, BM, BN, WM, WN>), dim3(static_cast<uint32_t>(tiles)), dim3(WM * WN * 64), 0, stream, a);
+  hipLaunchKernelGGL((tile_kernel<XF4, T, BM, BN, WM, WN, BUFS>), dim3(static_cast<uint32_t>(tiles)), dim3(WM * WN * 64), 0, stream, a);
   return hipGetLastError();
 }
 
@@ -458,8 +476,8 @@ template <bool XF4, class T>
 hipError_t project(const ProjectArgs& a, hipStream_t stream) {
   if (a.M <= 16) return few_go<XF4, T, 1>(a, stream);
   if (a.M <= 32) return few_go<XF4, T, 2>(a, stream);
-  if (static_cast<int64_t>((a.M + 255) / 256) * ((a.N + 255) / 256) >= 256) return tile_go<XF4, T, 256, 256, 2, 4>(a, stream);
-  return tile_go<XF4, T, 128, 128, 2, 2>(a, stream);
+  if (static_cast<int64_t>((a.M + 255) / 256) * ((a.N + 255) / 256) >= 256) return tile_go<XF4, T, 256, 256, 2, 4, XF4 ? 4 : 3>(a, stream);
+  return tile_go<XF4, T, 128, 128, 2, 2, XF4 ? 4 : 3>(a, stream);
 }
 
 }  // namespace
