@@ -112,6 +112,17 @@ __device__ inline int chunk_swizzle(int row) {
   return ROW == 128 ? (row >> 1) & 7 : (row >> 2) & 3;
 }
 
+// Order of a run of P matrix instructions and R LDS reads: the reads spread
+// evenly behind the products.
+template <int P, int R, int K = 0>
+__device__ inline void interleave() {
+  if constexpr (K < P) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    if constexpr (R * (K + 1) / P > R * K / P) __builtin_amdgcn_sched_group_barrier(0x100, R * (K + 1) / P - R * K / P, 0);
+    interleave<P, R, K + 1>();
+  }
+}
+
 template <bool XF4, class T, int BM, int BN, int WM, int WN, int BUFS>
 __global__ __launch_bounds__(WM* WN * 64) __attribute__((amdgpu_waves_per_eu(BM / WM * BN / WN > 128 * 64 ? 1 : 2)))
 void tile_kernel(ProjectArgs a) {
@@ -208,83 +219,103 @@ void tile_kernel(ProjectArgs a) {
 #pragma unroll
     for (int j = 0; j < TN; ++j) acc[i][j] = f32x16{};
 
-  const int nst = (a.NB + NBK - 1) / NBK;
-#pragma unroll
-  for (int i = 0; i < S::kBufs - 1; ++i) issue(i);
-  for (int st = 0; st < nst; ++st) {
-    // this wave's part of stage st has arrived; then everybody's has, and
-    // everybody is done with the buffer that the next transfers fill
-    wait_vmcnt<(S::kBufs - 2) * (NX + NW)>();
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    issue(st + S::kBufs - 1);
-    const char* B = lds + st % S::kBufs * S::kStage;
-    // The scales of a row's blocks 2 hh, 2 hh + 1 of the stage: byte j is step j's.
+  // Scales of a stage: byte j of a row's is matrix step j's (blocks 2 hh + j).
+  int sx[TM], sw[TN];
+  auto read_scales = [&](int st) {
     const char* SB = lds + S::kBufs * S::kStage + (st / S::kSuper & 1) * S::kScales + (st * NBK - scale_base(st)) + 2 * hh;
-    int sx[TM], sw[TN];
 #pragma unroll
     for (int i = 0; i < TM; ++i)
       sx[i] = XF4 ? *reinterpret_cast<const uint16_t*>(SB + ((wm * TM + i) * 32 + n32) * 16) : 0x7f7f;
 #pragma unroll
     for (int j = 0; j < TN; ++j)
       sw[j] = *reinterpret_cast<const uint16_t*>(SB + ((XF4 ? BM : 0) + (wn * TN + j) * 32 + n32) * 16);
-    auto step = [&](auto js) {
-      constexpr int J = decltype(js)::value;
-      if constexpr (kWide<XF4, T>) {
-        // lane half hh's block hh * NS + J, eight values at a time
-        const int c = hh * NS + J;
+  };
+  // Operands of step J of the stage at B.
+  i32x8 xv[2][TM];
+  i32x4 wv[2][TN];
+  auto read_step = [&](auto js, const char* B) {
+    constexpr int J = decltype(js)::value;
 #pragma unroll
-        for (int p = 0; p < 4; ++p) {
-          bf16x8 xw[TM], ww[TN];
-#pragma unroll
-          for (int i = 0; i < TM; ++i) {
-            const int row = (wm * TM + i) * 32 + n32;
-            const uint2 v = *reinterpret_cast<const uint2*>(B + row * XB + (((2 * c + (p >> 1)) ^ chunk_swizzle<XB>(row)) << 4) + (p & 1) * 8);
-            xw[i] = expand8(v.x, v.y);
-          }
-#pragma unroll
-          for (int j = 0; j < TN; ++j) {
-            const int row = (wn * TN + j) * 32 + n32;
-            const uint32_t v = *reinterpret_cast<const uint32_t*>(B + S::kXBytes + row * WB + ((c ^ chunk_swizzle<WB>(row)) << 4) + p * 4);
-            ww[j] = expand4(v, mx_scale((static_cast<uint32_t>(sw[j]) >> (8 * J)) & 255u));
-          }
-#pragma unroll
-          for (int i = 0; i < TM; ++i)
-#pragma unroll
-            for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ww[j], xw[i], acc[i][j], 0, 0, 0);
-        }
-        return;
+    for (int i = 0; i < TM; ++i) {
+      const int row = (wm * TM + i) * 32 + n32, s = chunk_swizzle<XB>(row);
+      if constexpr (XF4) {
+        xv[J][i] = widen(*reinterpret_cast<const i32x4*>(B + row * XB + (((hh * NS + J) ^ s) << 4)));
+      } else {
+        // e4m3: a lane's first 16 bytes are its half's piece of the first
+        // lane half's block, its last 16 bytes of the second's; expanded to
+        // bf16, a lane takes the block of its own half
+        const int c0 = kWide<XF4, T> ? 2 * (hh * NS + J) : 2 * J + hh, c1 = kWide<XF4, T> ? c0 + 1 : 2 * (NS + J) + hh;
+        const i32x4 lo = *reinterpret_cast<const i32x4*>(B + row * XB + ((c0 ^ s) << 4));
+        const i32x4 hi = *reinterpret_cast<const i32x4*>(B + row * XB + ((c1 ^ s) << 4));
+        xv[J][i] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
       }
-      i32x8 xv[TM], wv[TN];
+    }
 #pragma unroll
-      for (int i = 0; i < TM; ++i) {
-        const int row = (wm * TM + i) * 32 + n32, s = chunk_swizzle<XB>(row);
-        if constexpr (XF4) {
-          xv[i] = widen(*reinterpret_cast<const i32x4*>(B + row * XB + (((hh * NS + J) ^ s) << 4)));
-        } else {
-          // e4m3: a lane's first 16 bytes are its half's piece of the first
-          // lane half's block, its last 16 bytes of the second's
-          const i32x4 lo = *reinterpret_cast<const i32x4*>(B + row * XB + (((2 * J + hh) ^ s) << 4));
-          const i32x4 hi = *reinterpret_cast<const i32x4*>(B + row * XB + (((2 * (NS + J) + hh) ^ s) << 4));
-          xv[i] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-        }
-      }
+    for (int j = 0; j < TN; ++j) {
+      const int row = (wn * TN + j) * 32 + n32;
+      wv[J][j] = *reinterpret_cast<const i32x4*>(B + S::kXBytes + row * WB + (((hh * NS + J) ^ chunk_swizzle<WB>(row)) << 4));
+    }
+  };
+  auto multiply = [&](auto js) {
+    constexpr int J = decltype(js)::value;
+    if constexpr (kWide<XF4, T>) {
 #pragma unroll
-      for (int j = 0; j < TN; ++j) {
-        const int row = (wn * TN + j) * 32 + n32;
-        wv[j] = widen(*reinterpret_cast<const i32x4*>(B + S::kXBytes + row * WB + (((hh * NS + J) ^ chunk_swizzle<WB>(row)) << 4)));
+      for (int p = 0; p < 4; ++p) {  // eight values at a time
+        bf16x8 xw[TM], ww[TN];
+#pragma unroll
+        for (int i = 0; i < TM; ++i) xw[i] = expand8(xv[J][i][2 * p], xv[J][i][2 * p + 1]);
+#pragma unroll
+        for (int j = 0; j < TN; ++j) ww[j] = expand4(wv[J][j][p], mx_scale((static_cast<uint32_t>(sw[j]) >> (8 * J)) & 255u));
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ww[j], xw[i], acc[i][j], 0, 0, 0);
       }
+    } else {
 #pragma unroll
       for (int i = 0; i < TM; ++i)
 #pragma unroll
         for (int j = 0; j < TN; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wv[j], xv[i], acc[i][j], kFmtE2M1,
+          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(widen(wv[J][j]), xv[J][i], acc[i][j], kFmtE2M1,
                                                                      XF4 ? kFmtE2M1 : kFmtE4M3, J, sw[j], XF4 ? J : 0, sx[i]);
-    };
-    step(std::integral_constant<int, 0>{});
-    step(std::integral_constant<int, 1>{});
+    }
+  };
+  constexpr int kReads = TM * (XF4 ? 1 : 2) + TN, kProducts = kWide<XF4, T> ? 0 : TM * TN;
+
+  const int nst = (a.NB + NBK - 1) / NBK;
+  constexpr std::integral_constant<int, 0> s0{};
+  constexpr std::integral_constant<int, 1> s1{};
+#pragma unroll
+  for (int i = 0; i < S::kBufs; ++i) issue(i);
+  // The stage's second step is read while its first is multiplied, the next
+  // stage's first step while its second is: between the two every wave has
+  // read the whole stage, and its buffer takes the transfers of stage + kBufs.
+  wait_vmcnt<(S::kBufs - 1) * (NX + NW)>();
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  read_scales(0);
+  read_step(s0, lds);
+  for (int st = 0; st < nst; ++st) {
+    read_step(s1, lds + st % S::kBufs * S::kStage);
+    multiply(s0);
+    interleave<kProducts, kReads>();
+    __builtin_amdgcn_sched_barrier(0);
+    wait_vmcnt<(S::kBufs - 2) * (NX + NW)>();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    issue(st + S::kBufs);
+    __builtin_amdgcn_sched_barrier(0);
+    multiply(s1);
+    const int next = st + 1 < nst ? st + 1 : st;  // past the last stage: read again, not used
+    read_step(s0, lds + next % S::kBufs * S::kStage);
+    read_scales(next);
+    interleave<kProducts, kReads + (XF4 ? TM : 0) + TN>();
+    __builtin_amdgcn_sched_barrier(0);
   }
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+
   // Outputs leave through LDS, 32 rows of every wave at a time, as whole rows
   // of the tile: a lane's own runs of four features would be 8-byte stores
   // into 32 rows at once (half of the time of a short contraction).
