@@ -84,19 +84,20 @@ __device__ inline void store_features(const ProjectArgs& a, int64_t row, int col
 
 // Tiles.  A block of WM x WN waves owns BM tokens x BN features; the matrix
 // instruction computes the transposed tile (A = W rows, B = X rows), so a
-// lane holds one token and runs of four features.  A stage is four blocks (128
-// values) of every token and feature, moved by direct global -> LDS transfers.
-// kBufs - 1 stages are on their way or in LDS ahead of the one that is
-// multiplied: a stage takes the matrix cores half a microsecond, a transfer
-// up to two.  Scale bytes come sixteen to a row, for four stages at once.
+// lane holds one token and runs of four features.  A stage is 128 bytes
+// of every token (four blocks of e4m3, eight of MXFP4: whole cache lines) and
+// as many blocks of every feature, moved by direct global -> LDS transfers;
+// kBufs of them are in LDS or on their way.  Scale bytes come sixteen to a row, for four stages at once.
 template <bool XF4, int BM, int BN, int WM, int WN, int BUFS>
 struct TileShape {
   static constexpr int kThreads = WM * WN * 64, kWaves = WM * WN;
-  static constexpr int NBK = 4, NS = 2;            // blocks and matrix steps a stage
-  static constexpr int kSuper = 4;                 // stages that share a load of scales
-  static constexpr int XB = XF4 ? 64 : 128, WB = 64;  // bytes of a row a stage
+  static constexpr int NBK = XF4 ? 8 : 4, NS = NBK / 2;   // blocks and matrix steps a stage
+  static constexpr int kSuper = 16 / NBK;                 // stages that share a load of scales
+  static constexpr int XB = 128, WB = NBK * 16;           // bytes of a row a stage
   static constexpr int kBufs = BUFS;
+    // LDS: the X tiles of all buffers, the W tiles, two groups' scales
   static constexpr int kXBytes = BM * XB, kWBytes = BN * WB, kStage = kXBytes + kWBytes;
+  static constexpr int kWBase = BUFS * kXBytes, kSBase = BUFS * kStage;
   static constexpr int kSRows = (XF4 ? BM : 0) + BN, kScales = kSRows * NBK * kSuper;
   static constexpr int NX = kXBytes / 1024 / kWaves, NW = kWBytes / 1024 / kWaves;  // transfers of a wave a stage
   static_assert(NX * 1024 * kWaves == kXBytes && NW * 1024 * kWaves == kWBytes, "whole transfers");
@@ -153,64 +154,87 @@ void tile_kernel(ProjectArgs a) {
   // dwords of it; else through registers.
   const bool direct = a.NB % 4 == 0 && a.NB >= 16;
 
-  // Transfer i of a wave fills 1 KB of consecutive LDS; a lane's 16 bytes are
-  // its physical chunk's.  xb, wb: the block that chunk belongs to in a stage.
-  uint32_t xo[NX], wo[NW];
-  int xb[NX], wb[NW];
+  // Transfer i of a wave fills 1 KB of consecutive LDS, XB- or WB-byte rows of
+  // it; a lane's 16 bytes are its physical chunk's.  The rows of transfer i
+  // are i * (1024 / XB) further on, which moves the swizzle by a fixed pattern.
+  constexpr int kXRows = 1024 / XB, kWRows = 1024 / WB;
+  auto x_chunk = [&](int i) { return (lane % (XB / 16)) ^ chunk_swizzle<XB>((wave * NX + i) * kXRows + lane / (XB / 16)); };
+  auto w_chunk = [&](int i) { return (lane % (WB / 16)) ^ chunk_swizzle<WB>((wave * NW + i) * kWRows + lane / (WB / 16)); };
+  const uint32_t x_row = (wave * NX * kXRows + lane / (XB / 16)) * xp, w_row = (wave * NW * kWRows + lane / (WB / 16)) * wp;
+  // (1024 / 128 = 8 rows: the swizzle has two values; 16 rows of 64 bytes: one)
+  constexpr int kXAlt = XB == 128 ? 2 : 1, kWAlt = WB == 128 ? 2 : 1;
+  uint32_t xo[kXAlt], wo[kWAlt];
 #pragma unroll
-  for (int i = 0; i < NX; ++i) {
-    const int p = (wave * NX + i) * 1024 + 16 * lane, row = p / XB, lc = (p / 16) % (XB / 16) ^ chunk_swizzle<XB>(row);
-    xo[i] = row * xp + lc * 16;
-    xb[i] = XF4 ? lc : lc / 2;
-  }
+  for (int i = 0; i < kXAlt; ++i) xo[i] = x_row + x_chunk(i) * 16;
 #pragma unroll
-  for (int i = 0; i < NW; ++i) {
-    const int p = (wave * NW + i) * 1024 + 16 * lane, row = p / WB, lc = (p / 16) % (WB / 16) ^ chunk_swizzle<WB>(row);
-    wo[i] = row * wp + lc * 16;
-    wb[i] = lc;
-  }
+  for (int i = 0; i < kWAlt; ++i) wo[i] = w_row + w_chunk(i) * 16;
   const i32x4 rx = rsrc_of(X, static_cast<uint32_t>(mrows) * xp);
   const i32x4 rw = rsrc_of(W, static_cast<uint32_t>(nrows) * wp);
   const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(&lds[0]));
   // First block of a group's sixteen scales: the last group ends at the row's end.
   auto scale_base = [&](int st) { return direct ? min(st / S::kSuper * 16, a.NB - 16) : st / S::kSuper * 16; };
-  // Stage st into its buffer (stages past the last: zeros, which keep the
-  // count of transfers in flight the same).
+  // The scales of stage st's group, straight to LDS.  A wave takes 64 rows
+  // (where there are fewer groups than waves, two take the same).
+  auto issue_scales = [&](int st) {
+    const uint32_t dst = lds0 + S::kSBase + (st / S::kSuper & 1) * S::kScales;
+    const int first = scale_base(st);
+#pragma unroll
+    for (int i = 0; i < S::NSG; ++i) {
+      const int group = (wave + i * S::kWaves) % (S::kSRows / 64);  // rows of X first for MXFP4 tokens
+      const bool of_x = XF4 && group * 64 < BM;
+      const int row = group * 64 + lane - (XF4 && !of_x ? BM : 0), rows = of_x ? mrows : nrows;
+      dma16(rsrc_of(of_x ? XS : WS, static_cast<uint32_t>(rows) * a.NB),
+            row < rows ? row * static_cast<uint32_t>(a.NB) + first : kPastEnd,
+            __builtin_amdgcn_readfirstlane(dst + group * 1024));
+    }
+  };
+  // Stage st, all of its blocks inside the rows.
+  auto issue_full = [&](int st, int buf) {
+    const uint32_t bx = lds0 + buf * S::kXBytes, bw = lds0 + S::kWBase + buf * S::kWBytes;
+#pragma unroll
+    for (int i = 0; i < NX; ++i)
+      dma16(rx, xo[i % kXAlt] + (i * kXRows * xp + st * XB), __builtin_amdgcn_readfirstlane(bx + (wave * NX + i) * 1024));
+#pragma unroll
+    for (int i = 0; i < NW; ++i)
+      dma16(rw, wo[i % kWAlt] + (i * kWRows * wp + st * WB),
+            __builtin_amdgcn_readfirstlane(bw + (wave * NW + i) * 1024));
+  };
+  // Any stage (past the last: zeros, which keep the count of transfers in
+  // flight the same), with the scales of its group if it is the group's first.
   auto issue = [&](int st) {
     const int left = a.NB - st * NBK;
     if (st % S::kSuper == 0 && left > 0) {
-      const uint32_t dst = S::kBufs * S::kStage + (st / S::kSuper & 1) * S::kScales;
-      const int first = scale_base(st);
-#pragma unroll
-      for (int i = 0; i < S::NSG; ++i) {
-        const int group = wave + i * S::kWaves;  // 64 rows, those of X first for MXFP4 tokens
-        if (group * 64 >= S::kSRows) continue;
-        const bool of_x = XF4 && group * 64 < BM;
-        const int row = group * 64 + lane - (XF4 && !of_x ? BM : 0), rows = of_x ? mrows : nrows;
-        const uint8_t* base = of_x ? XS : WS;
-        if (direct) {
-          dma16(rsrc_of(base, static_cast<uint32_t>(rows) * a.NB),
-                row < rows ? row * static_cast<uint32_t>(a.NB) + first : kPastEnd,
-                __builtin_amdgcn_readfirstlane(lds0 + dst + group * 1024));
-        } else {
-          // rows past the tile and blocks past the row: zeros (their codes are)
+      if (direct) {
+        issue_scales(st);
+      } else {
+        // rows past the tile and blocks past the row: zeros (their codes are)
+        const uint32_t dst = S::kSBase + (st / S::kSuper & 1) * S::kScales;
+        const int first = scale_base(st);
+        for (int group = wave; group < S::kSRows / 64; group += S::kWaves) {
+          const bool of_x = XF4 && group * 64 < BM;
+          const int row = group * 64 + lane - (XF4 && !of_x ? BM : 0);
           uint32_t v[4] = {};
-          if (row < rows) {
-            const uint8_t* p = base + static_cast<int64_t>(row) * a.NB + first;
+          if (row < (of_x ? mrows : nrows)) {
+            const uint8_t* p = (of_x ? XS : WS) + static_cast<int64_t>(row) * a.NB + first;
             for (int k = 0; k < 16 && first + k < a.NB; ++k) v[k >> 2] |= static_cast<uint32_t>(p[k]) << (8 * (k & 3));
           }
           *reinterpret_cast<uint4*>(lds + dst + group * 1024 + lane * 16) = make_uint4(v[0], v[1], v[2], v[3]);
         }
       }
     }
-    const uint32_t base = lds0 + st % S::kBufs * S::kStage;
+    if (left >= NBK) {
+      issue_full(st, st % S::kBufs);
+      return;
+    }
+    const uint32_t bx = lds0 + st % S::kBufs * S::kXBytes, bw = lds0 + S::kWBase + st % S::kBufs * S::kWBytes;
 #pragma unroll
     for (int i = 0; i < NX; ++i)
-      dma16(rx, xb[i] < left ? xo[i] + st * XB : kPastEnd, __builtin_amdgcn_readfirstlane(base + (wave * NX + i) * 1024));
+      dma16(rx, x_chunk(i) / (XF4 ? 1 : 2) < left ? xo[i % kXAlt] + (i * kXRows * xp + st * XB) : kPastEnd,
+            __builtin_amdgcn_readfirstlane(bx + (wave * NX + i) * 1024));
 #pragma unroll
     for (int i = 0; i < NW; ++i)
-      dma16(rw, wb[i] < left ? wo[i] + st * WB : kPastEnd,
-            __builtin_amdgcn_readfirstlane(base + S::kXBytes + (wave * NW + i) * 1024));
+      dma16(rw, w_chunk(i) < left ? wo[i % kWAlt] + (i * kWRows * wp + st * WB) : kPastEnd,
+            __builtin_amdgcn_readfirstlane(bw + (wave * NW + i) * 1024));
   };
 
   f32x16 acc[TM][TN];
@@ -219,41 +243,50 @@ void tile_kernel(ProjectArgs a) {
 #pragma unroll
     for (int j = 0; j < TN; ++j) acc[i][j] = f32x16{};
 
-  // Scales of a stage: byte j of a row's is matrix step j's (blocks 2 hh + j).
+  // Scales of a stage: byte j of a row's is matrix step j's (block hh NS + j).
   int sx[TM], sw[TN];
+  using scales_t = std::conditional_t<NS == 4, uint32_t, uint16_t>;
   auto read_scales = [&](int st) {
-    const char* SB = lds + S::kBufs * S::kStage + (st / S::kSuper & 1) * S::kScales + (st * NBK - scale_base(st)) + 2 * hh;
+    const char* SB = lds + S::kSBase + (st / S::kSuper & 1) * S::kScales + (st * NBK - scale_base(st)) + NS * hh;
 #pragma unroll
     for (int i = 0; i < TM; ++i)
-      sx[i] = XF4 ? *reinterpret_cast<const uint16_t*>(SB + ((wm * TM + i) * 32 + n32) * 16) : 0x7f7f;
+      sx[i] = XF4 ? *reinterpret_cast<const scales_t*>(SB + ((wm * TM + i) * 32 + n32) * 16) : 0x7f7f;
 #pragma unroll
     for (int j = 0; j < TN; ++j)
-      sw[j] = *reinterpret_cast<const uint16_t*>(SB + ((XF4 ? BM : 0) + (wn * TN + j) * 32 + n32) * 16);
+      sw[j] = *reinterpret_cast<const scales_t*>(SB + ((XF4 ? BM : 0) + (wn * TN + j) * 32 + n32) * 16);
   };
-  // Operands of step J of the stage at B.
+  // Operands of step J of the stage in buffer buf: 32 rows further on is a
+  // fixed distance, for the swizzle too.
   i32x8 xv[2][TM];
   i32x4 wv[2][TN];
-  auto read_step = [&](auto js, const char* B) {
+  int xa[NS][XF4 ? 1 : 2], wa[NS];
+#pragma unroll
+  for (int J = 0; J < NS; ++J) {
+    const int xr = wm * TM * 32 + n32, wr = wn * TN * 32 + n32;
+    // e4m3: a lane's first 16 bytes are its half's piece of the first lane
+    // half's block, its last 16 bytes of the second's; expanded to bf16, a
+    // lane takes the block of its own half
+    const int c0 = XF4 ? hh * NS + J : kWide<XF4, T> ? 2 * (hh * NS + J) : 2 * J + hh;
+    const int c1 = kWide<XF4, T> ? c0 + 1 : 2 * (NS + J) + hh;
+    xa[J][0] = xr * XB + ((c0 ^ chunk_swizzle<XB>(xr)) << 4);
+    if constexpr (!XF4) xa[J][1] = xr * XB + ((c1 ^ chunk_swizzle<XB>(xr)) << 4);
+    wa[J] = S::kWBase + wr * WB + (((hh * NS + J) ^ chunk_swizzle<WB>(wr)) << 4);
+  }
+  auto read_step = [&](auto js, int buf) {
     constexpr int J = decltype(js)::value;
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-      const int row = (wm * TM + i) * 32 + n32, s = chunk_swizzle<XB>(row);
-      if constexpr (XF4) {
-        xv[J][i] = widen(*reinterpret_cast<const i32x4*>(B + row * XB + (((hh * NS + J) ^ s) << 4)));
-      } else {
-        // e4m3: a lane's first 16 bytes are its half's piece of the first
-        // lane half's block, its last 16 bytes of the second's; expanded to
-        // bf16, a lane takes the block of its own half
-        const int c0 = kWide<XF4, T> ? 2 * (hh * NS + J) : 2 * J + hh, c1 = kWide<XF4, T> ? c0 + 1 : 2 * (NS + J) + hh;
-        const i32x4 lo = *reinterpret_cast<const i32x4*>(B + row * XB + ((c0 ^ s) << 4));
-        const i32x4 hi = *reinterpret_cast<const i32x4*>(B + row * XB + ((c1 ^ s) << 4));
-        xv[J][i] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-      }
-    }
+    for (int j = 0; j < TN; ++j)
+      wv[J & 1][j] = *reinterpret_cast<const i32x4*>(lds + wa[J] + buf * S::kWBytes + j * 32 * WB);
 #pragma unroll
-    for (int j = 0; j < TN; ++j) {
-      const int row = (wn * TN + j) * 32 + n32;
-      wv[J][j] = *reinterpret_cast<const i32x4*>(B + S::kXBytes + row * WB + (((hh * NS + J) ^ chunk_swizzle<WB>(row)) << 4));
+    for (int i = 0; i < TM; ++i) {
+      const char* X0 = lds + xa[J][0] + buf * S::kXBytes + i * 32 * XB;
+      if constexpr (XF4) {
+        xv[J & 1][i] = widen(*reinterpret_cast<const i32x4*>(X0));
+      } else {
+        const i32x4 lo = *reinterpret_cast<const i32x4*>(X0);
+        const i32x4 hi = *reinterpret_cast<const i32x4*>(lds + xa[J][1] + buf * S::kXBytes + i * 32 * XB);
+        xv[J & 1][i] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      }
     }
   };
   auto multiply = [&](auto js) {
@@ -263,9 +296,9 @@ void tile_kernel(ProjectArgs a) {
       for (int p = 0; p < 4; ++p) {  // eight values at a time
         bf16x8 xw[TM], ww[TN];
 #pragma unroll
-        for (int i = 0; i < TM; ++i) xw[i] = expand8(xv[J][i][2 * p], xv[J][i][2 * p + 1]);
+        for (int i = 0; i < TM; ++i) xw[i] = expand8(xv[J & 1][i][2 * p], xv[J & 1][i][2 * p + 1]);
 #pragma unroll
-        for (int j = 0; j < TN; ++j) ww[j] = expand4(wv[J][j][p], mx_scale((static_cast<uint32_t>(sw[j]) >> (8 * J)) & 255u));
+        for (int j = 0; j < TN; ++j) ww[j] = expand4(wv[J & 1][j][p], mx_scale((static_cast<uint32_t>(sw[j]) >> (8 * J)) & 255u));
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -276,43 +309,66 @@ void tile_kernel(ProjectArgs a) {
       for (int i = 0; i < TM; ++i)
 #pragma unroll
         for (int j = 0; j < TN; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(widen(wv[J][j]), xv[J][i], acc[i][j], kFmtE2M1,
+          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(widen(wv[J & 1][j]), xv[J & 1][i], acc[i][j], kFmtE2M1,
                                                                      XF4 ? kFmtE2M1 : kFmtE4M3, J, sw[j], XF4 ? J : 0, sx[i]);
     }
   };
   constexpr int kReads = TM * (XF4 ? 1 : 2) + TN, kProducts = kWide<XF4, T> ? 0 : TM * TN;
 
   const int nst = (a.NB + NBK - 1) / NBK;
-  constexpr std::integral_constant<int, 0> s0{};
-  constexpr std::integral_constant<int, 1> s1{};
 #pragma unroll
   for (int i = 0; i < S::kBufs; ++i) issue(i);
-  // The stage's second step is read while its first is multiplied, the next
-  // stage's first step while its second is: between the two every wave has
-  // read the whole stage, and its buffer takes the transfers of stage + kBufs.
-  wait_vmcnt<(S::kBufs - 1) * (NX + NW)>();
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-  read_scales(0);
-  read_step(s0, lds);
-  for (int st = 0; st < nst; ++st) {
-    read_step(s1, lds + st % S::kBufs * S::kStage);
-    multiply(s0);
-    interleave<kProducts, kReads>();
-    __builtin_amdgcn_sched_barrier(0);
-    wait_vmcnt<(S::kBufs - 2) * (NX + NW)>();
+  // A step's operands are read while the step before is multiplied, across
+  // the stages' edges too: before the last step every wave has read the whole
+  // stage, and its buffer takes the transfers of stage + kBufs.
+  auto arrive = [&](auto later_c) {  // this wave's transfers but those of `later` stages, then everybody's
+    wait_vmcnt<decltype(later_c)::value * (NX + NW)>();
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    issue(st + S::kBufs);
+  };
+  arrive(std::integral_constant<int, S::kBufs - 1>{});
+  read_scales(0);
+  read_step(std::integral_constant<int, 0>{}, 0);
+  auto stage = [&](int buf, int next, int next_buf, auto refill) {
+    auto inner = [&](auto js) {
+      constexpr int J = decltype(js)::value;
+      read_step(std::integral_constant<int, J + 1>{}, buf);
+      multiply(js);
+      interleave<kProducts, kReads>();
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    inner(std::integral_constant<int, 0>{});
+    if constexpr (NS == 4) {
+      inner(std::integral_constant<int, 1>{});
+      inner(std::integral_constant<int, 2>{});
+    }
+    arrive(std::integral_constant<int, S::kBufs - 2>{});
+    refill();
     __builtin_amdgcn_sched_barrier(0);
-    multiply(s1);
-    const int next = st + 1 < nst ? st + 1 : st;  // past the last stage: read again, not used
-    read_step(s0, lds + next % S::kBufs * S::kStage);
+    multiply(std::integral_constant<int, NS - 1>{});
+    read_step(std::integral_constant<int, 0>{}, next_buf);
     read_scales(next);
     interleave<kProducts, kReads + (XF4 ? TM : 0) + TN>();
     __builtin_amdgcn_sched_barrier(0);
+  };
+  // Stages whose refill is a whole one, without a branch in the loop (the
+  // compiler would move products across it); then the rest.
+  int st = 0;
+  if (direct)
+    for (const int whole = a.NB / NBK; st + S::kSuper - 1 + S::kBufs < whole; st += S::kSuper)
+#pragma unroll
+      for (int u = 0; u < S::kSuper; ++u) {
+        // st is a multiple of kSuper: where that is one of kBufs the buffers are constants
+        const int s0 = S::kSuper % S::kBufs == 0 ? 0 : st;
+        stage((s0 + u) % S::kBufs, st + u + 1, (s0 + u + 1) % S::kBufs, [&] {
+          if ((u + S::kBufs) % S::kSuper == 0) issue_scales(st + u + S::kBufs);
+          issue_full(st + u + S::kBufs, (s0 + u) % S::kBufs);
+        });
+      }
+  for (; st < nst; ++st) {
+    const int next = st + 1 < nst ? st + 1 : st;  // past the last stage: read again, not used
+    stage(st % S::kBufs, next, next % S::kBufs, [&] { issue(st + S::kBufs); });
   }
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 
@@ -507,8 +563,8 @@ template <bool XF4, class T>
 hipError_t project(const ProjectArgs& a, hipStream_t stream) {
   if (a.M <= 16) return few_go<XF4, T, 1>(a, stream);
   if (a.M <= 32) return few_go<XF4, T, 2>(a, stream);
-  if (static_cast<int64_t>((a.M + 255) / 256) * ((a.N + 255) / 256) >= 256) return tile_go<XF4, T, 256, 256, 2, 4, XF4 ? 4 : 3>(a, stream);
-  return tile_go<XF4, T, 128, 128, 2, 2, XF4 ? 4 : 3>(a, stream);
+  if (static_cast<int64_t>((a.M + 255) / 256) * ((a.N + 255) / 256) >= 256) return tile_go<XF4, T, 256, 256, 2, 4, XF4 ? 2 : 3>(a, stream);
+  return tile_go<XF4, T, 128, 128, 2, 2, XF4 ? 2 : 3>(a, stream);
 }
 
 }  // namespace
