@@ -92,18 +92,21 @@ template <bool XF4, int BM, int BN, int WM, int WN, int BUFS>
 struct TileShape {
   static constexpr int kThreads = WM * WN * 64, kWaves = WM * WN;
   static constexpr int NBK = XF4 ? 8 : 4, NS = NBK / 2;   // blocks and matrix steps a stage
-  static constexpr int kSuper = 16 / NBK;                 // stages that share a load of scales
+  // stages that share a transfer of scales: 4 bytes of each feature are few
+  // beside the stage's 48 KB, 8 of both operands' rows are not
+  static constexpr int kSuper = XF4 ? 2 : 1, kSBytes = NBK * kSuper;
+  static constexpr int kSBufs = kSuper == 1 ? BUFS : 2;
   static constexpr int XB = 128, WB = NBK * 16;           // bytes of a row a stage
   static constexpr int kBufs = BUFS;
     // LDS: the X tiles of all buffers, the W tiles, two groups' scales
   static constexpr int kXBytes = BM * XB, kWBytes = BN * WB, kStage = kXBytes + kWBytes;
   static constexpr int kWBase = BUFS * kXBytes, kSBase = BUFS * kStage;
-  static constexpr int kSRows = (XF4 ? BM : 0) + BN, kScales = kSRows * NBK * kSuper;
+  static constexpr int kSRows = (XF4 ? BM : 0) + BN, kScales = kSRows * kSBytes;
   static constexpr int NX = kXBytes / 1024 / kWaves, NW = kWBytes / 1024 / kWaves;  // transfers of a wave a stage
   static_assert(NX * 1024 * kWaves == kXBytes && NW * 1024 * kWaves == kWBytes, "whole transfers");
   static constexpr int NSG = (kSRows / 64 + kWaves - 1) / kWaves;  // groups of 64 scale rows of a wave
   static_assert(kSRows % 64 == 0 && BM % 64 == 0, "whole groups of scale rows");
-  static_assert(kBufs * kStage + 2 * kScales <= 160 * 1024, "LDS of a CU");
+  static_assert(kBufs * kStage + kSBufs * kScales <= 160 * 1024, "LDS of a CU");
 };
 
 // Chunk (16 bytes) c of row r lies at chunk c ^ swizzle(r): sixteen rows read
@@ -132,7 +135,7 @@ void tile_kernel(ProjectArgs a) {
   constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
   // The output's rows, 32 of every wave, take the stages' place at the end.
   constexpr int kPitch = BN * static_cast<int>(sizeof(T)) + 16, kOut = WM * 32 * kPitch, kVec = 16 / sizeof(T);
-  constexpr int kIn = S::kBufs * S::kStage + 2 * S::kScales, kOutBufs = 2 * kOut <= kIn ? 2 : 1;
+  constexpr int kIn = S::kBufs * S::kStage + S::kSBufs * S::kScales, kOutBufs = 2 * kOut <= kIn ? 2 : 1;
   __shared__ __attribute__((aligned(16))) char lds[kIn > kOut ? kIn : kOut];
 
   // Tiles in panels of four feature tiles: the blocks of an XCD, a run of
@@ -150,9 +153,10 @@ void tile_kernel(ProjectArgs a) {
   const char* W = static_cast<const char*>(a.w) + static_cast<int64_t>(tn) * BN * wp;
   const uint8_t* XS = static_cast<const uint8_t*>(a.xs) + static_cast<int64_t>(tm) * BM * a.NB;
   const uint8_t* WS = static_cast<const uint8_t*>(a.ws) + static_cast<int64_t>(tn) * BN * a.NB;
-  // Scales go straight to LDS too where sixteen bytes of a row are whole
-  // dwords of it; else through registers.
-  const bool direct = a.NB % 4 == 0 && a.NB >= 16;
+  // Scales go straight to LDS too where a group of a row's is whole dwords of
+  // it; else through registers.
+  constexpr int SB = S::kSBytes;
+  const bool direct = a.NB % 4 == 0 && a.NB >= SB;
 
   // Transfer i of a wave fills 1 KB of consecutive LDS, XB- or WB-byte rows of
   // it; a lane's 16 bytes are its physical chunk's.  The rows of transfer i
@@ -171,21 +175,27 @@ void tile_kernel(ProjectArgs a) {
   const i32x4 rx = rsrc_of(X, static_cast<uint32_t>(mrows) * xp);
   const i32x4 rw = rsrc_of(W, static_cast<uint32_t>(nrows) * wp);
   const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(&lds[0]));
-  // First block of a group's sixteen scales: the last group ends at the row's end.
-  auto scale_base = [&](int st) { return direct ? min(st / S::kSuper * 16, a.NB - 16) : st / S::kSuper * 16; };
+  // First block of a stage's group of scales (the last group ends at the
+  // row's end), and the group's place in LDS.
+  auto scale_base = [&](int st) { return direct ? min(st / S::kSuper * SB, a.NB - SB) : st / S::kSuper * SB; };
+  auto scale_place = [&](int st) { return S::kSBase + st / S::kSuper % S::kSBufs * S::kScales; };
   // The scales of stage st's group, straight to LDS.  A wave takes 64 rows
   // (where there are fewer groups than waves, two take the same).
   auto issue_scales = [&](int st) {
-    const uint32_t dst = lds0 + S::kSBase + (st / S::kSuper & 1) * S::kScales;
+    const uint32_t dst = lds0 + scale_place(st);
     const int first = scale_base(st);
 #pragma unroll
     for (int i = 0; i < S::NSG; ++i) {
       const int group = (wave + i * S::kWaves) % (S::kSRows / 64);  // rows of X first for MXFP4 tokens
       const bool of_x = XF4 && group * 64 < BM;
       const int row = group * 64 + lane - (XF4 && !of_x ? BM : 0), rows = of_x ? mrows : nrows;
-      dma16(rsrc_of(of_x ? XS : WS, static_cast<uint32_t>(rows) * a.NB),
-            row < rows ? row * static_cast<uint32_t>(a.NB) + first : kPastEnd,
-            __builtin_amdgcn_readfirstlane(dst + group * 1024));
+      const i32x4 range = rsrc_of(of_x ? XS : WS, static_cast<uint32_t>(rows) * a.NB);
+      const uint32_t off = row < rows ? row * static_cast<uint32_t>(a.NB) + first : kPastEnd;
+      const uint32_t to = __builtin_amdgcn_readfirstlane(dst + group * 64 * SB);
+      if constexpr (SB == 16)
+        dma16(range, off, to);
+      else
+        dma4(range, off, to);
     }
   };
   // Stage st, all of its blocks inside the rows.
@@ -208,17 +218,20 @@ void tile_kernel(ProjectArgs a) {
         issue_scales(st);
       } else {
         // rows past the tile and blocks past the row: zeros (their codes are)
-        const uint32_t dst = S::kSBase + (st / S::kSuper & 1) * S::kScales;
         const int first = scale_base(st);
         for (int group = wave; group < S::kSRows / 64; group += S::kWaves) {
           const bool of_x = XF4 && group * 64 < BM;
           const int row = group * 64 + lane - (XF4 && !of_x ? BM : 0);
-          uint32_t v[4] = {};
+          uint32_t v[SB / 4] = {};
           if (row < (of_x ? mrows : nrows)) {
             const uint8_t* p = (of_x ? XS : WS) + static_cast<int64_t>(row) * a.NB + first;
-            for (int k = 0; k < 16 && first + k < a.NB; ++k) v[k >> 2] |= static_cast<uint32_t>(p[k]) << (8 * (k & 3));
+#pragma unroll
+            for (int k = 0; k < SB; ++k)
+              if (first + k < a.NB) v[k >> 2] |= static_cast<uint32_t>(p[k]) << (8 * (k & 3));
           }
-          *reinterpret_cast<uint4*>(lds + dst + group * 1024 + lane * 16) = make_uint4(v[0], v[1], v[2], v[3]);
+#pragma unroll
+          for (int k = 0; k < SB / 4; ++k)
+            *reinterpret_cast<uint32_t*>(lds + scale_place(st) + (group * 64 + lane) * SB + k * 4) = v[k];
         }
       }
     }
@@ -247,13 +260,13 @@ void tile_kernel(ProjectArgs a) {
   int sx[TM], sw[TN];
   using scales_t = std::conditional_t<NS == 4, uint32_t, uint16_t>;
   auto read_scales = [&](int st) {
-    const char* SB = lds + S::kSBase + (st / S::kSuper & 1) * S::kScales + (st * NBK - scale_base(st)) + NS * hh;
+    const char* P = lds + scale_place(st) + (st * NBK - scale_base(st)) + NS * hh;
 #pragma unroll
     for (int i = 0; i < TM; ++i)
-      sx[i] = XF4 ? *reinterpret_cast<const scales_t*>(SB + ((wm * TM + i) * 32 + n32) * 16) : 0x7f7f;
+      sx[i] = XF4 ? *reinterpret_cast<const scales_t*>(P + ((wm * TM + i) * 32 + n32) * SB) : 0x7f7f;
 #pragma unroll
     for (int j = 0; j < TN; ++j)
-      sw[j] = *reinterpret_cast<const scales_t*>(SB + ((XF4 ? BM : 0) + (wn * TN + j) * 32 + n32) * 16);
+      sw[j] = *reinterpret_cast<const scales_t*>(P + ((XF4 ? BM : 0) + (wn * TN + j) * 32 + n32) * SB);
   };
   // Operands of step J of the stage in buffer buf: 32 rows further on is a
   // fixed distance, for the swizzle too.
