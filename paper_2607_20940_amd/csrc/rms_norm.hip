@@ -186,6 +186,20 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_bwd_kernel(NormBwd
       load8(sp + c, a.cols - c, s[i]);
       load8(yp + c, a.cols - c, g[i]);
     }
+    // the residual's gradient is not needed before the row's sum: on its way meanwhile
+    [[maybe_unused]] typename Vec8<T>::type ds[NV];
+    if constexpr (DSUM) {
+      const T* dp = static_cast<const T*>(a.dsum) + row * a.cols;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int c = (i * TPR + tid) * 8;
+        if (c + 8 <= a.cols)
+          ds[i] = *reinterpret_cast<const typename Vec8<T>::type*>(dp + c);
+        else
+#pragma unroll
+          for (int e = 0; e < 8; ++e) ds[i][e] = c + e < a.cols ? dp[c + e] : static_cast<T>(0.f);
+      }
+    }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (i * TPR + tid) * 8;
@@ -205,14 +219,11 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_bwd_kernel(NormBwd
     for (int i = 0; i < NV; ++i) {
       const int c = (i * TPR + tid) * 8;
       float d[8];
-      if constexpr (DSUM) {
-        load8(static_cast<const T*>(a.dsum) + row * a.cols + c, a.cols - c, d);
-      } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) d[e] = 0.f;
+      for (int e = 0; e < 8; ++e) {
+        d[e] = rstd * (g[i][e] - s[i][e] * k);
+        if constexpr (DSUM) d[e] += static_cast<float>(ds[i][e]);
       }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) d[e] += rstd * (g[i][e] - s[i][e] * k);
       store8(static_cast<T*>(a.dx) + row * a.cols + c, a.cols - c, d);
     }
   }
