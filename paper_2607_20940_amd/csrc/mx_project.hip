@@ -447,8 +447,20 @@ void tile_kernel(ProjectArgs a) {
 // tokens are the 16 columns of B.  Sixteen features a block, whose waves take
 // pieces of the contraction and join their sums in LDS.  A lane group (lane /
 // 16) takes blocks 4 g .. 4 g + 3 of sixteen, one per matrix step, so its
-// codes are 64 consecutive bytes and its scales four.
+// codes are 64 consecutive bytes and its scales four.  What counts is bytes on
+// their way: each wave has its next piece loading.
 constexpr int kFewWaves = 4;
+
+// Four scale bytes, of which the first n are there.
+__device__ inline uint32_t four_scales(const uint8_t* p, int n) {
+  typedef uint32_t u32_u __attribute__((aligned(1)));
+  if (n >= 4) return *reinterpret_cast<const u32_u*>(p);
+  uint32_t v = 0;
+#pragma unroll
+  for (int i = 0; i < 3; ++i)
+    if (i < n) v |= static_cast<uint32_t>(p[i]) << (8 * i);
+  return v;
+}
 
 template <bool XF4, class T, int TT>
 __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(ProjectArgs a) {
@@ -465,27 +477,32 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(ProjectArgs a) {
   for (int t = 0; t < TT; ++t) acc[t] = f32x4{};
 
   const int nsb = (a.NB + 15) / 16;
+  struct Weights {
+    i32x4 v[4];
+    uint32_t s;
+  } now, later;
+  auto fetch = [&](Weights& w, int sb) {
+    const int b0 = sb * 16 + g * 4, left = a.NB - b0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w.v[j] = j < left ? *reinterpret_cast<const i32x4*>(W + (b0 + j) * 16) : i32x4{};
+    w.s = four_scales(WS + b0, left);
+  };
+  if (wave < nsb) fetch(now, wave);
   for (int sb = wave; sb < nsb; sb += kFewWaves) {
     const int b0 = sb * 16 + g * 4, left = a.NB - b0;
-    i32x4 wv[4], xv[TT][4][XF4 ? 1 : 2];
-    uint32_t sw = 0, sx[TT];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) wv[j] = j < left ? *reinterpret_cast<const i32x4*>(W + (b0 + j) * 16) : i32x4{};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) sw |= j < left ? static_cast<uint32_t>(WS[b0 + j]) << (8 * j) : 0u;
+    i32x4 xv[TT][4][XF4 ? 1 : 2];
+    uint32_t sx[TT];
 #pragma unroll
     for (int t = 0; t < TT; ++t) {
       const int64_t tok = t * 16 + m;
       const bool ok = tok < a.M;
       const char* X = static_cast<const char*>(a.x) + (ok ? tok : 0) * xp;
-      const uint8_t* XS = static_cast<const uint8_t*>(a.xs) + (ok ? tok : 0) * a.NB;
-      sx[t] = XF4 ? 0u : 0x7f7f7f7fu;
+      sx[t] = 0x7f7f7f7fu;
+      if constexpr (XF4) sx[t] = ok ? four_scales(static_cast<const uint8_t*>(a.xs) + tok * a.NB + b0, left) : 0u;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         if constexpr (XF4) {
-          const bool in = ok && j < left;
-          xv[t][j][0] = in ? *reinterpret_cast<const i32x4*>(X + (b0 + j) * 16) : i32x4{};
-          sx[t] |= in ? static_cast<uint32_t>(XS[b0 + j]) << (8 * j) : 0u;
+          xv[t][j][0] = ok && j < left ? *reinterpret_cast<const i32x4*>(X + (b0 + j) * 16) : i32x4{};
         } else if constexpr (kWide<XF4, T>) {
           xv[t][j][0] = ok && j < left ? *reinterpret_cast<const i32x4*>(X + (b0 + j) * 32) : i32x4{};
           xv[t][j][1] = ok && j < left ? *reinterpret_cast<const i32x4*>(X + (b0 + j) * 32 + 16) : i32x4{};
@@ -497,13 +514,14 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(ProjectArgs a) {
         }
       }
     }
+    if (sb + kFewWaves < nsb) fetch(later, sb + kFewWaves);
     auto step = [&](auto js) {
       constexpr int J = decltype(js)::value;
       if constexpr (kWide<XF4, T>) {
-        const float f = mx_scale((sw >> (8 * J)) & 255u);
+        const float f = mx_scale((now.s >> (8 * J)) & 255u);
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
-          const bf16x8 wa = expand4(static_cast<uint32_t>(wv[J][p]), f);
+          const bf16x8 wa = expand4(static_cast<uint32_t>(now.v[J][p]), f);
 #pragma unroll
           for (int t = 0; t < TT; ++t) {
             const i32x4 v = xv[t][J][p >> 1];
@@ -520,14 +538,15 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(ProjectArgs a) {
           b = widen(xv[t][J][0]);
         else
           b = __builtin_shufflevector(xv[t][J][0], xv[t][J][1], 0, 1, 2, 3, 4, 5, 6, 7);
-        acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(widen(wv[J]), b, acc[t], kFmtE2M1, XF4 ? kFmtE2M1 : kFmtE4M3,
-                                                                  J, sw, XF4 ? J : 0, sx[t]);
+        acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(widen(now.v[J]), b, acc[t], kFmtE2M1,
+                                                                  XF4 ? kFmtE2M1 : kFmtE4M3, J, now.s, XF4 ? J : 0, sx[t]);
       }
     };
     step(std::integral_constant<int, 0>{});
     step(std::integral_constant<int, 1>{});
     step(std::integral_constant<int, 2>{});
     step(std::integral_constant<int, 3>{});
+    now = later;
   }
   if (wave > 0) {
 #pragma unroll

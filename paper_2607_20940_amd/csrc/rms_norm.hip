@@ -161,70 +161,87 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_kernel(NormArgs a)
   }
 }
 
+// Eight values as they lie in memory (zeros past n).
+template <class T>
+__device__ inline typename Vec8<T>::type raw8(const T* p, int n) {
+  typename Vec8<T>::type v;
+  if (n >= 8) return *reinterpret_cast<const typename Vec8<T>::type*>(p);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = e < n ? p[e] : static_cast<T>(0.f);
+  return v;
+}
+
 // Gradients.  A block walks over rows blockIdx.x, + blocks, ... (kRows at a
 // time) and keeps its share of dweight in registers; the shares are summed
-// over the block's rows in LDS and over the blocks by a second launch.
+// over the block's rows in LDS and over the blocks by a second launch.  A row
+// is held as it lies in memory (half the registers in bf16), and the next one
+// is on its way while this one's sum goes round (not with 1024 threads a row,
+// which have no registers for two).  512 blocks: with 768 or 1024 the last
+// rows leave CUs idle or the shares cost more (27840 x 5120 bf16, forward and
+// backward: 428, 457, 435 us; 560 with a row at a time).
 template <class T, bool DSUM, int TPR, int NV>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_bwd_kernel(NormBwdArgs a) {
   constexpr int kThreads = TPR > 256 ? TPR : 256, kRows = kThreads / TPR;
+  constexpr bool kAhead = TPR <= 256;
+  typedef typename Vec8<T>::type raw_t;
   __shared__ float red[2][TPR / 64];
   __shared__ float share[kRows > 1 ? TPR * NV * 8 : 1];
   const int tid = threadIdx.x % TPR, sub = threadIdx.x / TPR;
-  const T* w = static_cast<const T*>(a.weight);
+  struct Row {
+    raw_t s[NV], g[NV], d[DSUM ? NV : 1];
+    float rstd;
+  };
+  raw_t w[NV];
+  auto at = [&](int i) { return (i * TPR + tid) * 8; };
+#pragma unroll
+  for (int i = 0; i < NV; ++i) w[i] = raw8(static_cast<const T*>(a.weight) + at(i), a.cols - at(i));
+  auto fetch = [&](Row& r, int64_t row) {
+    r.rstd = a.rstd[row];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = at(i), n = a.cols - c;
+      r.s[i] = raw8(static_cast<const T*>(a.sum) + row * a.sum_stride + c, n);
+      r.g[i] = raw8(static_cast<const T*>(a.dy) + row * a.cols + c, n);
+      if constexpr (DSUM) r.d[i] = raw8(static_cast<const T*>(a.dsum) + row * a.cols + c, n);
+    }
+  };
   float dw[NV][8] = {};
-  int it = 0;
-  for (int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + sub; row < a.rows;
-       row += static_cast<int64_t>(a.blocks) * kRows, ++it) {
-    const T* sp = static_cast<const T*>(a.sum) + row * a.sum_stride;
-    const T* yp = static_cast<const T*>(a.dy) + row * a.cols;
-    const float rstd = a.rstd[row];
-    float s[NV][8], g[NV][8];
+  const int64_t step = static_cast<int64_t>(a.blocks) * kRows;
+  int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + sub;
+  Row cur, next;
+  if (row < a.rows) fetch(cur, row);
+  for (int it = 0; row < a.rows; row += step, ++it) {
+    const bool more = row + step < a.rows;
+    if (kAhead && more) fetch(next, row + step);
     float inner = 0.f;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (i * TPR + tid) * 8;
-      load8(sp + c, a.cols - c, s[i]);
-      load8(yp + c, a.cols - c, g[i]);
-    }
-    // the residual's gradient is not needed before the row's sum: on its way meanwhile
-    [[maybe_unused]] typename Vec8<T>::type ds[NV];
-    if constexpr (DSUM) {
-      const T* dp = static_cast<const T*>(a.dsum) + row * a.cols;
-#pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const int c = (i * TPR + tid) * 8;
-        if (c + 8 <= a.cols)
-          ds[i] = *reinterpret_cast<const typename Vec8<T>::type*>(dp + c);
-        else
-#pragma unroll
-          for (int e = 0; e < 8; ++e) ds[i][e] = c + e < a.cols ? dp[c + e] : static_cast<T>(0.f);
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (i * TPR + tid) * 8;
-      float wv[8];
-      load8(w + c, a.cols - c, wv);
+    for (int i = 0; i < NV; ++i)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        dw[i][e] = __builtin_fmaf(g[i][e] * rstd, s[i][e], dw[i][e]);
-        g[i][e] *= wv[e];
-        inner = __builtin_fmaf(g[i][e], s[i][e], inner);
+        const float s = static_cast<float>(cur.s[i][e]), g = static_cast<float>(cur.g[i][e]);
+        dw[i][e] = __builtin_fmaf(g * cur.rstd, s, dw[i][e]);
+        inner = __builtin_fmaf(g * static_cast<float>(w[i][e]), s, inner);
       }
-    }
     // with more than one wave a row, alternating slots save a second barrier
     inner = row_sum<TPR>(inner, red[it & 1], tid) * a.inv_cols;
-    const float k = rstd * rstd * inner;
+    const float k = cur.rstd * cur.rstd * inner;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = (i * TPR + tid) * 8;
+      const int c = at(i);
       float d[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        d[e] = rstd * (g[i][e] - s[i][e] * k);
-        if constexpr (DSUM) d[e] += static_cast<float>(ds[i][e]);
+        const float g = static_cast<float>(cur.g[i][e]) * static_cast<float>(w[i][e]);
+        d[e] = cur.rstd * (g - static_cast<float>(cur.s[i][e]) * k);
+        if constexpr (DSUM) d[e] += static_cast<float>(cur.d[i][e]);
       }
       store8(static_cast<T*>(a.dx) + row * a.cols + c, a.cols - c, d);
+    }
+    if (more) {
+      if constexpr (kAhead)
+        cur = next;
+      else
+        fetch(cur, row + step);
     }
   }
   float* out = a.blocks > 1 ? a.partial + static_cast<int64_t>(blockIdx.x) * a.cols : a.dweight;
@@ -251,18 +268,22 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_bwd_kernel(NormBwd
   }
 }
 
-// dweight = sum of the blocks' shares: 16 threads a column, each every 16th
-// share, joined in order.
+// dweight = sum of the blocks' shares: 32 threads a column, each every 32nd
+// share with many of them on their way, joined in order.
 __global__ __launch_bounds__(1024) void norm_dweight_kernel(NormBwdArgs a) {
-  __shared__ float part[16][64];
-  const int c = blockIdx.x * 64 + threadIdx.x % 64, g = threadIdx.x / 64;
+  __shared__ float part[32][33];
+  const int x = threadIdx.x % 32, g = threadIdx.x / 32, c = blockIdx.x * 32 + x;
   float s = 0.f;
-  if (c < a.cols)
-    for (int b = g; b < a.blocks; b += 16) s += a.partial[static_cast<int64_t>(b) * a.cols + c];
-  part[g][threadIdx.x % 64] = s;
+  if (c < a.cols) {
+    const float* p = a.partial + c;
+#pragma unroll 16
+    for (int b = g; b < a.blocks; b += 32) s += p[static_cast<int64_t>(b) * a.cols];
+  }
+  part[g][x] = s;
   __syncthreads();
   if (g == 0 && c < a.cols) {
-    for (int i = 1; i < 16; ++i) s += part[i][threadIdx.x];
+#pragma unroll
+    for (int i = 1; i < 32; ++i) s += part[i][x];
     a.dweight[c] = s;
   }
 }
@@ -344,7 +365,7 @@ hipError_t launch_norm(const NormArgs& a, bool bf16, bool e4m3, hipStream_t stre
 int32_t norm_bwd_blocks(int64_t rows, int32_t cols) {
   const RowShape s = row_shape(cols);
   const int64_t per = s.tpr >= 256 ? 1 : 256 / s.tpr, want = (rows + per - 1) / per;
-  return static_cast<int32_t>(std::min<int64_t>(want, 1024));
+  return static_cast<int32_t>(std::min<int64_t>(want, 512));
 }
 
 hipError_t launch_norm_bwd(const NormBwdArgs& a, bool bf16, hipStream_t stream) {
@@ -356,7 +377,7 @@ hipError_t launch_norm_bwd(const NormBwdArgs& a, bool bf16, hipStream_t stream) 
       e = a.dsum ? bwd_tpr<float, true>(a, stream) : bwd_tpr<float, false>(a, stream);
     if (e != hipSuccess || a.blocks == 1) return e;
   }
-  hipLaunchKernelGGL(norm_dweight_kernel, dim3((a.cols + 63) / 64), dim3(1024), 0, stream, a);
+  hipLaunchKernelGGL(norm_dweight_kernel, dim3((a.cols + 31) / 32), dim3(1024), 0, stream, a);
   return hipGetLastError();
 }
 
