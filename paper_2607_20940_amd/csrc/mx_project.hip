@@ -591,12 +591,42 @@ hipError_t tile_go(const ProjectArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
+// Microseconds that `tiles` tiles of a shape take, of which n may share a CU:
+// whole rounds, then a rest with fewer blocks a CU.  (p0 + p1 n) a stage and
+// q0 + q1 n besides, fitted to ten products of 600 to 27840 tokens.
+struct ShapeCost {
+  int share;
+  double p0, p1, q0, q1;
+  double operator()(int64_t tiles, int stages) const {
+    auto round = [&](int64_t n) { return (p0 + p1 * static_cast<double>(n)) * stages + q0 + q1 * static_cast<double>(n); };
+    const int64_t slots = 256 * share, rest = tiles % slots;
+    return static_cast<double>(tiles / slots) * round(share) + (rest ? round((rest + 255) / 256) : 0.0);
+  }
+};
+
+// Which kernel.  Up to 32 tokens the weights' bytes are all that counts.
+// Above, large tiles need the fewest LDS bytes a product and small tiles fill
+// the CUs sooner.  8-bit tokens: 128 x 256 tiles, two blocks a CU, one's
+// outputs leaving while the other multiplies (12870 x 1536 -> 4608: 119 us;
+// one 256 x 256 block a CU 123, 128 x 128 tiles 148), or 64 x 128
+// (600 x 600 -> 1000: 9.5 us against 16.7).  MXFP4 tokens, whose products are
+// done twice as fast from LDS: 256 x 256 (27840 x 5120 -> 15360: 1.20 ms;
+// 128 x 256 tiles 1.54), or 64 x 128 (600 x 608 -> 1000: 9.0 us against 18.7).
 template <bool XF4, class T>
 hipError_t project(const ProjectArgs& a, hipStream_t stream) {
   if (a.M <= 16) return few_go<XF4, T, 1>(a, stream);
   if (a.M <= 32) return few_go<XF4, T, 2>(a, stream);
-  if (static_cast<int64_t>((a.M + 255) / 256) * ((a.N + 255) / 256) >= 256) return tile_go<XF4, T, 256, 256, 2, 4, XF4 ? 2 : 3>(a, stream);
-  return tile_go<XF4, T, 128, 128, 2, 2, XF4 ? 2 : 3>(a, stream);
+  constexpr int kLargeM = XF4 ? 256 : 128;
+  constexpr ShapeCost small = XF4 ? ShapeCost{3, 0., 0.63, 3., 0.} : ShapeCost{3, 0.3, 0.2, 3., 1.};
+  constexpr ShapeCost large = XF4 ? ShapeCost{1, 0., 1.74, 11.3, 0.} : ShapeCost{2, 0.43, 0.57, 5., 3.};
+  const int stages = (a.NB + (XF4 ? 7 : 3)) / (XF4 ? 8 : 4);
+  const int64_t n_small = static_cast<int64_t>((a.M + 63) / 64) * ((a.N + 127) / 128);
+  const int64_t n_large = static_cast<int64_t>((a.M + kLargeM - 1) / kLargeM) * ((a.N + 255) / 256);
+  if (small(n_small, stages) < large(n_large, stages)) return tile_go<XF4, T, 64, 128, 1, 4, XF4 ? 2 : 3>(a, stream);
+  if constexpr (XF4)
+    return tile_go<XF4, T, 256, 256, 2, 4, 2>(a, stream);
+  else
+    return tile_go<XF4, T, 128, 256, 1, 4, 2>(a, stream);
 }
 
 }  // namespace
