@@ -469,7 +469,8 @@ mssa_status mssa_head_ring_roll(mssa_plan plan, int32_t ring_frames, int32_t* ri
  *     3, 4, 6).  With NB = ceil(cols / 32) a row's codes are 16 NB bytes,
  *     value 2 i in the low half of byte i, and its scales NB bytes; the
  *     codes past `cols` in the last block are zeros.  Rows follow one another
- *     without gaps.  Code and scale arrays are 16-byte aligned.
+ *     without gaps.  Code and scale arrays are 16-byte aligned (for the
+ *     conversions 4-byte aligned codes are enough: rows inside an array).
  *   - 8-bit rows: OCP e4m3 codes, 32 NB bytes a row (zeros past `cols`),
  *     with one fp32 scale a row that multiplies them. */
 typedef enum {

@@ -91,15 +91,15 @@ def mx_pack(code):
 
 def mx_unpack(packed):
     packed = np.asarray(packed, dtype=np.int64)
-    return np.stack((packed & 15, packed >> 4), -1).reshape(packed.shape[0], -1)
+    return np.stack((packed & 15, packed >> 4), -1).reshape(packed.shape[0], 2 * packed.shape[1])
 
 
 def mx_values(packed, byte):
     """Values [rows, padded cols] of packed codes and scale bytes."""
-    v = e2m1_value(mx_unpack(packed)).reshape(len(packed), -1, BLOCK)
+    v = e2m1_value(mx_unpack(packed)).reshape(len(packed), 2 * np.shape(packed)[1] // BLOCK, BLOCK)
     byte = np.asarray(byte, dtype=np.float64)
     scale = np.where(byte == 255, np.nan, 2.0 ** (byte - 127))
-    return (v * scale[..., None]).reshape(len(packed), -1)
+    return (v * scale[..., None]).reshape(len(packed), 2 * np.shape(packed)[1])
 
 
 # ------------------------------------------------------------------ product

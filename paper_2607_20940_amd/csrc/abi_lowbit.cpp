@@ -57,8 +57,7 @@ mssa_status mx_convert(const char* who, bool quantize, int64_t rows, int32_t col
     if (rows == 0) return MSSA_OK;
     if (!values || !codes || !scales) return fail(MSSA_ERR_INVALID_ARG, "null argument");
     if (!aligned_to(values, elem_bytes(dtype))) return fail(MSSA_ERR_INVALID_ARG, "values must be aligned to their type");
-    if (!aligned16(codes) || !aligned16(scales))
-      return fail(MSSA_ERR_INVALID_ARG, "codes and scales must be 16-byte aligned");
+    if (!aligned_to(codes, 4)) return fail(MSSA_ERR_INVALID_ARG, "codes must be 4-byte aligned");
     mssa::MxArgs a{};
     a.in = quantize ? values : nullptr;
     a.out = quantize ? nullptr : const_cast<void*>(values);
