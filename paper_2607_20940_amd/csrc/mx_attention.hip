@@ -50,18 +50,14 @@ __device__ inline bf16x8 expand8(uint32_t codes, float scale) {
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// A value that all lanes share, in scalar registers.
-__device__ inline int64_t uniform(int64_t v) {
-  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<int>(v));
-  const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<int>(v >> 32));
-  return static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
-}
+// A value that all lanes share, in a scalar register.
+__device__ inline uint32_t uniform(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
 
 // Sum over the wave's lanes up to this one.
-__device__ inline int64_t wave_prefix(int64_t v) {
+__device__ inline uint32_t wave_prefix(uint32_t v) {
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) {
-    const int64_t u = __shfl_up(v, d);
+    const uint32_t u = __shfl_up(v, d);
     if (static_cast<int>(threadIdx.x & 63) >= d) v += u;
   }
   return v;
@@ -70,10 +66,11 @@ __device__ inline int64_t wave_prefix(int64_t v) {
 // How the work is shared out, whatever the lengths are.  An item is the query
 // rows of one block (a.items of them per sequence) against their sequence's
 // whole context; all items' tiles stand in a row, sequence by sequence and
-// item by item, and worker i of W takes tiles i T / W to (i + 1) T / W.  An
-// item that one worker holds whole is written by it; the sums of one that
-// several share go to slots, 2 i for the first item of worker i and 2 i + 1
-// for a later one (which then is its last), and a second launch joins them.
+// item by item, and each worker takes as many of them as every other (or one
+// more).  An item that one worker holds whole is written by it; the sums of
+// one that several share go to slots, 2 i for the first item of worker i and
+// 2 i + 1 for a later one (which then is its last), and a second launch joins
+// them.  (All tiles of a call are fewer than 2^31: the plan's check.)
 constexpr int kTile = 64;  // tokens of a tile
 
 __device__ inline int64_t tokens_of(const MxAttnArgs& a, int b) {
@@ -82,6 +79,11 @@ __device__ inline int64_t tokens_of(const MxAttnArgs& a, int b) {
 }
 __device__ inline int tiles_of(const MxAttnArgs& a, int b) { return static_cast<int>((tokens_of(a, b) + kTile - 1) / kTile); }
 
+// The same for a sequence that the whole wave shares, in scalar registers (the
+// loops' bounds and the last tile's mask are branches then, not lane masks).
+__device__ inline int len_of(const MxAttnArgs& a, int b) { return __builtin_amdgcn_readfirstlane(static_cast<int>(tokens_of(a, b))); }
+__device__ inline int tiles_in(int len) { return static_cast<int>((static_cast<int64_t>(len) + kTile - 1) / kTile); }
+
 // Tokens of tile t below `end`, at most a tile's; none past it.
 __device__ inline int left_of(int end, int t) {
   const int64_t left = end - static_cast<int64_t>(t) * kTile;
@@ -89,63 +91,67 @@ __device__ inline int left_of(int end, int t) {
 }
 
 struct Shares {
-  int64_t all;  // tiles of all items
-  int64_t workers;
-  __device__ int64_t first(int64_t i) const { return all * i / workers; }
-  __device__ int64_t worker_of(int64_t x) const { return ((x + 1) * workers - 1) / all; }
+  uint32_t all, workers, each, more;  // tiles of all items; the first `more` workers take each + 1, the others each
+  __device__ uint32_t first(uint32_t i) const { return i * each + min(i, more); }
+  __device__ uint32_t worker_of(uint32_t x) const {
+    const uint32_t big = more * (each + 1);
+    return x < big ? x / (each + 1) : more + (x - big) / each;
+  }
 };
 // Tiles of the sequences before b, times the items of a sequence, and the
 // shares.  Lengths are read 64 at a time: every lane of a wave calls these.
-__device__ inline Shares shares_of(const MxAttnArgs& a, int b, int64_t* before) {
+__device__ inline Shares shares_of(const MxAttnArgs& a, int b, uint32_t* before) {
   const int lane = threadIdx.x & 63;
-  int64_t all = 0, pre_b = 0;
-  if (!a.kv_len) {
-    all = static_cast<int64_t>(tiles_of(a, 0)) * a.batch;
-    pre_b = static_cast<int64_t>(tiles_of(a, 0)) * b;
+  uint32_t all = 0, pre_b = 0;
+  if (!a.kv_len || a.batch == 1) {
+    const uint32_t one = tiles_in(len_of(a, 0));
+    all = one * a.batch;
+    pre_b = one * b;
   } else {
     for (int c = 0; c < a.batch; c += 64) {
-      const int64_t pre = wave_prefix(c + lane < a.batch ? tiles_of(a, c + lane) : 0);
+      const uint32_t pre = wave_prefix(c + lane < a.batch ? tiles_of(a, c + lane) : 0);
       if (b >= c + 64)
         pre_b = all + __shfl(pre, 63);
       else if (b > c)
         pre_b = all + __shfl(pre, b - c - 1);
       all += __shfl(pre, 63);
     }
+    all = uniform(all);
+    pre_b = uniform(pre_b);
   }
-  all = uniform(all);
-  if (before) *before = uniform(pre_b) * a.items;
-  return {all * a.items, all * a.items < a.workers ? all * a.items : a.workers};
+  if (before) *before = pre_b * a.items;
+  all *= a.items;
+  const uint32_t workers = min(all, static_cast<uint32_t>(a.workers)), each = workers ? all / workers : 0;
+  return {all, workers, each, all - each * workers};
 }
 // The sequence, item and tile that tile x of all is.
 struct Spot {
   int b, item, tile;
 };
-__device__ inline Spot locate(const MxAttnArgs& a, int64_t x) {
+__device__ inline Spot locate(const MxAttnArgs& a, uint32_t x) {
   const int lane = threadIdx.x & 63;
-  int64_t y = x / a.items;  // sequences' tiles before: the sequence holds tiles items * P .. of all
-  int b = 0;
-  int64_t t = tiles_of(a, 0), base = 0;
-  if (!a.kv_len) {
-    b = static_cast<int>(y / t);
+  const uint32_t y = x / a.items;  // sequences' tiles before: the sequence holds tiles items * P .. of all
+  uint32_t b = 0, t = tiles_in(len_of(a, 0)), base = 0;
+  if (!a.kv_len || a.batch == 1) {
+    b = y / t;
     base = t * b;
   } else {
     for (int c = 0; c < a.batch; c += 64) {
-      const int64_t mine = c + lane < a.batch ? tiles_of(a, c + lane) : 0;
-      const int64_t pre = wave_prefix(mine);
+      const uint32_t mine = c + lane < a.batch ? tiles_of(a, c + lane) : 0;
+      const uint32_t pre = wave_prefix(mine);
       const uint64_t past = __ballot(base + pre > y);
       if (past) {
         const int i = __builtin_ctzll(past);
         b = c + i;
-        t = __shfl(mine, i);
-        base += __shfl(pre, i) - t;
+        t = uniform(__shfl(mine, i));
+        base = uniform(base + __shfl(pre, i) - t);
         break;
       }
       base += __shfl(pre, 63);
     }
   }
-  t = uniform(t);
-  const int64_t in = x - uniform(base) * a.items, item = in / t;
-  return {__builtin_amdgcn_readfirstlane(b), static_cast<int>(item), static_cast<int>(in - item * t)};
+  const uint32_t in = x - base * a.items, item = in / t;
+  return {static_cast<int>(uniform(b)), static_cast<int>(item), static_cast<int>(in - item * t)};
 }
 
 // Row `row` of slot `slot`: its sums, and its maximum and sum of exponentials
@@ -211,6 +217,14 @@ __device__ inline __amdgpu_buffer_rsrc_t range_of(const void* p, uint32_t bytes)
                                            __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
 }
 
+template <int NS>
+__device__ inline auto load_codes(__amdgpu_buffer_rsrc_t r, uint32_t off) {
+  if constexpr (NS == 4)
+    return __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0);
+  else
+    return __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0);
+}
+
 // Order of a run of NM matrix instructions and their ND LDS reads: LEAD reads
 // first, then a matrix instruction and its share of reads in turn.
 template <int NM, int ND, int LEAD>
@@ -224,53 +238,93 @@ __device__ inline void interleave() {
   __builtin_amdgcn_sched_group_barrier(0x008, NM - (ND - LEAD) / (ND / NM), 0);
 }
 
+// Many rows.  A wave's tile is two phases: matrix instructions (O += V^T P of
+// the tile before, then S = K Q^T), and vector work (softmax, and expanding
+// the next tile's codes).  Eight waves are two groups, one wave of each per
+// SIMD, and the second group runs one phase behind the first, so that a SIMD's
+// matrix core and vector unit both have a wave at work; a barrier ends each
+// phase.  The first group expands K, the second V.  Four waves (fewer rows)
+// are one group that expands both; two such blocks share a CU.
+//
+// With phases counted from the first group's S of tile t in 2 t: K of tile t + 1
+// is written in 2 t + 1 and read in 2 t + 2 and 2 t + 3, V of tile t + 1 written
+// in 2 t + 2 (four waves: 2 t + 1) and read in 2 t + 4 and 2 t + 5, each into the
+// buffer whose tile (two before) was last read in 2 t - 1 and 2 t + 1 (2 t).
 template <int D, int NW>
 __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) void attn_kernel(MxAttnArgs a) {
-  constexpr int KS = D / 16, DB = D / 32, kThreads = NW * 64, kTileElems = kTile * 128;  // 256-byte rows for both D
-  constexpr int kBlocks = kTile * DB * 2;                  // MXFP4 blocks of a tile, K then V
-  constexpr int NL = (kBlocks + kThreads - 1) / kThreads;  // per thread
-  static_assert(kBlocks % 128 == 0, "K and V split at a wave's edge");
+  constexpr int KS = D / 16, DB = D / 32, NS = D / 32, kTileElems = kTile * 128;  // 256-byte rows for both D
+  constexpr int NP = NW == 8 ? 1 : 2;  // operands (K, V) that a thread expands
+  typedef uint32_t codes_t __attribute__((ext_vector_type(NS)));
   __shared__ __attribute__((aligned(16))) __bf16 lds[2][2][kTileElems];  // [buffer][K | V]
 
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, hh = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), second = NW == 8 ? wave >> 2 : 0;
   const int tiles_r = a.items / a.kv_heads;
   // Workers next to one another share key heads: each XCD takes a run of them.
   const int worker = xcd_remap(blockIdx.x, gridDim.x);
   Spot at{worker / a.items, worker % a.items, 0};
-  int64_t todo = 0;
+  int todo = 0;  // tiles
   if (a.workers) {
     const Shares sh = shares_of(a, 0, nullptr);
-    if (worker >= sh.workers) return;
-    const int64_t x0 = sh.first(worker);
-    todo = sh.first(worker + 1) - x0;
+    if (static_cast<uint32_t>(worker) >= sh.workers) return;
+    const uint32_t x0 = sh.first(worker);
+    todo = static_cast<int>(sh.first(worker + 1) - x0);
     at = locate(a, x0);
   }
 
-  // A thread's MXFP4 blocks of a tile: block p is token (p / DB) % 64, piece
-  // p % DB, of K below kBlocks / 2, else of V (the same for a whole wave).
+  // 256 threads expand an operand's tile: four neighbours a token, D / 4 values
+  // each.  Sixteen lanes take tokens 0, 4, 8, 12 of sixteen, whose swizzles
+  // differ where their quarters' chunks agree: no bank conflicts.
   const uint32_t token_rows = static_cast<uint32_t>(a.kv_heads);
-  uint32_t c_off[NL], e_off[NL];
-  int dst[NL][4];
-#pragma unroll
-  for (int i = 0; i < NL; ++i) {
-    const int p = tid + i * kThreads, tok = (p / DB) % kTile, piece = p % DB;
-    e_off[i] = tok * token_rows * DB + piece;
-    c_off[i] = e_off[i] * 16;
-#pragma unroll
-    for (int c = 0; c < 4; ++c) dst[i][c] = (p >= kBlocks / 2 ? kTileElems : 0) + swz256(tok, piece * 32 + c * 8);
-  }
+  const int tok = (wave & 3) * 16 + ((lane >> 2) & 3) * 4 + (lane >> 4), quarter = lane & 3;
+  const uint32_t c_off = tok * token_rows * (D / 2) + quarter * (D / 8);
+  const uint32_t e_off = tok * token_rows * DB + quarter * (D / 4) / 32;
+  const int dst = swz256(tok, quarter * (D / 4));
   const float c = a.scale_log2e;
   const int k_rd = swz256(n, hh * 8);
   const int t_row = 4 * (lane >> 5) + ((lane & 15) >> 2);
   const int t_col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+  // The end of a phase.  Codes on their way to registers need not have arrived.
+  auto phase_end = [&]() {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
 
   for (int seg = 0;; ++seg) {
-    const int len = static_cast<int>(tokens_of(a, at.b)), nt = tiles_of(a, at.b);
+    const int len = len_of(a, at.b), nt = tiles_in(len);
     const int kvh = at.item / tiles_r, rt = at.item - kvh * tiles_r;
-    const int t0 = at.tile, t1 = a.workers && todo < nt - t0 ? t0 + static_cast<int>(todo) : nt;
+    const int t0 = at.tile, t1 = a.workers && todo < nt - t0 ? t0 + todo : nt;
     const bool whole = t0 == 0 && t1 == nt;
     todo -= t1 - t0;
+
+    // Reads past the sequence's last token return zeros: codes of zeros.
+    codes_t codes[NP];
+    uint32_t se[NP];
+    const int64_t row0 = static_cast<int64_t>(at.b) * a.cache_tokens * a.kv_heads + kvh;
+    auto fetch = [&](int t) {
+      const int64_t first = row0 + static_cast<int64_t>(t) * kTile * a.kv_heads;
+      const int left = left_of(len, t);
+      const uint32_t rows = left ? (left - 1) * token_rows + 1 : 0u;
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        const bool is_v = NW == 8 ? second != 0 : i == 1;
+        codes[i] = load_codes<NS>(range_of(static_cast<const char*>(is_v ? a.vc : a.kc) + first * (D / 2), rows * (D / 2)), c_off);
+        se[i] = __builtin_amdgcn_raw_buffer_load_b8(
+            range_of(static_cast<const char*>(is_v ? a.vs : a.ks) + first * DB, rows * DB), e_off, 0, 0);
+      }
+    };
+    auto put = [&](int buf) {
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        const float f = mx_scale(se[i]);
+        __bf16* P = lds[buf][NW == 8 ? second : i];
+#pragma unroll
+        for (int k = 0; k < NS; ++k) *reinterpret_cast<bf16x8*>(P + (dst ^ (k * 8))) = expand8(codes[i][k], f);
+      }
+    };
+    if (t0 < t1) fetch(t0);
+
     const int r_in = wave * 32 + n, r = rt * (NW * 32) + r_in;
     const bool ok = r < a.rows;
     const RowPlace row = row_place(a, at.b, kvh, ok ? r : 0, D);
@@ -281,52 +335,30 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
       qf[ks] = ok ? v : bf16x8{};
     }
 
-    // Reads past the sequence's last token return zeros: codes of zeros.
-    i32x4 codes[NL];
-    uint32_t se[NL];
-    const int64_t row0 = static_cast<int64_t>(at.b) * a.cache_tokens * a.kv_heads + kvh;
-    auto fetch = [&](int t) {
-      const int64_t first = row0 + static_cast<int64_t>(t) * kTile * a.kv_heads;
-      const uint32_t rows = (left_of(len, t) - 1) * token_rows + 1;
-#pragma unroll
-      for (int i = 0; i < NL; ++i) {
-        const int p = wave * 64 + i * kThreads;
-        if (p >= kBlocks) continue;
-        const bool is_v = p >= kBlocks / 2;
-        codes[i] = __builtin_bit_cast(
-            i32x4, __builtin_amdgcn_raw_buffer_load_b128(
-                       range_of(static_cast<const char*>(is_v ? a.vc : a.kc) + first * (D / 2), rows * (D / 2)), c_off[i], 0, 0));
-        se[i] = __builtin_amdgcn_raw_buffer_load_b8(
-            range_of(static_cast<const char*>(is_v ? a.vs : a.ks) + first * DB, rows * DB), e_off[i], 0, 0);
-      }
-    };
-    auto put = [&](int buf) {
-#pragma unroll
-      for (int i = 0; i < NL; ++i) {
-        if (wave * 64 + i * kThreads >= kBlocks) continue;
-        const float f = mx_scale(se[i]);
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-          *reinterpret_cast<bf16x8*>(&lds[buf][0][dst[i][c]]) = expand8(static_cast<uint32_t>(codes[i][c]), f);
-      }
-    };
-
-    f32x16 o[DB];
+    f32x16 o[DB], s[2];
 #pragma unroll
     for (int db = 0; db < DB; ++db) o[db] = f32x16{};
     float m = kNoMax, l = 0.f;  // running maximum (base 2), this lane's share of the sum
-    if (t0 < t1) {
-      fetch(t0);
-      put(0);
-    }
-    __syncthreads();
-    for (int t = t0; t < t1; ++t) {
-      const int buf = (t - t0) & 1;
-      const bool more = t + 1 < t1;
-      if (more) fetch(t + 1);
-      const __bf16* Ks = lds[buf][0];
+    bf16x8 pb[2][2];
+    auto add_pv = [&](int buf) {
       const __bf16* Vs = lds[buf][1];
-      f32x16 s[2];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int cc = 0; cc < 2; ++cc)
+#pragma unroll
+          for (int db = 0; db < DB; ++db) {
+            const __bf16* r0 = Vs + (kb * 32 + cc * 16) * 128;
+            const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(r0 + swz256(t_row, db * 32 + t_col)));
+            const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(r0 + swz256(t_row + 8, db * 32 + t_col)));
+            o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7),
+                                                            pb[kb][cc], o[db], 0, 0, 0);
+          }
+      // operand reads a few products ahead, not all of them at once (registers)
+      interleave<DB * 4, DB * 8, 8>();
+    };
+    auto scores = [&](int buf) {
+      const __bf16* Ks = lds[buf][0];
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) {
         s[kb] = f32x16{};
@@ -335,8 +367,9 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
           s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(Ks + kb * 32 * 128 + (k_rd ^ (ks * 16))),
                                                           qf[ks], s[kb], 0, 0, 0);
       }
-      // operand reads a few products ahead, not all of them at once (registers)
       interleave<KS * 2, KS * 2, 4>();
+    };
+    auto softmax = [&](int t) {
       const int left = left_of(len, t);
       if (left < kTile) {
 #pragma unroll
@@ -359,7 +392,6 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
 #pragma unroll
         for (int db = 0; db < DB; ++db) o[db] *= alpha;
       }
-      bf16x8 pb[2][2];
       float ls[2] = {0.f, 0.f};
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
@@ -370,21 +402,28 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
           pb[kb][e >> 3][e & 7] = static_cast<__bf16>(p);
         }
       l += ls[0] + ls[1];
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int cc = 0; cc < 2; ++cc)
-#pragma unroll
-          for (int db = 0; db < DB; ++db) {
-            const __bf16* r0 = Vs + (kb * 32 + cc * 16) * 128;
-            const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(r0 + swz256(t_row, db * 32 + t_col)));
-            const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(r0 + swz256(t_row + 8, db * 32 + t_col)));
-            o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7),
-                                                            pb[kb][cc], o[db], 0, 0, 0);
-          }
-      interleave<DB * 4, DB * 8, 8>();
-      if (more) put(buf ^ 1);
-      __syncthreads();
+    };
+
+    if (t0 < t1) {
+      if (seg > 0) phase_end();  // the last item's V has been read by all
+      put(0);
+      if (t0 + 1 < t1) fetch(t0 + 1);
+      phase_end();
+      if (second) phase_end();
+      for (int t = t0; t < t1; ++t) {
+        const int buf = (t - t0) & 1;
+        if (t > t0) add_pv(buf ^ 1);
+        scores(buf);
+        phase_end();
+        softmax(t);
+        if (t + 1 < t1) {
+          put(buf ^ 1);
+          if (t + 2 < t1) fetch(t + 2);
+        }
+        phase_end();
+      }
+      add_pv((t1 - 1 - t0) & 1);
+      if (NW == 8 && !second) phase_end();
     }
     l += other_half(l);
     // dims 32 db + 8 j + 4 hh .. + 3 of the row
@@ -420,7 +459,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
         at.item = 0;
         ++at.b;
       }
-    } while (tokens_of(a, at.b) == 0);
+    } while (len_of(a, at.b) == 0);
   }
 }
 
@@ -437,14 +476,6 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
 // them, the rest other tokens): whole cache lines are used at once.  An item is
 // a whole sequence, its heads' blocks side by side.
 constexpr int kFewWaves = 4;
-
-template <int NS>
-__device__ inline auto load_codes(__amdgpu_buffer_rsrc_t r, uint32_t off) {
-  if constexpr (NS == 4)
-    return __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0);
-  else
-    return __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0);
-}
 
 // Combine over the four lanes that hold one query row (lane % 16).
 template <class Op>
@@ -473,12 +504,12 @@ __global__ __launch_bounds__(kFewWaves * 64) __attribute__((amdgpu_waves_per_eu(
   const int kvh = j % head_blocks * a.head_waves + hw;
   int b = worker;
   int tile = 0;  // the sequence's first tile here
-  int64_t todo = 0;
+  int todo = 0;  // tiles
   if (a.workers) {
     const Shares sh = shares_of(a, 0, nullptr);
-    if (worker >= sh.workers) return;
-    const int64_t x0 = sh.first(worker);
-    todo = sh.first(worker + 1) - x0;
+    if (static_cast<uint32_t>(worker) >= sh.workers) return;
+    const uint32_t x0 = sh.first(worker);
+    todo = static_cast<int>(sh.first(worker + 1) - x0);
     const Spot at = locate(a, x0);
     b = at.b;
     tile = at.tile;
@@ -498,8 +529,8 @@ __global__ __launch_bounds__(kFewWaves * 64) __attribute__((amdgpu_waves_per_eu(
   };
 
   for (int seg = 0;; ++seg) {
-    const int len = static_cast<int>(tokens_of(a, b)), nt = tiles_of(a, b);
-    const int tile1 = a.workers && todo < nt - tile ? tile + static_cast<int>(todo) : nt;
+    const int len = len_of(a, b), nt = tiles_in(len);
+    const int tile1 = a.workers && todo < nt - tile ? tile + todo : nt;
     const bool whole = tile == 0 && tile1 == nt;
     const int end = tile1 < nt ? tile1 * kTile : len;
     todo -= tile1 - tile;
@@ -687,7 +718,7 @@ __global__ __launch_bounds__(kFewWaves * 64) __attribute__((amdgpu_waves_per_eu(
     if (todo <= 0) return;
     tile = 0;
     do ++b;
-    while (tokens_of(a, b) == 0);  // there is one: tiles are left to do
+    while (len_of(a, b) == 0);  // there is one: tiles are left to do
   }
 }
 
@@ -706,9 +737,9 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(MxAttnArgs a, int bl
   const int tid = threadIdx.x, wave = tid >> 6, side = tid % kSide, grp = tid / kSide;
   const int unit = blockIdx.x / row_groups, rg = blockIdx.x - unit * row_groups;
   const int b = unit / a.items, item = unit - b * a.items;
-  int64_t start;
+  uint32_t start;
   const Shares sh = shares_of(a, b, &start);
-  const int64_t nt = tiles_of(a, b);
+  const uint32_t nt = tiles_in(len_of(a, b));
   start += item * nt;
   // the workers that took the item's first and last tile
   const int64_t w0 = nt ? sh.worker_of(start) : 0, w1 = nt ? sh.worker_of(start + nt - 1) : 0;
@@ -724,19 +755,31 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(MxAttnArgs a, int bl
     return row_place(a, b, kvh, *ok ? r : 0, D);
   };
   const int r0 = rg * block_rows;
-  if (pieces <= kGroups && block_rows > 1) {
+  if (pieces <= kSide && block_rows > 1) {
     for (int k = grp; k < block_rows; k += kGroups) {
       bool ok;
       const RowPlace at = place(r0 + k, &ok);
-      if (!ok) continue;
-      float m = kNoMax, l = 0.f;
-      for (int s = 0; s < pieces; ++s) m = fmaxf(m, slot_stats(a, D, slot(s), r0 + k)->x);
+      if (!ok) continue;  // all threads of the row
+      // thread `side` holds slot side's statistics, then its weight
+      const float2 mine = side < pieces ? *slot_stats(a, D, slot(side), r0 + k) : make_float2(kNoMax, 0.f);
+      float m = mine.x;
+#pragma unroll
+      for (int d = 1; d < kSide; d *= 2) m = fmaxf(m, __shfl_xor(m, d, kSide));
+      const float f = __builtin_amdgcn_exp2f(mine.x - m);
+      float l = f * mine.y;
+#pragma unroll
+      for (int d = 1; d < kSide; d *= 2) l += __shfl_xor(l, d, kSide);
       f32x4 v = {};
-      for (int s = 0; s < pieces; ++s) {
-        const float2 st = *slot_stats(a, D, slot(s), r0 + k);
-        const float f = __builtin_amdgcn_exp2f(st.x - m);
-        l = __builtin_fmaf(f, st.y, l);
-        v += *reinterpret_cast<const f32x4*>(slot_sums(a, D, slot(s), r0 + k) + side * 4) * f;
+      for (int s0 = 0; s0 < pieces; s0 += 4) {
+        f32x4 part[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int s = min(s0 + u, pieces - 1);
+          part[u] = *reinterpret_cast<const f32x4*>(slot_sums(a, D, slot(s), r0 + k) + side * 4);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (s0 + u < pieces) v += part[u] * __shfl(f, s0 + u, kSide);
       }
       write_joined(a, at, m, l, a.prior_lse ? a.prior_lse[at.lse] : 0.f, v, side * 4);
     }
@@ -819,11 +862,12 @@ hipError_t plan_mx_attention(int32_t batch, int32_t n_q, int32_t q_heads, int32_
   const int64_t slots = p.waves == 8 ? 256 : 512;  // blocks resident at once
   // Work for more than one block per item: at least this many tiles a worker.
   const int64_t least = p.waves ? 4 : 2 * kFewWaves / p.head_waves;
+  if (items * batch > 0x7fffffff || items * batch * tiles > 0x7fffffff) return hipErrorInvalidValue;  // 31 bits of tiles
   const int64_t all = items * batch * tiles;
   if (tiles > least) p.workers = static_cast<int32_t>(std::max<int64_t>(1, std::min({kMaxWorkers, slots / side, all / least})));
   p.blocks = p.workers ? (p.waves ? p.workers : (p.workers + 7) / 8 * 8 * side)
                        : (p.waves ? items * batch : (batch + int64_t{7}) / 8 * 8 * side);
-  if (items > 0x7fffffff || slot_rows > 0x7fffffff || p.blocks > 0x7fffffff ||
+  if (slot_rows > 0x7fffffff || p.blocks > 0x7fffffff ||
       items * batch * (slot_rows / (p.waves ? 8 : 1)) > 0x7fffffff)
     return hipErrorInvalidValue;
   p.items = static_cast<int32_t>(items);
