@@ -151,7 +151,7 @@ __device__ inline Spot locate(const MxAttnArgs& a, uint32_t x) {
     }
   }
   const uint32_t in = x - base * a.items, item = in / t;
-  return {static_cast<int>(uniform(b)), static_cast<int>(item), static_cast<int>(in - item * t)};
+  return {static_cast<int>(uniform(b)), static_cast<int>(uniform(item)), static_cast<int>(uniform(in - item * t))};
 }
 
 // Row `row` of slot `slot`: its sums, and its maximum and sum of exponentials
@@ -268,7 +268,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
     const Shares sh = shares_of(a, 0, nullptr);
     if (static_cast<uint32_t>(worker) >= sh.workers) return;
     const uint32_t x0 = sh.first(worker);
-    todo = static_cast<int>(sh.first(worker + 1) - x0);
+    todo = static_cast<int>(uniform(sh.first(worker + 1) - x0));
     at = locate(a, x0);
   }
 
@@ -355,7 +355,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
                                                             pb[kb][cc], o[db], 0, 0, 0);
           }
       // operand reads a few products ahead, not all of them at once (registers)
-      interleave<DB * 4, DB * 8, 8>();
+      interleave<DB * 4, DB * 8, DB * 3>();
     };
     auto scores = [&](int buf) {
       const __bf16* Ks = lds[buf][0];
@@ -367,7 +367,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
           s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(Ks + kb * 32 * 128 + (k_rd ^ (ks * 16))),
                                                           qf[ks], s[kb], 0, 0, 0);
       }
-      interleave<KS * 2, KS * 2, 4>();
+      interleave<KS * 2, KS * 2, 6>();
     };
     auto softmax = [&](int t) {
       const int left = left_of(len, t);
@@ -412,8 +412,11 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
       if (second) phase_end();
       for (int t = t0; t < t1; ++t) {
         const int buf = (t - t0) & 1;
+        // the wave whose turn at the matrix core it is goes first elsewhere too
+        __builtin_amdgcn_s_setprio(1);
         if (t > t0) add_pv(buf ^ 1);
         scores(buf);
+        __builtin_amdgcn_s_setprio(0);
         phase_end();
         softmax(t);
         if (t + 1 < t1) {
@@ -509,7 +512,7 @@ __global__ __launch_bounds__(kFewWaves * 64) __attribute__((amdgpu_waves_per_eu(
     const Shares sh = shares_of(a, 0, nullptr);
     if (static_cast<uint32_t>(worker) >= sh.workers) return;
     const uint32_t x0 = sh.first(worker);
-    todo = static_cast<int>(sh.first(worker + 1) - x0);
+    todo = static_cast<int>(uniform(sh.first(worker + 1) - x0));
     const Spot at = locate(a, x0);
     b = at.b;
     tile = at.tile;
