@@ -6,6 +6,12 @@
 
 #include <cstdint>
 
+#ifdef __HIPCC__
+#define MSSA_HOST_DEVICE __host__ __device__
+#else
+#define MSSA_HOST_DEVICE
+#endif
+
 namespace mssa {
 
 constexpr int kMxBlock = 32;  // values under one MXFP4 scale
@@ -33,6 +39,13 @@ struct NormBwdArgs {
   int32_t cols, blocks;
   float inv_cols;
 };
+
+// Threads of a row of `cols` values and 8-value pieces of a thread
+// (lowbit_plan.cpp, as every rule on sizes that needs no device).
+struct NormRowShape {
+  int tpr, nv;
+};
+NormRowShape norm_row_shape(int cols);
 
 hipError_t launch_norm(const NormArgs& a, bool bf16, bool e4m3, hipStream_t stream);
 // Blocks of the backward's first launch: a static rule on the sizes.
@@ -64,6 +77,25 @@ struct ProjectArgs {
 hipError_t launch_mx_project(const ProjectArgs& a, bool x_fp4, bool out_bf16, hipStream_t stream);
 
 // -------------------------------------------------------------- attention
+constexpr int kMxAttnTile = 64;          // tokens of a tile
+constexpr int kMxAttnMaxWorkers = 512;
+constexpr int kMxAttnFewWaves = 4;       // waves of a block of the kernel for few rows
+
+// `all` tiles in a row, shared out to at most `most` workers: the first `more`
+// workers take each + 1 tiles, the others `each`; none is without.
+struct Shares {
+  uint32_t all, workers, each, more;
+  MSSA_HOST_DEVICE static Shares of(uint32_t all, uint32_t most) {
+    const uint32_t workers = all < most ? all : most, each = workers ? all / workers : 0;
+    return {all, workers, each, all - each * workers};
+  }
+  MSSA_HOST_DEVICE uint32_t first(uint32_t i) const { return i * each + (i < more ? i : more); }
+  MSSA_HOST_DEVICE uint32_t worker_of(uint32_t x) const {
+    const uint32_t big = more * (each + 1);
+    return x < big ? x / (each + 1) : more + (x - big) / each;
+  }
+};
+
 struct MxAttnArgs {
   const void *q, *kc, *ks, *vc, *vs, *prior_out;
   const int32_t* kv_len;

@@ -32,7 +32,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
 
-constexpr int64_t kMaxWorkers = 512;
+constexpr int kMaxWorkers = kMxAttnMaxWorkers;
 constexpr float kRescaleLog2 = 8.f;
 constexpr float kNoMax = -__FLT_MAX__;       // a finite running maximum before the first score
 constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
@@ -71,7 +71,7 @@ __device__ inline uint32_t wave_prefix(uint32_t v) {
 // one that several share go to slots, 2 i for the first item of worker i and
 // 2 i + 1 for a later one (which then is its last), and a second launch joins
 // them.  (All tiles of a call are fewer than 2^31: the plan's check.)
-constexpr int kTile = 64;  // tokens of a tile
+constexpr int kTile = kMxAttnTile;
 
 __device__ inline int64_t tokens_of(const MxAttnArgs& a, int b) {
   const int64_t len = a.kv_len ? a.kv_len[b] : a.cache_tokens;
@@ -90,14 +90,6 @@ __device__ inline int left_of(int end, int t) {
   return left > kTile ? kTile : left < 0 ? 0 : static_cast<int>(left);
 }
 
-struct Shares {
-  uint32_t all, workers, each, more;  // tiles of all items; the first `more` workers take each + 1, the others each
-  __device__ uint32_t first(uint32_t i) const { return i * each + min(i, more); }
-  __device__ uint32_t worker_of(uint32_t x) const {
-    const uint32_t big = more * (each + 1);
-    return x < big ? x / (each + 1) : more + (x - big) / each;
-  }
-};
 // Tiles of the sequences before b, times the items of a sequence, and the
 // shares.  Lengths are read 64 at a time: every lane of a wave calls these.
 __device__ inline Shares shares_of(const MxAttnArgs& a, int b, uint32_t* before) {
@@ -121,8 +113,7 @@ __device__ inline Shares shares_of(const MxAttnArgs& a, int b, uint32_t* before)
   }
   if (before) *before = pre_b * a.items;
   all *= a.items;
-  const uint32_t workers = min(all, static_cast<uint32_t>(a.workers)), each = workers ? all / workers : 0;
-  return {all, workers, each, all - each * workers};
+  return Shares::of(all, static_cast<uint32_t>(a.workers));
 }
 // The sequence, item and tile that tile x of all is.
 struct Spot {
@@ -478,7 +469,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
 // block's waves take neighbouring key heads of the same tokens (head_waves of
 // them, the rest other tokens): whole cache lines are used at once.  An item is
 // a whole sequence, its heads' blocks side by side.
-constexpr int kFewWaves = 4;
+constexpr int kFewWaves = kMxAttnFewWaves;
 
 // Combine over the four lanes that hold one query row (lane % 16).
 template <class Op>
@@ -852,33 +843,6 @@ hipError_t attn_dim(const MxAttnArgs& a, const MxAttnPlan& plan, hipStream_t str
 }
 
 }  // namespace
-
-hipError_t plan_mx_attention(int32_t batch, int32_t n_q, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
-                             int64_t cache_tokens, MxAttnPlan* plan) {
-  MxAttnPlan p{};
-  const int64_t rows = static_cast<int64_t>(n_q) * (q_heads / kv_heads), tiles = (cache_tokens + kTile - 1) / kTile;
-  p.waves = rows <= 32 ? 0 : rows <= 1024 ? 4 : 8;
-  p.head_waves = kv_heads % 4 == 0 ? 4 : kv_heads % 2 == 0 ? 2 : 1;
-  const int64_t side = p.waves ? 1 : kv_heads / p.head_waves;  // blocks of one worker
-  const int64_t items = p.waves ? (rows + p.waves * 32 - 1) / (p.waves * 32) * kv_heads : 1;
-  const int64_t slot_rows = p.waves ? p.waves * 32 : rows * kv_heads;
-  const int64_t slots = p.waves == 8 ? 256 : 512;  // blocks resident at once
-  // Work for more than one block per item: at least this many tiles a worker.
-  const int64_t least = p.waves ? 4 : 2 * kFewWaves / p.head_waves;
-  if (items * batch > 0x7fffffff || items * batch * tiles > 0x7fffffff) return hipErrorInvalidValue;  // 31 bits of tiles
-  const int64_t all = items * batch * tiles;
-  if (tiles > least) p.workers = static_cast<int32_t>(std::max<int64_t>(1, std::min({kMaxWorkers, slots / side, all / least})));
-  p.blocks = p.workers ? (p.waves ? p.workers : (p.workers + 7) / 8 * 8 * side)
-                       : (p.waves ? items * batch : (batch + int64_t{7}) / 8 * 8 * side);
-  if (slot_rows > 0x7fffffff || p.blocks > 0x7fffffff ||
-      items * batch * (slot_rows / (p.waves ? 8 : 1)) > 0x7fffffff)
-    return hipErrorInvalidValue;
-  p.items = static_cast<int32_t>(items);
-  p.slot_rows = static_cast<int32_t>(slot_rows);
-  p.workspace_bytes = int64_t{2} * p.workers * slot_rows * (head_dim + 2) * 4;
-  *plan = p;
-  return hipSuccess;
-}
 
 hipError_t launch_mx_attention(const MxAttnArgs& a, const MxAttnPlan& plan, int head_dim, hipStream_t stream) {
   return head_dim == 128 ? attn_dim<128>(a, plan, stream) : attn_dim<64>(a, plan, stream);

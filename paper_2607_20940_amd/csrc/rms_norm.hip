@@ -288,17 +288,6 @@ __global__ __launch_bounds__(1024) void norm_dweight_kernel(NormBwdArgs a) {
   }
 }
 
-// Threads and 8-value pieces per thread of a row of `cols` values.
-struct RowShape {
-  int tpr, nv;
-};
-RowShape row_shape(int cols) {
-  const int pieces = (cols + 7) / 8;
-  if (pieces <= 256) return {64, (pieces + 63) / 64};
-  if (pieces <= 1024) return {256, (pieces + 255) / 256};
-  return {1024, (pieces + 1023) / 1024};
-}
-
 template <class T, bool RES, bool E4, int TPR, int NV>
 hipError_t norm_go(const NormArgs& a, hipStream_t stream) {
   constexpr int kThreads = TPR > 256 ? TPR : 256, kRows = kThreads / TPR;
@@ -320,7 +309,7 @@ hipError_t norm_nv(const NormArgs& a, int nv, hipStream_t stream) {
 
 template <class T, bool RES, bool E4>
 hipError_t norm_tpr(const NormArgs& a, hipStream_t stream) {
-  const RowShape s = row_shape(E4 ? a.y_pitch : a.cols);
+  const NormRowShape s = norm_row_shape(E4 ? a.y_pitch : a.cols);
   if (s.tpr == 64) return norm_nv<T, RES, E4, 64>(a, s.nv, stream);
   if (s.tpr == 256) return norm_nv<T, RES, E4, 256>(a, s.nv, stream);
   return norm_nv<T, RES, E4, 1024>(a, s.nv, stream);
@@ -350,7 +339,7 @@ hipError_t bwd_nv(const NormBwdArgs& a, int nv, hipStream_t stream) {
 
 template <class T, bool DSUM>
 hipError_t bwd_tpr(const NormBwdArgs& a, hipStream_t stream) {
-  const RowShape s = row_shape(a.cols);
+  const NormRowShape s = norm_row_shape(a.cols);
   if (s.tpr == 64) return bwd_nv<T, DSUM, 64>(a, s.nv, stream);
   if (s.tpr == 256) return bwd_nv<T, DSUM, 256>(a, s.nv, stream);
   return bwd_nv<T, DSUM, 1024>(a, s.nv, stream);
@@ -360,12 +349,6 @@ hipError_t bwd_tpr(const NormBwdArgs& a, hipStream_t stream) {
 
 hipError_t launch_norm(const NormArgs& a, bool bf16, bool e4m3, hipStream_t stream) {
   return bf16 ? norm_type<__bf16>(a, e4m3, stream) : norm_type<float>(a, e4m3, stream);
-}
-
-int32_t norm_bwd_blocks(int64_t rows, int32_t cols) {
-  const RowShape s = row_shape(cols);
-  const int64_t per = s.tpr >= 256 ? 1 : 256 / s.tpr, want = (rows + per - 1) / per;
-  return static_cast<int32_t>(std::min<int64_t>(want, 512));
 }
 
 hipError_t launch_norm_bwd(const NormBwdArgs& a, bool bf16, hipStream_t stream) {
