@@ -563,7 +563,7 @@ typedef struct {
   int32_t batch;          /* >= 1 */
   int32_t n_q;            /* queries per sequence, >= 1 */
   int32_t q_heads;        /* a multiple of kv_heads: query head h reads key head h / (q_heads / kv_heads) */
-  int32_t kv_heads;       /* >= 1 */
+  int32_t kv_heads;       /* 1..65536 */
   int32_t head_dim;       /* 64 or 128 */
   int64_t cache_tokens;   /* capacity of each sequence's cache, 1..2^31 - 1 */
   int64_t lse_stride;     /* floats between the heads of lse, 0 = n_q */

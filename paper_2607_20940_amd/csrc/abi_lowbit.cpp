@@ -88,6 +88,8 @@ mssa_status attention_check(const mssa_mx_attention_desc* d) {
   if (static_cast<int64_t>(d->n_q) * (d->q_heads / d->kv_heads) > 0x3fffffff ||
       static_cast<int64_t>(d->batch) * d->q_heads > 0x3fffffff)
     return fail(MSSA_ERR_UNSUPPORTED, "too many query rows or heads");
+  // the kernels' byte offsets inside a tile of 64 tokens have 32 bits: 2^16 heads x 64 bytes x 64 tokens
+  if (d->kv_heads > (1 << 16)) return fail(MSSA_ERR_UNSUPPORTED, "more than 65536 key heads");
   return MSSA_OK;
 }
 

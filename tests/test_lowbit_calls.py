@@ -151,3 +151,13 @@ def test_attention_workspace_is_bounded(n_q, tokens):
     rows = 2 * 12 * n_q
     assert 0 <= n <= 256 * rows * 130 * 4
     assert mssa.mx_shapes(7, 33) == ((7, 32), (7, 2))
+
+
+@pytest.mark.parametrize("kv_heads,ok", [(1 << 16, True), ((1 << 16) + 1, False), (1 << 26, False)])
+def test_key_heads_whose_tiles_pass_32_bit_offsets_are_refused(kv_heads, ok):
+    desc = mssa.mx_attention_desc(1, 1, kv_heads, kv_heads, 128, 64)
+    if ok:
+        assert mssa.mssa_mx_attention_workspace_size(desc) >= 0
+    else:
+        with pytest.raises(mssa.MssaError, match="key heads"):
+            mssa.mssa_mx_attention_workspace_size(desc)
