@@ -24,7 +24,11 @@ hipError_t plan_mx_attention(int32_t batch, int32_t n_q, int32_t q_heads, int32_
                              int64_t cache_tokens, MxAttnPlan* plan) {
   MxAttnPlan p{};
   const int64_t rows = static_cast<int64_t>(n_q) * (q_heads / kv_heads), tiles = (cache_tokens + kMxAttnTile - 1) / kMxAttnTile;
-  p.waves = rows <= 32 ? 0 : rows <= 1024 ? 4 : 8;
+  // Up to 2048 rows blocks of four waves, two on a CU: an item's rows fit
+  // better and one block starts while the other works (1173 rows over 1955
+  // tokens 25.2 -> 23.0 us, 1800 rows over 9000 tokens 46.0 and 46.2); above,
+  // eight waves share each expanded tile.
+  p.waves = rows <= 32 ? 0 : rows <= 2048 ? 4 : 8;
   p.head_waves = kv_heads % 4 == 0 ? 4 : kv_heads % 2 == 0 ? 2 : 1;
   const int64_t side = p.waves ? 1 : kv_heads / p.head_waves;  // blocks of one worker
   const int64_t items = p.waves ? (rows + p.waves * 32 - 1) / (p.waves * 32) * kv_heads : 1;
@@ -34,7 +38,13 @@ hipError_t plan_mx_attention(int32_t batch, int32_t n_q, int32_t q_heads, int32_
   const int64_t least = p.waves ? 4 : 2 * kMxAttnFewWaves / p.head_waves;
   if (items * batch > 0x7fffffff || items * batch * tiles > 0x7fffffff) return hipErrorInvalidValue;  // 31 bits of tiles
   const int64_t all = items * batch * tiles;
-  if (tiles > least) p.workers = static_cast<int32_t>(std::max<int64_t>(1, std::min({int64_t{kMxAttnMaxWorkers}, slots / side, all / least})));
+  // A second worker a CU only where each has 8 tiles: with fewer the slots that
+  // the joining launch reads cost more (1173 rows over 1955 tokens 23.0 -> 21.8
+  // us; with 8 tiles a worker at least everywhere, 100 rows over 1500 tokens
+  // 13.8 -> 17.5).
+  int64_t most = all / least;
+  if (p.waves == 4) most = std::min(most, std::max<int64_t>(256, all / 8));
+  if (tiles > least) p.workers = static_cast<int32_t>(std::max<int64_t>(1, std::min({int64_t{kMxAttnMaxWorkers}, slots / side, most})));
   p.blocks = p.workers ? (p.waves ? p.workers : (p.workers + 7) / 8 * 8 * side)
                        : (p.waves ? items * batch : (batch + int64_t{7}) / 8 * 8 * side);
   if (slot_rows > 0x7fffffff || p.blocks > 0x7fffffff ||
