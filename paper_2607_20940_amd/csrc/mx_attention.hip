@@ -13,6 +13,11 @@
 // Softmax in base 2 on fp32 scores with a running maximum that only moves
 // when a score passes it by 2^8, sums in fp32, P rounded to bf16 as a matrix
 // operand.
+//
+// Many rows are bound by the matrix cores and the softmax between them (9360
+// queries, 12 heads, 32760 tokens, d 128: 1.75 ms, 1.08 PFLOP/s), few rows by
+// the cache's bytes (16 streams of one token, 40 over 8 heads, up to 32760
+// tokens: 73 us, 3.9 TB/s).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

@@ -3,10 +3,17 @@
 //
 // The block-scaled matrix instructions take both operands as they lie in
 // memory: a lane holds the 32 values of one MXFP4 block (16 bytes) and the
-// block's scale byte; e4m3 operands are 16-byte pieces of two such blocks.  The contraction runs over blocks in
-// any order as long as both operands take the same one, so the two lane
+// block's scale byte; e4m3 operands are 16-byte pieces of two such blocks.
+// The contraction runs over blocks in any order as long as both operands take the same one, so the two lane
 // halves take the first and the second half of a stage's blocks and each
 // lane's scales of a stage are consecutive bytes.
+//
+// Bound by LDS operand reads and transfers where there are many tokens (27840 x
+// 5120 -> 15360 in MXFP4: 1.20 ms, 3.6 PFLOP/s; 12870 x 1536 -> 4608 in e4m3:
+// 104 us, 1.7 PFLOP/s, a fifth of it the 118 MB of outputs), by the weights'
+// bytes where there are few (1 x 5120 -> 15360: 12 us, 3.5 TB/s).  Waves of
+// 128 x 128 outputs read a quarter fewer bytes but are alone on their SIMD:
+// 1.34 ms and 141 us.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -87,7 +94,8 @@ __device__ inline void store_features(const ProjectArgs& a, int64_t row, int col
 // lane holds one token and runs of four features.  A stage is 128 bytes
 // of every token (four blocks of e4m3, eight of MXFP4: whole cache lines) and
 // as many blocks of every feature, moved by direct global -> LDS transfers;
-// kBufs of them are in LDS or on their way.  Scale bytes come sixteen to a row, for four stages at once.
+// kBufs of them are in LDS or on their way.  Scale bytes come four to a row and
+// stage with 8-bit tokens, sixteen for two stages at once with MXFP4 tokens.
 template <bool XF4, int BM, int BN, int WM, int WN, int BUFS>
 struct TileShape {
   static constexpr int kThreads = WM * WN * 64, kWaves = WM * WN;
@@ -98,7 +106,7 @@ struct TileShape {
   static constexpr int kSBufs = kSuper == 1 ? BUFS : 2;
   static constexpr int XB = 128, WB = NBK * 16;           // bytes of a row a stage
   static constexpr int kBufs = BUFS;
-    // LDS: the X tiles of all buffers, the W tiles, two groups' scales
+  // LDS: the X tiles of all buffers, the W tiles, two groups' scales
   static constexpr int kXBytes = BM * XB, kWBytes = BN * WB, kStage = kXBytes + kWBytes;
   static constexpr int kWBase = BUFS * kXBytes, kSBase = BUFS * kStage;
   static constexpr int kSRows = (XF4 ? BM : 0) + BN, kScales = kSRows * kSBytes;
