@@ -8,12 +8,12 @@
 // halves take the first and the second half of a stage's blocks and each
 // lane's scales of a stage are consecutive bytes.
 //
-// Bound by LDS operand reads and transfers where there are many tokens (27840 x
-// 5120 -> 15360 in MXFP4: 1.20 ms, 3.6 PFLOP/s; 12870 x 1536 -> 4608 in e4m3:
-// 104 us, 1.7 PFLOP/s, a fifth of it the 118 MB of outputs), by the weights'
-// bytes where there are few (1 x 5120 -> 15360: 12 us, 3.5 TB/s).  Waves of
-// 128 x 128 outputs read a quarter fewer bytes but are alone on their SIMD:
-// 1.34 ms and 141 us.
+// Bound by the stages' transfers where there are many tokens (27840 x 5120 ->
+// 15360 in MXFP4: 1.20 ms, 3.6 PFLOP/s, matrix cores busy 42 % of the time;
+// 12870 x 1536 -> 4608 in e4m3: 104 us, 1.7 PFLOP/s, busy 35 %, an eighth of
+// it the 118 MB of outputs), by the weights' bytes where there are few (1 x
+// 5120 -> 15360: 12 us, 3.5 TB/s).  Waves of 128 x 128 outputs read a quarter
+// fewer LDS bytes but are alone on their SIMD: 1.34 ms and 141 us.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
