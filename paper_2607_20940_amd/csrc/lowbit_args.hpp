@@ -74,6 +74,28 @@ struct ProjectArgs {
   float part0_scale;
 };
 
+// Scale bytes of the product's tiles.  The bytes of SUPER stages of NBK blocks
+// are moved to LDS as one group of kBytes for each row.  Where a row's bytes go
+// there straight from memory the last group ends at the row's end, else it is
+// filled up with zeros.  A lane half takes one half of a stage's blocks.
+template <int NBK, int SUPER>
+struct ScaleGroups {
+  static constexpr int kBytes = NBK * SUPER, kHalf = NBK / 2;
+  int blocks;  // of a row
+  MSSA_HOST_DEVICE bool direct() const { return blocks % 4 == 0 && blocks >= kBytes; }  // whole dwords of a row
+  // First block of stage st's group.
+  MSSA_HOST_DEVICE int first(int st) const {
+    const int at = st / SUPER * kBytes;
+    return direct() && at > blocks - kBytes ? blocks - kBytes : at;
+  }
+  // The group's byte with the scale of a lane half's first block.
+  MSSA_HOST_DEVICE int offset(int st, int half) const { return st * NBK - first(st) + kHalf * half; }
+  // Whether the row has blocks for a lane half at all.  If not, a group that
+  // ends at the row's end has no bytes for it: what follows there belongs to
+  // the next row, whose NaN scales are not to meet this row's zeros.
+  MSSA_HOST_DEVICE bool there(int st, int half) const { return st * NBK + kHalf * half < blocks; }
+};
+
 hipError_t launch_mx_project(const ProjectArgs& a, bool x_fp4, bool out_bf16, hipStream_t stream);
 
 // -------------------------------------------------------------- attention

@@ -164,7 +164,8 @@ void tile_kernel(ProjectArgs a) {
   // Scales go straight to LDS too where a group of a row's is whole dwords of
   // it; else through registers.
   constexpr int SB = S::kSBytes;
-  const bool direct = a.NB % 4 == 0 && a.NB >= SB;
+  const ScaleGroups<NBK, S::kSuper> groups{a.NB};
+  const bool direct = groups.direct();
 
   // Transfer i of a wave fills 1 KB of consecutive LDS, XB- or WB-byte rows of
   // it; a lane's 16 bytes are its physical chunk's.  The rows of transfer i
@@ -183,15 +184,13 @@ void tile_kernel(ProjectArgs a) {
   const i32x4 rx = rsrc_of(X, static_cast<uint32_t>(mrows) * xp);
   const i32x4 rw = rsrc_of(W, static_cast<uint32_t>(nrows) * wp);
   const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(&lds[0]));
-  // First block of a stage's group of scales (the last group ends at the
-  // row's end), and the group's place in LDS.
-  auto scale_base = [&](int st) { return direct ? min(st / S::kSuper * SB, a.NB - SB) : st / S::kSuper * SB; };
+  // The place in LDS of a stage's group of scales.
   auto scale_place = [&](int st) { return S::kSBase + st / S::kSuper % S::kSBufs * S::kScales; };
   // The scales of stage st's group, straight to LDS.  A wave takes 64 rows
   // (where there are fewer groups than waves, two take the same).
   auto issue_scales = [&](int st) {
     const uint32_t dst = lds0 + scale_place(st);
-    const int first = scale_base(st);
+    const int first = groups.first(st);
 #pragma unroll
     for (int i = 0; i < S::NSG; ++i) {
       const int group = (wave + i * S::kWaves) % (S::kSRows / 64);  // rows of X first for MXFP4 tokens
@@ -226,7 +225,7 @@ void tile_kernel(ProjectArgs a) {
         issue_scales(st);
       } else {
         // rows past the tile and blocks past the row: zeros (their codes are)
-        const int first = scale_base(st);
+        const int first = groups.first(st);
         for (int group = wave; group < S::kSRows / 64; group += S::kWaves) {
           const bool of_x = XF4 && group * 64 < BM;
           const int row = group * 64 + lane - (XF4 && !of_x ? BM : 0);
@@ -265,16 +264,23 @@ void tile_kernel(ProjectArgs a) {
     for (int j = 0; j < TN; ++j) acc[i][j] = f32x16{};
 
   // Scales of a stage: byte j of a row's is matrix step j's (block hh NS + j).
+  // Of a short last stage (with 8-bit tokens its group is filled with zeros)
+  // a lane half may have none: zeros then, as its codes are.
   int sx[TM], sw[TN];
   using scales_t = std::conditional_t<NS == 4, uint32_t, uint16_t>;
-  auto read_scales = [&](int st) {
-    const char* P = lds + scale_place(st) + (st * NBK - scale_base(st)) + NS * hh;
+  auto read_scales = [&](int st, auto full) {
+    const bool there = !XF4 || decltype(full)::value || groups.there(st, hh);
+    const char* P = lds + scale_place(st) + (there ? groups.offset(st, hh) : 0);
 #pragma unroll
-    for (int i = 0; i < TM; ++i)
+    for (int i = 0; i < TM; ++i) {
       sx[i] = XF4 ? *reinterpret_cast<const scales_t*>(P + ((wm * TM + i) * 32 + n32) * SB) : 0x7f7f;
+      if (!there) sx[i] = 0;
+    }
 #pragma unroll
-    for (int j = 0; j < TN; ++j)
+    for (int j = 0; j < TN; ++j) {
       sw[j] = *reinterpret_cast<const scales_t*>(P + ((XF4 ? BM : 0) + (wn * TN + j) * 32 + n32) * SB);
+      if (!there) sw[j] = 0;
+    }
   };
   // Operands of step J of the stage in buffer buf: 32 rows further on is a
   // fixed distance, for the swizzle too.
@@ -349,9 +355,9 @@ void tile_kernel(ProjectArgs a) {
     asm volatile("" ::: "memory");
   };
   arrive(std::integral_constant<int, S::kBufs - 1>{});
-  read_scales(0);
+  read_scales(0, std::false_type{});
   read_step(std::integral_constant<int, 0>{}, 0);
-  auto stage = [&](int buf, int next, int next_buf, auto refill) {
+  auto stage = [&](int buf, int next, int next_buf, auto next_full, auto refill) {
     auto inner = [&](auto js) {
       constexpr int J = decltype(js)::value;
       read_step(std::integral_constant<int, J + 1>{}, buf);
@@ -369,11 +375,11 @@ void tile_kernel(ProjectArgs a) {
     __builtin_amdgcn_sched_barrier(0);
     multiply(std::integral_constant<int, NS - 1>{});
     read_step(std::integral_constant<int, 0>{}, next_buf);
-    read_scales(next);
+    read_scales(next, next_full);
     interleave<kProducts, kReads + (XF4 ? TM : 0) + TN>();
     __builtin_amdgcn_sched_barrier(0);
   };
-  // Stages whose refill is a whole one, without a branch in the loop (the
+  // Stages whose refill is a whole one (and the next stage with it), without a branch in the loop (the
   // compiler would move products across it); then the rest.
   int st = 0;
   if (direct)
@@ -382,14 +388,14 @@ void tile_kernel(ProjectArgs a) {
       for (int u = 0; u < S::kSuper; ++u) {
         // st is a multiple of kSuper: where that is one of kBufs the buffers are constants
         const int s0 = S::kSuper % S::kBufs == 0 ? 0 : st;
-        stage((s0 + u) % S::kBufs, st + u + 1, (s0 + u + 1) % S::kBufs, [&] {
+        stage((s0 + u) % S::kBufs, st + u + 1, (s0 + u + 1) % S::kBufs, std::true_type{}, [&] {
           if ((u + S::kBufs) % S::kSuper == 0) issue_scales(st + u + S::kBufs);
           issue_full(st + u + S::kBufs, (s0 + u) % S::kBufs);
         });
       }
   for (; st < nst; ++st) {
     const int next = st + 1 < nst ? st + 1 : st;  // past the last stage: read again, not used
-    stage(st % S::kBufs, next, next % S::kBufs, [&] { issue(st + S::kBufs); });
+    stage(st % S::kBufs, next, next % S::kBufs, std::false_type{}, [&] { issue(st + S::kBufs); });
   }
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 
