@@ -170,7 +170,8 @@ __device__ inline RowPlace row_place(const MxAttnArgs& a, int b, int kvh, int r,
 }
 
 // Shares of this result (sum l with maximum m, base 2) and of the prior in
-// the joint softmax, and the joint log sum (natural).
+// the joint softmax, and the joint log sum (natural).  A NaN on either side
+// makes all of it NaN.
 struct Joined {
   float own, prior, lse;
 };
@@ -179,8 +180,8 @@ __device__ inline Joined join(bool has_prior, float m, float l, float prior_lse)
   const float own = any ? m + __builtin_amdgcn_logf(l) : -INFINITY;
   if (!has_prior) return {any ? 1.f / l : 0.f, 0.f, any ? own * kLn2 : -INFINITY};
   const float prior = prior_lse * kLog2e;
-  const float top = fmaxf(own, prior);
-  if (top == -INFINITY) return {0.f, 0.f, -INFINITY};
+  if (own == -INFINITY && prior == -INFINITY) return {0.f, 0.f, -INFINITY};
+  const float top = fmaxf(own, prior);  // of a NaN and a number the number: the NaN's share is a NaN, and so is the sum
   const float wo = __builtin_amdgcn_exp2f(own - top), wp = __builtin_amdgcn_exp2f(prior - top), w = wo + wp;
   return {any ? wo / (l * w) : 0.f, wp / w, (top + __builtin_amdgcn_logf(w)) * kLn2};
 }
@@ -197,7 +198,8 @@ __device__ inline void write_joined(const MxAttnArgs& a, const RowPlace& at, flo
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     float f = v[i] * w.own;
-    if (a.prior_out && w.prior != 0.f) f += w.prior * static_cast<float>(p[i]);
+    // a prior without keys adds nothing, whatever it holds; one whose share is too small for fp32 still adds its NaNs
+    if (a.prior_out && prior_lse != -INFINITY) f += w.prior * static_cast<float>(p[i]);
     u[i] = static_cast<__bf16>(f);
   }
   *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(a.out) + at.q + d) = u;
