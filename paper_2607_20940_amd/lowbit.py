@@ -25,6 +25,16 @@ allocations); all arithmetic runs in the library.
 from . import mssa
 
 
+def _bf16(name, t, values):
+    """The layer's calls read `values` consecutive bf16 values from t (a tensor; None and addresses pass)."""
+    import torch
+
+    if t is None or isinstance(t, int):
+        return
+    if t.dtype != torch.bfloat16 or not t.is_contiguous() or t.numel() < values:
+        raise ValueError(f"{name} must be contiguous bf16 with {values} values at least, not {t.dtype} {tuple(t.shape)}")
+
+
 class _Ring:
     """K and V of one query scale's history: codes and scales of cap frames."""
 
@@ -95,13 +105,25 @@ class LowBitStreamingMSSA:
         return sum(t.numel() for layer in self.rings for r in layer for t in (*r.k, *r.v))
 
     def init_layer(self, layer, norm_weight, w_qkv, b_qkv, k_sink=None, v_sink=None, k_hist=None, v_hist=None):
-        """Weights (norm_weight [hidden], w_qkv [3 width, hidden], b_qkv [3 width], bf16; the product's are quantised
+        """Weights (norm_weight [hidden] and b_qkv [3 width] in bf16; w_qkv [3 width, hidden] in bf16 or fp32, quantised
         here, once), sink K/V and initial history (bf16, oldest first) of one layer."""
         import torch
 
+        _bf16("norm_weight", norm_weight, self.hidden)
+        _bf16("b_qkv", b_qkv, 3 * self.width)
+        for name, t in (("k_sink", k_sink), ("v_sink", v_sink)):
+            _bf16(name, t, self.info["n_sink_tok"] * self.width)
+        for name, t in (("k_hist", k_hist), ("v_hist", v_hist)):
+            _bf16(name, t, 0 if k_hist is None else k_hist.shape[0] * self.width)
+        w_type = "bf16"
+        if not isinstance(w_qkv, int):
+            w_type = {torch.bfloat16: "bf16", torch.float32: "f32"}.get(w_qkv.dtype)
+            if w_type is None or not w_qkv.is_contiguous() or w_qkv.numel() < 3 * self.width * self.hidden:
+                raise ValueError(f"w_qkv must be contiguous bf16 or fp32 [{3 * self.width}, {self.hidden}], not "
+                                 f"{w_qkv.dtype} {tuple(w_qkv.shape)}")
         codes, scales = (torch.empty(s, dtype=torch.uint8, device=self.device)
                          for s in mssa.mx_shapes(3 * self.width, self.hidden))
-        mssa.mssa_mx_quantize(3 * self.width, self.hidden, "bf16", w_qkv, codes, scales)
+        mssa.mssa_mx_quantize(3 * self.width, self.hidden, w_type, w_qkv, codes, scales)
         self.weights[layer] = (norm_weight, codes, scales, b_qkv)
         self.sink[layer] = (k_sink, v_sink)
         n = 0 if k_hist is None else k_hist.shape[0] // self.tokens[self.info["group_scale"].index(1)]
@@ -129,7 +151,9 @@ class LowBitStreamingMSSA:
 
     def layer_pass(self, layer, x, residual, out, stream=None):
         """x [n_q, hidden] (the previous block's output) joins residual [n_q, hidden], in place; out [n_q, heads,
-        head_dim] is the attention of the pass.  The emitted frames enter the rings."""
+        head_dim] is the attention of the pass, all bf16.  The emitted frames enter the rings."""
+        for name, t, values in (("x", x, self.hidden), ("residual", residual, self.hidden), ("out", out, self.width)):
+            _bf16(name, t, self.n_q * values)
         w_norm, w, w_scales, bias = self.weights[layer]
         mssa.mssa_add_rms_norm(self.norm, x, residual, w_norm, residual, self.x8, self.x8_scale, stream=stream)
         mssa.mssa_mx_project(self.project, self.x8, self.x8_scale, w, w_scales, bias, [self.q, self.k, self.v],
