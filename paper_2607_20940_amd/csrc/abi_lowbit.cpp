@@ -1,5 +1,6 @@
 // C ABI of the low-bit layers (declared in include/libmssa.h): every call is
 // checked before anything is enqueued.
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 
@@ -16,6 +17,10 @@ using mssa::guarded;
 int elem_bytes(int32_t dtype) { return dtype == MSSA_BF16 ? 2 : 4; }
 
 bool aligned_to(const void* p, int bytes) { return reinterpret_cast<uintptr_t>(p) % static_cast<uintptr_t>(bytes) == 0; }
+
+// `bytes` further on; null stays null.
+const void* at_byte(const void* p, int64_t bytes) { return p ? static_cast<const char*>(p) + bytes : nullptr; }
+void* at_byte(void* p, int64_t bytes) { return p ? static_cast<char*>(p) + bytes : nullptr; }
 
 hipStream_t stream_of(void* s) { return static_cast<hipStream_t>(s); }
 
@@ -127,19 +132,25 @@ mssa_status mssa_add_rms_norm(const mssa_norm_desc* desc, const void* x, const v
     a.sum_stride = stride_or(desc->sum_stride, desc->cols);
     if (sum && ((sum == x && a.sum_stride != a.x_stride) || (sum == residual && a.sum_stride != a.residual_stride)))
       return fail(MSSA_ERR_INVALID_ARG, "sum may be x or residual only with the same stride");
-    a.x = x;
-    a.residual = residual;
     a.weight = weight;
-    a.sum = sum;
-    a.y = y;
-    a.y_scale = y_scale;
-    a.rstd = rstd;
-    a.rows = desc->rows;
     a.cols = desc->cols;
     a.y_pitch = e4m3 ? static_cast<int32_t>(mssa::mx_blocks(desc->cols) * mssa::kMxBlock) : desc->cols;
     a.eps = desc->eps;
     a.inv_cols = 1.f / static_cast<float>(desc->cols);
-    return check_device(mssa::launch_norm(a, desc->dtype == MSSA_BF16, e4m3, stream_of(stream)), "norm launch");
+    const int64_t step = mssa::norm_launch_rows(a.y_pitch);
+    for (int64_t row = 0; row < desc->rows; row += step) {
+      a.x = at_byte(x, row * a.x_stride * eb);
+      a.residual = at_byte(residual, row * a.residual_stride * eb);
+      a.sum = at_byte(sum, row * a.sum_stride * eb);
+      a.y = at_byte(y, row * a.y_pitch * (e4m3 ? 1 : eb));
+      a.y_scale = y_scale ? y_scale + row : nullptr;
+      a.rstd = rstd ? rstd + row : nullptr;
+      a.rows = std::min(step, desc->rows - row);
+      const mssa_status launched =
+          check_device(mssa::launch_norm(a, desc->dtype == MSSA_BF16, e4m3, stream_of(stream)), "norm launch");
+      if (launched != MSSA_OK) return launched;
+    }
+    return MSSA_OK;
   });
 }
 

@@ -18,6 +18,10 @@ constexpr int kMxBlock = 32;  // values under one MXFP4 scale
 
 inline int64_t mx_blocks(int64_t cols) { return (cols + kMxBlock - 1) / kMxBlock; }
 
+// Threads of a launch.  A grid's axis has to have fewer than 2^32 of them;
+// calls with more rows are made in slices of at most this many.
+constexpr int64_t kLaunchThreads = int64_t{1} << 31;
+
 // ------------------------------------------------------------------- norm
 constexpr int kNormMaxCols = 32768;
 
@@ -46,7 +50,10 @@ struct NormRowShape {
   int tpr, nv;
 };
 NormRowShape norm_row_shape(int cols);
+// Rows of one launch of the norm, whose output rows have y_pitch elements.
+int64_t norm_launch_rows(int y_pitch);
 
+// At most norm_launch_rows rows.
 hipError_t launch_norm(const NormArgs& a, bool bf16, bool e4m3, hipStream_t stream);
 // Blocks of the backward's first launch: a static rule on the sizes.
 int32_t norm_bwd_blocks(int64_t rows, int32_t cols);

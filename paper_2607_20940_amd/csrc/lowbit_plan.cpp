@@ -14,6 +14,8 @@ NormRowShape norm_row_shape(int cols) {
   return {1024, (pieces + 1023) / 1024};
 }
 
+int64_t norm_launch_rows(int y_pitch) { return kLaunchThreads / norm_row_shape(y_pitch).tpr; }
+
 int32_t norm_bwd_blocks(int64_t rows, int32_t cols) {
   const NormRowShape s = norm_row_shape(cols);
   const int64_t per = s.tpr >= 256 ? 1 : 256 / s.tpr, want = (rows + per - 1) / per;

@@ -293,7 +293,7 @@ template <class T, bool RES, bool E4, int TPR, int NV>
 hipError_t norm_go(const NormArgs& a, hipStream_t stream) {
   constexpr int kThreads = TPR > 256 ? TPR : 256, kRows = kThreads / TPR;
   const int64_t blocks = (a.rows + kRows - 1) / kRows;
-  if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+  if (blocks * kThreads > kLaunchThreads) return hipErrorInvalidValue;
   hipLaunchKernelGGL((norm_kernel<T, RES, E4, TPR, NV>), dim3(static_cast<uint32_t>(blocks)), dim3(kThreads), 0, stream, a);
   return hipGetLastError();
 }

@@ -1,15 +1,19 @@
 // Host harness of the low-bit kernels' rules on sizes, built without any GPU
 // code (under AddressSanitizer and UndefinedBehaviorSanitizer by
 // tests/test_lowbit_rules.py).  The harness walks each rule the way its kernel
-// does and checks what the kernel relies on.  Exit status 0 iff every check
-// passed.
+// does and checks what the kernel relies on.  Launchers are stubs that record
+// what they are asked for; device addresses are never dereferenced.  Exit
+// status 0 iff every check passed.
 #include <hip/hip_runtime_api.h>
 
+#include <algorithm>
 #include <cstdio>
 #include <cstring>
 #include <string>
 #include <vector>
 
+#include "../../include/libmssa.h"
+#include "../../paper_2607_20940_amd/csrc/abi_status.hpp"
 #include "../../paper_2607_20940_amd/csrc/lowbit_args.hpp"
 
 namespace {
@@ -19,6 +23,69 @@ int g_failures = 0, g_checks = 0;
 void check(bool ok, const std::string& what) {
   ++g_checks;
   if (!ok && ++g_failures <= 40) std::fprintf(stderr, "FAIL %s\n", what.c_str());
+}
+
+constexpr int64_t kAxis = int64_t{1} << 32;  // threads along a grid's axis: fewer than this
+
+std::vector<mssa::NormArgs> g_norms;
+
+// An address that stands for a large device array.
+char* dev(int i) { return reinterpret_cast<char*>(uintptr_t{1} << 50) + (int64_t{i} << 54); }
+
+}  // namespace
+
+extern "C" const char* hipGetErrorString(hipError_t) { return "stub"; }
+
+namespace mssa {
+
+mssa_status fail(mssa_status s, const char*) noexcept { return s; }
+mssa_status fail(mssa_status s, const char*, const char*) noexcept { return s; }
+
+hipError_t launch_norm(const NormArgs& a, bool, bool, hipStream_t) {
+  const int tpr = norm_row_shape(a.y_pitch).tpr, threads = std::max(256, tpr), rows = threads / tpr;
+  check((a.rows + rows - 1) / rows * threads < kAxis, "a norm launch of 2^32 threads");
+  g_norms.push_back(a);
+  return hipSuccess;
+}
+hipError_t launch_norm_bwd(const NormBwdArgs&, bool, hipStream_t) { return hipSuccess; }
+hipError_t launch_mx_quantize(const MxArgs&, bool, hipStream_t) { return hipSuccess; }
+hipError_t launch_mx_dequantize(const MxArgs&, bool, hipStream_t) { return hipSuccess; }
+hipError_t launch_mx_project(const ProjectArgs&, bool, bool, hipStream_t) { return hipSuccess; }
+hipError_t launch_mx_attention(const MxAttnArgs&, const MxAttnPlan&, int, hipStream_t) { return hipSuccess; }
+
+}  // namespace mssa
+
+namespace {
+
+// The slices of a norm of many rows: together all rows, each in its place.
+void norm_slices() {
+  for (int32_t cols : {1, 64, 2048, 2049, 8192, 8193, 32768})
+    for (int64_t rows : {int64_t{1}, int64_t{1} << 21, (int64_t{1} << 25) + 1, (int64_t{1} << 26) + 3, int64_t{1} << 32})
+      for (int e4m3 : {0, 1}) {
+        const std::string what = "norm " + std::to_string(rows) + " x " + std::to_string(cols);
+        mssa_norm_desc d{};
+        d.rows = rows;
+        d.cols = cols;
+        d.dtype = MSSA_BF16;
+        d.out_dtype = e4m3 ? MSSA_E4M3 : MSSA_BF16;
+        d.x_stride = cols + 3;
+        g_norms.clear();
+        char *x = dev(0), *r = dev(1), *w = dev(2), *s = dev(3), *y = dev(4), *ys = dev(5), *rstd = dev(6);
+        check(mssa_add_rms_norm(&d, x, r, w, s, y, e4m3 ? reinterpret_cast<float*>(ys) : nullptr,
+                                reinterpret_cast<float*>(rstd), nullptr) == MSSA_OK,
+              what);
+        int64_t row = 0;
+        for (const mssa::NormArgs& a : g_norms) {
+          check(a.rows > 0 && a.weight == w && a.cols == cols, what + ": a slice");
+          check(a.x == x + row * (cols + 3) * 2 && a.residual == r + row * cols * 2 && a.sum == s + row * cols * 2 &&
+                    a.y == y + row * (e4m3 ? a.y_pitch : cols * 2) &&
+                    reinterpret_cast<char*>(a.rstd) == rstd + row * 4 &&
+                    reinterpret_cast<char*>(a.y_scale) == (e4m3 ? ys + row * 4 : nullptr),
+                what + ": a slice's place");
+          row += a.rows;
+        }
+        check(row == rows, what + ": the slices' rows");
+      }
 }
 
 // Every scale that a tile of the product reads is its own row's: the group as
@@ -54,6 +121,7 @@ void scale_groups() {
 int main() {
   scale_groups<8, 2>();  // MXFP4 tokens
   scale_groups<4, 1>();  // 8-bit tokens
+  norm_slices();
   std::printf("%d checks, %d failures\n", g_checks, g_failures);
   return g_failures ? 1 : 0;
 }

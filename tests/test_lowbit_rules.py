@@ -1,6 +1,6 @@
 """The low-bit kernels' rules on sizes under AddressSanitizer and
 UndefinedBehaviorSanitizer (no GPU): tests/host_harness/lowbit_rules_harness.cpp,
-built with g++ together with lowbit_plan.cpp."""
+built with g++ together with lowbit_plan.cpp and abi_lowbit.cpp."""
 
 import os
 import shutil
@@ -21,7 +21,8 @@ def harness(tmp_path_factory):
     cmd = [gxx, "-std=c++17", "-g", "-O1", "-fsanitize=address,undefined", "-fno-sanitize-recover=undefined",
            "-fno-omit-frame-pointer", "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include",
            os.path.join(ROOT, "tests", "host_harness", "lowbit_rules_harness.cpp"),
-           os.path.join(CSRC, "lowbit_plan.cpp"), "-o", exe]
+           "-I" + os.path.join(ROOT, "include"), os.path.join(CSRC, "lowbit_plan.cpp"),
+           os.path.join(CSRC, "abi_lowbit.cpp"), "-o", exe]
     r = subprocess.run(cmd, capture_output=True, text=True)
     assert r.returncode == 0, r.stdout + r.stderr
     return exe
