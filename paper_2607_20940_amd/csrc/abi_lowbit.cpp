@@ -64,18 +64,24 @@ mssa_status mx_convert(const char* who, bool quantize, int64_t rows, int32_t col
     if (!aligned_to(values, elem_bytes(dtype))) return fail(MSSA_ERR_INVALID_ARG, "values must be aligned to their type");
     if (!aligned_to(codes, 4)) return fail(MSSA_ERR_INVALID_ARG, "codes must be 4-byte aligned");
     mssa::MxArgs a{};
-    a.in = quantize ? values : nullptr;
-    a.out = quantize ? nullptr : const_cast<void*>(values);
-    a.codes = const_cast<void*>(codes);
-    a.scales = const_cast<void*>(scales);
-    a.rows = rows;
     a.stride = stride_or(stride, cols);
     a.cols = cols;
     a.blocks = static_cast<int32_t>(mssa::mx_blocks(cols));
     const bool bf16 = dtype == MSSA_BF16;
-    return check_device(quantize ? mssa::launch_mx_quantize(a, bf16, stream_of(stream))
-                                 : mssa::launch_mx_dequantize(a, bf16, stream_of(stream)),
-                        who);
+    const int64_t step = mssa::mx_launch_rows(a.blocks);
+    for (int64_t row = 0; row < rows; row += step) {
+      const void* v = at_byte(values, row * a.stride * elem_bytes(dtype));
+      a.in = quantize ? v : nullptr;
+      a.out = quantize ? nullptr : const_cast<void*>(v);
+      a.codes = const_cast<void*>(at_byte(codes, row * a.blocks * 16));
+      a.scales = const_cast<void*>(at_byte(scales, row * a.blocks));
+      a.rows = std::min(step, rows - row);
+      const mssa_status launched = check_device(quantize ? mssa::launch_mx_quantize(a, bf16, stream_of(stream))
+                                                         : mssa::launch_mx_dequantize(a, bf16, stream_of(stream)),
+                                                who);
+      if (launched != MSSA_OK) return launched;
+    }
+    return MSSA_OK;
   });
 }
 

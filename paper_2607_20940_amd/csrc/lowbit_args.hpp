@@ -67,6 +67,10 @@ struct MxArgs {
   int32_t cols, blocks;  // blocks of 32 a row
 };
 
+// Rows of one launch, of `blocks` blocks each: a thread takes eight values.
+int64_t mx_launch_rows(int32_t blocks);
+
+// At most mx_launch_rows rows.
 hipError_t launch_mx_quantize(const MxArgs& a, bool bf16, hipStream_t stream);    // in -> codes, scales
 hipError_t launch_mx_dequantize(const MxArgs& a, bool bf16, hipStream_t stream);  // codes, scales -> out
 

@@ -22,6 +22,8 @@ int32_t norm_bwd_blocks(int64_t rows, int32_t cols) {
   return static_cast<int32_t>(std::min<int64_t>(want, 512));
 }
 
+int64_t mx_launch_rows(int32_t blocks) { return kLaunchThreads / (int64_t{4} * blocks); }
+
 hipError_t plan_mx_attention(int32_t batch, int32_t n_q, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
                              int64_t cache_tokens, MxAttnPlan* plan) {
   MxAttnPlan p{};

@@ -109,10 +109,10 @@ __global__ __launch_bounds__(kThreads) void dequantize_kernel(MxArgs a) {
   }
 }
 
-// One thread per eight values; at most 2^38 threads (the caller's check).
+// One thread per eight values.
 hipError_t grid_of(const MxArgs& a, uint32_t* blocks) {
   const int64_t n = (a.rows * a.blocks * 4 + kThreads - 1) / kThreads;
-  if (n > 0x7fffffff) return hipErrorInvalidValue;
+  if (n * kThreads > kLaunchThreads) return hipErrorInvalidValue;
   *blocks = static_cast<uint32_t>(n);
   return hipSuccess;
 }

@@ -28,6 +28,7 @@ void check(bool ok, const std::string& what) {
 constexpr int64_t kAxis = int64_t{1} << 32;  // threads along a grid's axis: fewer than this
 
 std::vector<mssa::NormArgs> g_norms;
+std::vector<mssa::MxArgs> g_conversions;
 
 // An address that stands for a large device array.
 char* dev(int i) { return reinterpret_cast<char*>(uintptr_t{1} << 50) + (int64_t{i} << 54); }
@@ -48,8 +49,12 @@ hipError_t launch_norm(const NormArgs& a, bool, bool, hipStream_t) {
   return hipSuccess;
 }
 hipError_t launch_norm_bwd(const NormBwdArgs&, bool, hipStream_t) { return hipSuccess; }
-hipError_t launch_mx_quantize(const MxArgs&, bool, hipStream_t) { return hipSuccess; }
-hipError_t launch_mx_dequantize(const MxArgs&, bool, hipStream_t) { return hipSuccess; }
+hipError_t launch_mx_quantize(const MxArgs& a, bool, hipStream_t) {
+  check((a.rows * a.blocks * 4 + 255) / 256 * 256 < kAxis, "a conversion launch of 2^32 threads");
+  g_conversions.push_back(a);
+  return hipSuccess;
+}
+hipError_t launch_mx_dequantize(const MxArgs& a, bool bf16, hipStream_t stream) { return launch_mx_quantize(a, bf16, stream); }
 hipError_t launch_mx_project(const ProjectArgs&, bool, bool, hipStream_t) { return hipSuccess; }
 hipError_t launch_mx_attention(const MxAttnArgs&, const MxAttnPlan&, int, hipStream_t) { return hipSuccess; }
 
@@ -81,6 +86,29 @@ void norm_slices() {
                     a.y == y + row * (e4m3 ? a.y_pitch : cols * 2) &&
                     reinterpret_cast<char*>(a.rstd) == rstd + row * 4 &&
                     reinterpret_cast<char*>(a.y_scale) == (e4m3 ? ys + row * 4 : nullptr),
+                what + ": a slice's place");
+          row += a.rows;
+        }
+        check(row == rows, what + ": the slices' rows");
+      }
+}
+
+void conversion_slices() {
+  for (int32_t cols : {1, 64, 5120, 1 << 20})
+    for (int64_t rows : {int64_t{1}, int64_t{1} << 16, (int64_t{1} << 20) + 7, (int64_t{1} << 30) + 1, int64_t{1} << 35})
+      for (int back : {0, 1}) {
+        const int64_t blocks = mssa::mx_blocks(cols), stride = cols + 5;
+        if (rows * blocks > int64_t{1} << 36) continue;  // refused
+        const std::string what = "conversion " + std::to_string(rows) + " x " + std::to_string(cols);
+        g_conversions.clear();
+        char *v = dev(0), *c = dev(1), *s = dev(2);
+        check((back ? mssa_mx_dequantize(rows, cols, MSSA_F32, c, s, v, stride, nullptr)
+                    : mssa_mx_quantize(rows, cols, MSSA_F32, v, stride, c, s, nullptr)) == MSSA_OK,
+              what);
+        int64_t row = 0;
+        for (const mssa::MxArgs& a : g_conversions) {
+          check(a.rows > 0 && (back ? a.out : a.in) == v + row * stride * 4 && (back ? a.in : a.out) == nullptr &&
+                    a.codes == c + row * blocks * 16 && a.scales == s + row * blocks,
                 what + ": a slice's place");
           row += a.rows;
         }
@@ -122,6 +150,7 @@ int main() {
   scale_groups<8, 2>();  // MXFP4 tokens
   scale_groups<4, 1>();  // 8-bit tokens
   norm_slices();
+  conversion_slices();
   std::printf("%d checks, %d failures\n", g_checks, g_failures);
   return g_failures ? 1 : 0;
 }

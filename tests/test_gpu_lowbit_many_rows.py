@@ -43,3 +43,22 @@ def test_norm(out):
     short = run(x, r)
     for got, want in zip(run(_repeated(x, rows), _repeated(r, rows)), short):
         assert _same(got, want)
+
+
+def test_conversion():
+    """Single values, a block each: 2^32 threads and more there and back."""
+    rows = (1 << 30) + 5
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn(STRETCH, 1, generator=g, device="cuda").bfloat16()
+
+    def run(x):
+        n = x.shape[0]
+        codes, scales = (torch.empty(s, dtype=torch.uint8, device="cuda") for s in mssa.mx_shapes(n, 1))
+        mssa.mssa_mx_quantize(n, 1, "bf16", x, codes, scales)
+        y = torch.empty_like(x)
+        mssa.mssa_mx_dequantize(n, 1, "bf16", codes, scales, y)
+        return codes, scales, y
+
+    short = run(x)
+    for got, want in zip(run(_repeated(x, rows)), short):
+        assert _same(got, want)
