@@ -554,7 +554,8 @@ typedef struct {
  *   bias         [out_features], or NULL
  *   y            host array of `parts` device pointers, each [rows, N]
  * With part0_scale = softmax_scale * log2(e) part 0 is the queries of a
- * MSSA_PLAN_Q_PRESCALED plan.  Outputs must not alias the inputs. */
+ * MSSA_PLAN_Q_PRESCALED plan.  Outputs must not alias the inputs.  Outputs of
+ * 2^38 values and more can be MSSA_ERR_UNSUPPORTED (a launch's limit). */
 mssa_status mssa_mx_project(const mssa_mx_project_desc* desc, const void* x, const void* x_scales, const void* w,
                             const void* w_scales, const void* bias, void* const* y, void* stream);
 

@@ -237,6 +237,11 @@ mssa_status mssa_mx_project(const mssa_mx_project_desc* desc, const void* x, con
     if (!x || !x_scales || !w || !w_scales || !y) return fail(MSSA_ERR_INVALID_ARG, "null argument");
     for (const void* t : {x, x_scales, w, w_scales, bias})
       if (!aligned16(t)) return fail(MSSA_ERR_INVALID_ARG, "tensors must be 16-byte aligned");
+    const int64_t blocks = mssa::mx_blocks(desc->in_features);
+    mssa::ProjectPlan plan;
+    if (mssa::plan_mx_project(static_cast<int32_t>(desc->rows), desc->out_features, static_cast<int32_t>(blocks),
+                              desc->x_format == MSSA_MXFP4, &plan) != hipSuccess)
+      return fail(MSSA_ERR_UNSUPPORTED, "too many outputs for one launch");
     mssa::ProjectArgs a{};
     for (int p = 0; p < desc->parts; ++p) {
       if (!y[p]) return fail(MSSA_ERR_INVALID_ARG, "null output");
@@ -252,7 +257,7 @@ mssa_status mssa_mx_project(const mssa_mx_project_desc* desc, const void* x, con
     a.bias = bias;
     a.M = static_cast<int32_t>(desc->rows);
     a.N = desc->out_features;
-    a.NB = static_cast<int32_t>(mssa::mx_blocks(desc->in_features));
+    a.NB = static_cast<int32_t>(blocks);
     a.split = desc->out_features / desc->parts;
     a.part0_scale = desc->part0_scale;
     return check_device(mssa::launch_mx_project(a, desc->x_format == MSSA_MXFP4, desc->out_dtype == MSSA_BF16,

@@ -19,8 +19,9 @@ constexpr int kMxBlock = 32;  // values under one MXFP4 scale
 inline int64_t mx_blocks(int64_t cols) { return (cols + kMxBlock - 1) / kMxBlock; }
 
 // Threads of a launch.  A grid's axis has to have fewer than 2^32 of them;
-// calls with more rows are made in slices of at most this many.
+// calls with more rows are made in slices of at most kLaunchThreads.
 constexpr int64_t kLaunchThreads = int64_t{1} << 31;
+inline bool launchable(int64_t blocks, int threads) { return blocks < ((int64_t{1} << 32) + threads - 1) / threads; }
 
 // ------------------------------------------------------------------- norm
 constexpr int kNormMaxCols = 32768;
@@ -106,6 +107,28 @@ struct ScaleGroups {
   // the next row, whose NaN scales are not to meet this row's zeros.
   MSSA_HOST_DEVICE bool there(int st, int half) const { return st * NBK + kHalf * half < blocks; }
 };
+
+// Which kernel makes a product: one of the two for few tokens, whose blocks
+// take kProjectFewFeatures features each, or one of the two tile sizes.
+enum class ProjectKernel { kFew16, kFew32, kSmallTiles, kLargeTiles };
+constexpr int kProjectFewFeatures = 16, kProjectFewWaves = 4;
+
+// A block's tile: tokens x features, its waves, its stages in LDS.
+struct TileSize {
+  int tokens, features, waves_m, waves_n, stages;
+  constexpr int threads() const { return waves_m * waves_n * 64; }
+};
+constexpr TileSize tile_size(bool x_fp4, bool large) {
+  if (x_fp4) return large ? TileSize{256, 256, 2, 4, 2} : TileSize{64, 128, 1, 4, 2};
+  return large ? TileSize{128, 256, 1, 4, 2} : TileSize{64, 128, 1, 4, 3};
+}
+
+struct ProjectPlan {
+  ProjectKernel kernel;
+  int64_t blocks;
+};
+// Sizes whose launch would have 2^32 threads are refused.
+hipError_t plan_mx_project(int32_t tokens, int32_t features, int32_t blocks, bool x_fp4, ProjectPlan* plan);
 
 hipError_t launch_mx_project(const ProjectArgs& a, bool x_fp4, bool out_bf16, hipStream_t stream);
 

@@ -24,6 +24,55 @@ int32_t norm_bwd_blocks(int64_t rows, int32_t cols) {
 
 int64_t mx_launch_rows(int32_t blocks) { return kLaunchThreads / (int64_t{4} * blocks); }
 
+namespace {
+
+// Microseconds that `tiles` tiles of a shape take, of which n may share a CU:
+// whole rounds, then a rest with fewer blocks a CU.  (p0 + p1 n) a stage and
+// q0 + q1 n besides, fitted to ten products of 600 to 27840 tokens.
+struct ShapeCost {
+  int share;
+  double p0, p1, q0, q1;
+  double operator()(int64_t tiles, int stages) const {
+    auto round = [&](int64_t n) { return (p0 + p1 * static_cast<double>(n)) * stages + q0 + q1 * static_cast<double>(n); };
+    const int64_t slots = 256 * share, rest = tiles % slots;
+    return static_cast<double>(tiles / slots) * round(share) + (rest ? round((rest + 255) / 256) : 0.0);
+  }
+};
+
+int64_t tiles_of(const TileSize& t, int64_t tokens, int64_t features) {
+  return (tokens + t.tokens - 1) / t.tokens * ((features + t.features - 1) / t.features);
+}
+
+}  // namespace
+
+// Up to 32 tokens the weights' bytes are all that counts.  Above, large tiles
+// need the fewest LDS bytes a product and small tiles fill the CUs sooner.
+// 8-bit tokens: 128 x 256 tiles, two blocks a CU, one's outputs leaving while
+// the other multiplies (12870 x 1536 -> 4608: 119 us; one 256 x 256 block a CU
+// 123, 128 x 128 tiles 148), or 64 x 128 (600 x 600 -> 1000: 9.5 us against
+// 16.7).  MXFP4 tokens, whose products are done twice as fast from LDS:
+// 256 x 256 (27840 x 5120 -> 15360: 1.20 ms; 128 x 256 tiles 1.54), or 64 x 128
+// (600 x 608 -> 1000: 9.0 us against 18.7).
+hipError_t plan_mx_project(int32_t tokens, int32_t features, int32_t blocks, bool x_fp4, ProjectPlan* plan) {
+  if (tokens <= 32) {
+    *plan = {tokens <= 16 ? ProjectKernel::kFew16 : ProjectKernel::kFew32,
+             (int64_t{features} + kProjectFewFeatures - 1) / kProjectFewFeatures};
+    return hipSuccess;
+  }
+  const ShapeCost small = x_fp4 ? ShapeCost{3, 0., 0.63, 3., 0.} : ShapeCost{3, 0.3, 0.2, 3., 1.};
+  const ShapeCost large = x_fp4 ? ShapeCost{1, 0., 1.74, 11.3, 0.} : ShapeCost{2, 0.43, 0.57, 5., 3.};
+  const int stages = (blocks + (x_fp4 ? 7 : 3)) / (x_fp4 ? 8 : 4);
+  const TileSize ts = tile_size(x_fp4, false), tl = tile_size(x_fp4, true);
+  const int64_t n_small = tiles_of(ts, tokens, features), n_large = tiles_of(tl, tokens, features);
+  if (launchable(n_small, ts.threads()) && small(n_small, stages) < large(n_large, stages))
+    *plan = {ProjectKernel::kSmallTiles, n_small};
+  else if (launchable(n_large, tl.threads()))
+    *plan = {ProjectKernel::kLargeTiles, n_large};
+  else
+    return hipErrorInvalidValue;
+  return hipSuccess;
+}
+
 hipError_t plan_mx_attention(int32_t batch, int32_t n_q, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
                              int64_t cache_tokens, MxAttnPlan* plan) {
   MxAttnPlan p{};

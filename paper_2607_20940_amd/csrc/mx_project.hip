@@ -463,7 +463,7 @@ void tile_kernel(ProjectArgs a) {
 // 16) takes blocks 4 g .. 4 g + 3 of sixteen, one per matrix step, so its
 // codes are 64 consecutive bytes and its scales four.  What counts is bytes on
 // their way: each wave has its next piece loading.
-constexpr int kFewWaves = 4;
+constexpr int kFewWaves = kProjectFewWaves;
 
 // Four scale bytes, of which the first n are there.
 __device__ inline uint32_t four_scales(const uint8_t* p, int n) {
@@ -481,7 +481,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(ProjectArgs a) {
   __shared__ float red[kFewWaves - 1][TT][4][64];
   const int tid = threadIdx.x, lane = tid & 63, m = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int n0 = blockIdx.x * 16;
+  const int n0 = blockIdx.x * kProjectFewFeatures;
   const int64_t xp = static_cast<int64_t>(a.NB) * (XF4 ? 16 : 32);
   const int feature = min(n0 + m, a.N - 1);
   const char* W = static_cast<const char*>(a.w) + static_cast<int64_t>(feature) * a.NB * 16;
@@ -592,55 +592,29 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(ProjectArgs a) {
 }
 
 template <bool XF4, class T, int TT>
-hipError_t few_go(const ProjectArgs& a, hipStream_t stream) {
-  hipLaunchKernelGGL((few_kernel<XF4, T, TT>), dim3((a.N + 15) / 16), dim3(kFewWaves * 64), 0, stream, a);
+hipError_t few_go(const ProjectArgs& a, const ProjectPlan& plan, hipStream_t stream) {
+  hipLaunchKernelGGL((few_kernel<XF4, T, TT>), dim3(static_cast<uint32_t>(plan.blocks)), dim3(kFewWaves * 64), 0, stream, a);
   return hipGetLastError();
 }
 
-template <bool XF4, class T, int BM, int BN, int WM, int WN, int BUFS>
-hipError_t tile_go(const ProjectArgs& a, hipStream_t stream) {
-  const int64_t tiles = static_cast<int64_t>((a.M + BM - 1) / BM) * ((a.N + BN - 1) / BN);
-  if (tiles > 0x7fffffff) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((tile_kernel<XF4, T, BM, BN, WM, WN, BUFS>), dim3(static_cast<uint32_t>(tiles)), dim3(WM * WN * 64), 0, stream, a);
+template <bool XF4, class T, bool LARGE>
+hipError_t tile_go(const ProjectArgs& a, const ProjectPlan& plan, hipStream_t stream) {
+  constexpr TileSize t = tile_size(XF4, LARGE);
+  hipLaunchKernelGGL((tile_kernel<XF4, T, t.tokens, t.features, t.waves_m, t.waves_n, t.stages>),
+                     dim3(static_cast<uint32_t>(plan.blocks)), dim3(t.threads()), 0, stream, a);
   return hipGetLastError();
 }
 
-// Microseconds that `tiles` tiles of a shape take, of which n may share a CU:
-// whole rounds, then a rest with fewer blocks a CU.  (p0 + p1 n) a stage and
-// q0 + q1 n besides, fitted to ten products of 600 to 27840 tokens.
-struct ShapeCost {
-  int share;
-  double p0, p1, q0, q1;
-  double operator()(int64_t tiles, int stages) const {
-    auto round = [&](int64_t n) { return (p0 + p1 * static_cast<double>(n)) * stages + q0 + q1 * static_cast<double>(n); };
-    const int64_t slots = 256 * share, rest = tiles % slots;
-    return static_cast<double>(tiles / slots) * round(share) + (rest ? round((rest + 255) / 256) : 0.0);
-  }
-};
-
-// Which kernel.  Up to 32 tokens the weights' bytes are all that counts.
-// Above, large tiles need the fewest LDS bytes a product and small tiles fill
-// the CUs sooner.  8-bit tokens: 128 x 256 tiles, two blocks a CU, one's
-// outputs leaving while the other multiplies (12870 x 1536 -> 4608: 119 us;
-// one 256 x 256 block a CU 123, 128 x 128 tiles 148), or 64 x 128
-// (600 x 600 -> 1000: 9.5 us against 16.7).  MXFP4 tokens, whose products are
-// done twice as fast from LDS: 256 x 256 (27840 x 5120 -> 15360: 1.20 ms;
-// 128 x 256 tiles 1.54), or 64 x 128 (600 x 608 -> 1000: 9.0 us against 18.7).
 template <bool XF4, class T>
 hipError_t project(const ProjectArgs& a, hipStream_t stream) {
-  if (a.M <= 16) return few_go<XF4, T, 1>(a, stream);
-  if (a.M <= 32) return few_go<XF4, T, 2>(a, stream);
-  constexpr int kLargeM = XF4 ? 256 : 128;
-  constexpr ShapeCost small = XF4 ? ShapeCost{3, 0., 0.63, 3., 0.} : ShapeCost{3, 0.3, 0.2, 3., 1.};
-  constexpr ShapeCost large = XF4 ? ShapeCost{1, 0., 1.74, 11.3, 0.} : ShapeCost{2, 0.43, 0.57, 5., 3.};
-  const int stages = (a.NB + (XF4 ? 7 : 3)) / (XF4 ? 8 : 4);
-  const int64_t n_small = static_cast<int64_t>((a.M + 63) / 64) * ((a.N + 127) / 128);
-  const int64_t n_large = static_cast<int64_t>((a.M + kLargeM - 1) / kLargeM) * ((a.N + 255) / 256);
-  if (small(n_small, stages) < large(n_large, stages)) return tile_go<XF4, T, 64, 128, 1, 4, XF4 ? 2 : 3>(a, stream);
-  if constexpr (XF4)
-    return tile_go<XF4, T, 256, 256, 2, 4, 2>(a, stream);
-  else
-    return tile_go<XF4, T, 128, 256, 1, 4, 2>(a, stream);
+  ProjectPlan plan;
+  if (const hipError_t e = plan_mx_project(a.M, a.N, a.NB, XF4, &plan); e != hipSuccess) return e;
+  switch (plan.kernel) {
+    case ProjectKernel::kFew16: return few_go<XF4, T, 1>(a, plan, stream);
+    case ProjectKernel::kFew32: return few_go<XF4, T, 2>(a, plan, stream);
+    case ProjectKernel::kSmallTiles: return tile_go<XF4, T, false>(a, plan, stream);
+    default: return tile_go<XF4, T, true>(a, plan, stream);
+  }
 }
 
 }  // namespace

@@ -55,7 +55,17 @@ hipError_t launch_mx_quantize(const MxArgs& a, bool, hipStream_t) {
   return hipSuccess;
 }
 hipError_t launch_mx_dequantize(const MxArgs& a, bool bf16, hipStream_t stream) { return launch_mx_quantize(a, bf16, stream); }
-hipError_t launch_mx_project(const ProjectArgs&, bool, bool, hipStream_t) { return hipSuccess; }
+hipError_t launch_mx_project(const ProjectArgs& a, bool x_fp4, bool, hipStream_t) {
+  ProjectPlan plan;
+  check(plan_mx_project(a.M, a.N, a.NB, x_fp4, &plan) == hipSuccess, "the plan of a product that was let through");
+  const bool few = plan.kernel == ProjectKernel::kFew16 || plan.kernel == ProjectKernel::kFew32;
+  const TileSize t = tile_size(x_fp4, plan.kernel == ProjectKernel::kLargeTiles);
+  const int64_t want = few ? (a.N + kProjectFewFeatures - 1) / kProjectFewFeatures
+                           : (int64_t{a.M} + t.tokens - 1) / t.tokens * ((a.N + t.features - 1) / t.features);
+  check(plan.blocks == want, "a product's blocks");
+  check(plan.blocks * (few ? kProjectFewWaves * 64 : t.threads()) < kAxis, "a product launch of 2^32 threads");
+  return hipSuccess;
+}
 hipError_t launch_mx_attention(const MxAttnArgs&, const MxAttnPlan&, int, hipStream_t) { return hipSuccess; }
 
 }  // namespace mssa
@@ -116,6 +126,27 @@ void conversion_slices() {
       }
 }
 
+// Products at the limits: made in one launch, or refused where the outputs are 2^38 and more.
+void product_launches() {
+  for (int64_t rows : {int64_t{1}, int64_t{33}, int64_t{1} << 20, (int64_t{1} << 30) - 64, (int64_t{1} << 30) - 63, int64_t{1} << 30})
+    for (int32_t in : {1, 32, 5120, 1 << 20})
+      for (int32_t features : {1, 128, 129, 256, 257, 15360, 1 << 20})
+        for (int32_t format : {MSSA_E4M3, MSSA_MXFP4}) {
+          mssa_mx_project_desc d{};
+          d.rows = rows;
+          d.in_features = in;
+          d.out_features = features;
+          d.parts = 1;
+          d.x_format = format;
+          d.out_dtype = MSSA_BF16;
+          d.part0_scale = 1.f;
+          void* y = dev(4);
+          const mssa_status s = mssa_mx_project(&d, dev(0), dev(1), dev(2), dev(3), nullptr, &y, nullptr);
+          check(s == MSSA_OK || (s == MSSA_ERR_UNSUPPORTED && rows * features >= int64_t{1} << 38),
+                "product " + std::to_string(rows) + " x " + std::to_string(in) + " -> " + std::to_string(features));
+        }
+}
+
 // Every scale that a tile of the product reads is its own row's: the group as
 // the kernel fills it (from memory where it is direct, else with zeros past
 // the row), and the bytes that a lane half takes of it.
@@ -151,6 +182,7 @@ int main() {
   scale_groups<4, 1>();  // 8-bit tokens
   norm_slices();
   conversion_slices();
+  product_launches();
   std::printf("%d checks, %d failures\n", g_checks, g_failures);
   return g_failures ? 1 : 0;
 }

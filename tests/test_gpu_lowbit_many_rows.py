@@ -62,3 +62,21 @@ def test_conversion():
     short = run(x)
     for got, want in zip(run(_repeated(x, rows)), short):
         assert _same(got, want)
+
+
+def test_product():
+    """Tiles of 64 tokens would be 2^24 blocks of 256 threads."""
+    rows = 1 << 30
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x = torch.randint(0, 127, (STRETCH, 32), generator=g, device="cuda", dtype=torch.uint8)
+    xs = torch.rand(STRETCH, generator=g, device="cuda")
+    w = torch.randint(0, 256, (2, 16), generator=g, device="cuda", dtype=torch.uint8)
+    ws = torch.full((2, 1), 127, dtype=torch.uint8, device="cuda")
+
+    def run(x, xs):
+        y = torch.empty(x.shape[0], 2, dtype=torch.bfloat16, device="cuda")
+        mssa.mssa_mx_project(mssa.mx_project_desc(x.shape[0], 32, 2), x, xs, w, ws, None, [y])
+        return y
+
+    short = run(x, xs)
+    assert _same(run(_repeated(x, rows), _repeated(xs, rows)), short)
