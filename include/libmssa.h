@@ -589,7 +589,9 @@ mssa_status mssa_mx_attention_workspace_size(const mssa_mx_attention_desc* desc,
  *                neither; they may be out and lse themselves.
  *   lse          [batch, q_heads, n_q] (lse_stride) natural log of the sum of
  *                exp(scale q k) over all keys, or NULL
- * A query with no keys at all has out = 0 and lse = -inf. */
+ * A query with no keys at all has out = 0 and lse = -inf.  Sizes that need
+ * 2^32 threads in one launch (from 2^23 pairs of a sequence and a key head on)
+ * or 2^31 tiles of 64 tokens in all are MSSA_ERR_UNSUPPORTED. */
 mssa_status mssa_mx_attention(const mssa_mx_attention_desc* desc, const void* q, const void* k_codes,
                               const void* k_scales, const void* v_codes, const void* v_scales, const int32_t* kv_len,
                               const void* prior_out, const float* prior_lse, void* workspace,

@@ -173,7 +173,12 @@ struct MxAttnPlan {
   int32_t slot_rows;   // query rows of an item
   int32_t head_waves;  // few rows: waves of a block on neighbouring key heads
   int64_t blocks, workspace_bytes;
+  int32_t join_rows;   // rows of a block of the joining launch
+  int64_t join_blocks;  // blocks of the joining launch (made in slices), 0 without workers
+  int32_t threads() const { return (waves ? waves : kMxAttnFewWaves) * 64; }
 };
+constexpr int kMxAttnJoinThreads = 256;
+// Sizes whose first launch would have 2^32 threads are refused.
 hipError_t plan_mx_attention(int32_t batch, int32_t n_q, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
                              int64_t cache_tokens, MxAttnPlan* plan);
 hipError_t launch_mx_attention(const MxAttnArgs& a, const MxAttnPlan& plan, int head_dim, hipStream_t stream);

@@ -100,9 +100,9 @@ hipError_t plan_mx_attention(int32_t batch, int32_t n_q, int32_t q_heads, int32_
   if (tiles > least) p.workers = static_cast<int32_t>(std::max<int64_t>(1, std::min({int64_t{kMxAttnMaxWorkers}, slots / side, most})));
   p.blocks = p.workers ? (p.waves ? p.workers : (p.workers + 7) / 8 * 8 * side)
                        : (p.waves ? items * batch : (batch + int64_t{7}) / 8 * 8 * side);
-  if (slot_rows > 0x7fffffff || p.blocks > 0x7fffffff ||
-      items * batch * (slot_rows / (p.waves ? 8 : 1)) > 0x7fffffff)
-    return hipErrorInvalidValue;
+  p.join_rows = p.waves ? 8 : 1;
+  p.join_blocks = p.workers ? items * batch * (slot_rows / p.join_rows) : 0;
+  if (slot_rows > 0x7fffffff || !launchable(p.blocks, p.threads()) || p.join_blocks > 0x7fffffff) return hipErrorInvalidValue;
   p.items = static_cast<int32_t>(items);
   p.slot_rows = static_cast<int32_t>(slot_rows);
   p.workspace_bytes = int64_t{2} * p.workers * slot_rows * (head_dim + 2) * 4;

@@ -727,16 +727,17 @@ __global__ __launch_bounds__(kFewWaves * 64) __attribute__((amdgpu_waves_per_eu(
 // of sequences without tokens.  D / 4 threads side by side on a row's dims.
 // Items in many slots (few rows, long contexts): a row at a time, the groups
 // of threads on different slots; else a row per group.  Fixed orders.
-constexpr int kJoinThreads = 256;
+constexpr int kJoinThreads = kMxAttnJoinThreads;
 
 template <int D>
-__global__ __launch_bounds__(kJoinThreads) void join_kernel(MxAttnArgs a, int block_rows, int row_groups) {
+__global__ __launch_bounds__(kJoinThreads) void join_kernel(MxAttnArgs a, int block_rows, int row_groups, int first) {
   constexpr int kSide = D / 4, kGroups = kJoinThreads / kSide;
   __shared__ float weight[kMaxWorkers];
   __shared__ f32x4 part[kGroups][kSide];
   __shared__ float red[2][kJoinThreads / 64];
   const int tid = threadIdx.x, wave = tid >> 6, side = tid % kSide, grp = tid / kSide;
-  const int unit = blockIdx.x / row_groups, rg = blockIdx.x - unit * row_groups;
+  const int block = first + static_cast<int>(blockIdx.x);
+  const int unit = block / row_groups, rg = block - unit * row_groups;
   const int b = unit / a.items, item = unit - b * a.items;
   uint32_t start;
   const Shares sh = shares_of(a, b, &start);
@@ -843,10 +844,14 @@ hipError_t attn_dim(const MxAttnArgs& a, const MxAttnPlan& plan, hipStream_t str
     hipLaunchKernelGGL((attn_kernel<D, 8>), grid, dim3(8 * 64), 0, stream, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || plan.workers == 0) return e;
-  const int block_rows = plan.waves ? 8 : 1, row_groups = plan.slot_rows / block_rows;
-  hipLaunchKernelGGL((join_kernel<D>), dim3(static_cast<uint32_t>(static_cast<int64_t>(a.batch) * a.items * row_groups)),
-                     dim3(kJoinThreads), 0, stream, a, block_rows, row_groups);
-  return hipGetLastError();
+  const int row_groups = plan.slot_rows / plan.join_rows;
+  constexpr int64_t kSlice = kLaunchThreads / kJoinThreads;
+  for (int64_t first = 0; first < plan.join_blocks; first += kSlice) {
+    hipLaunchKernelGGL((join_kernel<D>), dim3(static_cast<uint32_t>(std::min(kSlice, plan.join_blocks - first))),
+                       dim3(kJoinThreads), 0, stream, a, plan.join_rows, row_groups, static_cast<int>(first));
+    if (const hipError_t joined = hipGetLastError(); joined != hipSuccess) return joined;
+  }
+  return hipSuccess;
 }
 
 }  // namespace

@@ -66,7 +66,14 @@ hipError_t launch_mx_project(const ProjectArgs& a, bool x_fp4, bool, hipStream_t
   check(plan.blocks * (few ? kProjectFewWaves * 64 : t.threads()) < kAxis, "a product launch of 2^32 threads");
   return hipSuccess;
 }
-hipError_t launch_mx_attention(const MxAttnArgs&, const MxAttnPlan&, int, hipStream_t) { return hipSuccess; }
+hipError_t launch_mx_attention(const MxAttnArgs& a, const MxAttnPlan& p, int, hipStream_t) {
+  check(p.blocks * p.threads() < kAxis, "an attention launch of 2^32 threads");
+  // the joining launch is made in slices: all rows of all items, in 31 bits
+  check(p.join_blocks == (p.workers ? int64_t{a.items} * a.batch * p.slot_rows / p.join_rows : 0) &&
+            p.slot_rows % p.join_rows == 0 && p.join_blocks <= 0x7fffffff,
+        "the joining launch's blocks");
+  return hipSuccess;
+}
 
 }  // namespace mssa
 
@@ -147,6 +154,29 @@ void product_launches() {
         }
 }
 
+// Attentions at the limits: made, or refused where they have 2^24 blocks and more (the sizes of single calls).
+void attention_launches() {
+  for (int32_t batch : {1, 4096, 1 << 20, (1 << 24) - 8, 1 << 24})
+    for (int32_t n_q : {1, 32, 33, 2048, 2049, 1 << 20})
+      for (int32_t heads : {1, 5, 128})
+        for (int64_t tokens : {1, 192, 32760}) {
+          mssa_mx_attention_desc d{};
+          d.batch = batch;
+          d.n_q = n_q;
+          d.q_heads = d.kv_heads = heads;
+          d.head_dim = 64;
+          d.cache_tokens = tokens;
+          int64_t bytes = 0;
+          const mssa_status sized = mssa_mx_attention_workspace_size(&d, &bytes);
+          const mssa_status s = mssa_mx_attention(&d, dev(0), dev(1), dev(2), dev(3), dev(4), nullptr, nullptr, nullptr,
+                                                  dev(5), bytes, dev(6), nullptr, nullptr);
+          const std::string what = "attention " + std::to_string(batch) + " x " + std::to_string(n_q) + " x " +
+                                   std::to_string(heads) + ", " + std::to_string(tokens);
+          check(s == sized && (s == MSSA_OK || s == MSSA_ERR_UNSUPPORTED), what);
+          if (int64_t{batch} * n_q * heads <= 1 << 24 && int64_t{batch} * heads < 1 << 23) check(s == MSSA_OK, what + ": refused");
+        }
+}
+
 // Every scale that a tile of the product reads is its own row's: the group as
 // the kernel fills it (from memory where it is direct, else with zeros past
 // the row), and the bytes that a lane half takes of it.
@@ -183,6 +213,7 @@ int main() {
   norm_slices();
   conversion_slices();
   product_launches();
+  attention_launches();
   std::printf("%d checks, %d failures\n", g_checks, g_failures);
   return g_failures ? 1 : 0;
 }

@@ -2,10 +2,14 @@
 axis): the rows repeat a short stretch, whose own call gives the bytes that
 every stretch has to have."""
 
+import numpy as np
 import pytest
 import torch
 
+from oracle import lowbit
 from paper_2607_20940_amd import mssa
+
+from lowbit_common import f64
 
 pytestmark = pytest.mark.gpu
 
@@ -80,3 +84,31 @@ def test_product():
 
     short = run(x, xs)
     assert _same(run(_repeated(x, rows), _repeated(xs, rows)), short)
+
+
+def test_attention_of_many_queries():
+    """2^24 query rows of a few rows each, whose joining launch takes a block a row; 16 sequences, again and again.
+    The bounds are those of test_gpu_mx_attention.py."""
+    few, times, n_q, heads, D, T = 16, 256, 32, 128, 64, 192
+    g = torch.Generator(device="cuda").manual_seed(3)
+    q = torch.randn(few, n_q, heads, D, generator=g, device="cuda").bfloat16()
+    (kc, ks), (vc, vs) = ((torch.randint(0, 256, (few, T, heads, D // 2), generator=g, device="cuda", dtype=torch.uint8),
+                           torch.randint(124, 127, (few, T, heads, D // 32), generator=g, device="cuda", dtype=torch.uint8))
+                          for _ in range(2))
+    d = mssa.mx_attention_desc(few * times, n_q, heads, heads, D, T)
+    size = mssa.mssa_mx_attention_workspace_size(d)
+    assert size > 0  # shared items: there is a joining launch
+    ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+    out = torch.empty(few * times, n_q, heads, D, dtype=torch.bfloat16, device="cuda")
+    many = [t.repeat(times, 1, 1, 1) for t in (q, kc, ks, vc, vs)]
+    mssa.mssa_mx_attention(d, *many, None, None, None, ws, out)
+    torch.cuda.synchronize()
+
+    def values(c, s):
+        return lowbit.mx_values(c.cpu().numpy().reshape(-1, D // 2), s.cpu().numpy().reshape(-1, D // 32)).reshape(few, T, heads, D)
+
+    ref, _, mag = lowbit.attention(f64(q), values(kc, ks), values(vc, vs), D ** -0.5, [T] * few)
+    bound = 2.0 ** -8 * 1.02 * np.abs(ref) + (2.0 ** -8 * 1.02 + 1e-4) * mag + 1e-30
+    ref, bound = (torch.from_numpy(t).cuda() for t in (ref, bound))
+    for got in out.view(times, few, n_q, heads, D):
+        assert bool(((got.double() - ref).abs() <= bound).all())
