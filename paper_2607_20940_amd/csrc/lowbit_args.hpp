@@ -123,6 +123,17 @@ constexpr TileSize tile_size(bool x_fp4, bool large) {
   return large ? TileSize{128, 256, 1, 4, 2} : TileSize{64, 128, 1, 4, 3};
 }
 
+// LDS bytes of a block: 128 bytes of every token and as many blocks of every
+// feature a stage, and groups of scales (ScaleGroups) of both operands' rows
+// for two pairs of stages (MXFP4 tokens), or of the features for every stage.
+constexpr int tile_lds(const TileSize& t, bool x_fp4) {
+  return x_fp4 ? t.stages * (t.tokens + t.features) * 128 + 2 * (t.tokens + t.features) * 16
+               : t.stages * (t.tokens * 128 + t.features * 64 + t.features * 4);
+}
+// Blocks that share a CU: its LDS decides (the kernels' registers allow as many).
+constexpr int kLdsBytes = 160 * 1024;
+constexpr int tile_share(const TileSize& t, bool x_fp4) { return kLdsBytes / tile_lds(t, x_fp4); }
+
 struct ProjectPlan {
   ProjectKernel kernel;
   int64_t blocks;

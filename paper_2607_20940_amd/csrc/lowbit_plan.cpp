@@ -26,13 +26,12 @@ int64_t mx_launch_rows(int32_t blocks) { return kLaunchThreads / (int64_t{4} * b
 
 namespace {
 
-// Microseconds that `tiles` tiles of a shape take, of which n may share a CU:
-// whole rounds, then a rest with fewer blocks a CU.  (p0 + p1 n) a stage and
-// q0 + q1 n besides, fitted to ten products of 600 to 27840 tokens.
+// Microseconds that `tiles` tiles take: whole rounds of `share` blocks a CU,
+// then a rest with fewer.  A round of n blocks a CU takes p0 + p1 n a stage and
+// q0 + q1 n besides.
 struct ShapeCost {
-  int share;
   double p0, p1, q0, q1;
-  double operator()(int64_t tiles, int stages) const {
+  double operator()(int64_t tiles, int share, int stages) const {
     auto round = [&](int64_t n) { return (p0 + p1 * static_cast<double>(n)) * stages + q0 + q1 * static_cast<double>(n); };
     const int64_t slots = 256 * share, rest = tiles % slots;
     return static_cast<double>(tiles / slots) * round(share) + (rest ? round((rest + 255) / 256) : 0.0);
@@ -48,23 +47,29 @@ int64_t tiles_of(const TileSize& t, int64_t tokens, int64_t features) {
 // Up to 32 tokens the weights' bytes are all that counts.  Above, large tiles
 // need the fewest LDS bytes a product and small tiles fill the CUs sooner.
 // 8-bit tokens: 128 x 256 tiles, two blocks a CU, one's outputs leaving while
-// the other multiplies (12870 x 1536 -> 4608: 119 us; one 256 x 256 block a CU
-// 123, 128 x 128 tiles 148), or 64 x 128 (600 x 600 -> 1000: 9.5 us against
-// 16.7).  MXFP4 tokens, whose products are done twice as fast from LDS:
-// 256 x 256 (27840 x 5120 -> 15360: 1.20 ms; 128 x 256 tiles 1.54), or 64 x 128
-// (600 x 608 -> 1000: 9.0 us against 18.7).
+// the other multiplies (12870 x 1536 -> 4608: 104 us, 64 x 128 tiles 131; at 119
+// us one 256 x 256 block a CU took 123 and 128 x 128 tiles 148), or 64 x 128
+// (600 x 608 -> 1000: 8.4 us against 14.7).  MXFP4 tokens, whose products are
+// done twice as fast from LDS: 256 x 256 (8000 x 5120 -> 15360: 352 us, 64 x 128
+// tiles 537; 27840 tokens 1.20 ms, 128 x 256 tiles 1.54), or 64 x 128
+// (600 x 608 -> 1000: 8.1 us against 16.7).  The costs are fitted to both tile
+// sizes' times of bf16 products of 33 to 12870 tokens, 608 to 5120 values and
+// 1000 to 15360 features (58 of each format, each within 40 %): the tiles that
+// they choose are the faster ones, or within 3 % of them.  With fp32 outputs
+// of 8-bit tokens, which take another path, within 11 %.
 hipError_t plan_mx_project(int32_t tokens, int32_t features, int32_t blocks, bool x_fp4, ProjectPlan* plan) {
   if (tokens <= 32) {
     *plan = {tokens <= 16 ? ProjectKernel::kFew16 : ProjectKernel::kFew32,
              (int64_t{features} + kProjectFewFeatures - 1) / kProjectFewFeatures};
     return hipSuccess;
   }
-  const ShapeCost small = x_fp4 ? ShapeCost{3, 0., 0.63, 3., 0.} : ShapeCost{3, 0.3, 0.2, 3., 1.};
-  const ShapeCost large = x_fp4 ? ShapeCost{1, 0., 1.74, 11.3, 0.} : ShapeCost{2, 0.43, 0.57, 5., 3.};
+  const ShapeCost small = x_fp4 ? ShapeCost{0.35, 0.15, 5.3, 0.} : ShapeCost{0.06, 0.29, 5.6, 0.};
+  const ShapeCost large = x_fp4 ? ShapeCost{0., 1.36, 0., 11.5} : ShapeCost{0., 0.75, 9.5, 0.5};
   const int stages = (blocks + (x_fp4 ? 7 : 3)) / (x_fp4 ? 8 : 4);
   const TileSize ts = tile_size(x_fp4, false), tl = tile_size(x_fp4, true);
   const int64_t n_small = tiles_of(ts, tokens, features), n_large = tiles_of(tl, tokens, features);
-  if (launchable(n_small, ts.threads()) && small(n_small, stages) < large(n_large, stages))
+  if (launchable(n_small, ts.threads()) &&
+      small(n_small, tile_share(ts, x_fp4), stages) < large(n_large, tile_share(tl, x_fp4), stages))
     *plan = {ProjectKernel::kSmallTiles, n_small};
   else if (launchable(n_large, tl.threads()))
     *plan = {ProjectKernel::kLargeTiles, n_large};

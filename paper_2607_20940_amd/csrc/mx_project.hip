@@ -114,7 +114,8 @@ struct TileShape {
   static_assert(NX * 1024 * kWaves == kXBytes && NW * 1024 * kWaves == kWBytes, "whole transfers");
   static constexpr int NSG = (kSRows / 64 + kWaves - 1) / kWaves;  // groups of 64 scale rows of a wave
   static_assert(kSRows % 64 == 0 && BM % 64 == 0, "whole groups of scale rows");
-  static_assert(kBufs * kStage + kSBufs * kScales <= 160 * 1024, "LDS of a CU");
+  static_assert(kBufs * kStage + kSBufs * kScales == tile_lds({BM, BN, WM, WN, BUFS}, XF4), "the tile choice's LDS");
+  static_assert(kBufs * kStage + kSBufs * kScales <= kLdsBytes, "LDS of a CU");
 };
 
 // Chunk (16 bytes) c of row r lies at chunk c ^ swizzle(r): sixteen rows read
@@ -144,7 +145,8 @@ void tile_kernel(ProjectArgs a) {
   // The output's rows, 32 of every wave, take the stages' place at the end.
   constexpr int kPitch = BN * static_cast<int>(sizeof(T)) + 16, kOut = WM * 32 * kPitch, kVec = 16 / sizeof(T);
   constexpr int kIn = S::kBufs * S::kStage + S::kSBufs * S::kScales, kOutBufs = 2 * kOut <= kIn ? 2 : 1;
-  __shared__ __attribute__((aligned(16))) char lds[kIn > kOut ? kIn : kOut];
+  static_assert(kIn >= kOut, "the outputs' rows fit the stages' place");
+  __shared__ __attribute__((aligned(16))) char lds[kIn];
 
   // Tiles in panels of four feature tiles: the blocks of an XCD, a run of
   // them, share rows of both operands in its L2.

@@ -154,6 +154,36 @@ void product_launches() {
         }
 }
 
+// The tile choice's model of a CU: as many blocks as its LDS holds, and no more.  The choices of some sizes, by
+// both tiles' measured times, and of the GPU tests that are to
+// reach one or the other.
+void tile_choices() {
+  for (bool x_fp4 : {false, true})
+    for (bool large : {false, true}) {
+      const mssa::TileSize t = mssa::tile_size(x_fp4, large);
+      const int stage = t.tokens * 128 + t.features * (x_fp4 ? 128 : 64);
+      // 16 bytes a row and operand for two pairs of stages, or 4 a feature and stage
+      const int lds = t.stages * stage + (x_fp4 ? 2 * 16 * (t.tokens + t.features) : t.stages * 4 * t.features);
+      const int share = mssa::tile_share(t, x_fp4);
+      check(mssa::tile_lds(t, x_fp4) == lds && share * lds <= 163840 && (share + 1) * lds > 163840, "blocks of a CU");
+    }
+  const struct {
+    int32_t tokens, cols, features;
+    bool x_fp4, large;
+  } cases[] = {{600, 608, 1000, false, false},     {600, 608, 1000, true, false},   {12870, 1536, 4608, false, true},
+               {12870, 1536, 4608, true, true},    {400, 5120, 15360, false, true}, {256, 5120, 15360, true, false},
+               {1200, 5120, 5120, false, true},    {1200, 5120, 5120, true, false}, {2000, 5120, 5120, true, true},
+               {27840, 5120, 15360, true, true},   {70, 1152, 260, true, false},    {4090, 640, 4090, true, true},
+               {4090, 1152, 4090, true, true},     {4096, 1536, 4608, false, true}, {4096, 1536, 4608, true, true},
+               {2050, 1120, 8001, false, true},    {2050, 1120, 8001, true, true}};
+  for (const auto& c : cases) {
+    mssa::ProjectPlan p;
+    const hipError_t e = mssa::plan_mx_project(c.tokens, c.features, static_cast<int32_t>(mssa::mx_blocks(c.cols)), c.x_fp4, &p);
+    check(e == hipSuccess && p.kernel == (c.large ? mssa::ProjectKernel::kLargeTiles : mssa::ProjectKernel::kSmallTiles),
+          "tiles of " + std::to_string(c.tokens) + " x " + std::to_string(c.cols) + " -> " + std::to_string(c.features));
+  }
+}
+
 // Attentions at the limits: made, or refused where they have 2^24 blocks and more (the sizes of single calls).
 void attention_launches() {
   for (int32_t batch : {1, 4096, 1 << 20, (1 << 24) - 8, 1 << 24})
@@ -213,6 +243,7 @@ int main() {
   norm_slices();
   conversion_slices();
   product_launches();
+  tile_choices();
   attention_launches();
   std::printf("%d checks, %d failures\n", g_checks, g_failures);
   return g_failures ? 1 : 0;
