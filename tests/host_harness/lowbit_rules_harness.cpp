@@ -8,6 +8,7 @@
 
 #include <algorithm>
 #include <cstdio>
+#include <cstdlib>
 #include <cstring>
 #include <string>
 #include <vector>
@@ -89,7 +90,7 @@ void norm_slices() {
         d.rows = rows;
         d.cols = cols;
         d.dtype = MSSA_BF16;
-        d.out_dtype = e4m3 ? MSSA_E4M3 : MSSA_BF16;
+        d.out_dtype = e4m3 ? int32_t{MSSA_E4M3} : int32_t{MSSA_BF16};
         d.x_stride = cols + 3;
         g_norms.clear();
         char *x = dev(0), *r = dev(1), *w = dev(2), *s = dev(3), *y = dev(4), *ys = dev(5), *rstd = dev(6);
@@ -237,7 +238,16 @@ void scale_groups() {
 
 }  // namespace
 
-int main() {
+// With arguments "attention" and a size (batch, n_q, q_heads, kv_heads,
+// head_dim, tokens) prints the plan's waves a block, items of a sequence and workers.
+int main(int argc, char** argv) {
+  if (argc == 8 && std::strcmp(argv[1], "attention") == 0) {
+    const auto n = [&](int i) { return static_cast<int32_t>(std::atoi(argv[i])); };
+    mssa::MxAttnPlan p;
+    if (mssa::plan_mx_attention(n(2), n(3), n(4), n(5), n(6), n(7), &p) != hipSuccess) return 1;
+    std::printf("%d %d %d\n", p.waves, p.items, p.workers);
+    return 0;
+  }
   scale_groups<8, 2>();  // MXFP4 tokens
   scale_groups<4, 1>();  // 8-bit tokens
   norm_slices();

@@ -37,3 +37,23 @@ def test_rules_hold_under_sanitizers(harness):
     assert r.returncode == 0, r.stdout[-3000:] + r.stderr[-3000:]
     assert " 0 failures" in r.stdout
     assert "runtime error" not in r.stderr and "AddressSanitizer" not in r.stderr
+
+
+def test_wide_attention_cases_reach_the_kernel_of_eight_waves(harness):
+    """Every GPU case that is to check that kernel gets it, some with a block an item, some with workers that share
+    items and take more than one."""
+    from test_gpu_mx_attention_wide import CASES
+
+    whole = crossing = 0
+    for case in CASES:
+        r = _run(harness, "attention", *case)
+        assert r.returncode == 0
+        waves, items, workers = map(int, r.stdout.split())
+        assert waves == 8, case
+        whole += workers == 0
+        # shares of the tiles, the first ones a tile larger: does a worker take tiles of two items?
+        of_item = -(-case[5] // 64)
+        each, more = divmod(items * case[0] * of_item, max(1, workers))
+        first = [w * each + min(w, more) for w in range(workers + 1)]
+        crossing += any(a // of_item != (b - 1) // of_item for a, b in zip(first, first[1:]))
+    assert whole >= 10 and crossing >= 10
