@@ -24,15 +24,14 @@
 
 #include "lds_stage.hpp"
 #include "lowbit_args.hpp"
+#include "lowbit_values.hpp"
 #include "wave_ops.hpp"
 #include "xcd.hpp"
 
 namespace mssa {
 namespace {
 
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
@@ -41,19 +40,6 @@ constexpr int kMaxWorkers = kMxAttnMaxWorkers;
 constexpr float kRescaleLog2 = 8.f;
 constexpr float kNoMax = -__FLT_MAX__;       // a finite running maximum before the first score
 constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
-
-// The conversion instructions read a scale's exponent field alone, as the
-// format's scale byte: 255 makes NaNs.
-__device__ inline float mx_scale(uint32_t e) { return __builtin_bit_cast(float, e << 23); }
-
-// Eight codes to bf16, in order.
-__device__ inline bf16x8 expand8(uint32_t codes, float scale) {
-  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0);
-  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1);
-  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2);
-  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3);
-  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-}
 
 // A value that all lanes share, in a scalar register.
 __device__ inline uint32_t uniform(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
@@ -318,7 +304,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
         const float f = mx_scale(se[i]);
         __bf16* P = lds[buf][NW == 8 ? second : i];
 #pragma unroll
-        for (int k = 0; k < NS; ++k) *reinterpret_cast<bf16x8*>(P + (dst ^ (k * 8))) = expand8(codes[i][k], f);
+        for (int k = 0; k < NS; ++k) *reinterpret_cast<bf16x8*>(P + (dst ^ (k * 8))) = expand_e2m1(codes[i][k], f);
       }
     };
     if (t0 < t1) fetch(t0);
@@ -589,7 +575,7 @@ __global__ __launch_bounds__(kFewWaves * 64) __attribute__((amdgpu_waves_per_eu(
         const float f = scale_of(ke, u);
 #pragma unroll
         for (int i = 0; i < NS; ++i) {
-          const bf16x8 kv = expand8(kc[u][i], f);
+          const bf16x8 kv = expand_e2m1(kc[u][i], f);
 #pragma unroll
           for (int t = 0; t < RT; ++t) s[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kv, qf[t][i], s[t][u], 0, 0, 0);
         }
@@ -638,7 +624,7 @@ __global__ __launch_bounds__(kFewWaves * 64) __attribute__((amdgpu_waves_per_eu(
           const float f = scale_of(ve, w * 2 + u);
 #pragma unroll
           for (int i = 0; i < NS; ++i)
-            *reinterpret_cast<bf16x8*>(V + swz256(u * 16 + n, g * (D / 4) + i * 8)) = expand8(vc[w * 2 + u][i], f);
+            *reinterpret_cast<bf16x8*>(V + swz256(u * 16 + n, g * (D / 4) + i * 8)) = expand_e2m1(vc[w * 2 + u][i], f);
         }
         if (w == NU / 2 - 1) fetch(vc, ve, a.vc, a.vs, t64 + token_waves);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");

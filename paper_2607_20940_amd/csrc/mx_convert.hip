@@ -10,6 +10,7 @@
 #include <hip/hip_runtime.h>
 
 #include "lowbit_args.hpp"
+#include "lowbit_values.hpp"
 #include "wave_ops.hpp"
 
 namespace mssa {
@@ -17,18 +18,7 @@ namespace {
 
 constexpr int kThreads = 256;
 
-typedef __bf16 bf16x8_u __attribute__((ext_vector_type(8), aligned(2)));
-typedef float f32x8_u __attribute__((ext_vector_type(8), aligned(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
-
-template <class T>
-struct Vec8 {
-  typedef bf16x8_u type;
-};
-template <>
-struct Vec8<float> {
-  typedef f32x8_u type;
-};
 
 // Where a thread's eight values lie: row and first column.  A block of
 // threads starts at one row, found once in scalar registers.

@@ -21,6 +21,7 @@
 
 #include "lds_stage.hpp"
 #include "lowbit_args.hpp"
+#include "lowbit_values.hpp"
 #include "xcd.hpp"
 
 namespace mssa {
@@ -43,28 +44,6 @@ constexpr uint32_t kPastEnd = 0xfffffff0u;  // a buffer offset outside every ran
 // half the rate.  (e2m1 by e2m1 steps add exactly enough for both.)
 template <bool XF4, class T>
 constexpr bool kWide = !XF4 && std::is_same_v<T, float>;
-
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-
-// Eight consecutive values of an MXFP4 block, or of e4m3, in bf16.
-__device__ inline bf16x8 expand4(uint32_t codes, float scale) {
-  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0);
-  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1);
-  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2);
-  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3);
-  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-}
-__device__ inline bf16x8 expand8(uint32_t lo, uint32_t hi) {
-  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false);
-  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true);
-  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false);
-  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true);
-  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-}
-__device__ inline float mx_scale(uint32_t e) {
-  return __builtin_bit_cast(float, e == 255 ? 0x7fc00000u : e == 0 ? 0x00400000u : e << 23);
-}
 
 __device__ inline i32x8 widen(i32x4 v) { return i32x8{v[0], v[1], v[2], v[3], 0, 0, 0, 0}; }
 
@@ -325,9 +304,9 @@ void tile_kernel(ProjectArgs a) {
       for (int p = 0; p < 4; ++p) {  // eight values at a time
         bf16x8 xw[TM], ww[TN];
 #pragma unroll
-        for (int i = 0; i < TM; ++i) xw[i] = expand8(xv[J & 1][i][2 * p], xv[J & 1][i][2 * p + 1]);
+        for (int i = 0; i < TM; ++i) xw[i] = expand_e4m3(xv[J & 1][i][2 * p], xv[J & 1][i][2 * p + 1]);
 #pragma unroll
-        for (int j = 0; j < TN; ++j) ww[j] = expand4(wv[J & 1][j][p], mx_scale((static_cast<uint32_t>(sw[j]) >> (8 * J)) & 255u));
+        for (int j = 0; j < TN; ++j) ww[j] = expand_e2m1(wv[J & 1][j][p], mx_scale((static_cast<uint32_t>(sw[j]) >> (8 * J)) & 255u));
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -537,11 +516,11 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(ProjectArgs a) {
         const float f = mx_scale((now.s >> (8 * J)) & 255u);
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
-          const bf16x8 wa = expand4(static_cast<uint32_t>(now.v[J][p]), f);
+          const bf16x8 wa = expand_e2m1(static_cast<uint32_t>(now.v[J][p]), f);
 #pragma unroll
           for (int t = 0; t < TT; ++t) {
             const i32x4 v = xv[t][J][p >> 1];
-            const bf16x8 xw = expand8(static_cast<uint32_t>(v[2 * (p & 1)]), static_cast<uint32_t>(v[2 * (p & 1) + 1]));
+            const bf16x8 xw = expand_e4m3(static_cast<uint32_t>(v[2 * (p & 1)]), static_cast<uint32_t>(v[2 * (p & 1) + 1]));
             acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wa, xw, acc[t], 0, 0, 0);
           }
         }

@@ -13,6 +13,7 @@
 #include <algorithm>
 
 #include "lowbit_args.hpp"
+#include "lowbit_values.hpp"
 #include "wave_ops.hpp"
 
 namespace mssa {
@@ -20,19 +21,6 @@ namespace {
 
 constexpr int kE4M3Max = 448;
 constexpr float kTiny = 0x1p-100f;  // smallest row maximum that a scale is made from
-
-// Eight consecutive values, aligned to the element only (rows cut out of a
-// wider tensor, odd widths): global accesses need no more.
-template <class T>
-struct Vec8;
-template <>
-struct Vec8<__bf16> {
-  typedef __bf16 type __attribute__((ext_vector_type(8), aligned(2)));
-};
-template <>
-struct Vec8<float> {
-  typedef float type __attribute__((ext_vector_type(8), aligned(4)));
-};
 
 template <class T>
 __device__ inline void load8(const T* p, int n, float (&v)[8]) {
