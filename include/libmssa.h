@@ -547,7 +547,9 @@ typedef struct {
 } mssa_mx_project_desc;
 
 /* y[p][row, n] = sum_k x[row, k] w[p * N + n, k] + bias, N = out_features /
- * parts, fp32 accumulation, rounded once.
+ * parts, fp32 sums, rounded once.  (With 8-bit tokens and bf16 outputs up to
+ * 2^-12 of the sum of magnitudes can be lost where 64 or 128 products are added
+ * in one step, 6e-6 of the result on ordinary tokens; with fp32 outputs not.)
  *   x, x_scales  tokens as 8-bit rows with fp32 scales [rows], or as MXFP4
  *                with scale bytes [rows, ceil(in_features / 32)]
  *   w, w_scales  MXFP4 rows, one per output feature

@@ -11,11 +11,15 @@
 // that the lanes already hold.
 //
 // Softmax in base 2 on fp32 scores with a running maximum that only moves
-// when a score passes it by 2^8, sums in fp32, P rounded to bf16 as a matrix
-// operand.
+// when a score passes it by 2^8, sums in fp32.  P is rounded to bf16 as a
+// matrix operand (fp32 products would run at a sixteenth of the rate), the sum
+// that divides it is not: an error of up to 2^-8 of each term, on top of the
+// output's own rounding.  Where a few keys carry the softmax it shows: against
+// 64 bits 0.0023 of the output's norm on single queries and short caches, 0.0017
+// without it; 9360 queries joined with other keys 0.0017 either way.
 //
 // Many rows are bound by the matrix cores and the softmax between them (9360
-// queries, 12 heads, 32760 tokens, d 128: 1.75 ms, 1.08 PFLOP/s), few rows by
+// queries, 12 heads, 32760 tokens, d 128: 1.74 ms, 1.08 PFLOP/s), few rows by
 // the cache's bytes (16 streams of one token, 40 over 8 heads, up to 32760
 // tokens: 73 us, 3.9 TB/s).
 #include <hip/hip_runtime.h>

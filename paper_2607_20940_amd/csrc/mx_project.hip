@@ -8,11 +8,13 @@
 // halves take the first and the second half of a stage's blocks and each
 // lane's scales of a stage are consecutive bytes.
 //
-// Bound by the stages' transfers where there are many tokens (27840 x 5120 ->
-// 15360 in MXFP4: 1.20 ms, 3.6 PFLOP/s, matrix cores busy 42 % of the time;
-// 12870 x 1536 -> 4608 in e4m3: 104 us, 1.7 PFLOP/s, busy 35 %, an eighth of
-// it the 118 MB of outputs), by the weights' bytes where there are few (1 x
-// 5120 -> 15360: 12 us, 3.5 TB/s).  Waves of 128 x 128 outputs read a quarter
+// Bound by waiting for the stages' transfers where there are many tokens
+// (27840 x 5120 -> 15360 in MXFP4: 1.20 ms, 3.6 PFLOP/s, matrix cores busy 42 %
+// of the time; 12870 x 1536 -> 4608 in e4m3: 104 us, 1.7 PFLOP/s, busy 35 %, an
+// eighth of it the 118 MB of outputs), by the weights' bytes where there are
+// few (1 x 5120 -> 15360: 12.1 us with 8-bit tokens, 3.5 TB/s, 11.3 with MXFP4
+// ones), by 36 to 160 blocks for 256 CUs in between (64 x 5120 -> 15360: 22 and
+// 17 us).  Waves of 128 x 128 outputs read a quarter
 // fewer LDS bytes but are alone on their SIMD: 1.34 ms and 141 us.
 #include <hip/hip_runtime.h>
 
@@ -40,8 +42,10 @@ constexpr uint32_t kPastEnd = 0xfffffff0u;  // a buffer offset outside every ran
 // measured on codes of every size, 6e-6 of the result's norm on ordinary
 // tokens, far below the output's own rounding.  fp32 outputs of 8-bit tokens
 // are asked for to be more exact than that: both operands are expanded to
-// bf16, which holds them exactly, and multiplied with fp32 sums, at less than
-// half the rate.  (e2m1 by e2m1 steps add exactly enough for both.)
+// bf16, which holds them exactly, and multiplied with fp32 sums (12870 x 1536 ->
+// 4608: 171-189 us against 104-107 with bf16 outputs, which are half the bytes;
+// each wave expands its own copy of both operands).  (e2m1 by e2m1 steps add
+// exactly enough for both.)
 template <bool XF4, class T>
 constexpr bool kWide = !XF4 && std::is_same_v<T, float>;
 

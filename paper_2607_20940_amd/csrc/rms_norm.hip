@@ -167,7 +167,10 @@ __device__ inline typename Vec8<T>::type raw8(const T* p, int n) {
 // is on its way while this one's sum goes round (not with 1024 threads a row,
 // which have no registers for two).  512 blocks: with 768 or 1024 the last
 // rows leave CUs idle or the shares cost more (27840 x 5120 bf16, forward and
-// backward: 428, 457, 435 us; 560 with a row at a time).
+// backward: 428, 457, 435 us; 560 with a row at a time).  Rows of up to 16384
+// values run at 5.0 to 5.6 TB/s; above, a row's values and its gradients' shares
+// no longer fit a thread's 128 registers and spill (bf16, 24576: 2.0, 32768:
+// 1.4 to 1.6 TB/s).
 template <class T, bool DSUM, int TPR, int NV>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_bwd_kernel(NormBwdArgs a) {
   constexpr int kThreads = TPR > 256 ? TPR : 256, kRows = kThreads / TPR;

@@ -16,7 +16,10 @@ One layer pass (``layer_pass``), all on the caller's stream:
 
 A history frame is quantised once, when it is emitted, at every scale that
 reads it; the rings of a Wan-1.3B layer stack (30 layers, 21 frames of 1560
-tokens and their 2x2 means) are 2.0 GB instead of 7.5.
+tokens and their 2x2 means) are 2.0 GB instead of 7.5.  The gain is memory: one
+of these layers over full rings takes 3.12 ms on an MI355X, 1.91 of it the
+history's attention, where the bf16 layer's pass takes 2.70 and its QKV product
+0.17.
 
 This module only sequences library calls and owns device buffers (torch
 allocations); all arithmetic runs in the library.
