@@ -599,6 +599,142 @@ mssa_status mssa_mx_attention(const mssa_mx_attention_desc* desc, const void* q,
                               const void* prior_out, const float* prior_lse, void* workspace,
                               int64_t workspace_bytes, void* out, float* lse, void* stream);
 
+/* ------------------------------------------------- streams served together
+ * What a layer does for several streams at once: their new tokens lie packed
+ * behind one another, each stream has its own K/V history in pages of one
+ * pool, and its own low-rank adapter beside the shared projection.  No plan is
+ * needed; the conventions above hold (caller-owned device memory, caller's
+ * stream, no synchronisation, fixed reduction orders, tensors 16-byte
+ * aligned, bf16), with these layouts besides:
+ *   - A packed batch: `tokens` rows, sequence b's chunk of new tokens in rows
+ *     chunk_begin[b] .. chunk_begin[b + 1] - 1 (chunk_begin [batch + 1] int32
+ *     on the device, not decreasing; NULL: tokens / batch rows each).  Rows
+ *     before the first chunk and behind the last belong to no sequence and
+ *     are left as they were.  A chunk may be empty.
+ *   - kv_len [batch] int32 on the device: tokens of each sequence's cache, its
+ *     chunk's among them.  Chunk token i of n has cache index
+ *     kv_len[b] - n + i.
+ *   - Pages: k_pages and v_pages [pages, page_tokens, kv_heads, head_dim];
+ *     cache index c of sequence b is token c % page_tokens of page
+ *     page_table[b][c / page_tokens] (page_table [batch, table_pages] int32 on
+ *     the device).  An entry outside [0, pages) names no page: nothing is
+ *     stored there, and attention has no such keys.  A page may stand in
+ *     several tables (a shared beginning), but nothing may be appended to a
+ *     cache index that two sequences share: which one stays is not defined.
+ * Values on the device are not known to the host: they are clamped to what the
+ * tensors hold, so that no value of them leads outside. */
+
+/* Shared projection with low-rank adapters. */
+typedef struct {
+  int64_t rows;           /* tokens, 0..2^30 */
+  int32_t in_features;    /* 1..2^20 */
+  int32_t out_features;   /* 1..2^20, a multiple of parts */
+  int32_t parts;          /* 1..8: the features are split evenly over so many outputs (3: q, k, v) */
+  int32_t segments;       /* runs of rows with one adapter each, 0..2^20 */
+  int32_t adapters;       /* >= 0 */
+  int32_t rank;           /* 1..256, or 0 with no adapters */
+  float part0_scale;      /* finite; multiplies part 0 (bias and adapter included), 1 to leave it */
+  int64_t x_stride;       /* elements between rows of x, 0 = in_features */
+} mssa_adapter_project_desc;
+
+/* Device workspace bytes of mssa_adapter_project. */
+mssa_status mssa_adapter_project_workspace_size(const mssa_adapter_project_desc* desc, int64_t* bytes);
+
+/* y[p][row, n] = sum_k x[row, k] w[p N + n, k] + bias + scale[j] sum_r
+ * (sum_k x[row, k] a[j][p][r, k]) b[j][p N + n, r], N = out_features / parts, j
+ * the adapter of the row's segment; fp32 sums, the low-rank product rounded to
+ * bf16 between its two factors, outputs rounded once.
+ *   x              [rows, in_features] (x_stride)
+ *   w, bias        [out_features, in_features]; [out_features] or NULL
+ *   segment_begin  [segments + 1] int32 on the device, not decreasing: segment
+ *                  s is rows segment_begin[s] .. segment_begin[s + 1] - 1.
+ *                  Rows in no segment have no adapter.
+ *   adapter        [segments] int32 on the device; outside [0, adapters): none
+ *   a, b           [adapters, parts, rank, in_features] and [adapters,
+ *                  out_features, rank]
+ *   scale          [adapters] fp32, NULL: 1
+ *   y              host array of `parts` device pointers, each [rows, N]
+ * An adapter's infinities and NaN reach its own rows only.  Outputs must not
+ * alias the inputs.  Tensors need the alignment of their type only; x, w, a, b
+ * and outputs that are 16-byte aligned, in_features a multiple of 64, rank and
+ * N of 8 take a faster path. */
+mssa_status mssa_adapter_project(const mssa_adapter_project_desc* desc, const void* x, const void* w, const void* bias,
+                                 const int32_t* segment_begin, const int32_t* adapter, const void* a, const void* b,
+                                 const float* scale, void* workspace, int64_t workspace_bytes, void* const* y,
+                                 void* stream);
+
+/* Rotation of queries and keys, and storing of keys and values in pages. */
+typedef struct {
+  int64_t tokens;         /* packed rows, 0..2^30 */
+  int32_t batch;          /* sequences, >= 1 */
+  int32_t q_heads;        /* >= 0; 0: no queries */
+  int32_t kv_heads;       /* >= 1 */
+  int32_t head_dim;       /* a multiple of 16, 16..256 */
+  int32_t page_tokens;    /* tokens of a page, 1..2^20 */
+  int32_t table_pages;    /* entries of a sequence in page_table; x page_tokens < 2^31 */
+  int64_t pages;          /* pages of the pool; x page_tokens < 2^31 */
+  int32_t rotate_dims;    /* dims 0 .. rotate_dims - 1 of a head are turned: even, 0..head_dim */
+  int32_t halves;         /* pairs: 0 (2 i, 2 i + 1); 1 (i, i + rotate_dims / 2), rotate_dims a multiple of 16 */
+  int32_t axes;           /* 1..3 positions a token */
+  int32_t axis_pairs[3];  /* pairs of each axis, in order: rotate_dims / 2 in all */
+  int64_t q_stride, k_stride, v_stride; /* elements between rows, multiples of 8; 0 = heads * head_dim */
+} mssa_paged_append_desc;
+
+/* For every chunk token: pair i of each query and key head turns by the angle
+ * positions[axis of i][token] * freqs[i] (taken in 64 bits, sines and cosines
+ * in 32):  (u, v) -> (u cos - v sin, u sin + v cos), fp32, rounded once.  The
+ * queries go to q_out, keys and values to their cache index's place in the pages; tokens
+ * whose cache index is negative, past the table or in no page are not stored.
+ *   q, k, v      [tokens, q_heads | kv_heads, head_dim] (strides); q NULL iff q_heads == 0
+ *   chunk_begin, kv_len, page_table  as above
+ *   positions    [axes, tokens] int32 on the device, or NULL with one axis: the cache index
+ *   freqs        [rotate_dims / 2] fp32 on the device, radians a position
+ *   q_out        [tokens, q_heads, head_dim]; may be q itself where q is contiguous
+ *   k_pages, v_pages  the pool; must not overlap the inputs */
+mssa_status mssa_paged_append(const mssa_paged_append_desc* desc, const void* q, const void* k, const void* v,
+                              const int32_t* chunk_begin, const int32_t* kv_len, const int32_t* page_table,
+                              const int32_t* positions, const float* freqs, void* q_out, void* k_pages, void* v_pages,
+                              void* stream);
+
+/* Attention of chunks of new tokens over paged caches. */
+typedef struct {
+  int64_t tokens;         /* packed rows, 0..2^30 */
+  int32_t batch;          /* sequences, >= 1 */
+  int32_t max_chunk;      /* the longest chunk, 1..2^30 (of longer ones the first max_chunk tokens are attended) */
+  int32_t q_heads;        /* a multiple of kv_heads: query head h reads key head h / (q_heads / kv_heads) */
+  int32_t kv_heads;       /* >= 1 */
+  int32_t head_dim;       /* 64 or 128 */
+  int32_t page_tokens;    /* as in mssa_paged_append_desc */
+  int32_t table_pages;
+  int64_t pages;
+  int32_t mask_block;     /* 0: a query sees its sequence's whole cache; m > 0: chunk token i sees cache indices below
+                             that of the chunk's token (i / m + 1) m (1: causal; a frame's tokens: frame by frame) */
+  int64_t q_stride;       /* elements between rows of q, a multiple of 8; 0 = q_heads * head_dim */
+  int64_t lse_stride;     /* floats between the heads of lse, 0 = tokens */
+  float softmax_scale;    /* <= 0 selects 1/sqrt(head_dim) */
+} mssa_paged_attention_desc;
+
+/* Device workspace bytes of mssa_paged_attention. */
+mssa_status mssa_paged_attention_workspace_size(const mssa_paged_attention_desc* desc, int64_t* bytes);
+
+/* out = softmax(scale q k^T) v over the keys that the mask leaves of the first
+ * kv_len[b] cache indices, joined with an earlier result over other keys of
+ * the same queries if one is given.
+ *   q            [tokens, q_heads, head_dim] (q_stride)
+ *   k_pages, v_pages, chunk_begin, kv_len, page_table  as above; kv_len is
+ *                clamped to [0, table_pages * page_tokens]
+ *   prior_out, prior_lse  as for mssa_mx_attention, rows and heads as out and
+ *                lse; both or neither; they may be out and lse themselves
+ *   out          [tokens, q_heads, head_dim]
+ *   lse          [q_heads, tokens] (lse_stride) natural log of the sum of
+ *                exp(scale q k) over all keys, or NULL
+ * A query with no keys at all has out = 0 and lse = -inf.  What pages hold at
+ * indices that a query does not see is not used, whatever it is. */
+mssa_status mssa_paged_attention(const mssa_paged_attention_desc* desc, const void* q, const void* k_pages,
+                                 const void* v_pages, const int32_t* chunk_begin, const int32_t* kv_len,
+                                 const int32_t* page_table, const void* prior_out, const float* prior_lse,
+                                 void* workspace, int64_t workspace_bytes, void* out, float* lse, void* stream);
+
 /* Name of a status code (static string). */
 const char* mssa_status_string(mssa_status s);
 

@@ -81,6 +81,17 @@ __device__ inline void dma16_soff(i32x4 rsrc, uint32_t voff, uint32_t soff, uint
 #pragma clang diagnostic pop
 }
 
+// Direct global -> LDS load of 16 bytes from each lane's own address, for rows
+// whose places a buffer's 32-bit offsets do not reach: lane i's bytes land at
+// LDS byte address lds_addr + 16 i.  Nothing is range checked.
+__device__ inline void gdma16(const void* from, uint32_t lds_addr) {
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+               :: "s"(lds_addr), "v"(from) : "memory", "m0");
+#pragma clang diagnostic pop
+}
+
 // Store of lane i's 16 bytes at buffer offset voff + soff + IMM
 // (buffer_store_dwordx4, non-temporal: data that another kernel reads once);
 // lanes whose offset is past the buffer's range store nothing.  The s_nop is

@@ -1,0 +1,193 @@
+// Kernel arguments and launchers of the operators for streams served together
+// (projection with adapters, append to a paged cache, attention over it), and
+// the rules on sizes that need no device.
+#pragma once
+
+#include <hip/hip_runtime_api.h>
+
+#include <cstdint>
+
+#include "lowbit_args.hpp"
+
+namespace mssa {
+
+// n / d for n < 2^31, by a multiplication: with 2^(l-1) < d <= 2^l and
+// m = floor(2^(31+l) / d) + 1, m d exceeds 2^(31+l) by at most 2^l, too little
+// to reach the next quotient.
+struct Divisor {
+  uint32_t d, m;
+  int32_t shift;
+  static Divisor of(uint32_t d) {
+    int l = 0;
+    while ((uint64_t{1} << l) < d) ++l;
+    return {d, static_cast<uint32_t>((uint64_t{1} << (31 + l)) / d + 1), 31 + l};
+  }
+  MSSA_HOST_DEVICE uint32_t quotient(uint32_t n) const { return static_cast<uint32_t>(static_cast<uint64_t>(n) * m >> shift); }
+};
+
+// Row `first` of sequence b's chunk and the row behind its last, whatever
+// chunk_begin holds: inside [0, tokens], none where it decreases.
+struct ChunkRows {
+  int32_t first, end;
+  MSSA_HOST_DEVICE static ChunkRows of(const int32_t* begin, int32_t b, int32_t each, int32_t tokens) {
+    if (!begin) return {b * each, (b + 1) * each};
+    auto in = [&](int32_t r) { return r < 0 ? 0 : r > tokens ? tokens : r; };
+    const int32_t first = in(begin[b]), end = in(begin[b + 1]);
+    return {first, end < first ? first : end};
+  }
+};
+
+// ----------------------------------------------------------------- append
+constexpr int kAppendThreads = 256;
+constexpr int kAppendMaxTokens = 16;  // tokens of a block
+constexpr int kAppendMaxPairs = 128;  // rotated pairs of a head
+
+struct AppendArgs {
+  const void *q, *k, *v;
+  const int32_t *chunk_begin, *kv_len, *page_table, *positions;
+  const float* freqs;
+  void *q_out, *k_pages, *v_pages;
+  int64_t q_stride, k_stride, v_stride, pages;
+  int32_t tokens, token0, token1;  // rows in all; rows of this launch
+  int32_t batch, each;             // each: rows of a sequence without chunk_begin
+  int32_t q_heads, kv_heads, head_dim, table_pages;
+  int32_t pairs, halves, axis_end[2];  // rotated pairs; first pair of the second and third axis
+  int32_t block_tokens;
+  Divisor page, units, head_units;  // units: pieces of 16 values of a token's heads (q, k, v); of a head
+};
+
+// Tokens of a block: a static rule on the sizes.
+int32_t append_block_tokens(int64_t tokens, int32_t units);
+hipError_t launch_paged_append(const AppendArgs& a, hipStream_t stream);
+
+// -------------------------------------------------------------- attention
+constexpr int kPagedTile = 64;  // tokens of a tile
+constexpr int kPagedMaxWorkers = 512;
+constexpr int kPagedFewWaves = 4;  // waves of a block of the kernel for few rows
+constexpr int kPagedJoinThreads = 256;
+
+struct PagedAttnArgs {
+  const void *q, *k_pages, *v_pages, *prior_out;
+  const int32_t *chunk_begin, *kv_len, *page_table;
+  const float* prior_lse;
+  void* out;
+  float *lse, *partial;
+  int64_t q_stride, lse_stride, pages, capacity;  // capacity: tokens that a row of the table can name
+  int32_t tokens, batch, each, max_chunk;
+  int32_t q_heads, kv_heads, group, table_pages;
+  int32_t mask_block;
+  int32_t slot_rows;  // query rows of an item
+  int32_t workers;    // shares of all items' contexts, 0: an item a block and no joining launch
+  int32_t least;      // units of a share at least
+  Divisor page;
+  float scale_log2e;
+};
+
+// One sequence's work.  Its query rows (chunk token, head of the group) that
+// share a key head are cut into items of slot_rows rows; an item reads the
+// tiles up to the last index that its last row sees.  Items are weighed in
+// units, linear in their number so that sums have a closed form: a tile each
+// where there is no mask, and up to the mask's steps where there is one.  Every
+// item has a unit at least, also one without keys, whose rows are written
+// all the same.
+struct PagedSeq {
+  int32_t first, n;  // chunk: first row, tokens (at most max_chunk)
+  int32_t len;       // cache indices in use
+  int64_t start;     // cache index of the chunk's first token (negative where the cache is shorter than the chunk)
+  int32_t rows, items;
+  uint32_t cost0, step;  // item i weighs cost0 + i step
+
+  // Cache indices below this one are seen by chunk token i.
+  MSSA_HOST_DEVICE int32_t seen(int32_t i, int32_t mask_block) const {
+    if (!mask_block) return len;
+    const int64_t end = start + (static_cast<int64_t>(i / mask_block) + 1) * mask_block;
+    return end < 0 ? 0 : end < len ? static_cast<int32_t>(end) : len;
+  }
+  MSSA_HOST_DEVICE int32_t tiles(int32_t item, const PagedAttnArgs& a) const {
+    const int64_t past = (static_cast<int64_t>(item) + 1) * a.slot_rows;
+    const int32_t last = (past < rows ? static_cast<int32_t>(past) : rows) - 1;
+    return static_cast<int32_t>((static_cast<int64_t>(seen(last / a.group, a.mask_block)) + kPagedTile - 1) / kPagedTile);
+  }
+  MSSA_HOST_DEVICE uint32_t cost(int32_t item) const { return cost0 + static_cast<uint32_t>(item) * step; }
+  // Units of a key head's items before this one.
+  MSSA_HOST_DEVICE uint32_t before(int32_t item) const {
+    const uint64_t i = static_cast<uint64_t>(item);
+    return static_cast<uint32_t>(i * cost0 + (item > 0 ? i * (i - 1) / 2 * step : 0));
+  }
+  // The item that unit x of a key head belongs to.
+  MSSA_HOST_DEVICE int32_t item_of(uint32_t x) const {
+    int32_t lo = 0, hi = items - 1;
+    while (lo < hi) {
+      const int32_t mid = lo + (hi - lo + 1) / 2;
+      if (before(mid) <= x)
+        lo = mid;
+      else
+        hi = mid - 1;
+    }
+    return lo;
+  }
+  MSSA_HOST_DEVICE static PagedSeq of(const PagedAttnArgs& a, int32_t b) {
+    PagedSeq s;
+    const ChunkRows c = ChunkRows::of(a.chunk_begin, b, a.each, a.tokens);
+    const int64_t all = a.kv_len[b], n = c.end - c.first;
+    s.first = c.first;
+    s.start = all - n;
+    s.n = n < a.max_chunk ? static_cast<int32_t>(n) : a.max_chunk;
+    s.len = all < 0 ? 0 : static_cast<int32_t>(all < a.capacity ? all : a.capacity);
+    s.rows = s.n * a.group;
+    s.items = (s.rows + a.slot_rows - 1) / a.slot_rows;
+    s.cost0 = 1;
+    s.step = 0;
+    if (a.workers && s.items) {
+      const uint32_t low = s.tiles(0, a), high = s.items > 1 ? s.tiles(s.items - 1, a) : low;
+      s.cost0 = low ? low : 1;
+      if (high > s.cost0) s.step = (high - s.cost0) / static_cast<uint32_t>(s.items - 1);
+    }
+    return s;
+  }
+  MSSA_HOST_DEVICE uint32_t head_units() const { return before(items); }
+  // First tile of unit u (of cost) of an item with `tiles` tiles.
+  MSSA_HOST_DEVICE static int32_t tile_at(uint32_t u, int32_t tiles, uint32_t cost) {
+    return static_cast<uint32_t>(tiles) == cost ? static_cast<int32_t>(u)
+                                                : static_cast<int32_t>(static_cast<uint64_t>(u) * static_cast<uint32_t>(tiles) / cost);
+  }
+};
+
+struct PagedAttnPlan {
+  int32_t waves;      // 32 rows each in a block; 0: the kernel for few rows
+  int32_t slot_rows, workers, least;
+  int64_t blocks, workspace_bytes;
+  int32_t join_rows;  // rows of a block of the joining launch
+  int32_t threads() const { return (waves ? waves : kPagedFewWaves) * 64; }
+};
+// Sizes whose launch would have 2^32 threads, or 2^31 units, are refused.
+hipError_t plan_paged_attention(int64_t tokens, int32_t batch, int32_t max_chunk, int32_t q_heads, int32_t kv_heads,
+                                int32_t head_dim, int64_t capacity, PagedAttnPlan* plan);
+hipError_t launch_paged_attention(const PagedAttnArgs& a, const PagedAttnPlan& plan, int head_dim, hipStream_t stream);
+
+// ---------------------------------------------------------------- project
+struct AdapterArgs {
+  const void *x, *w, *bias, *a, *b;
+  const int32_t *segment_begin, *adapter;
+  const float* scale;
+  void* low;  // [M, parts, low_rank] bf16: the rows' low-rank factors, times scale
+  void* y[kMaxParts];
+  int64_t x_stride;
+  int32_t M, N, K;
+  int32_t parts, split;  // split: features of a part
+  int32_t segments, adapters, rank, low_rank;
+  float part0_scale;
+};
+
+constexpr int kLowRows = 32;  // rows of a tile of the low-rank factor
+struct AdapterPlan {
+  int64_t low_blocks;  // blocks of the low-rank factor's launch, 0: none
+  int64_t blocks;      // of the product
+  int64_t workspace_bytes;
+  int32_t low_rank;    // rank rounded up to whole 16 values
+};
+hipError_t plan_adapter_project(int64_t rows, int32_t in_features, int32_t out_features, int32_t parts, int32_t segments,
+                                int32_t adapters, int32_t rank, AdapterPlan* plan);
+hipError_t launch_adapter_project(const AdapterArgs& a, const AdapterPlan& plan, hipStream_t stream);
+
+}  // namespace mssa

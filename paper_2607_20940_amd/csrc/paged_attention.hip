@@ -1,0 +1,850 @@
+// Attention of chunks of new tokens over paged K/V caches
+// (mssa_paged_attention).
+//
+// The query rows of a sequence that share a key head (chunk tokens x heads of
+// the group) are cut into items; the cache is read in tiles of 64 tokens,
+// whose rows are found one by one in the page table (a page may end anywhere
+// inside a tile).  The products are S^T = K Q^T (a lane holds one query row)
+// and O^T += V^T P^T, where P leaves S's registers without an exchange: the
+// contraction's token order is the one that the lanes already hold.  Softmax in
+// base 2 on fp32 scores with a running maximum that only moves when a score
+// passes it by 2^8, sums in fp32.  P is rounded to bf16 as a matrix operand (up
+// to 2^-8 of each term; fp32 products would run at a sixteenth of the rate),
+// the sum that divides it is not.
+//
+// Tokens past the sequence's last, and those whose page is none, are read from
+// a row of zeros and masked.  A token that some rows see and others do not (the
+// mask's steps) has P = 0 for the latter, which an infinity or a NaN among its
+// values would turn into a NaN: tiles with such a step look for them, and add
+// such a tile's tokens one by one.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "attend_parts.hpp"
+#include "lds_stage.hpp"
+#include "paged_args.hpp"
+#include "wave_ops.hpp"
+#include "xcd.hpp"
+
+namespace mssa {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kTile = kPagedTile;
+constexpr uint64_t kAll = ~uint64_t{0};
+
+// What stands for a token that is not there.
+__device__ __attribute__((aligned(256))) const uint32_t zero_row[64] = {};
+
+// -------------------------------------------------------------- sharing out
+// All items stand in a row, sequence by sequence, key head by key head, item by
+// item, each as long as it weighs (PagedSeq), and each worker takes as many
+// units as every other (or one more).  An item that one worker holds whole is
+// written by it; the sums of one that several share go to slots, 2 i for the
+// first item of worker i and 2 i + 1 for a later one (which then is its last),
+// and a second launch joins them.
+
+__device__ inline uint32_t units_of(const PagedAttnArgs& a, int b) {
+  return b < a.batch ? PagedSeq::of(a, b).head_units() * static_cast<uint32_t>(a.kv_heads) : 0u;
+}
+
+// A sequence that the whole wave shares, in scalar registers.
+__device__ inline PagedSeq sequence(const PagedAttnArgs& a, int b) {
+  PagedSeq s = PagedSeq::of(a, b);
+  auto one = [](auto v) { return static_cast<decltype(v)>(__builtin_amdgcn_readfirstlane(static_cast<int>(v))); };
+  s.first = one(s.first);
+  s.n = one(s.n);
+  s.len = one(s.len);
+  s.start = static_cast<int64_t>(one(static_cast<uint32_t>(s.start >> 32))) << 32 | one(static_cast<uint32_t>(s.start));
+  s.rows = one(s.rows);
+  s.items = one(s.items);
+  s.cost0 = one(s.cost0);
+  s.step = one(s.step);
+  return s;
+}
+
+__device__ inline Shares shares_of(const PagedAttnArgs& a) {
+  const int lane = threadIdx.x & 63;
+  uint32_t all = 0;
+  for (int c = 0; c < a.batch; c += 64) all += __shfl(wave_prefix(units_of(a, c + lane)), 63);
+  all = uniform(all);
+  if (!a.workers) return Shares::of(all, all);  // a unit an item, an item a block
+  const uint32_t most = all / static_cast<uint32_t>(a.least), workers = static_cast<uint32_t>(a.workers);
+  return Shares::of(all, most < 1 ? 1 : most < workers ? most : workers);
+}
+
+// Unit x of all: its sequence, key head and item, and its place in the item.
+// Where chunk_begin decreases somewhere, chunks overlap and sums can pass 32
+// bits: what is not found then, or lies past its sequence, is no work (b < 0).
+struct Spot {
+  int b, kvh, item;
+  uint32_t unit;
+  PagedSeq seq;
+};
+__device__ inline Spot locate(const PagedAttnArgs& a, uint32_t x) {
+  const int lane = threadIdx.x & 63;
+  Spot at{};
+  at.b = -1;
+  uint32_t base = 0, units = 0;
+  for (int c = 0; c < a.batch; c += 64) {
+    const uint32_t mine = units_of(a, c + lane), pre = wave_prefix(mine);
+    const uint64_t past = __ballot(base + pre > x);
+    if (past) {
+      const int i = __builtin_ctzll(past);
+      at.b = c + i;
+      units = uniform(__shfl(mine, i));
+      base = uniform(base + __shfl(pre, i) - units);
+      break;
+    }
+    base += __shfl(pre, 63);
+  }
+  const uint32_t y = x - base;
+  if (at.b < 0 || y >= units) {
+    at.b = -1;
+    return at;
+  }
+  at.seq = sequence(a, at.b);
+  const uint32_t of_head = at.seq.head_units();
+  at.kvh = static_cast<int>(y / of_head);
+  const uint32_t z = y - static_cast<uint32_t>(at.kvh) * of_head;
+  at.item = at.seq.item_of(z);
+  at.unit = z - at.seq.before(at.item);
+  return at;
+}
+// The item after this one; whether there is one.
+__device__ inline bool next_item(const PagedAttnArgs& a, Spot* at) {
+  at->unit = 0;
+  if (++at->item < at->seq.items) return true;
+  at->item = 0;
+  if (++at->kvh < a.kv_heads) return true;
+  at->kvh = 0;
+  do {
+    if (++at->b >= a.batch) return false;
+    at->seq = sequence(a, at->b);
+  } while (at->seq.items == 0);
+  return true;
+}
+
+// Row `row` of slot `slot`: its sums, and its maximum and sum of exponentials
+// (behind all slots' sums).
+__device__ inline float* slot_sums(const PagedAttnArgs& a, int D, int64_t slot, int row) {
+  return a.partial + (slot * a.slot_rows + row) * D;
+}
+__device__ inline float2* slot_stats(const PagedAttnArgs& a, int D, int64_t slot, int row) {
+  return reinterpret_cast<float2*>(a.partial + 2 * static_cast<int64_t>(a.workers) * a.slot_rows * D) + slot * a.slot_rows + row;
+}
+
+// Where query row r of a key head lies, and which cache indices it sees.
+struct RowPlace {
+  int64_t q, out, lse;
+  int32_t seen;
+};
+__device__ inline RowPlace row_place(const PagedAttnArgs& a, const PagedSeq& s, int kvh, int r, int D) {
+  const int i = r / a.group, h = kvh * a.group + (r - i * a.group);
+  const int64_t row = static_cast<int64_t>(s.first) + i;
+  return {row * a.q_stride + static_cast<int64_t>(h) * D, (row * a.q_heads + h) * D, h * a.lse_stride + row,
+          s.seen(i, a.mask_block)};
+}
+
+// Four dims d .. d + 3 of a row's result from its sums v, maximum m and sum l.
+// The row's lse is written by the thread of d = 0: callers read prior_lse,
+// which may be the same memory, before any thread of the row gets here (the
+// threads of a row belong to one wave).
+__device__ inline void write_joined(const PagedAttnArgs& a, const RowPlace& at, float m, float l, float prior_lse, f32x4 v,
+                                    int d) {
+  const Joined w = join(a.prior_lse != nullptr, m, l, prior_lse);
+  bf16x4 p = {}, u;
+  if (a.prior_out) p = *reinterpret_cast<const bf16x4*>(static_cast<const __bf16*>(a.prior_out) + at.out + d);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float f = v[i] * w.own;
+    // a prior without keys adds nothing, whatever it holds; one whose share is too small for fp32 still adds its NaNs
+    if (a.prior_out && prior_lse != -INFINITY) f += w.prior * static_cast<float>(p[i]);
+    u[i] = static_cast<__bf16>(f);
+  }
+  *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(a.out) + at.out + d) = u;
+  if (a.lse && d == 0) a.lse[at.lse] = w.lse;
+}
+
+// The pages of one sequence: lane i of a wave looks token i of a tile up.
+struct PageWalk {
+  const int32_t* table;
+  uint32_t len;  // at least 1 where a tile is looked up
+  int64_t pages;
+  Divisor page;
+  __device__ uint32_t token(int tile) const {
+    const uint32_t at = static_cast<uint32_t>(tile) * kTile + (threadIdx.x & 63);
+    return at < len ? at : len - 1;
+  }
+  __device__ int32_t entry(int tile) const { return table[page.quotient(token(tile))]; }
+  // The token's row in the pool, -1 where it has none; `there` is a bit per token.
+  __device__ int32_t row(int tile, int32_t found, uint64_t* there) const {
+    const uint32_t tok = token(tile);
+    const bool ok = static_cast<uint32_t>(tile) * kTile + (threadIdx.x & 63) < len && found >= 0 && found < pages;
+    *there = __ballot(ok);
+    return ok ? found * static_cast<int32_t>(page.d) + static_cast<int32_t>(tok - page.quotient(tok) * page.d) : -1;
+  }
+};
+__device__ inline PageWalk walk_of(const PagedAttnArgs& a, int b, int len) {
+  return {a.page_table + static_cast<int64_t>(b) * a.table_pages, static_cast<uint32_t>(len), a.pages, a.page};
+}
+
+// Lane `from`'s value.
+__device__ inline int32_t of_lane(int32_t v, int from) { return __builtin_amdgcn_ds_bpermute(from * 4, v); }
+
+__device__ inline bool not_finite(bf16x8 v) {
+  const u32x4 w = __builtin_bit_cast(u32x4, v);
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) bad = bad || (w[i] & 0x7f80u) == 0x7f80u || (w[i] & 0x7f800000u) == 0x7f800000u;
+  return bad;
+}
+
+// v's element j, zeros elsewhere; all zeros unless `mine`.
+__device__ inline bf16x8 only(bf16x8 v, int j, bool mine) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = mine && e == j ? v[e] : static_cast<__bf16>(0.f);
+  return v;
+}
+
+// ------------------------------------------------------------------ many rows
+// A wave's tile is two phases: matrix instructions (O += V^T P of the tile
+// before, then S = K Q^T), and the softmax.  Eight waves are two groups, one
+// wave of each per SIMD, and the second group runs one phase behind the first,
+// so that a SIMD's matrix core and vector unit both have a wave at work; a
+// barrier ends each phase.  Tiles come by direct transfers, issued in the
+// softmax phase and waited for at its end: the first group brings K, the second
+// V.  Four waves (fewer rows) are one group that brings both; two such blocks
+// share a CU.
+//
+// With phases counted from the first group's S of tile t in 2 t: K of tile t + 1
+// is brought in 2 t + 1 and read in 2 t + 2 and 2 t + 3, V of tile t + 1 brought
+// in 2 t + 2 (four waves: 2 t + 1) and read in 2 t + 4 and 2 t + 5, each into the
+// buffer whose tile (two before) was last read in 2 t - 1 and 2 t + 1 (2 t).
+template <int D, int NW, bool MASK>
+__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) void attn_kernel(PagedAttnArgs a) {
+  constexpr int KS = D / 16, DB = D / 32, kTileElems = kTile * 128;  // 256-byte rows for both D
+  __shared__ __attribute__((aligned(16))) __bf16 lds[2][2][kTileElems];  // [buffer][K | V]
+
+  const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, hh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), second = NW == 8 ? wave >> 2 : 0;
+  // Workers next to one another share key heads: each XCD takes a run of them.
+  const int worker = xcd_remap(blockIdx.x, gridDim.x);
+  const Shares sh = shares_of(a);
+  if (static_cast<uint32_t>(worker) >= sh.workers) return;
+  const uint32_t x0 = sh.first(worker);
+  uint32_t todo = uniform(sh.first(worker + 1) - x0);
+  Spot at = locate(a, x0);
+  if (at.b < 0) return;
+
+  // Transfers: a wave instruction fills four rows of 256 bytes, lane l bytes
+  // 16 l, i.e. row l / 16, whose chunk l % 16 holds chunk t_lc ^ i of the token.
+  const int t_lc = (lane & 15) ^ ((lane >> 4) << 2);
+  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(&lds[0][0][0]));
+  const int64_t row_bytes = static_cast<int64_t>(a.kv_heads) * D * 2;
+  const float c = a.scale_log2e;
+  const int k_rd = swz256(n, hh * 8);
+  const int t_row = 4 * (lane >> 5) + ((lane & 15) >> 2);
+  const int t_col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+  auto phase_end = [&]() {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+
+  for (int seg = 0;; ++seg) {
+    const int tiles = at.seq.tiles(at.item, a);
+    const uint32_t cost = at.seq.cost(at.item), take = todo < cost - at.unit ? todo : cost - at.unit;
+    const int t0 = __builtin_amdgcn_readfirstlane(PagedSeq::tile_at(at.unit, tiles, cost));
+    const int t1 = __builtin_amdgcn_readfirstlane(PagedSeq::tile_at(at.unit + take, tiles, cost));
+    const bool whole = take == cost;
+    todo -= take;
+
+    const int len = at.seq.len;
+    const PageWalk walk = walk_of(a, at.b, len);
+    const char* const k_base = static_cast<const char*>(a.k_pages) + static_cast<int64_t>(at.kvh) * D * 2;
+    const char* const v_base = static_cast<const char*>(a.v_pages) + static_cast<int64_t>(at.kvh) * D * 2;
+    // A wave brings rows 16 (wave & 3) .. + 15 of its group's tiles.
+    auto bring = [&](int32_t row, int buf) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int chunk = t_lc ^ i;
+        const int32_t r = of_lane(row, (wave & 3) * 16 + i * 4 + (lane >> 4));
+        const bool there = r >= 0 && (D == 128 || chunk < D / 8);
+        const int64_t off = static_cast<int64_t>(r) * row_bytes + chunk * 16;
+        const char* const zero = reinterpret_cast<const char*>(zero_row) + chunk * 16;
+#pragma unroll
+        for (int is_v = 0; is_v < 2; ++is_v) {
+          if (NW == 8 && is_v != second) continue;
+          gdma16(there ? (is_v ? v_base : k_base) + off : zero,
+                 __builtin_amdgcn_readfirstlane(lds0 + ((buf * 2 + is_v) * kTile + (wave & 3) * 16 + i * 4) * 256));
+        }
+      }
+    };
+
+    const int r_in = wave * 32 + n, r = at.item * (NW * 32) + r_in;
+    const bool ok = r < at.seq.rows;
+    const RowPlace row = row_place(a, at.seq, at.kvh, ok ? r : 0, D);
+    const int seen = ok ? row.seen : len;
+    bf16x8 qf[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const bf16x8 v = *reinterpret_cast<const bf16x8*>(static_cast<const __bf16*>(a.q) + row.q + ks * 16 + hh * 8);
+      qf[ks] = ok ? v : bf16x8{};
+    }
+
+    f32x16 o[DB], s[2];
+#pragma unroll
+    for (int db = 0; db < DB; ++db) o[db] = f32x16{};
+    float m = kNoMax, l = 0.f;  // running maximum (base 2), this lane's share of the sum
+    bf16x8 pb[2][2];
+    bool step = false;  // the tile of pb has a step of the mask
+    auto v_operand = [&](int buf, int kb, int cc, int db) {
+      const __bf16* r0 = lds[buf][1] + (kb * 32 + cc * 16) * 128;
+      const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(r0 + swz256(t_row, db * 32 + t_col)));
+      const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(r0 + swz256(t_row + 8, db * 32 + t_col)));
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    // Tile t whose values are not all finite: its tokens one by one, each added
+    // to the rows that see it.
+    auto add_pv_one_by_one = [&](int buf, int t) {
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int cc = 0; cc < 2; ++cc)
+#pragma unroll
+          for (int db = 0; db < DB; ++db) {
+            const bf16x8 v = v_operand(buf, kb, cc, db);
+#pragma unroll 1
+            for (int i = 0; i < 16; ++i) {
+              const int j = i & 7, half = i >> 3, tok = kb * 32 + cc * 16 + 8 * (j >> 2) + 4 * half + (j & 3);
+              const f32x16 one = __builtin_amdgcn_mfma_f32_32x32x16_bf16(only(v, j, hh == half), only(pb[kb][cc], j, hh == half),
+                                                                         f32x16{}, 0, 0, 0);
+              const bool sees = static_cast<int64_t>(t) * kTile + tok < seen;
+#pragma unroll
+              for (int e = 0; e < 16; ++e) o[db][e] += sees ? one[e] : 0.f;
+            }
+          }
+    };
+    auto add_pv = [&](int buf, int t) {
+      if (MASK && step) {
+        bool bad = false;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int cc = 0; cc < 2; ++cc)
+#pragma unroll
+            for (int db = 0; db < DB; ++db) bad = bad || not_finite(v_operand(buf, kb, cc, db));
+        if (__any(bad)) {
+          add_pv_one_by_one(buf, t);
+          return;
+        }
+      }
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int cc = 0; cc < 2; ++cc)
+#pragma unroll
+          for (int db = 0; db < DB; ++db)
+            o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand(buf, kb, cc, db), pb[kb][cc], o[db], 0, 0, 0);
+      // operand reads a few products ahead, not all of them at once (registers)
+      interleave<DB * 4, DB * 8, DB * 3>();
+    };
+    auto scores = [&](int buf) {
+      const __bf16* Ks = lds[buf][0];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+        s[kb] = f32x16{};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+          s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(Ks + kb * 32 * 128 + (k_rd ^ (ks * 16))),
+                                                          qf[ks], s[kb], 0, 0, 0);
+      }
+      interleave<KS * 2, KS * 2, 6>();
+    };
+    auto softmax = [&](int t, uint64_t there) {
+      // token kb * 32 + 8 (e / 4) + 4 hh + e % 4 of the tile in s[kb][e]
+      if (there != kAll) {
+        const uint64_t mine = there >> (4 * hh);
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (!(mine >> (kb * 32 + 8 * (e >> 2) + (e & 3)) & 1)) s[kb][e] = -INFINITY;
+      }
+      if constexpr (MASK) {
+        const int64_t left = static_cast<int64_t>(seen) - static_cast<int64_t>(t) * kTile;
+        step = __any(seen < len && left < kTile);
+        if (step) {
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              if (kb * 32 + 8 * (e >> 2) + 4 * hh + (e & 3) >= left) s[kb][e] = -INFINITY;
+        }
+      }
+      float mx = s[0][0];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[kb][e]);
+      mx = fmaxf(mx, other_half(mx)) * c;  // the scale is positive
+      if (__any(mx > m + kRescaleLog2)) {
+        const float mn = fmaxf(m, mx);
+        const float alpha = __builtin_amdgcn_exp2f(m - mn);
+        m = mn;
+        l *= alpha;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) o[db] *= alpha;
+      }
+      float ls[2] = {0.f, 0.f};
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][e], c, -m));
+          ls[e & 1] += p;
+          pb[kb][e >> 3][e & 7] = static_cast<__bf16>(p);
+        }
+      l += ls[0] + ls[1];
+    };
+
+    if (t0 < t1) {
+      uint64_t there, there_next = 0;
+      int32_t found = walk.entry(t0);
+      if (seg > 0) phase_end();  // the last item's V has been read by all
+      bring(walk.row(t0, found, &there), 0);
+      if (t0 + 1 < t1) found = walk.entry(t0 + 1);
+      wait_vmcnt<0>();
+      phase_end();
+      if (second) phase_end();
+      for (int t = t0; t < t1; ++t) {
+        const int buf = (t - t0) & 1;
+        // the wave whose turn at the matrix core it is goes first elsewhere too
+        __builtin_amdgcn_s_setprio(1);
+        if (t > t0) add_pv(buf ^ 1, t - 1);
+        scores(buf);
+        __builtin_amdgcn_s_setprio(0);
+        phase_end();
+        if (t + 1 < t1) {
+          bring(walk.row(t + 1, found, &there_next), buf ^ 1);
+          if (t + 2 < t1) found = walk.entry(t + 2);
+        }
+        softmax(t, there);
+        there = there_next;
+        wait_vmcnt<0>();
+        phase_end();
+      }
+      add_pv((t1 - 1 - t0) & 1, t1 - 1);
+      if (NW == 8 && !second) phase_end();
+    }
+    l += other_half(l);
+    // dims 32 db + 8 j + 4 hh .. + 3 of the row
+    if (ok) {
+      const int64_t slot = 2 * static_cast<int64_t>(worker) + (seg > 0);
+      float* P = whole ? nullptr : slot_sums(a, D, slot, r_in);
+      const float prior = whole && a.prior_lse ? a.prior_lse[row.lse] : 0.f;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          f32x4 v;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[i] = o[db][4 * j + i];
+          const int d = db * 32 + 8 * j + 4 * hh;
+          if (whole)
+            write_joined(a, row, m, l, prior, v, d);
+          else
+            *reinterpret_cast<f32x4*>(P + d) = v;
+        }
+      if (!whole && hh == 0) *slot_stats(a, D, slot, r_in) = make_float2(m, l);
+    }
+    if (todo == 0 || !next_item(a, &at)) return;
+  }
+}
+
+// ------------------------------------------------------------------- few rows
+// Single tokens of a stream, or a few: at most RT x 16 rows share a key head.
+// Memory bound (the cache is read once), so a wave works alone on every fourth
+// tile of the block's, the next one's rows on their way to registers.  K is used
+// where it arrives: lane (n, g) of a 16x16x32 product holds 8 dims of token n.
+// V goes through a tile of the wave's own in LDS and is read transposed.
+constexpr int kFewWaves = kPagedFewWaves;
+
+template <int D, int RT, bool MASK>
+__global__ __launch_bounds__(kFewWaves * 64) __attribute__((amdgpu_waves_per_eu(2))) void few_rows_kernel(PagedAttnArgs a) {
+  constexpr int NS = D / 32, DT = D / 16, NU = kTile / 16, kRows = 16 * RT;
+  __shared__ __attribute__((aligned(16))) __bf16 lds[kFewWaves][32 * 128];
+  __shared__ float stat[2][kFewWaves][kRows];
+
+  const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int worker = xcd_remap(blockIdx.x, gridDim.x);
+  const Shares sh = shares_of(a);
+  if (static_cast<uint32_t>(worker) >= sh.workers) return;
+  const uint32_t x0 = sh.first(worker);
+  uint32_t todo = uniform(sh.first(worker + 1) - x0);
+  Spot at = locate(a, x0);
+  if (at.b < 0) return;
+
+  const int64_t row_bytes = static_cast<int64_t>(a.kv_heads) * D * 2;
+  const float c = a.scale_log2e;
+  __bf16* V = lds[wave];
+  const int t_row = 4 * g + (n >> 2), t_col = 4 * (n & 3);
+
+  for (int seg = 0;; ++seg) {
+    const int tiles = at.seq.tiles(at.item, a);
+    const uint32_t cost = at.seq.cost(at.item), take = todo < cost - at.unit ? todo : cost - at.unit;
+    const int t0 = __builtin_amdgcn_readfirstlane(PagedSeq::tile_at(at.unit, tiles, cost));
+    const int t1 = __builtin_amdgcn_readfirstlane(PagedSeq::tile_at(at.unit + take, tiles, cost));
+    const bool whole = take == cost;
+    todo -= take;
+    const int len = at.seq.len;
+    const PageWalk walk = walk_of(a, at.b, len);
+    const char* const k_base = static_cast<const char*>(a.k_pages) + static_cast<int64_t>(at.kvh) * D * 2;
+    const char* const v_base = static_cast<const char*>(a.v_pages) + static_cast<int64_t>(at.kvh) * D * 2;
+
+    RowPlace place[RT];
+    bool ok[RT];
+    int seen[RT];
+    bf16x8 qf[RT][NS];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      const int r = at.item * kRows + t * 16 + n;
+      ok[t] = r < at.seq.rows;
+      place[t] = row_place(a, at.seq, at.kvh, ok[t] ? r : 0, D);
+      seen[t] = ok[t] ? place[t].seen : len;
+#pragma unroll
+      for (int i = 0; i < NS; ++i) {
+        const bf16x8 v = *reinterpret_cast<const bf16x8*>(static_cast<const __bf16*>(a.q) + place[t].q + i * 32 + g * 8);
+        qf[t][i] = ok[t] ? v : bf16x8{};
+      }
+    }
+
+    // Lane (n, g) holds dims 32 i + 8 g .. + 7 of tokens 16 u + n.
+    bf16x8 kc[NU][NS], vc[NU][NS];
+    auto fetch = [&](bf16x8 (&to)[NU][NS], const char* base, int32_t row) {
+#pragma unroll
+      for (int u = 0; u < NU; ++u) {
+        const int32_t r = of_lane(row, u * 16 + n);
+        const char* p = r >= 0 ? base + static_cast<int64_t>(r) * row_bytes : reinterpret_cast<const char*>(zero_row);
+#pragma unroll
+        for (int i = 0; i < NS; ++i) to[u][i] = *reinterpret_cast<const bf16x8*>(p + i * 64 + g * 16);
+      }
+    };
+    f32x4 o[RT][DT];
+    float m[RT], l[RT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      m[t] = kNoMax;
+      l[t] = 0.f;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) o[t][d] = f32x4{};
+    }
+    uint64_t there = 0, there_next = 0;
+    int32_t row = -1, found = 0;
+    if (t0 + wave < t1) {
+      row = walk.row(t0 + wave, walk.entry(t0 + wave), &there);
+      if (t0 + wave + kFewWaves < t1) found = walk.entry(t0 + wave + kFewWaves);
+      fetch(kc, k_base, row);
+      fetch(vc, v_base, row);
+    }
+    for (int t64 = t0 + wave; t64 < t1; t64 += kFewWaves) {
+      const bool more = t64 + kFewWaves < t1;
+      f32x4 s[RT][NU];
+#pragma unroll
+      for (int u = 0; u < NU; ++u) {
+#pragma unroll
+        for (int t = 0; t < RT; ++t) s[t][u] = f32x4{};
+#pragma unroll
+        for (int i = 0; i < NS; ++i)
+#pragma unroll
+          for (int t = 0; t < RT; ++t) s[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kc[u][i], qf[t][i], s[t][u], 0, 0, 0);
+      }
+      if (more) {
+        row = walk.row(t64 + kFewWaves, found, &there_next);
+        if (t64 + 2 * kFewWaves < t1) found = walk.entry(t64 + 2 * kFewWaves);
+        fetch(kc, k_base, row);
+      }
+      bool step = false;
+      bf16x8 pb[RT][NU / 2];
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+        // token 16 u + 4 g + i of the tile in s[t][u][i]
+        if (there != kAll) {
+          const uint64_t mine = there >> (4 * g);
+#pragma unroll
+          for (int u = 0; u < NU; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (!(mine >> (u * 16 + i) & 1)) s[t][u][i] = -INFINITY;
+        }
+        if constexpr (MASK) {
+          const int64_t left = static_cast<int64_t>(seen[t]) - static_cast<int64_t>(t64) * kTile;
+          if (__any(seen[t] < len && left < kTile)) {
+            step = true;
+#pragma unroll
+            for (int u = 0; u < NU; ++u)
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (u * 16 + 4 * g + i >= left) s[t][u][i] = -INFINITY;
+          }
+        }
+        float mx = s[t][0][0];
+#pragma unroll
+        for (int u = 0; u < NU; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[t][u][i]);
+        mx = over_row(mx, [](float x, float y) { return fmaxf(x, y); }) * c;
+        if (__any(mx > m[t] + kRescaleLog2)) {
+          const float mn = fmaxf(m[t], mx);
+          const float alpha = __builtin_amdgcn_exp2f(m[t] - mn);
+          m[t] = mn;
+          l[t] *= alpha;
+#pragma unroll
+          for (int d = 0; d < DT; ++d) o[t][d] *= alpha;
+        }
+#pragma unroll
+        for (int u = 0; u < NU; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][u][i], c, -m[t]));
+            l[t] += p;
+            pb[t][u / 2][u % 2 * 4 + i] = static_cast<__bf16>(p);
+          }
+      }
+      bool bad = false;
+      if (MASK && step) {
+#pragma unroll
+        for (int u = 0; u < NU; ++u)
+#pragma unroll
+          for (int i = 0; i < NS; ++i) bad = bad || not_finite(vc[u][i]);
+      }
+      const bool one_by_one = MASK && __any(bad);
+      // V in halves of 32 tokens through the wave's tile.  A wave's LDS accesses
+      // happen in their order; the fences keep the compiler to it.
+#pragma unroll
+      for (int w = 0; w < NU / 2; ++w) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int i = 0; i < NS; ++i)
+            *reinterpret_cast<bf16x8*>(V + swz256(u * 16 + n, i * 32 + g * 8)) = vc[w * 2 + u][i];
+        if (w == NU / 2 - 1 && more) fetch(vc, v_base, row);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(V + swz256(t_row, d * 16 + t_col)));
+          const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(V + swz256(t_row + 16, d * 16 + t_col)));
+          const bf16x8 vt = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+          if (one_by_one) {
+            // the tokens one by one, each added to the rows that see it
+#pragma unroll 1
+            for (int i = 0; i < 32; ++i) {
+              const int j = i & 7, q = i >> 3, tok = w * 32 + (j >> 2) * 16 + 4 * q + (j & 3);
+#pragma unroll
+              for (int t = 0; t < RT; ++t) {
+                const f32x4 one =
+                    __builtin_amdgcn_mfma_f32_16x16x32_bf16(only(vt, j, g == q), only(pb[t][w], j, g == q), f32x4{}, 0, 0, 0);
+                const bool sees = static_cast<int64_t>(t64) * kTile + tok < seen[t];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[t][d][e] += sees ? one[e] : 0.f;
+              }
+            }
+          } else {
+#pragma unroll
+            for (int t = 0; t < RT; ++t) o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, pb[t][w], o[t][d], 0, 0, 0);
+          }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      }
+      there = there_next;
+    }
+
+    // Join the waves: their maximum, then the scaled sums one by one.
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      l[t] = over_row(l[t], [](float x, float y) { return x + y; });
+      if (g == 0) {
+        stat[0][wave][t * 16 + n] = m[t];
+        stat[1][wave][t * 16 + n] = l[t];
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      float top = m[t];
+      for (int w = 0; w < kFewWaves; ++w) top = fmaxf(top, stat[0][w][t * 16 + n]);
+      const float alpha = __builtin_amdgcn_exp2f(m[t] - top);
+      m[t] = top;
+      l[t] = 0.f;
+      for (int w = 0; w < kFewWaves; ++w)
+        l[t] = __builtin_fmaf(__builtin_amdgcn_exp2f(stat[0][w][t * 16 + n] - top), stat[1][w][t * 16 + n], l[t]);
+#pragma unroll
+      for (int d = 0; d < DT; ++d) o[t][d] *= alpha;
+    }
+    f32x4* O = reinterpret_cast<f32x4*>(&lds[0][0]) + lane;
+    static_assert(RT * DT * 64 * 16 <= static_cast<int>(sizeof(lds)), "a wave's sums fit the V tiles' place");
+    for (int w = 1; w < kFewWaves; ++w) {
+      if (wave == w) {
+#pragma unroll
+        for (int t = 0; t < RT; ++t)
+#pragma unroll
+          for (int d = 0; d < DT; ++d) O[(t * DT + d) * 64] = o[t][d];
+      }
+      __syncthreads();
+      if (wave == 0) {
+#pragma unroll
+        for (int t = 0; t < RT; ++t)
+#pragma unroll
+          for (int d = 0; d < DT; ++d) o[t][d] += O[(t * DT + d) * 64];
+      }
+      __syncthreads();
+    }
+    // dims 16 d + 4 g .. + 3 of row 16 t + n
+    if (wave == 0) {
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+        if (!ok[t]) continue;
+        if (!whole) {
+          const int64_t slot = 2 * static_cast<int64_t>(worker) + (seg > 0);
+          float* P = slot_sums(a, D, slot, t * 16 + n);
+#pragma unroll
+          for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(P + d * 16 + 4 * g) = o[t][d];
+          if (g == 0) *slot_stats(a, D, slot, t * 16 + n) = make_float2(m[t], l[t]);
+        } else {
+          const float prior = a.prior_lse ? a.prior_lse[place[t].lse] : 0.f;
+#pragma unroll
+          for (int d = 0; d < DT; ++d) write_joined(a, place[t], m[t], l[t], prior, o[t][d], d * 16 + 4 * g);
+        }
+      }
+    }
+    if (todo == 0 || !next_item(a, &at)) return;
+  }
+}
+
+// ------------------------------------------------------------------- joining
+// Blocks of worker boundary j (between workers j and j + 1) join the slots of
+// the item that the boundary cuts, if worker j holds the item's first piece.
+// D / 4 threads side by side on a row's dims.  Items in many slots (few rows,
+// long contexts): a row at a time, the groups of threads on different slots;
+// else a row per group.  Fixed orders.
+constexpr int kJoinThreads = kPagedJoinThreads;
+
+template <int D>
+__global__ __launch_bounds__(kJoinThreads) void join_kernel(PagedAttnArgs a, int join_rows, int row_groups) {
+  constexpr int kSide = D / 4, kGroups = kJoinThreads / kSide;
+  __shared__ float weight[kPagedMaxWorkers];
+  __shared__ f32x4 part[kGroups][kSide];
+  __shared__ float red[2][kJoinThreads / 64];
+  const int tid = threadIdx.x, wave = tid >> 6, side = tid % kSide, grp = tid / kSide;
+  const int j = static_cast<int>(blockIdx.x) / row_groups, r0 = (static_cast<int>(blockIdx.x) - j * row_groups) * join_rows;
+  const Shares sh = shares_of(a);
+  if (static_cast<uint32_t>(j) + 1 >= sh.workers) return;
+  const uint32_t cut = sh.first(j + 1);
+  const Spot at = locate(a, cut);
+  const uint32_t start = cut - at.unit;
+  if (at.b < 0 || at.unit == 0 || sh.first(j) > start) return;
+  const int w1 = static_cast<int>(min(sh.worker_of(start + at.seq.cost(at.item) - 1), sh.workers - 1));
+  const int pieces = w1 - j + 1;
+  const int64_t slot0 = sh.first(j) != start ? 2 * static_cast<int64_t>(j) + 1 : 2 * static_cast<int64_t>(j);
+  auto slot = [&](int s) { return s == 0 ? slot0 : 2 * static_cast<int64_t>(j + s); };
+  const int rows = min(a.slot_rows, at.seq.rows - at.item * a.slot_rows), r1 = min(r0 + join_rows, rows);
+  auto place = [&](int in) { return row_place(a, at.seq, at.kvh, at.item * a.slot_rows + in, D); };
+  if (pieces <= kSide && join_rows > 1) {
+    for (int k = r0 + grp; k < r1; k += kGroups) {
+      const RowPlace to = place(k);
+      // thread `side` holds slot side's statistics, then its weight
+      const float2 mine = side < pieces ? *slot_stats(a, D, slot(side), k) : make_float2(kNoMax, 0.f);
+      float m = mine.x;
+#pragma unroll
+      for (int d = 1; d < kSide; d *= 2) m = fmaxf(m, __shfl_xor(m, d, kSide));
+      const float f = __builtin_amdgcn_exp2f(mine.x - m);
+      float l = f * mine.y;
+#pragma unroll
+      for (int d = 1; d < kSide; d *= 2) l += __shfl_xor(l, d, kSide);
+      f32x4 v = {};
+      for (int s0 = 0; s0 < pieces; s0 += 4) {
+        f32x4 some[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) some[u] = *reinterpret_cast<const f32x4*>(slot_sums(a, D, slot(min(s0 + u, pieces - 1)), k) + side * 4);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (s0 + u < pieces) v += some[u] * __shfl(f, s0 + u, kSide);
+      }
+      write_joined(a, to, m, l, a.prior_lse ? a.prior_lse[to.lse] : 0.f, v, side * 4);
+    }
+    return;
+  }
+  for (int k = r0; k < r1; ++k) {
+    const RowPlace to = place(k);
+    float2 mine[kPagedMaxWorkers / kJoinThreads];
+    float m = kNoMax, l = 0.f;
+#pragma unroll
+    for (int i = 0; i < kPagedMaxWorkers / kJoinThreads; ++i) {
+      const int s = tid + i * kJoinThreads;
+      mine[i] = s < pieces ? *slot_stats(a, D, slot(s), k) : make_float2(kNoMax, 0.f);
+      m = fmaxf(m, mine[i].x);
+    }
+    m = wave_fmax(m);
+    if ((tid & 63) == 0) red[0][wave] = m;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kJoinThreads / 64; ++w) m = fmaxf(m, red[0][w]);
+#pragma unroll
+    for (int i = 0; i < kPagedMaxWorkers / kJoinThreads; ++i) {
+      const float f = __builtin_amdgcn_exp2f(mine[i].x - m);
+      weight[tid + i * kJoinThreads] = f;
+      l = __builtin_fmaf(f, mine[i].y, l);
+    }
+    l = wave_sum(l);
+    if ((tid & 63) == 0) red[1][wave] = l;
+    __syncthreads();
+    l = 0.f;
+#pragma unroll
+    for (int w = 0; w < kJoinThreads / 64; ++w) l += red[1][w];
+    f32x4 v = {};
+#pragma unroll 4
+    for (int s = grp; s < pieces; s += kGroups)
+      v += *reinterpret_cast<const f32x4*>(slot_sums(a, D, slot(s), k) + side * 4) * weight[s];
+    part[grp][side] = v;
+    __syncthreads();
+    if (grp == 0) {
+#pragma unroll
+      for (int i = 1; i < kGroups; ++i) v += part[i][side];
+      write_joined(a, to, m, l, a.prior_lse ? a.prior_lse[to.lse] : 0.f, v, side * 4);
+    }
+    __syncthreads();
+  }
+}
+
+template <int D, bool MASK>
+hipError_t attend(const PagedAttnArgs& a, const PagedAttnPlan& plan, hipStream_t stream) {
+  const dim3 grid(static_cast<uint32_t>(plan.blocks)), block(plan.threads());
+  if (plan.waves == 0 && plan.slot_rows == 16)
+    hipLaunchKernelGGL((few_rows_kernel<D, 1, MASK>), grid, block, 0, stream, a);
+  else if (plan.waves == 0)
+    hipLaunchKernelGGL((few_rows_kernel<D, 2, MASK>), grid, block, 0, stream, a);
+  else if (plan.waves == 4)
+    hipLaunchKernelGGL((attn_kernel<D, 4, MASK>), grid, block, 0, stream, a);
+  else
+    hipLaunchKernelGGL((attn_kernel<D, 8, MASK>), grid, block, 0, stream, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || plan.workers < 2) return e;
+  const int row_groups = plan.slot_rows / plan.join_rows;
+  hipLaunchKernelGGL((join_kernel<D>), dim3(static_cast<uint32_t>((plan.workers - 1) * row_groups)), dim3(kJoinThreads), 0,
+                     stream, a, plan.join_rows, row_groups);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_paged_attention(const PagedAttnArgs& a, const PagedAttnPlan& plan, int head_dim, hipStream_t stream) {
+  if (head_dim == 128) return a.mask_block ? attend<128, true>(a, plan, stream) : attend<128, false>(a, plan, stream);
+  return a.mask_block ? attend<64, true>(a, plan, stream) : attend<64, false>(a, plan, stream);
+}
+
+}  // namespace mssa

@@ -1,0 +1,56 @@
+// How the operators for streams served together cut their work: static rules
+// on sizes, no device code.
+#include <algorithm>
+
+#include "paged_args.hpp"
+
+namespace mssa {
+
+// A block's threads take two pieces of 16 values each at a time; while there
+// are blocks enough for two on every CU, several tokens share a block.
+int32_t append_block_tokens(int64_t tokens, int32_t units) {
+  const int64_t most = std::min<int64_t>(std::max(1, 2 * kAppendThreads / units), kAppendMaxTokens);
+  return static_cast<int32_t>(std::max<int64_t>(1, std::min(most, tokens / 512)));
+}
+
+hipError_t plan_paged_attention(int64_t tokens, int32_t batch, int32_t max_chunk, int32_t q_heads, int32_t kv_heads,
+                                int32_t head_dim, int64_t capacity, PagedAttnPlan* plan) {
+  PagedAttnPlan p{};
+  const int64_t group = q_heads / kv_heads, rows = std::min<int64_t>(max_chunk, std::max<int64_t>(tokens, 1)) * group;
+  p.waves = rows <= 32 ? 0 : rows <= 2048 ? 4 : 8;
+  p.slot_rows = p.waves ? p.waves * 32 : rows <= 16 ? 16 : 32;
+  // every sequence's items: whole ones, and one that is not full
+  const int64_t items = kv_heads * std::min(batch * ((rows + p.slot_rows - 1) / p.slot_rows), batch + tokens * group / p.slot_rows);
+  const int64_t tiles = (capacity + kPagedTile - 1) / kPagedTile;
+  if (items > 0x7fffffff || items * std::max<int64_t>(1, tiles) > 0x7fffffff) return hipErrorInvalidValue;
+  const int64_t slots = p.waves == 8 ? 256 : 512;  // blocks resident at once
+  p.least = p.waves ? 4 : 2 * kPagedFewWaves;
+  if (tiles > p.least) p.workers = static_cast<int32_t>(std::max<int64_t>(1, std::min(slots, items * tiles / p.least)));
+  p.blocks = p.workers ? p.workers : items;
+  if (!launchable(p.blocks, p.threads())) return hipErrorInvalidValue;
+  p.join_rows = p.waves ? 8 : 1;
+  p.workspace_bytes = int64_t{2} * p.workers * p.slot_rows * (head_dim + 2) * 4;
+  *plan = p;
+  return hipSuccess;
+}
+
+hipError_t plan_adapter_project(int64_t rows, int32_t in_features, int32_t out_features, int32_t parts, int32_t segments,
+                                int32_t adapters, int32_t rank, AdapterPlan* plan) {
+  (void)in_features;
+  AdapterPlan p{};
+  const int64_t tiles = (rows + 127) / 128 * ((int64_t{out_features} + 127) / 128);
+  if (!launchable(tiles, 256)) return hipErrorInvalidValue;
+  p.blocks = tiles;
+  if (segments > 0 && adapters > 0) {
+    p.low_rank = (rank + 15) / 16 * 16;
+    // every segment's tiles: whole ones, and one that is not full
+    const int64_t low_tiles = std::min<int64_t>(rows, segments + rows / kLowRows);
+    p.low_blocks = low_tiles * parts;
+    if (!launchable(p.low_blocks, 256)) return hipErrorInvalidValue;
+    p.workspace_bytes = rows * parts * p.low_rank * 2;
+  }
+  *plan = p;
+  return hipSuccess;
+}
+
+}  // namespace mssa

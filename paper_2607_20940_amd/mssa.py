@@ -32,7 +32,9 @@ EXPORTS = ("mssa_plan_create", "mssa_plan_create_ex", "mssa_plan_destroy", "mssa
            "mssa_qkv_project", "mssa_qkv_project_scaled", "mssa_attention_noalloc", "mssa_pool_kv_head_ring", "mssa_forward_head_ring",
            "mssa_head_ring_roll", "mssa_add_rms_norm", "mssa_add_rms_norm_workspace_size",
            "mssa_add_rms_norm_backward", "mssa_mx_quantize", "mssa_mx_dequantize", "mssa_mx_project",
-           "mssa_mx_attention_workspace_size", "mssa_mx_attention", "mssa_status_string", "mssa_last_error")
+           "mssa_mx_attention_workspace_size", "mssa_mx_attention", "mssa_adapter_project_workspace_size",
+           "mssa_adapter_project", "mssa_paged_append", "mssa_paged_attention_workspace_size", "mssa_paged_attention",
+           "mssa_status_string", "mssa_last_error")
 
 MSSA_NOALLOC_SCRATCH_BYTES = 256 << 20
 
@@ -57,6 +59,28 @@ class mssa_mx_attention_desc(ctypes.Structure):
     _fields_ = [("batch", ctypes.c_int32), ("n_q", ctypes.c_int32), ("q_heads", ctypes.c_int32),
                 ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("cache_tokens", ctypes.c_int64),
                 ("lse_stride", ctypes.c_int64), ("softmax_scale", ctypes.c_float)]
+
+
+class mssa_adapter_project_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("in_features", ctypes.c_int32), ("out_features", ctypes.c_int32),
+                ("parts", ctypes.c_int32), ("segments", ctypes.c_int32), ("adapters", ctypes.c_int32),
+                ("rank", ctypes.c_int32), ("part0_scale", ctypes.c_float), ("x_stride", ctypes.c_int64)]
+
+
+class mssa_paged_append_desc(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64), ("batch", ctypes.c_int32), ("q_heads", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("page_tokens", ctypes.c_int32),
+                ("table_pages", ctypes.c_int32), ("pages", ctypes.c_int64), ("rotate_dims", ctypes.c_int32),
+                ("halves", ctypes.c_int32), ("axes", ctypes.c_int32), ("axis_pairs", ctypes.c_int32 * 3),
+                ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64)]
+
+
+class mssa_paged_attention_desc(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64), ("batch", ctypes.c_int32), ("max_chunk", ctypes.c_int32),
+                ("q_heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("page_tokens", ctypes.c_int32), ("table_pages", ctypes.c_int32), ("pages", ctypes.c_int64),
+                ("mask_block", ctypes.c_int32), ("q_stride", ctypes.c_int64), ("lse_stride", ctypes.c_int64),
+                ("softmax_scale", ctypes.c_float)]
 
 
 class mssa_plan_desc(ctypes.Structure):
@@ -130,6 +154,13 @@ def _load():
     lib.mssa_mx_project.argtypes = [PD, V, V, V, V, V, PP, V]
     lib.mssa_mx_attention_workspace_size.argtypes = [AD, ctypes.POINTER(I64)]
     lib.mssa_mx_attention.argtypes = [AD, V, V, V, V, V, V, V, V, V, I64, V, V, V]
+    APD, PPD, PAD = (ctypes.POINTER(t) for t in (mssa_adapter_project_desc, mssa_paged_append_desc,
+                                                 mssa_paged_attention_desc))
+    lib.mssa_adapter_project_workspace_size.argtypes = [APD, ctypes.POINTER(I64)]
+    lib.mssa_adapter_project.argtypes = [APD, V, V, V, V, V, V, V, V, V, I64, PP, V]
+    lib.mssa_paged_append.argtypes = [PPD, V, V, V, V, V, V, V, V, V, V, V, V]
+    lib.mssa_paged_attention_workspace_size.argtypes = [PAD, ctypes.POINTER(I64)]
+    lib.mssa_paged_attention.argtypes = [PAD, V, V, V, V, V, V, V, V, V, I64, V, V, V]
     lib.mssa_status_string.argtypes = [ctypes.c_int]
     lib.mssa_status_string.restype = ctypes.c_char_p
     lib.mssa_last_error.argtypes = []
@@ -466,6 +497,73 @@ def mssa_mx_attention(desc, q, k_codes, k_scales, v_codes, v_scales, kv_len, pri
     _check(lib.mssa_mx_attention(ctypes.byref(desc), _ptr(q), _ptr(k_codes), _ptr(k_scales), _ptr(v_codes),
                                  _ptr(v_scales), _ptr(kv_len), _ptr(prior_out), _ptr(prior_lse), _ptr(workspace), wb,
                                  _ptr(out), _ptr(lse), _stream(stream)), "mssa_mx_attention")
+
+
+def adapter_project_desc(rows, in_features, out_features, segments, adapters, rank, parts=1, part0_scale=1.0,
+                         x_stride=0):
+    return mssa_adapter_project_desc(int(rows), int(in_features), int(out_features), int(parts), int(segments),
+                                     int(adapters), int(rank), float(part0_scale), int(x_stride))
+
+
+def paged_append_desc(tokens, batch, q_heads, kv_heads, head_dim, page_tokens, pages, table_pages, rotate_dims=None,
+                      halves=False, axis_pairs=None, q_stride=0, k_stride=0, v_stride=0):
+    """Descriptor of mssa_paged_append (rotate_dims: None turns the whole head;
+    axis_pairs: the pairs of each position axis, None: one axis has them all)."""
+    turned = int(head_dim if rotate_dims is None else rotate_dims)
+    split = [turned // 2] if axis_pairs is None else [int(p) for p in axis_pairs]
+    if not 1 <= len(split) <= 3:
+        raise ValueError("axis_pairs has one to three entries")
+    pairs = (ctypes.c_int32 * 3)(*split, *[0] * (3 - len(split)))
+    return mssa_paged_append_desc(int(tokens), int(batch), int(q_heads), int(kv_heads), int(head_dim), int(page_tokens),
+                                  int(table_pages), int(pages), turned, int(halves), len(split), pairs, int(q_stride),
+                                  int(k_stride), int(v_stride))
+
+
+def paged_attention_desc(tokens, batch, max_chunk, q_heads, kv_heads, head_dim, page_tokens, pages, table_pages,
+                         mask_block=0, softmax_scale=0.0, q_stride=0, lse_stride=0):
+    return mssa_paged_attention_desc(int(tokens), int(batch), int(max_chunk), int(q_heads), int(kv_heads), int(head_dim),
+                                     int(page_tokens), int(table_pages), int(pages), int(mask_block), int(q_stride),
+                                     int(lse_stride), float(softmax_scale))
+
+
+def mssa_adapter_project_workspace_size(desc):
+    n = ctypes.c_int64()
+    _check(lib.mssa_adapter_project_workspace_size(ctypes.byref(desc), ctypes.byref(n)),
+           "mssa_adapter_project_workspace_size")
+    return n.value
+
+
+def mssa_adapter_project(desc, x, w, bias, segment_begin, adapter, a, b, scale, workspace, y, workspace_bytes=None,
+                         stream=None):
+    """y: the desc.parts outputs."""
+    if len(y) != desc.parts:
+        raise ValueError("one output per part")
+    wb = _nbytes(workspace) if workspace_bytes is None else int(workspace_bytes)
+    _check(lib.mssa_adapter_project(ctypes.byref(desc), _ptr(x), _ptr(w), _ptr(bias), _ptr(segment_begin), _ptr(adapter),
+                                    _ptr(a), _ptr(b), _ptr(scale), _ptr(workspace), wb, _ptr_array(y), _stream(stream)),
+           "mssa_adapter_project")
+
+
+def mssa_paged_append(desc, q, k, v, chunk_begin, kv_len, page_table, positions, freqs, q_out, k_pages, v_pages,
+                      stream=None):
+    _check(lib.mssa_paged_append(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(chunk_begin), _ptr(kv_len),
+                                 _ptr(page_table), _ptr(positions), _ptr(freqs), _ptr(q_out), _ptr(k_pages),
+                                 _ptr(v_pages), _stream(stream)), "mssa_paged_append")
+
+
+def mssa_paged_attention_workspace_size(desc):
+    n = ctypes.c_int64()
+    _check(lib.mssa_paged_attention_workspace_size(ctypes.byref(desc), ctypes.byref(n)),
+           "mssa_paged_attention_workspace_size")
+    return n.value
+
+
+def mssa_paged_attention(desc, q, k_pages, v_pages, chunk_begin, kv_len, page_table, prior_out, prior_lse, workspace, out,
+                         lse=None, workspace_bytes=None, stream=None):
+    wb = _nbytes(workspace) if workspace_bytes is None else int(workspace_bytes)
+    _check(lib.mssa_paged_attention(ctypes.byref(desc), _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(chunk_begin),
+                                    _ptr(kv_len), _ptr(page_table), _ptr(prior_out), _ptr(prior_lse), _ptr(workspace), wb,
+                                    _ptr(out), _ptr(lse), _stream(stream)), "mssa_paged_attention")
 
 
 class HeadRing:
