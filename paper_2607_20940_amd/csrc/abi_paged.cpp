@@ -62,9 +62,8 @@ mssa_status project_check(const mssa_adapter_project_desc* d) {
   return MSSA_OK;
 }
 
-mssa_status plan_of(const mssa_adapter_project_desc* d, mssa::AdapterPlan* plan) {
-  if (mssa::plan_adapter_project(d->rows, d->in_features, d->out_features, d->parts, d->segments, d->adapters, d->rank, plan) !=
-      hipSuccess)
+mssa_status plan_of(const mssa_adapter_project_desc* d, bool aligned, mssa::AdapterPlan* plan) {
+  if (mssa::plan_adapter_project(d->rows, d->out_features, d->parts, d->segments, d->adapters, d->rank, aligned, plan) != hipSuccess)
     return fail(MSSA_ERR_UNSUPPORTED, "too many outputs for one launch");
   return MSSA_OK;
 }
@@ -102,8 +101,9 @@ mssa_status mssa_adapter_project_workspace_size(const mssa_adapter_project_desc*
   return guarded("mssa_adapter_project_workspace_size", [&]() -> mssa_status {
     if (const mssa_status s = project_check(desc); s != MSSA_OK) return s;
     if (!bytes) return fail(MSSA_ERR_INVALID_ARG, "null argument");
+    // the same for both kinds of tensors
     mssa::AdapterPlan plan;
-    const mssa_status planned = plan_of(desc, &plan);
+    const mssa_status planned = plan_of(desc, false, &plan);
     if (planned == MSSA_OK) *bytes = plan.workspace_bytes;
     return planned;
   });
@@ -123,8 +123,14 @@ mssa_status mssa_adapter_project(const mssa_adapter_project_desc* desc, const vo
       if (!aligned_to(t, 2)) return fail(MSSA_ERR_INVALID_ARG, "a tensor is not aligned to its type");
     for (const void* t : {static_cast<const void*>(segment_begin), static_cast<const void*>(adapter), static_cast<const void*>(scale)})
       if (!aligned_to(t, 4)) return fail(MSSA_ERR_INVALID_ARG, "segments, adapters and scales must be aligned to 4 bytes");
+    const int64_t x_stride = stride_or(desc->x_stride, desc->in_features);
+    // the tiles' byte offsets have 32 bits: 256 rows of x
+    bool aligned = desc->in_features % 64 == 0 && x_stride % 8 == 0 && x_stride <= (1 << 21) && desc->out_features / desc->parts % 8 == 0 &&
+                   (!low || desc->rank % 8 == 0);
+    for (const void* t : {x, w, bias, a, b}) aligned = aligned && aligned16(t);
+    for (int p = 0; p < desc->parts; ++p) aligned = aligned && aligned16(y[p]);
     mssa::AdapterPlan plan;
-    if (const mssa_status planned = plan_of(desc, &plan); planned != MSSA_OK) return planned;
+    if (const mssa_status planned = plan_of(desc, aligned, &plan); planned != MSSA_OK) return planned;
     if (plan.workspace_bytes > 0) {
       if (!workspace || workspace_bytes < plan.workspace_bytes)
         return fail(MSSA_ERR_WORKSPACE, "workspace smaller than mssa_adapter_project_workspace_size");
@@ -147,7 +153,7 @@ mssa_status mssa_adapter_project(const mssa_adapter_project_desc* desc, const vo
     args.adapter = adapter;
     args.scale = scale;
     args.low = workspace;
-    args.x_stride = stride_or(desc->x_stride, desc->in_features);
+    args.x_stride = x_stride;
     args.M = static_cast<int32_t>(desc->rows);
     args.N = desc->out_features;
     args.K = desc->in_features;

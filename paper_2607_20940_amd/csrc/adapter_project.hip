@@ -10,14 +10,17 @@
 // rows only, so that an infinity or a NaN of one adapter stays with its rows.
 #include <hip/hip_runtime.h>
 
+#include "kernel_args.hpp"
 #include "lds_stage.hpp"
 #include "lowbit_values.hpp"
 #include "paged_args.hpp"
+#include "xcd.hpp"
 
 namespace mssa {
 namespace {
 
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int kThreads = 256;
@@ -59,15 +62,17 @@ __device__ inline int32_t first_segment(const AdapterArgs& a, int32_t row) {
   return lo;
 }
 
-// The low-rank factor of 32 rows of one segment and one part: a wave takes
-// every fourth 16 values of the contraction, 32 ranks at a time, and the four
-// sums meet in LDS.
-__global__ __launch_bounds__(kThreads) void low_kernel(AdapterArgs a) {
-  __shared__ float sums[4][32 * 33];
+// The low-rank factors of 32 rows of one segment: NT x 32 of the parts' rank
+// columns, which stand behind one another.  The block's waves share out the
+// contraction, and their sums meet in LDS, in a fixed order.  kWhole: rows of
+// whole, aligned 16-byte chunks.
+template <int NW, int NT, bool kWhole>
+__global__ __launch_bounds__(NW * 64) void low_kernel(AdapterArgs a) {
+  constexpr int kUnroll = 4;
+  __shared__ float sums[NW][32 * 33];
   const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, hh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int part = blockIdx.x % a.parts;
-  int32_t tile = blockIdx.x / a.parts;
+  int32_t tile = blockIdx.x;
   // the segment that the tile belongs to, and the tile's place in it
   int32_t s = -1;
   for (int32_t c = 0; c < a.segments && s < 0; c += 64) {
@@ -98,30 +103,54 @@ __global__ __launch_bounds__(kThreads) void low_kernel(AdapterArgs a) {
   const int32_t row0 = g.first + tile * kLowRows;
   if (g.adapter < 0 || tile < 0 || row0 >= g.end) return;
   const int32_t row = row0 + n32;
-  const bool ok = row < g.end;
-  const __bf16* x = static_cast<const __bf16*>(a.x) + static_cast<int64_t>(ok ? row : row0) * a.x_stride;
-  const __bf16* A = static_cast<const __bf16*>(a.a) + (static_cast<int64_t>(g.adapter) * a.parts + part) * a.rank * a.K;
-  const float scale = a.scale ? a.scale[g.adapter] : 1.f;
-  for (int r0 = 0; r0 < a.rank; r0 += 32) {
-    const int r = r0 + n32;
-    const __bf16* ar = A + static_cast<int64_t>(r < a.rank ? r : 0) * a.K;
-    f32x16 acc = f32x16{};
-#pragma unroll 4
-    for (int k = wave * 16; k < a.K; k += 64) {
-      const int at = k + hh * 8;
-      acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(eight(ar + at, a.K - at), eight(x + at, a.K - at), acc, 0, 0, 0);
-    }
-    __syncthreads();
+  const __bf16* x = static_cast<const __bf16*>(a.x) + static_cast<int64_t>(row < g.end ? row : row0) * a.x_stride;
+  const __bf16* A = static_cast<const __bf16*>(a.a) + static_cast<int64_t>(g.adapter) * a.parts * a.rank * a.K;
+  const int cols = a.parts * a.low_rank, c0 = blockIdx.y * NT * 32;
+  const __bf16* ar[NT];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) sums[wave][n32 * 33 + 8 * (e >> 2) + 4 * hh + (e & 3)] = acc[e];
+  for (int t = 0; t < NT; ++t) {  // columns past the ranks are read as others' and written as zeros
+    const int c = min(c0 + t * 32 + n32, cols - 1), part = c / a.low_rank, r = min(c - part * a.low_rank, a.rank - 1);
+    ar[t] = A + (static_cast<int64_t>(part) * a.rank + r) * a.K;
+  }
+  auto get = [&](const __bf16* p, int at) -> bf16x8 {
+    if constexpr (kWhole)
+      return *reinterpret_cast<const bf16x8*>(p + at);
+    else
+      return eight(p + at, a.K - at);
+  };
+  f32x16 acc[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) acc[t] = f32x16{};
+#pragma unroll 1
+  for (int k0 = wave * 16 * kUnroll; k0 < a.K; k0 += NW * 16 * kUnroll) {
+    bf16x8 xv[kUnroll], av[kUnroll][NT];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const int k = k0 + u * 16 + hh * 8;  // kWhole: a multiple of 64 values
+      xv[u] = get(x, k);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) av[u][t] = get(ar[t], k);
+    }
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av[u][t], xv[u], acc[t], 0, 0, 0);
+  }
+  const float scale = a.scale ? a.scale[g.adapter] : 1.f;
+  __bf16* out = static_cast<__bf16*>(a.low);
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    if (t > 0) __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 16; ++e) sums[wave][n32 * 33 + 8 * (e >> 2) + 4 * hh + (e & 3)] = acc[t][e];
     __syncthreads();
-    __bf16* out = static_cast<__bf16*>(a.low);
-    for (int i = tid; i < 32 * 32; i += kThreads) {
-      const int q = i >> 5, rr = i & 31, at = q * 33 + rr;
-      if (row0 + q >= g.end || r0 + rr >= a.low_rank) continue;
-      const float u = (sums[0][at] + sums[1][at]) + (sums[2][at] + sums[3][at]);
-      out[(static_cast<int64_t>(row0 + q) * a.parts + part) * a.low_rank + r0 + rr] =
-          static_cast<__bf16>(r0 + rr < a.rank ? u * scale : 0.f);
+    for (int i = tid; i < 32 * 32; i += NW * 64) {
+      const int q = i >> 5, c = c0 + t * 32 + (i & 31), at = q * 33 + (i & 31);
+      if (row0 + q >= g.end || c >= cols) continue;
+      float u = 0.f;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) u += sums[w][at];
+      out[static_cast<int64_t>(row0 + q) * cols + c] = static_cast<__bf16>(c % a.low_rank < a.rank ? u * scale : 0.f);
     }
   }
 }
@@ -244,14 +273,346 @@ __global__ __launch_bounds__(kThreads) void any_kernel(AdapterArgs a) {
   }
 }
 
+// ------------------------------------------------------------- few tokens
+// Up to 64 tokens: bound by the weights' bytes, each read once.  A block takes
+// 16 features, its waves share out the contraction, 256 values of it on their
+// way at once; W and X go from memory to the matrix cores' registers as they
+// lie.  The adapters' share is a dot product of `rank` values for each output.
+constexpr int kFewFeatures = 16, kFewWaves = 4;
+
+template <int RT>
+__global__ __launch_bounds__(kFewWaves * 64) void few_kernel(AdapterArgs a) {
+  constexpr int kUnroll = 8, kRows = RT * 16, kStr = kFewFeatures + 1;
+  __shared__ float sums[kFewWaves][kRows * kStr];
+  __shared__ int32_t which[kRows];
+  const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int32_t f0 = static_cast<int32_t>(blockIdx.x) * kFewFeatures;
+  const __bf16* w = static_cast<const __bf16*>(a.w) + static_cast<int64_t>(min(f0 + n, a.N - 1)) * a.K + g * 8;
+  const __bf16* x[RT];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) x[t] = static_cast<const __bf16*>(a.x) + min(t * 16 + n, a.M - 1) * a.x_stride + g * 8;
+  f32x4 acc[RT];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) acc[t] = f32x4{};
+#pragma unroll 1
+  for (int k0 = wave * 32 * kUnroll; k0 < a.K; k0 += kFewWaves * 32 * kUnroll) {
+    bf16x8 wv[kUnroll], xv[kUnroll][RT];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const int k = k0 + u * 32;  // K is a multiple of 32
+      wv[u] = bf16x8{};
+      if (k < a.K) wv[u] = __builtin_nontemporal_load(reinterpret_cast<const bf16x8*>(w + k));
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+        xv[u][t] = bf16x8{};
+        if (k < a.K) xv[u][t] = *reinterpret_cast<const bf16x8*>(x[t] + k);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+      for (int t = 0; t < RT; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[u], xv[u][t], acc[t], 0, 0, 0);
+  }
+  // element e of acc[t]: row 16 t + n, feature 4 g + e
+#pragma unroll
+  for (int t = 0; t < RT; ++t)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sums[wave][(t * 16 + n) * kStr + 4 * g + e] = acc[t][e];
+  for (int r = wave; r < kRows; r += kFewWaves) {
+    int32_t j = -1;
+    if (a.segments && r < a.M) {
+      const int32_t s = first_segment(a, r);
+      if (s < a.segments) {
+        const Segment sg = segment(a, s);
+        if (sg.first <= r && r < sg.end) j = sg.adapter;
+      }
+    }
+    if (lane == 0) which[r] = j;
+  }
+  __syncthreads();
+  const __bf16* bias = static_cast<const __bf16*>(a.bias);
+#pragma unroll
+  for (int i = tid; i < kRows * kFewFeatures; i += kFewWaves * 64) {
+    const int r = i / kFewFeatures, f = f0 + i % kFewFeatures;
+    if (r >= a.M || f >= a.N) continue;
+    const int part = f / a.split, j = which[r];
+    float v = 0.f;
+#pragma unroll
+    for (int k = 0; k < kFewWaves; ++k) v += sums[k][r * kStr + i % kFewFeatures];
+    if (j >= 0) {
+      const __bf16* u = static_cast<const __bf16*>(a.low) + (r * a.parts + part) * a.low_rank;
+      const __bf16* b = static_cast<const __bf16*>(a.b) + (static_cast<int64_t>(j) * a.N + f) * a.rank;
+      float d = 0.f;
+      for (int q = 0; q < a.rank; q += 8) {
+        const bf16x8 uv = *reinterpret_cast<const bf16x8*>(u + q), bv = *reinterpret_cast<const bf16x8*>(b + q);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) d = __builtin_fmaf(static_cast<float>(uv[e]), static_cast<float>(bv[e]), d);
+      }
+      v += d;
+    }
+    v = (v + (bias ? static_cast<float>(bias[f]) : 0.f)) * (part == 0 ? a.part0_scale : 1.f);
+    static_cast<__bf16*>(a.y[part])[static_cast<int64_t>(r) * a.split + (f - part * a.split)] = static_cast<__bf16>(v);
+  }
+}
+
+// ------------------------------------------------------------ many tokens
+// Tiles of WM x MB x 32 rows and WN x NB x 32 features, WM x WN waves of
+// MB x NB matrix-core tiles each (A = W rows, B = X rows).  The contraction
+// comes in 64-deep stages of 128-byte rows (the swizzle of lds_stage.hpp)
+// through two LDS buffers, filled by direct transfers while the stage before
+// is multiplied; one barrier a stage.  The adapters follow as further stages: 64
+// ranks of one part of one segment, its rows' low-rank factors against B.
+// Tiles are taken in panels of four feature tiles, each XCD a run of them.
+// The outputs leave through LDS as whole-row 16-byte stores.
+constexpr int kBK = 64, kPanel = 4;
+
+template <int WM, int WN, int MB, int NB>
+__global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void tile_kernel(AdapterArgs a) {
+  constexpr int NW = WM * WN, BM = WM * MB * 32, BN = WN * NB * 32;
+  constexpr int kX = BM * 128, kW = BN * 128, kStage = kX + kW;  // bytes
+  constexpr int TX = BM / 8 / NW, TW = BN / 8 / NW;              // transfers (8 rows) of a wave
+  __shared__ __attribute__((aligned(16))) char lds[2][kStage];
+  const int tiles_m = (a.M + BM - 1) / BM, tiles_n = (a.N + BN - 1) / BN;
+  const int t = xcd_remap(blockIdx.x, tiles_m * tiles_n);
+  const int panel = t / (tiles_m * kPanel), pw = min(kPanel, tiles_n - panel * kPanel);
+  const int ip = t - panel * tiles_m * kPanel;
+  const int32_t m0 = ip / pw * BM, f0 = (panel * kPanel + ip % pw) * BN;
+  const int32_t m1 = min(m0 + BM, a.M), f1 = min(f0 + BN, a.N);
+
+  const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, hh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave % WM, wn = wave / WM;
+
+  // A transfer: rows 8 i + lane / 8, physical chunk lane % 8 holding logical
+  // chunk unswz128(row, lane % 8).  Rows past the matrix read zeros.
+  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(&lds[0][0]));
+  auto put = [&](int buf, const __bf16* x, uint32_t xrb, uint32_t xbytes, const __bf16* w, uint32_t wrb, uint32_t wbytes, int chunks) {
+    const i32x4 rx = rsrc_of(x, xbytes), rw = rsrc_of(w, wbytes);
+    const uint32_t base = lds0 + buf * kStage;
+#pragma unroll
+    for (int i = 0; i < TX; ++i) {
+      const int row = (wave * TX + i) * 8 + (lane >> 3), lc = unswz128(row, lane & 7);
+      dma16(rx, lc < chunks ? row * xrb + lc * 16 : kPastEnd, __builtin_amdgcn_readfirstlane(base + (wave * TX + i) * 1024));
+    }
+#pragma unroll
+    for (int i = 0; i < TW; ++i) {
+      const int row = (wave * TW + i) * 8 + (lane >> 3), lc = unswz128(row, lane & 7);
+      dma16(rw, lc < chunks ? row * wrb + lc * 16 : kPastEnd, __builtin_amdgcn_readfirstlane(base + kX + (wave * TW + i) * 1024));
+    }
+  };
+  const __bf16* X = static_cast<const __bf16*>(a.x) + static_cast<int64_t>(m0) * a.x_stride;
+  const __bf16* W = static_cast<const __bf16*>(a.w) + static_cast<int64_t>(f0) * a.K;
+  const uint32_t xrb = static_cast<uint32_t>(a.x_stride) * 2, wrb = static_cast<uint32_t>(a.K) * 2;
+  const uint32_t xbytes = static_cast<uint32_t>(m1 - m0 - 1) * xrb + kBK * 2, wbytes = static_cast<uint32_t>(f1 - f0 - 1) * wrb + kBK * 2;
+  auto put_main = [&](int st) { put(st & 1, X + st * kBK, xrb, xbytes, W + st * kBK, wrb, wbytes, 8); };
+  put_main(0);
+
+  // The adapters' stages, found one after the other: a segment with an adapter
+  // among the tile's rows, a part among its features, 64 ranks.
+  const int p0 = f0 / a.split, p1 = (f1 - 1) / a.split;
+  struct {
+    int32_t s, first, end, adapter, part, r0;
+  } next{};
+  auto to_segment = [&](int32_t s) {  // s or the next that has an adapter here; first = m1 where none does
+    next.first = m1;
+    for (; s < a.segments; ++s) {
+      const Segment g = segment(a, s);
+      const int32_t first = __builtin_amdgcn_readfirstlane(g.first), end = __builtin_amdgcn_readfirstlane(g.end);
+      const int32_t adapter = __builtin_amdgcn_readfirstlane(g.adapter);
+      if (first >= m1) break;
+      if (adapter < 0 || first >= end || end <= m0) continue;
+      next = {s, first, end, adapter, p0, 0};
+      break;
+    }
+  };
+  auto advance = [&]() {
+    if ((next.r0 += kBK) < a.rank) return;
+    next.r0 = 0;
+    if (++next.part <= p1) return;
+    to_segment(next.s + 1);
+  };
+  const uint32_t urb = static_cast<uint32_t>(a.parts * a.low_rank) * 2, brb = static_cast<uint32_t>(a.rank) * 2;
+  auto put_low = [&](int buf) {
+    const __bf16* u = static_cast<const __bf16*>(a.low) + static_cast<int64_t>(m0) * a.parts * a.low_rank + next.part * a.low_rank + next.r0;
+    const __bf16* b = static_cast<const __bf16*>(a.b) + (static_cast<int64_t>(next.adapter) * a.N + f0) * a.rank + next.r0;
+    const int left = min(a.rank - next.r0, kBK);  // a multiple of 8
+    put(buf, u, urb, static_cast<uint32_t>(m1 - m0 - 1) * urb + left * 2, b, brb, static_cast<uint32_t>(f1 - f0 - 1) * brb + left * 2, left / 8);
+  };
+  next.first = m1;
+  if (a.segments) to_segment(__builtin_amdgcn_readfirstlane(first_segment(a, m0)));
+
+  f32x16 acc[MB][NB];
+#pragma unroll
+  for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) acc[mb][nb] = f32x16{};
+  // Operand reads: row (block base + n32), columns 16 ks + 8 hh; the swizzle
+  // of a row depends only on n32 (block bases are multiples of 32).
+  int rd[kBK / 16];
+#pragma unroll
+  for (int ks = 0; ks < kBK / 16; ++ks) rd[ks] = swz128(n32, ks * 16 + hh * 8) * 2;
+
+  const int nst = a.K / kBK;
+  for (int st = 0; st < nst; ++st) {
+    wait_vmcnt<0>();
+    __syncthreads();
+    if (st + 1 < nst)
+      put_main(st + 1);
+    else if (next.first < m1)
+      put_low(nst & 1);
+    const char* Xs = lds[st & 1] + wm * MB * 32 * 128;
+    const char* Ws = lds[st & 1] + kX + wn * NB * 32 * 128;
+    // Operands of k step ks in register set ks & 1: the reads of step ks + 1
+    // run between the matrix instructions of step ks.
+    bf16x8 op[2][NB + MB];
+    auto rd_op = [&](int ks, int j) -> bf16x8 {
+      return j < NB ? *reinterpret_cast<const bf16x8*>(Ws + j * 32 * 128 + rd[ks])
+                    : *reinterpret_cast<const bf16x8*>(Xs + (j - NB) * 32 * 128 + rd[ks]);
+    };
+#pragma unroll
+    for (int j = 0; j < NB + MB; ++j) op[0][j] = rd_op(0, j);
+#pragma unroll
+    for (int ks = 0; ks < kBK / 16; ++ks) {
+      const int c = ks & 1;
+#pragma unroll
+      for (int i = 0; i < MB * NB; ++i) {
+        const int mb = i / NB, nb = i % NB;
+        acc[mb][nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[c][nb], op[c][NB + mb], acc[mb][nb], 0, 0, 0);
+        if (ks + 1 < kBK / 16 && i < NB + MB) op[c ^ 1][i] = rd_op(ks + 1, i);
+      }
+    }
+    static_assert(MB * NB >= NB + MB, "a read after every matrix instruction");
+#pragma unroll
+    for (int j = 0; j < NB + MB; ++j) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+#pragma unroll
+    for (int ks = 0; ks < kBK / 16; ++ks)
+#pragma unroll
+      for (int i = 0; i < MB * NB; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        if (ks + 1 < kBK / 16 && i < NB + MB) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  for (int st = nst; next.first < m1; ++st) {
+    const int32_t first = next.first, end = next.end, fa = next.part * a.split, fb = fa + a.split;
+    const int steps = (min(a.rank - next.r0, kBK) + 15) / 16;
+    wait_vmcnt<0>();
+    __syncthreads();
+    advance();
+    if (next.first < m1) put_low((st + 1) & 1);
+    const char* Xs = lds[st & 1] + wm * MB * 32 * 128;
+    const char* Ws = lds[st & 1] + kX + wn * NB * 32 * 128;
+    const bool all_f = fa <= f0 && f1 <= fb;
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) {
+      const int32_t row = m0 + (wm * MB + mb) * 32 + n32;
+      const bool mine = row >= first && row < end;
+      if (!__any(mine)) continue;
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        f32x16 add = f32x16{};
+#pragma unroll
+        for (int ks = 0; ks < kBK / 16; ++ks)
+          if (ks < steps)
+            add = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(Ws + nb * 32 * 128 + rd[ks]),
+                                                          *reinterpret_cast<const bf16x8*>(Xs + mb * 32 * 128 + rd[ks]), add, 0, 0, 0);
+        if (all_f) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) acc[mb][nb][e] += mine ? add[e] : 0.f;
+        } else {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int32_t f = f0 + (wn * NB + nb) * 32 + 8 * (e >> 2) + 4 * hh + (e & 3);
+            acc[mb][nb][e] += mine && f >= fa && f < fb ? add[e] : 0.f;
+          }
+        }
+      }
+    }
+  }
+
+  // Epilogue through LDS, one wave row's rows at a time.
+  constexpr int kEStr = BN + 8, kERows = MB * 32;
+  static_assert(kERows * kEStr * 2 <= static_cast<int>(sizeof(lds)), "a wave row's outputs fit the stage buffers");
+  __bf16* E = reinterpret_cast<__bf16*>(&lds[0][0]);
+  const __bf16* bias = static_cast<const __bf16*>(a.bias);
+#pragma unroll 1
+  for (int part_m = 0; part_m < WM; ++part_m) {
+    __syncthreads();  // the stage buffers, or the rows before, are free
+    if (wm == part_m) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int jj = 0; jj < 4; ++jj) {
+          const int at = (wn * NB + nb) * 32 + 8 * jj + 4 * hh;
+          const int32_t f = f0 + at;
+          bf16x4 bv = {};
+          if (bias && f < a.N) bv = *reinterpret_cast<const bf16x4*>(bias + f);
+          const float factor = f < a.split ? a.part0_scale : 1.f;
+#pragma unroll
+          for (int mb = 0; mb < MB; ++mb) {
+            bf16x4 v;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = static_cast<__bf16>((acc[mb][nb][4 * jj + i] + static_cast<float>(bv[i])) * factor);
+            *reinterpret_cast<bf16x4*>(E + (mb * 32 + n32) * kEStr + at) = v;
+          }
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int p = 0; p < kERows * BN / 8 / (NW * 64); ++p) {
+      const int c = p * NW * 64 + tid, rt = c / (BN / 8), ch = c % (BN / 8);
+      const int32_t row = m0 + part_m * kERows + rt, f = f0 + ch * 8;
+      if (row < m1 && f < a.N) {
+        const int part = f / a.split;  // 8 features never straddle a part (split % 8 == 0)
+        *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(a.y[part]) + static_cast<int64_t>(row) * a.split + (f - part * a.split)) =
+            *reinterpret_cast<const bf16x8*>(E + rt * kEStr + ch * 8);
+      }
+    }
+  }
+}
+
+template <int NW, bool kWhole>
+void low_launch(const AdapterArgs& a, const AdapterPlan& plan, hipStream_t stream) {
+  const int tiles = (a.parts * a.low_rank + 31) / 32;
+  const uint32_t rows = static_cast<uint32_t>(plan.low_blocks);
+  if (tiles == 1)
+    hipLaunchKernelGGL((low_kernel<NW, 1, kWhole>), dim3(rows), dim3(NW * 64), 0, stream, a);
+  else if (tiles == 2)
+    hipLaunchKernelGGL((low_kernel<NW, 2, kWhole>), dim3(rows), dim3(NW * 64), 0, stream, a);
+  else
+    hipLaunchKernelGGL((low_kernel<NW, 3, kWhole>), dim3(rows, (tiles + 2) / 3), dim3(NW * 64), 0, stream, a);
+}
+
 }  // namespace
 
 hipError_t launch_adapter_project(const AdapterArgs& a, const AdapterPlan& plan, hipStream_t stream) {
   if (plan.low_blocks) {
-    hipLaunchKernelGGL(low_kernel, dim3(static_cast<uint32_t>(plan.low_blocks)), dim3(kThreads), 0, stream, a);
+    if (plan.low_waves == 16)
+      plan.kernel != AdapterKernel::kAny ? low_launch<16, true>(a, plan, stream) : low_launch<16, false>(a, plan, stream);
+    else
+      plan.kernel != AdapterKernel::kAny ? low_launch<4, true>(a, plan, stream) : low_launch<4, false>(a, plan, stream);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(any_kernel, dim3(static_cast<uint32_t>(plan.blocks)), dim3(kThreads), 0, stream, a);
+  const dim3 grid(static_cast<uint32_t>(plan.blocks));
+  switch (plan.kernel) {
+    case AdapterKernel::kFew:
+      if (a.M <= 16)
+        hipLaunchKernelGGL(few_kernel<1>, grid, dim3(kFewWaves * 64), 0, stream, a);
+      else if (a.M <= 32)
+        hipLaunchKernelGGL(few_kernel<2>, grid, dim3(kFewWaves * 64), 0, stream, a);
+      else
+        hipLaunchKernelGGL(few_kernel<4>, grid, dim3(kFewWaves * 64), 0, stream, a);
+      break;
+    case AdapterKernel::kSmallTiles:
+      hipLaunchKernelGGL((tile_kernel<2, 2, 2, 2>), grid, dim3(256), 0, stream, a);
+      break;
+    case AdapterKernel::kLargeTiles:
+      hipLaunchKernelGGL((tile_kernel<2, 4, 4, 2>), grid, dim3(512), 0, stream, a);
+      break;
+    case AdapterKernel::kAny:
+      hipLaunchKernelGGL(any_kernel, grid, dim3(kThreads), 0, stream, a);
+  }
   return hipGetLastError();
 }
 

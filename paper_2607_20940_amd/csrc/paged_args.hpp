@@ -179,15 +179,24 @@ struct AdapterArgs {
   float part0_scale;
 };
 
+// Which kernel makes a product: the one for few tokens, one of two tile sizes,
+// or the one for any sizes, strides and alignments.
+enum class AdapterKernel { kFew, kSmallTiles, kLargeTiles, kAny };
+constexpr int kAdapterFewTokens = 64, kAdapterFewFeatures = 16;
+
 constexpr int kLowRows = 32;  // rows of a tile of the low-rank factor
 struct AdapterPlan {
-  int64_t low_blocks;  // blocks of the low-rank factor's launch, 0: none
+  AdapterKernel kernel;
+  int32_t low_waves;   // of a block of the low-rank factor's launch
+  int64_t low_blocks;  // row tiles of the low-rank factor's launch, 0: none
   int64_t blocks;      // of the product
   int64_t workspace_bytes;
   int32_t low_rank;    // rank rounded up to whole 16 values
 };
-hipError_t plan_adapter_project(int64_t rows, int32_t in_features, int32_t out_features, int32_t parts, int32_t segments,
-                                int32_t adapters, int32_t rank, AdapterPlan* plan);
+// aligned: rows of x, w, a, b and the outputs are whole aligned 16-byte chunks,
+// the contraction whole stages.
+hipError_t plan_adapter_project(int64_t rows, int32_t out_features, int32_t parts, int32_t segments, int32_t adapters,
+                                int32_t rank, bool aligned, AdapterPlan* plan);
 hipError_t launch_adapter_project(const AdapterArgs& a, const AdapterPlan& plan, hipStream_t stream);
 
 }  // namespace mssa

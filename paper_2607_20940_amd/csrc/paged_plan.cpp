@@ -34,19 +34,30 @@ hipError_t plan_paged_attention(int64_t tokens, int32_t batch, int32_t max_chunk
   return hipSuccess;
 }
 
-hipError_t plan_adapter_project(int64_t rows, int32_t in_features, int32_t out_features, int32_t parts, int32_t segments,
-                                int32_t adapters, int32_t rank, AdapterPlan* plan) {
-  (void)in_features;
+hipError_t plan_adapter_project(int64_t rows, int32_t out_features, int32_t parts, int32_t segments, int32_t adapters,
+                                int32_t rank, bool aligned, AdapterPlan* plan) {
   AdapterPlan p{};
-  const int64_t tiles = (rows + 127) / 128 * ((int64_t{out_features} + 127) / 128);
-  if (!launchable(tiles, 256)) return hipErrorInvalidValue;
-  p.blocks = tiles;
+  auto tiles = [&](int64_t m, int64_t n) { return (rows + m - 1) / m * ((out_features + n - 1) / n); };
+  p.kernel = AdapterKernel::kAny;
+  p.blocks = tiles(128, 128);
+  if (aligned) {
+    if (rows <= kAdapterFewTokens) {
+      p.kernel = AdapterKernel::kFew;
+      p.blocks = tiles(kAdapterFewTokens, kAdapterFewFeatures);
+    } else if (tiles(256, 256) >= 256) {
+      p.kernel = AdapterKernel::kLargeTiles;
+      p.blocks = tiles(256, 256);
+    } else {
+      p.kernel = AdapterKernel::kSmallTiles;
+    }
+  }
+  if (!launchable(p.blocks, p.kernel == AdapterKernel::kLargeTiles ? 512 : 256)) return hipErrorInvalidValue;
   if (segments > 0 && adapters > 0) {
     p.low_rank = (rank + 15) / 16 * 16;
     // every segment's tiles: whole ones, and one that is not full
-    const int64_t low_tiles = std::min<int64_t>(rows, segments + rows / kLowRows);
-    p.low_blocks = low_tiles * parts;
-    if (!launchable(p.low_blocks, 256)) return hipErrorInvalidValue;
+    p.low_blocks = std::min<int64_t>(rows, segments + rows / kLowRows);
+    p.low_waves = p.low_blocks <= 128 ? 16 : 4;
+    if (!launchable(p.low_blocks, p.low_waves * 64)) return hipErrorInvalidValue;
     p.workspace_bytes = rows * parts * p.low_rank * 2;
   }
   *plan = p;
