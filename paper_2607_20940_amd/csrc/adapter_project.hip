@@ -62,25 +62,18 @@ __device__ inline int32_t first_segment(const AdapterArgs& a, int32_t row) {
   return lo;
 }
 
-// The low-rank factors of 32 rows of one segment: NT x 32 of the parts' rank
-// columns, which stand behind one another.  The block's waves share out the
-// contraction, and their sums meet in LDS, in a fixed order.  kWhole: rows of
-// whole, aligned 16-byte chunks.
-template <int NW, int NT, bool kWhole>
-__global__ __launch_bounds__(NW * 64) void low_kernel(AdapterArgs a) {
-  constexpr int kUnroll = 4;
-  __shared__ float sums[NW][32 * 33];
-  const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, hh = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  int32_t tile = blockIdx.x;
-  // the segment that the tile belongs to, and the tile's place in it
-  int32_t s = -1;
-  for (int32_t c = 0; c < a.segments && s < 0; c += 64) {
-    int32_t mine = 0;
-    if (c + lane < a.segments) {
-      const Segment g = segment(a, c + lane);
-      mine = (g.end - g.first + kLowRows - 1) / kLowRows;
-    }
+// The segment that tile `tile` of `rows` rows belongs to (every segment has tiles
+// of its own, one after the other) and the tile's first row; adapter -1 where
+// the tile has nothing to do.
+struct LowTile {
+  int32_t first, end, adapter;
+};
+__device__ inline LowTile low_tile(const AdapterArgs& a, int32_t tile, int32_t rows) {
+  const int lane = threadIdx.x & 63;
+  for (int32_t c = 0; c < a.segments; c += 64) {
+    Segment g{0, 0, -1};
+    if (c + lane < a.segments) g = segment(a, c + lane);
+    const int32_t mine = (g.end - g.first + rows - 1) / rows;
     int32_t pre = mine;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
@@ -90,18 +83,28 @@ __global__ __launch_bounds__(NW * 64) void low_kernel(AdapterArgs a) {
     const uint64_t past = __ballot(pre > tile);
     if (past) {
       const int i = __builtin_ctzll(past);
-      s = c + i;
-      tile -= __shfl(pre, i) - __shfl(mine, i);
-    } else {
-      tile -= __shfl(pre, 63);
+      const int32_t at = tile - (__shfl(pre, i) - __shfl(mine, i)), first = __shfl(g.first, i) + at * rows, end = __shfl(g.end, i);
+      const bool ok = at >= 0 && first < end;
+      return {__builtin_amdgcn_readfirstlane(first), __builtin_amdgcn_readfirstlane(end),
+              __builtin_amdgcn_readfirstlane(ok ? __shfl(g.adapter, i) : -1)};
     }
+    tile -= __shfl(pre, 63);
   }
-  if (s < 0) return;
-  s = __builtin_amdgcn_readfirstlane(s);
-  tile = __builtin_amdgcn_readfirstlane(tile);
-  const Segment g = segment(a, s);
-  const int32_t row0 = g.first + tile * kLowRows;
-  if (g.adapter < 0 || tile < 0 || row0 >= g.end) return;
+  return {0, 0, -1};
+}
+
+// The low-rank factors of 32 rows of one segment: NT x 32 of the parts' rank
+// columns, which stand behind one another.  The block's waves share out the
+// contraction, and their sums meet in LDS, in a fixed order.  kWhole: rows of
+// whole, aligned 16-byte chunks.
+template <int NW, int NT, int kUnroll, bool kWhole>
+__global__ __launch_bounds__(NW * 64) void low_kernel(AdapterArgs a) {
+  __shared__ float sums[NW][32 * 33];
+  const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, hh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const LowTile g = low_tile(a, blockIdx.x, kLowRows);
+  if (g.adapter < 0) return;
+  const int32_t row0 = g.first;
   const int32_t row = row0 + n32;
   const __bf16* x = static_cast<const __bf16*>(a.x) + static_cast<int64_t>(row < g.end ? row : row0) * a.x_stride;
   const __bf16* A = static_cast<const __bf16*>(a.a) + static_cast<int64_t>(g.adapter) * a.parts * a.rank * a.K;
@@ -121,20 +124,23 @@ __global__ __launch_bounds__(NW * 64) void low_kernel(AdapterArgs a) {
   f32x16 acc[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) acc[t] = f32x16{};
+  const int steps = (a.K + 15) / 16, each = (steps + NW - 1) / NW, s0 = wave * each, s1 = min(s0 + each, steps);
 #pragma unroll 1
-  for (int k0 = wave * 16 * kUnroll; k0 < a.K; k0 += NW * 16 * kUnroll) {
+  for (int s = s0; s < s1; s += kUnroll) {
     bf16x8 xv[kUnroll], av[kUnroll][NT];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-      const int k = k0 + u * 16 + hh * 8;  // kWhole: a multiple of 64 values
+      const int k = min(s + u, s1 - 1) * 16 + hh * 8;
       xv[u] = get(x, k);
 #pragma unroll
       for (int t = 0; t < NT; ++t) av[u][t] = get(ar[t], k);
     }
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u)
+    for (int u = 0; u < kUnroll; ++u) {
 #pragma unroll
-      for (int t = 0; t < NT; ++t) acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av[u][t], xv[u], acc[t], 0, 0, 0);
+      for (int t = 0; t < NT; ++t)
+        if (s + u < s1) acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av[u][t], xv[u], acc[t], 0, 0, 0);
+    }
   }
   const float scale = a.scale ? a.scale[g.adapter] : 1.f;
   __bf16* out = static_cast<__bf16*>(a.low);
@@ -273,52 +279,158 @@ __global__ __launch_bounds__(kThreads) void any_kernel(AdapterArgs a) {
   }
 }
 
+// The same for many rows: 64 rows of one segment and NB x 32 rank columns a
+// block, two by two waves of 32 rows and NB x 16 columns.  The contraction comes
+// in 64-deep stages of 128-byte rows through four LDS buffers, three of them on
+// their way.  Bound by the latency of that chain and by X's bytes.
+constexpr int kLowTileRows = kLowManyRows, kLowStages = 4;
+
+template <int NB>
+__global__ __launch_bounds__(256) void low_tile_kernel(AdapterArgs a) {
+  constexpr int BN = NB * 32, kX = kLowTileRows * 128, kStage = kX + BN * 128, kMine = 2 + NB;  // kMine: a wave's transfers of a stage
+  __shared__ __attribute__((aligned(16))) char lds[kLowStages][kStage];
+  const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, q = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave & 1, wn = wave >> 1;
+  const int cols = a.parts * a.low_rank, across = (cols + BN - 1) / BN;
+  const int at = xcd_remap(blockIdx.x, gridDim.x), c0 = at % across * BN;
+  const LowTile g = low_tile(a, at / across, kLowTileRows);
+  if (g.adapter < 0) return;
+  const int32_t rows = min(g.end - g.first, kLowTileRows);
+
+  // A transfer: rows 8 i + lane / 8, physical chunk lane % 8 holding logical chunk unswz128(row, lane % 8).
+  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(&lds[0][0]));
+  const uint32_t xrb = static_cast<uint32_t>(a.x_stride) * 2;
+  const __bf16* X = static_cast<const __bf16*>(a.x) + static_cast<int64_t>(g.first) * a.x_stride;
+  const __bf16* A = static_cast<const __bf16*>(a.a) + static_cast<int64_t>(g.adapter) * a.parts * a.rank * a.K;
+  uint32_t xo[2];
+  const __bf16* ap[NB];  // columns past the ranks are read as others' and written as zeros
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int row = (wave * 2 + i) * 8 + (lane >> 3);
+    xo[i] = row * xrb + unswz128(row, lane & 7) * 16;
+  }
+#pragma unroll
+  for (int i = 0; i < NB; ++i) {
+    const int row = (wave * NB + i) * 8 + (lane >> 3), c = min(c0 + row, cols - 1), part = c / a.low_rank;
+    ap[i] = A + (static_cast<int64_t>(part) * a.rank + min(c - part * a.low_rank, a.rank - 1)) * a.K + unswz128(row, lane & 7) * 8;
+  }
+  auto put = [&](int st) {
+    const i32x4 rx = rsrc_of(X + st * 64, static_cast<uint32_t>(rows - 1) * xrb + 128);
+    const uint32_t base = lds0 + st % kLowStages * kStage;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) dma16(rx, xo[i], __builtin_amdgcn_readfirstlane(base + (wave * 2 + i) * 1024));
+#pragma unroll
+    for (int i = 0; i < NB; ++i) gdma16(ap[i] + st * 64, __builtin_amdgcn_readfirstlane(base + kX + (wave * NB + i) * 1024));
+  };
+  f32x4 acc[2][NB];
+#pragma unroll
+  for (int m = 0; m < 2; ++m)
+#pragma unroll
+    for (int b = 0; b < NB; ++b) acc[m][b] = f32x4{};
+  const int nst = a.K / 64;
+  for (int st = 0; st < kLowStages - 1 && st < nst; ++st) put(st);
+  for (int st = 0; st < nst; ++st) {
+    // this stage's transfers are done where no more than those of the later ones are left
+    if (st + 2 < nst)
+      wait_vmcnt<2 * kMine>();
+    else if (st + 1 < nst)
+      wait_vmcnt<kMine>();
+    else
+      wait_vmcnt<0>();
+    // the stage before has been read by all: its buffer is filled next
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    if (st + kLowStages - 1 < nst) put(st + kLowStages - 1);
+    const char* Xs = lds[st % kLowStages] + wm * 32 * 128;
+    const char* As = lds[st % kLowStages] + kX + wn * NB * 16 * 128;
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      bf16x8 xv[2], av[NB];
+#pragma unroll
+      for (int m = 0; m < 2; ++m) xv[m] = *reinterpret_cast<const bf16x8*>(Xs + swz128(m * 16 + n, ks * 32 + q * 8) * 2);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) av[b] = *reinterpret_cast<const bf16x8*>(As + swz128(b * 16 + n, ks * 32 + q * 8) * 2);
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int b = 0; b < NB; ++b) acc[m][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[b], xv[m], acc[m][b], 0, 0, 0);
+    }
+  }
+  // element e of acc[m][b]: row wm 32 + m 16 + n, column (wn NB + b) 16 + 4 q + e
+  const float scale = a.scale ? a.scale[g.adapter] : 1.f;
+#pragma unroll
+  for (int m = 0; m < 2; ++m) {
+    const int32_t row = wm * 32 + m * 16 + n;
+    if (row >= rows) continue;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const int c = c0 + (wn * NB + b) * 16 + 4 * q;
+      if (c >= cols) continue;
+      const int r = c % a.low_rank;  // four columns of one part
+      bf16x4 v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = static_cast<__bf16>(r + e < a.rank ? acc[m][b][e] * scale : 0.f);
+      *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(a.low) + static_cast<int64_t>(g.first + row) * cols + c) = v;
+    }
+  }
+}
+
 // ------------------------------------------------------------- few tokens
 // Up to 64 tokens: bound by the weights' bytes, each read once.  A block takes
-// 16 features, its waves share out the contraction, 256 values of it on their
-// way at once; W and X go from memory to the matrix cores' registers as they
-// lie.  The adapters' share is a dot product of `rank` values for each output.
-constexpr int kFewFeatures = 16, kFewWaves = 4;
+// 32 features, its eight waves share out the contraction; W and X go from
+// memory to the matrix cores' registers as they lie, kUnroll steps of 32 values
+// on their way at once.  The adapters' share is a dot product of `rank` values
+// for each output.
+constexpr int kFewFeatures = kAdapterFewFeatures, kFewWaves = 8;
 
-template <int RT>
+template <int RT, int kUnroll>
 __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(AdapterArgs a) {
-  constexpr int kUnroll = 8, kRows = RT * 16, kStr = kFewFeatures + 1;
+  constexpr int FT = kFewFeatures / 16, kRows = RT * 16, kStr = kFewFeatures + 1;
   __shared__ float sums[kFewWaves][kRows * kStr];
   __shared__ int32_t which[kRows];
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int32_t f0 = static_cast<int32_t>(blockIdx.x) * kFewFeatures;
-  const __bf16* w = static_cast<const __bf16*>(a.w) + static_cast<int64_t>(min(f0 + n, a.N - 1)) * a.K + g * 8;
-  const __bf16* x[RT];
+  const __bf16 *w[FT], *x[RT];
+#pragma unroll
+  for (int f = 0; f < FT; ++f) w[f] = static_cast<const __bf16*>(a.w) + static_cast<int64_t>(min(f0 + f * 16 + n, a.N - 1)) * a.K + g * 8;
 #pragma unroll
   for (int t = 0; t < RT; ++t) x[t] = static_cast<const __bf16*>(a.x) + min(t * 16 + n, a.M - 1) * a.x_stride + g * 8;
-  f32x4 acc[RT];
+  f32x4 acc[FT][RT];
 #pragma unroll
-  for (int t = 0; t < RT; ++t) acc[t] = f32x4{};
+  for (int f = 0; f < FT; ++f)
+#pragma unroll
+    for (int t = 0; t < RT; ++t) acc[f][t] = f32x4{};
+  const int steps = a.K / 32, each = (steps + kFewWaves - 1) / kFewWaves;  // K is a multiple of 32
+  const int s0 = wave * each, s1 = min(s0 + each, steps);
 #pragma unroll 1
-  for (int k0 = wave * 32 * kUnroll; k0 < a.K; k0 += kFewWaves * 32 * kUnroll) {
-    bf16x8 wv[kUnroll], xv[kUnroll][RT];
+  for (int s = s0; s < s1; s += kUnroll) {
+    bf16x8 wv[kUnroll][FT], xv[kUnroll][RT];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-      const int k = k0 + u * 32;  // K is a multiple of 32
-      wv[u] = bf16x8{};
-      if (k < a.K) wv[u] = __builtin_nontemporal_load(reinterpret_cast<const bf16x8*>(w + k));
+      const int k = min(s + u, s1 - 1) * 32;
 #pragma unroll
-      for (int t = 0; t < RT; ++t) {
-        xv[u][t] = bf16x8{};
-        if (k < a.K) xv[u][t] = *reinterpret_cast<const bf16x8*>(x[t] + k);
-      }
+      for (int f = 0; f < FT; ++f) wv[u][f] = __builtin_nontemporal_load(reinterpret_cast<const bf16x8*>(w[f] + k));
+#pragma unroll
+      for (int t = 0; t < RT; ++t) xv[u][t] = *reinterpret_cast<const bf16x8*>(x[t] + k);
     }
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u)
+    for (int u = 0; u < kUnroll; ++u) {
 #pragma unroll
-      for (int t = 0; t < RT; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[u], xv[u][t], acc[t], 0, 0, 0);
+      for (int f = 0; f < FT; ++f)
+#pragma unroll
+        for (int t = 0; t < RT; ++t)
+          if (s + u < s1) acc[f][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[u][f], xv[u][t], acc[f][t], 0, 0, 0);
+    }
   }
-  // element e of acc[t]: row 16 t + n, feature 4 g + e
+  // element e of acc[f][t]: row 16 t + n, feature 16 f + 4 g + e
 #pragma unroll
-  for (int t = 0; t < RT; ++t)
+  for (int f = 0; f < FT; ++f)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) sums[wave][(t * 16 + n) * kStr + 4 * g + e] = acc[t][e];
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sums[wave][(t * 16 + n) * kStr + f * 16 + 4 * g + e] = acc[f][t][e];
   for (int r = wave; r < kRows; r += kFewWaves) {
     int32_t j = -1;
     if (a.segments && r < a.M) {
@@ -332,7 +444,6 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(AdapterArgs a) {
   }
   __syncthreads();
   const __bf16* bias = static_cast<const __bf16*>(a.bias);
-#pragma unroll
   for (int i = tid; i < kRows * kFewFeatures; i += kFewWaves * 64) {
     const int r = i / kFewFeatures, f = f0 + i % kFewFeatures;
     if (r >= a.M || f >= a.N) continue;
@@ -572,37 +683,42 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2,
   }
 }
 
-template <int NW, bool kWhole>
-void low_launch(const AdapterArgs& a, const AdapterPlan& plan, hipStream_t stream) {
-  const int tiles = (a.parts * a.low_rank + 31) / 32;
-  const uint32_t rows = static_cast<uint32_t>(plan.low_blocks);
-  if (tiles == 1)
-    hipLaunchKernelGGL((low_kernel<NW, 1, kWhole>), dim3(rows), dim3(NW * 64), 0, stream, a);
-  else if (tiles == 2)
-    hipLaunchKernelGGL((low_kernel<NW, 2, kWhole>), dim3(rows), dim3(NW * 64), 0, stream, a);
-  else
-    hipLaunchKernelGGL((low_kernel<NW, 3, kWhole>), dim3(rows, (tiles + 2) / 3), dim3(NW * 64), 0, stream, a);
+hipError_t launch_low(const AdapterArgs& a, const AdapterPlan& plan, hipStream_t stream) {
+  const uint32_t tiles = static_cast<uint32_t>(plan.low_tiles), cols = static_cast<uint32_t>(a.parts * a.low_rank + 31) / 32;
+  if (plan.kernel == AdapterKernel::kAny) {
+    hipLaunchKernelGGL((low_kernel<4, 2, 2, false>), dim3(tiles, (cols + 1) / 2), dim3(4 * 64), 0, stream, a);
+  } else if (plan.low_rows == kLowRows) {
+    hipLaunchKernelGGL((low_kernel<16, 1, 10, true>), dim3(tiles, cols), dim3(16 * 64), 0, stream, a);
+  } else {
+    switch (cols) {
+      case 1:
+        hipLaunchKernelGGL((low_tile_kernel<1>), dim3(tiles), dim3(256), 0, stream, a);
+        break;
+      case 2:
+        hipLaunchKernelGGL((low_tile_kernel<2>), dim3(tiles), dim3(256), 0, stream, a);
+        break;
+      default:
+        hipLaunchKernelGGL((low_tile_kernel<3>), dim3(tiles * ((cols + 2) / 3)), dim3(256), 0, stream, a);
+    }
+  }
+  return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_adapter_project(const AdapterArgs& a, const AdapterPlan& plan, hipStream_t stream) {
-  if (plan.low_blocks) {
-    if (plan.low_waves == 16)
-      plan.kernel != AdapterKernel::kAny ? low_launch<16, true>(a, plan, stream) : low_launch<16, false>(a, plan, stream);
-    else
-      plan.kernel != AdapterKernel::kAny ? low_launch<4, true>(a, plan, stream) : low_launch<4, false>(a, plan, stream);
-    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  if (plan.low_tiles) {
+    if (const hipError_t e = launch_low(a, plan, stream); e != hipSuccess) return e;
   }
   const dim3 grid(static_cast<uint32_t>(plan.blocks));
   switch (plan.kernel) {
     case AdapterKernel::kFew:
       if (a.M <= 16)
-        hipLaunchKernelGGL(few_kernel<1>, grid, dim3(kFewWaves * 64), 0, stream, a);
+        hipLaunchKernelGGL((few_kernel<1, 10>), grid, dim3(kFewWaves * 64), 0, stream, a);
       else if (a.M <= 32)
-        hipLaunchKernelGGL(few_kernel<2>, grid, dim3(kFewWaves * 64), 0, stream, a);
+        hipLaunchKernelGGL((few_kernel<2, 6>), grid, dim3(kFewWaves * 64), 0, stream, a);
       else
-        hipLaunchKernelGGL(few_kernel<4>, grid, dim3(kFewWaves * 64), 0, stream, a);
+        hipLaunchKernelGGL((few_kernel<4, 4>), grid, dim3(kFewWaves * 64), 0, stream, a);
       break;
     case AdapterKernel::kSmallTiles:
       hipLaunchKernelGGL((tile_kernel<2, 2, 2, 2>), grid, dim3(256), 0, stream, a);

@@ -182,13 +182,13 @@ struct AdapterArgs {
 // Which kernel makes a product: the one for few tokens, one of two tile sizes,
 // or the one for any sizes, strides and alignments.
 enum class AdapterKernel { kFew, kSmallTiles, kLargeTiles, kAny };
-constexpr int kAdapterFewTokens = 64, kAdapterFewFeatures = 16;
+constexpr int kAdapterFewTokens = 64, kAdapterFewFeatures = 32;
 
-constexpr int kLowRows = 32;  // rows of a tile of the low-rank factor
+constexpr int kLowRows = 32, kLowManyRows = 64;  // rows of a tile of the low-rank factor
 struct AdapterPlan {
   AdapterKernel kernel;
-  int32_t low_waves;   // of a block of the low-rank factor's launch
-  int64_t low_blocks;  // row tiles of the low-rank factor's launch, 0: none
+  int32_t low_rows;   // of a tile of the low-rank factor's launch
+  int64_t low_tiles;  // its row tiles, 0: none
   int64_t blocks;      // of the product
   int64_t workspace_bytes;
   int32_t low_rank;    // rank rounded up to whole 16 values

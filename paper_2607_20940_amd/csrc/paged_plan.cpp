@@ -51,13 +51,14 @@ hipError_t plan_adapter_project(int64_t rows, int32_t out_features, int32_t part
       p.kernel = AdapterKernel::kSmallTiles;
     }
   }
-  if (!launchable(p.blocks, p.kernel == AdapterKernel::kLargeTiles ? 512 : 256)) return hipErrorInvalidValue;
+  if (!launchable(p.blocks, p.kernel == AdapterKernel::kLargeTiles || p.kernel == AdapterKernel::kFew ? 512 : 256)) return hipErrorInvalidValue;
   if (segments > 0 && adapters > 0) {
     p.low_rank = (rank + 15) / 16 * 16;
+    // tiles of 64 rows where each is nearly full and there are some for most CUs
+    p.low_rows = p.kernel != AdapterKernel::kAny && rows > 4096 && rows / segments >= kLowManyRows ? kLowManyRows : kLowRows;
     // every segment's tiles: whole ones, and one that is not full
-    p.low_blocks = std::min<int64_t>(rows, segments + rows / kLowRows);
-    p.low_waves = p.low_blocks <= 128 ? 16 : 4;
-    if (!launchable(p.low_blocks, p.low_waves * 64)) return hipErrorInvalidValue;
+    p.low_tiles = std::min<int64_t>(rows, segments + rows / p.low_rows);
+    if (!launchable(p.low_tiles * ((int64_t{parts} * p.low_rank + 31) / 32), 1024)) return hipErrorInvalidValue;
     p.workspace_bytes = rows * parts * p.low_rank * 2;
   }
   *plan = p;
