@@ -15,6 +15,7 @@
 #include "lowbit_values.hpp"
 #include "paged_args.hpp"
 #include "xcd.hpp"
+#include "zero_row.hpp"
 
 namespace mssa {
 namespace {
@@ -93,190 +94,56 @@ __device__ inline LowTile low_tile(const AdapterArgs& a, int32_t tile, int32_t r
   return {0, 0, -1};
 }
 
-// The low-rank factors of 32 rows of one segment: NT x 32 of the parts' rank
-// columns, which stand behind one another.  The block's waves share out the
-// contraction, and their sums meet in LDS, in a fixed order.  kWhole: rows of
-// whole, aligned 16-byte chunks.
-template <int NW, int NT, int kUnroll, bool kWhole>
-__global__ __launch_bounds__(NW * 64) void low_kernel(AdapterArgs a) {
-  __shared__ float sums[NW][32 * 33];
-  const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, hh = lane >> 5;
+// The low-rank factors of 16 rows of one segment, 16 of the parts' rank columns,
+// which stand behind one another.  The block's 16 waves share out the
+// contraction, 320 values each on their way at once, and their sums meet in LDS,
+// in a fixed order.  kWhole: rows of whole, aligned 16-byte chunks.
+constexpr int kLowWaves = 16;
+
+template <bool kWhole>
+__global__ __launch_bounds__(kLowWaves * 64) void low_kernel(AdapterArgs a) {
+  constexpr int kUnroll = 10;
+  __shared__ float sums[kLowWaves][16 * 17];
+  const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, q = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const LowTile g = low_tile(a, blockIdx.x, kLowRows);
   if (g.adapter < 0) return;
-  const int32_t row0 = g.first;
-  const int32_t row = row0 + n32;
-  const __bf16* x = static_cast<const __bf16*>(a.x) + static_cast<int64_t>(row < g.end ? row : row0) * a.x_stride;
-  const __bf16* A = static_cast<const __bf16*>(a.a) + static_cast<int64_t>(g.adapter) * a.parts * a.rank * a.K;
-  const int cols = a.parts * a.low_rank, c0 = blockIdx.y * NT * 32;
-  const __bf16* ar[NT];
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {  // columns past the ranks are read as others' and written as zeros
-    const int c = min(c0 + t * 32 + n32, cols - 1), part = c / a.low_rank, r = min(c - part * a.low_rank, a.rank - 1);
-    ar[t] = A + (static_cast<int64_t>(part) * a.rank + r) * a.K;
-  }
-  auto get = [&](const __bf16* p, int at) -> bf16x8 {
-    if constexpr (kWhole)
-      return *reinterpret_cast<const bf16x8*>(p + at);
-    else
-      return eight(p + at, a.K - at);
+  const int32_t row = min(g.first + n, g.end - 1);
+  const int cols = a.parts * a.low_rank, c0 = blockIdx.y * 16;  // columns of one part
+  const int part = c0 / a.low_rank, r = min(c0 + n - part * a.low_rank, a.rank - 1);
+  const __bf16* x = static_cast<const __bf16*>(a.x) + static_cast<int64_t>(row) * a.x_stride + q * 8;
+  const __bf16* A = static_cast<const __bf16*>(a.a) + ((static_cast<int64_t>(g.adapter) * a.parts + part) * a.rank + r) * a.K + q * 8;
+  auto get = [&](const __bf16* p, int k) -> bf16x8 {
+    if constexpr (!kWhole) return eight(p + k, a.K - k - q * 8);
+    return k + q * 8 < a.K ? *reinterpret_cast<const bf16x8*>(p + k) : bf16x8{};
   };
-  f32x16 acc[NT];
-#pragma unroll
-  for (int t = 0; t < NT; ++t) acc[t] = f32x16{};
-  const int steps = (a.K + 15) / 16, each = (steps + NW - 1) / NW, s0 = wave * each, s1 = min(s0 + each, steps);
+  f32x4 acc = f32x4{};
+  const int steps = (a.K + 31) / 32, each = (steps + kLowWaves - 1) / kLowWaves, s0 = wave * each, s1 = min(s0 + each, steps);
 #pragma unroll 1
   for (int s = s0; s < s1; s += kUnroll) {
-    bf16x8 xv[kUnroll], av[kUnroll][NT];
+    bf16x8 xv[kUnroll], av[kUnroll];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-      const int k = min(s + u, s1 - 1) * 16 + hh * 8;
+      const int k = min(s + u, s1 - 1) * 32;
+      av[u] = get(A, k);
       xv[u] = get(x, k);
-#pragma unroll
-      for (int t = 0; t < NT; ++t) av[u][t] = get(ar[t], k);
     }
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-        if (s + u < s1) acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av[u][t], xv[u], acc[t], 0, 0, 0);
-    }
+    for (int u = 0; u < kUnroll; ++u)
+      if (s + u < s1) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[u], xv[u], acc, 0, 0, 0);
   }
-  const float scale = a.scale ? a.scale[g.adapter] : 1.f;
-  __bf16* out = static_cast<__bf16*>(a.low);
 #pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    if (t > 0) __syncthreads();
-#pragma unroll
-    for (int e = 0; e < 16; ++e) sums[wave][n32 * 33 + 8 * (e >> 2) + 4 * hh + (e & 3)] = acc[t][e];
-    __syncthreads();
-    for (int i = tid; i < 32 * 32; i += NW * 64) {
-      const int q = i >> 5, c = c0 + t * 32 + (i & 31), at = q * 33 + (i & 31);
-      if (row0 + q >= g.end || c >= cols) continue;
-      float u = 0.f;
-#pragma unroll
-      for (int w = 0; w < NW; ++w) u += sums[w][at];
-      out[static_cast<int64_t>(row0 + q) * cols + c] = static_cast<__bf16>(c % a.low_rank < a.rank ? u * scale : 0.f);
-    }
-  }
-}
-
-// The product in 128 x 128 tiles, a wave 64 x 64 of it (A = W rows, B = X rows,
-// so that a lane holds one row's sums), the contraction in 32-deep stages
-// through registers and LDS.  Any sizes, strides and alignments.
-constexpr int kGM = 128, kGN = 128, kGK = 32, kGStr = kGK + 8;  // LDS row stride: conflict-free 16-byte reads
-
-__global__ __launch_bounds__(kThreads) void any_kernel(AdapterArgs a) {
-  __shared__ __attribute__((aligned(16))) __bf16 lds[2][2][kGM * kGStr];  // [stage][X | W]
-  const int tiles_m = (a.M + kGM - 1) / kGM;
-  const int tm = blockIdx.x % tiles_m, tn = blockIdx.x / tiles_m;
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wm = wave & 1, wn = wave >> 1;
-  const int n32 = lane & 31, hh = lane >> 5;
-  const int32_t m0 = tm * kGM, m1 = min(m0 + kGM, a.M), f0 = tn * kGN, f1 = min(f0 + kGN, a.N);
-
-  // Stage loads: 128 rows x 4 pieces of 8 values per matrix, 2 pieces per thread.
-  const int lr = tid >> 2, lc = (tid & 3) * 8;
-  bf16x8 px[2], pw[2];
-  auto load = [&](const __bf16* x, int64_t xs, int32_t xa, int32_t xb, const __bf16* w, int64_t ws, int32_t wa, int32_t wb, int left) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int32_t xr = m0 + lr + i * 64, wr = f0 + lr + i * 64;
-      px[i] = xr >= xa && xr < xb ? eight(x + xr * xs + lc, left - lc) : bf16x8{};
-      pw[i] = wr >= wa && wr < wb ? eight(w + wr * ws + lc, left - lc) : bf16x8{};
-    }
-  };
-  auto store = [&](int s) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int r = lr + i * 64;
-      *reinterpret_cast<bf16x8*>(&lds[s][0][r * kGStr + lc]) = px[i];
-      *reinterpret_cast<bf16x8*>(&lds[s][1][r * kGStr + lc]) = pw[i];
-    }
-  };
-  auto operand = [&](int s, int which, int block, int ks) {
-    return *reinterpret_cast<const bf16x8*>(&lds[s][which][((which ? wn : wm) * 64 + block * 32 + n32) * kGStr + ks * 16 + hh * 8]);
-  };
-
-  f32x16 acc[2][2];
-#pragma unroll
-  for (int rb = 0; rb < 2; ++rb)
-#pragma unroll
-    for (int cb = 0; cb < 2; ++cb) acc[rb][cb] = f32x16{};
-
-  const __bf16* X = static_cast<const __bf16*>(a.x);
-  const __bf16* W = static_cast<const __bf16*>(a.w);
-  const int nst = (a.K + kGK - 1) / kGK;
-  auto load_stage = [&](int st) { load(X + st * kGK, a.x_stride, m0, m1, W + st * kGK, a.K, f0, f1, a.K - st * kGK); };
-  load_stage(0);
-  store(0);
+  for (int e = 0; e < 4; ++e) sums[wave][n * 17 + 4 * q + e] = acc[e];
   __syncthreads();
-  for (int st = 0; st < nst; ++st) {
-    if (st + 1 < nst) load_stage(st + 1);
+  const int at = tid >> 4, c = tid & 15;
+  if (tid >= 256 || g.first + at >= g.end) return;
+  float u = 0.f;
 #pragma unroll
-    for (int ks = 0; ks < kGK / 16; ++ks)
-#pragma unroll
-      for (int rb = 0; rb < 2; ++rb)
-#pragma unroll
-        for (int cb = 0; cb < 2; ++cb)
-          acc[rb][cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand(st & 1, 1, cb, ks), operand(st & 1, 0, rb, ks), acc[rb][cb], 0, 0, 0);
-    if (st + 1 < nst) store((st + 1) & 1);
-    __syncthreads();
-  }
-
-  // Element e of acc[rb][cb]: row wm 64 + rb 32 + n32, feature wn 64 + cb 32 + 8 (e / 4) + 4 hh + e % 4 of the tile.
-  const int p0 = f0 / a.split, p1 = (f1 - 1) / a.split;
-  for (int32_t s = __builtin_amdgcn_readfirstlane(first_segment(a, m0)); s < a.segments; ++s) {
-    const Segment g = segment(a, s);
-    if (g.first >= m1) break;
-    if (g.adapter < 0 || g.first >= g.end) continue;
-    for (int p = p0; p <= p1; ++p) {
-      const __bf16* u = static_cast<const __bf16*>(a.low) + p * a.low_rank;
-      const __bf16* B = static_cast<const __bf16*>(a.b) + static_cast<int64_t>(g.adapter) * a.N * a.rank;
-      const int32_t fa = p * a.split, fb = fa + a.split;
-      for (int r0 = 0; r0 < a.rank; r0 += kGK) {
-        load(u + r0, static_cast<int64_t>(a.parts) * a.low_rank, g.first, g.end, B + r0, a.rank, fa, min(fb, f1), a.rank - r0);
-        store(0);
-        __syncthreads();
-#pragma unroll
-        for (int rb = 0; rb < 2; ++rb) {
-          const int32_t row = m0 + wm * 64 + rb * 32 + n32;
-          const bool mine = row >= g.first && row < g.end;
-#pragma unroll
-          for (int cb = 0; cb < 2; ++cb) {
-            f32x16 add = f32x16{};
-#pragma unroll
-            for (int ks = 0; ks < kGK / 16; ++ks)
-              add = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand(0, 1, cb, ks), operand(0, 0, rb, ks), add, 0, 0, 0);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const int32_t f = f0 + wn * 64 + cb * 32 + 8 * (e >> 2) + 4 * hh + (e & 3);
-              acc[rb][cb][e] += mine && f >= fa && f < fb ? add[e] : 0.f;
-            }
-          }
-        }
-        __syncthreads();
-      }
-    }
-  }
-
-  const __bf16* bias = static_cast<const __bf16*>(a.bias);
-#pragma unroll
-  for (int rb = 0; rb < 2; ++rb) {
-    const int32_t row = m0 + wm * 64 + rb * 32 + n32;
-    if (row >= m1) continue;
-#pragma unroll
-    for (int cb = 0; cb < 2; ++cb)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int32_t f = f0 + wn * 64 + cb * 32 + 8 * (e >> 2) + 4 * hh + (e & 3);
-        if (f >= f1) continue;
-        const int part = f / a.split;
-        const float v = (acc[rb][cb][e] + (bias ? static_cast<float>(bias[f]) : 0.f)) * (part == 0 ? a.part0_scale : 1.f);
-        static_cast<__bf16*>(a.y[part])[static_cast<int64_t>(row) * a.split + (f - part * a.split)] = static_cast<__bf16>(v);
-      }
-  }
+  for (int w = 0; w < kLowWaves; ++w) u += sums[w][at * 17 + c];
+  const float scale = a.scale ? a.scale[g.adapter] : 1.f;
+  // ranks are rounded up with zeros
+  static_cast<__bf16*>(a.low)[static_cast<int64_t>(g.first + at) * cols + c0 + c] =
+      static_cast<__bf16>(c0 + c - part * a.low_rank < a.rank ? u * scale : 0.f);
 }
 
 // The same for many rows: 64 rows of one segment and NB x 32 rank columns a
@@ -303,31 +170,35 @@ __global__ __launch_bounds__(256) void low_tile_kernel(AdapterArgs a) {
   const __bf16* X = static_cast<const __bf16*>(a.x) + static_cast<int64_t>(g.first) * a.x_stride;
   const __bf16* A = static_cast<const __bf16*>(a.a) + static_cast<int64_t>(g.adapter) * a.parts * a.rank * a.K;
   uint32_t xo[2];
+  int xc[2], ac[NB];     // logical chunks
   const __bf16* ap[NB];  // columns past the ranks are read as others' and written as zeros
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const int row = (wave * 2 + i) * 8 + (lane >> 3);
-    xo[i] = row * xrb + unswz128(row, lane & 7) * 16;
+    xc[i] = unswz128(row, lane & 7);
+    xo[i] = row * xrb + xc[i] * 16;
   }
 #pragma unroll
   for (int i = 0; i < NB; ++i) {
     const int row = (wave * NB + i) * 8 + (lane >> 3), c = min(c0 + row, cols - 1), part = c / a.low_rank;
-    ap[i] = A + (static_cast<int64_t>(part) * a.rank + min(c - part * a.low_rank, a.rank - 1)) * a.K + unswz128(row, lane & 7) * 8;
+    ac[i] = unswz128(row, lane & 7);
+    ap[i] = A + (static_cast<int64_t>(part) * a.rank + min(c - part * a.low_rank, a.rank - 1)) * a.K + ac[i] * 8;
   }
   auto put = [&](int st) {
-    const i32x4 rx = rsrc_of(X + st * 64, static_cast<uint32_t>(rows - 1) * xrb + 128);
+    const int left = min(a.K - st * 64, 64);  // a multiple of 8; zeros past it
+    const i32x4 rx = rsrc_of(X + st * 64, static_cast<uint32_t>(rows - 1) * xrb + left * 2);
     const uint32_t base = lds0 + st % kLowStages * kStage;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) dma16(rx, xo[i], __builtin_amdgcn_readfirstlane(base + (wave * 2 + i) * 1024));
+    for (int i = 0; i < 2; ++i) dma16(rx, xc[i] * 8 < left ? xo[i] : kPastEnd, __builtin_amdgcn_readfirstlane(base + (wave * 2 + i) * 1024));
 #pragma unroll
-    for (int i = 0; i < NB; ++i) gdma16(ap[i] + st * 64, __builtin_amdgcn_readfirstlane(base + kX + (wave * NB + i) * 1024));
+    for (int i = 0; i < NB; ++i) gdma16(ac[i] * 8 < left ? static_cast<const void*>(ap[i] + st * 64) : zero_row, __builtin_amdgcn_readfirstlane(base + kX + (wave * NB + i) * 1024));
   };
   f32x4 acc[2][NB];
 #pragma unroll
   for (int m = 0; m < 2; ++m)
 #pragma unroll
     for (int b = 0; b < NB; ++b) acc[m][b] = f32x4{};
-  const int nst = a.K / 64;
+  const int nst = (a.K + 63) / 64;
   for (int st = 0; st < kLowStages - 1 && st < nst; ++st) put(st);
   for (int st = 0; st < nst; ++st) {
     // this stage's transfers are done where no more than those of the later ones are left
@@ -381,10 +252,10 @@ __global__ __launch_bounds__(256) void low_tile_kernel(AdapterArgs a) {
 // 32 features, its eight waves share out the contraction; W and X go from
 // memory to the matrix cores' registers as they lie, kUnroll steps of 32 values
 // on their way at once.  The adapters' share is a dot product of `rank` values
-// for each output.
+// for each output.  kWhole: rows of whole, aligned 16-byte chunks.
 constexpr int kFewFeatures = kAdapterFewFeatures, kFewWaves = 8;
 
-template <int RT, int kUnroll>
+template <int RT, int kUnroll, bool kWhole>
 __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(AdapterArgs a) {
   constexpr int FT = kFewFeatures / 16, kRows = RT * 16, kStr = kFewFeatures + 1;
   __shared__ float sums[kFewWaves][kRows * kStr];
@@ -392,6 +263,13 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(AdapterArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int32_t f0 = static_cast<int32_t>(blockIdx.x) * kFewFeatures;
+  // a thread's segments write their adapter to their rows (a row is in one segment)
+  if (tid < kRows) which[tid] = -1;
+  __syncthreads();
+  for (int32_t s = tid; s < a.segments; s += kFewWaves * 64) {
+    const Segment sg = segment(a, s);
+    for (int32_t r = sg.first; r < sg.end; ++r) which[r] = sg.adapter;
+  }
   const __bf16 *w[FT], *x[RT];
 #pragma unroll
   for (int f = 0; f < FT; ++f) w[f] = static_cast<const __bf16*>(a.w) + static_cast<int64_t>(min(f0 + f * 16 + n, a.N - 1)) * a.K + g * 8;
@@ -402,7 +280,12 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(AdapterArgs a) {
   for (int f = 0; f < FT; ++f)
 #pragma unroll
     for (int t = 0; t < RT; ++t) acc[f][t] = f32x4{};
-  const int steps = a.K / 32, each = (steps + kFewWaves - 1) / kFewWaves;  // K is a multiple of 32
+  auto get = [&](const __bf16* p, int k) -> bf16x8 {
+    if constexpr (!kWhole) return eight(p + k, a.K - k - g * 8);
+    // the last step's chunks past the row
+    return k + g * 8 < a.K ? *reinterpret_cast<const bf16x8*>(p + k) : bf16x8{};
+  };
+  const int steps = (a.K + 31) / 32, each = (steps + kFewWaves - 1) / kFewWaves;
   const int s0 = wave * each, s1 = min(s0 + each, steps);
 #pragma unroll 1
   for (int s = s0; s < s1; s += kUnroll) {
@@ -411,9 +294,9 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(AdapterArgs a) {
     for (int u = 0; u < kUnroll; ++u) {
       const int k = min(s + u, s1 - 1) * 32;
 #pragma unroll
-      for (int f = 0; f < FT; ++f) wv[u][f] = __builtin_nontemporal_load(reinterpret_cast<const bf16x8*>(w[f] + k));
+      for (int f = 0; f < FT; ++f) wv[u][f] = get(w[f], k);
 #pragma unroll
-      for (int t = 0; t < RT; ++t) xv[u][t] = *reinterpret_cast<const bf16x8*>(x[t] + k);
+      for (int t = 0; t < RT; ++t) xv[u][t] = get(x[t], k);
     }
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
@@ -431,17 +314,6 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(AdapterArgs a) {
     for (int t = 0; t < RT; ++t)
 #pragma unroll
       for (int e = 0; e < 4; ++e) sums[wave][(t * 16 + n) * kStr + f * 16 + 4 * g + e] = acc[f][t][e];
-  for (int r = wave; r < kRows; r += kFewWaves) {
-    int32_t j = -1;
-    if (a.segments && r < a.M) {
-      const int32_t s = first_segment(a, r);
-      if (s < a.segments) {
-        const Segment sg = segment(a, s);
-        if (sg.first <= r && r < sg.end) j = sg.adapter;
-      }
-    }
-    if (lane == 0) which[r] = j;
-  }
   __syncthreads();
   const __bf16* bias = static_cast<const __bf16*>(a.bias);
   for (int i = tid; i < kRows * kFewFeatures; i += kFewWaves * 64) {
@@ -456,7 +328,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(AdapterArgs a) {
       const __bf16* b = static_cast<const __bf16*>(a.b) + (static_cast<int64_t>(j) * a.N + f) * a.rank;
       float d = 0.f;
       for (int q = 0; q < a.rank; q += 8) {
-        const bf16x8 uv = *reinterpret_cast<const bf16x8*>(u + q), bv = *reinterpret_cast<const bf16x8*>(b + q);
+        const bf16x8 uv = *reinterpret_cast<const bf16x8*>(u + q), bv = eight(b + q, a.rank - q);
 #pragma unroll
         for (int e = 0; e < 8; ++e) d = __builtin_fmaf(static_cast<float>(uv[e]), static_cast<float>(bv[e]), d);
       }
@@ -484,6 +356,7 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2,
   constexpr int kX = BM * 128, kW = BN * 128, kStage = kX + kW;  // bytes
   constexpr int TX = BM / 8 / NW, TW = BN / 8 / NW;              // transfers (8 rows) of a wave
   __shared__ __attribute__((aligned(16))) char lds[2][kStage];
+  __shared__ float biases[BN];
   const int tiles_m = (a.M + BM - 1) / BM, tiles_n = (a.N + BN - 1) / BN;
   const int t = xcd_remap(blockIdx.x, tiles_m * tiles_n);
   const int panel = t / (tiles_m * kPanel), pw = min(kPanel, tiles_n - panel * kPanel);
@@ -515,8 +388,11 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2,
   const __bf16* X = static_cast<const __bf16*>(a.x) + static_cast<int64_t>(m0) * a.x_stride;
   const __bf16* W = static_cast<const __bf16*>(a.w) + static_cast<int64_t>(f0) * a.K;
   const uint32_t xrb = static_cast<uint32_t>(a.x_stride) * 2, wrb = static_cast<uint32_t>(a.K) * 2;
-  const uint32_t xbytes = static_cast<uint32_t>(m1 - m0 - 1) * xrb + kBK * 2, wbytes = static_cast<uint32_t>(f1 - f0 - 1) * wrb + kBK * 2;
-  auto put_main = [&](int st) { put(st & 1, X + st * kBK, xrb, xbytes, W + st * kBK, wrb, wbytes, 8); };
+  auto put_main = [&](int st) {
+    const int left = min(a.K - st * kBK, kBK);  // a multiple of 8
+    put(st & 1, X + st * kBK, xrb, static_cast<uint32_t>(m1 - m0 - 1) * xrb + left * 2, W + st * kBK, wrb,
+        static_cast<uint32_t>(f1 - f0 - 1) * wrb + left * 2, left / 8);
+  };
   put_main(0);
 
   // The adapters' stages, found one after the other: a segment with an adapter
@@ -547,9 +423,28 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2,
   auto put_low = [&](int buf) {
     const __bf16* u = static_cast<const __bf16*>(a.low) + static_cast<int64_t>(m0) * a.parts * a.low_rank + next.part * a.low_rank + next.r0;
     const __bf16* b = static_cast<const __bf16*>(a.b) + (static_cast<int64_t>(next.adapter) * a.N + f0) * a.rank + next.r0;
-    const int left = min(a.rank - next.r0, kBK);  // a multiple of 8
-    put(buf, u, urb, static_cast<uint32_t>(m1 - m0 - 1) * urb + left * 2, b, brb, static_cast<uint32_t>(f1 - f0 - 1) * brb + left * 2, left / 8);
+    const int left = min(a.rank - next.r0, kBK), chunks = (left + 7) / 8;
+    const uint32_t ubytes = static_cast<uint32_t>(m1 - m0 - 1) * urb + chunks * 16;
+    if (a.whole_b) {
+      put(buf, u, urb, ubytes, b, brb, static_cast<uint32_t>(f1 - f0 - 1) * brb + left * 2, chunks);
+    } else {
+      // rows that are not whole aligned chunks: through registers
+      const i32x4 ru = rsrc_of(u, ubytes);
+#pragma unroll
+      for (int i = 0; i < TX; ++i) {
+        const int row = (wave * TX + i) * 8 + (lane >> 3), lc = unswz128(row, lane & 7);
+        dma16(ru, lc < chunks ? row * urb + lc * 16 : kPastEnd,
+              __builtin_amdgcn_readfirstlane(lds0 + buf * kStage + (wave * TX + i) * 1024));
+      }
+      for (int c = tid; c < BN * 8; c += NW * 64) {
+        const int row = c >> 3, chunk = c & 7;
+        const int n = f0 + row < f1 ? left - chunk * 8 : 0;
+        *reinterpret_cast<bf16x8*>(lds[buf] + kX + swz128(row, chunk * 8) * 2) = eight(b + static_cast<int64_t>(row) * a.rank + chunk * 8, n);
+      }
+    }
   };
+  const __bf16* bias = static_cast<const __bf16*>(a.bias);
+  if (tid < BN) biases[tid] = bias && f0 + tid < a.N ? static_cast<float>(bias[f0 + tid]) : 0.f;
   next.first = m1;
   if (a.segments) to_segment(__builtin_amdgcn_readfirstlane(first_segment(a, m0)));
 
@@ -564,7 +459,7 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2,
 #pragma unroll
   for (int ks = 0; ks < kBK / 16; ++ks) rd[ks] = swz128(n32, ks * 16 + hh * 8) * 2;
 
-  const int nst = a.K / kBK;
+  const int nst = (a.K + kBK - 1) / kBK;
   for (int st = 0; st < nst; ++st) {
     wait_vmcnt<0>();
     __syncthreads();
@@ -592,8 +487,12 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2,
         acc[mb][nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[c][nb], op[c][NB + mb], acc[mb][nb], 0, 0, 0);
         if (ks + 1 < kBK / 16 && i < NB + MB) op[c ^ 1][i] = rd_op(ks + 1, i);
       }
+      if constexpr (MB * NB < NB + MB)
+#pragma unroll
+        for (int j = MB * NB; j < NB + MB; ++j)
+          if (ks + 1 < kBK / 16) op[c ^ 1][j] = rd_op(ks + 1, j);
     }
-    static_assert(MB * NB >= NB + MB, "a read after every matrix instruction");
+    if constexpr (MB * NB < NB + MB) continue;  // fewer matrix instructions than reads: the compiler's order
 #pragma unroll
     for (int j = 0; j < NB + MB; ++j) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
 #pragma unroll
@@ -646,7 +545,6 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2,
   constexpr int kEStr = BN + 8, kERows = MB * 32;
   static_assert(kERows * kEStr * 2 <= static_cast<int>(sizeof(lds)), "a wave row's outputs fit the stage buffers");
   __bf16* E = reinterpret_cast<__bf16*>(&lds[0][0]);
-  const __bf16* bias = static_cast<const __bf16*>(a.bias);
 #pragma unroll 1
   for (int part_m = 0; part_m < WM; ++part_m) {
     __syncthreads();  // the stage buffers, or the rows before, are free
@@ -657,14 +555,17 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2,
         for (int jj = 0; jj < 4; ++jj) {
           const int at = (wn * NB + nb) * 32 + 8 * jj + 4 * hh;
           const int32_t f = f0 + at;
-          bf16x4 bv = {};
-          if (bias && f < a.N) bv = *reinterpret_cast<const bf16x4*>(bias + f);
-          const float factor = f < a.split ? a.part0_scale : 1.f;
+          float bv[4], factor[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            bv[i] = biases[at + i];
+            factor[i] = f + i < a.split ? a.part0_scale : 1.f;
+          }
 #pragma unroll
           for (int mb = 0; mb < MB; ++mb) {
             bf16x4 v;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = static_cast<__bf16>((acc[mb][nb][4 * jj + i] + static_cast<float>(bv[i])) * factor);
+            for (int i = 0; i < 4; ++i) v[i] = static_cast<__bf16>((acc[mb][nb][4 * jj + i] + bv[i]) * factor[i]);
             *reinterpret_cast<bf16x4*>(E + (mb * 32 + n32) * kEStr + at) = v;
           }
         }
@@ -674,23 +575,161 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2,
     for (int p = 0; p < kERows * BN / 8 / (NW * 64); ++p) {
       const int c = p * NW * 64 + tid, rt = c / (BN / 8), ch = c % (BN / 8);
       const int32_t row = m0 + part_m * kERows + rt, f = f0 + ch * 8;
-      if (row < m1 && f < a.N) {
+      if (row >= m1 || f >= a.N) continue;
+      const bf16x8 v = *reinterpret_cast<const bf16x8*>(E + rt * kEStr + ch * 8);
+      if (a.whole_y) {
         const int part = f / a.split;  // 8 features never straddle a part (split % 8 == 0)
-        *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(a.y[part]) + static_cast<int64_t>(row) * a.split + (f - part * a.split)) =
-            *reinterpret_cast<const bf16x8*>(E + rt * kEStr + ch * 8);
+        *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(a.y[part]) + static_cast<int64_t>(row) * a.split + (f - part * a.split)) = v;
+      } else {
+        for (int i = 0; i < 8 && f + i < a.N; ++i) {
+          const int part = (f + i) / a.split;
+          static_cast<__bf16*>(a.y[part])[static_cast<int64_t>(row) * a.split + (f + i - part * a.split)] = v[i];
+        }
       }
     }
   }
 }
 
+// ------------------------------------------------------------ any alignment
+// Tiles of MB x 64 rows and as many features, a wave half by half of it, the
+// contraction in 32-deep stages through registers and LDS: rows that begin
+// anywhere.
+constexpr int kGK = 32, kGStr = kGK + 8;  // LDS row stride: conflict-free 16-byte reads
+
+template <int MB>
+__global__ __launch_bounds__(kThreads) void any_kernel(AdapterArgs a) {
+  constexpr int kGM = MB * 64, kGN = kGM;
+  __shared__ __attribute__((aligned(16))) __bf16 lds[2][2][kGM * kGStr];  // [stage][X | W]
+  const int tiles_m = (a.M + kGM - 1) / kGM;
+  const int tm = blockIdx.x % tiles_m, tn = blockIdx.x / tiles_m;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave & 1, wn = wave >> 1;
+  const int n32 = lane & 31, hh = lane >> 5;
+  const int32_t m0 = tm * kGM, m1 = min(m0 + kGM, a.M), f0 = tn * kGN, f1 = min(f0 + kGN, a.N);
+
+  // Stage loads: kGM rows x 4 pieces of 8 values per matrix, MB pieces per thread.
+  const int lr = tid >> 2, lc = (tid & 3) * 8;
+  bf16x8 px[MB], pw[MB];
+  auto load = [&](const __bf16* x, int64_t xs, int32_t xa, int32_t xb, const __bf16* w, int64_t ws, int32_t wa, int32_t wb, int left) {
+#pragma unroll
+    for (int i = 0; i < MB; ++i) {
+      const int32_t xr = m0 + lr + i * 64, wr = f0 + lr + i * 64;
+      px[i] = xr >= xa && xr < xb ? eight(x + xr * xs + lc, left - lc) : bf16x8{};
+      pw[i] = wr >= wa && wr < wb ? eight(w + wr * ws + lc, left - lc) : bf16x8{};
+    }
+  };
+  auto store = [&](int s) {
+#pragma unroll
+    for (int i = 0; i < MB; ++i) {
+      const int r = lr + i * 64;
+      *reinterpret_cast<bf16x8*>(&lds[s][0][r * kGStr + lc]) = px[i];
+      *reinterpret_cast<bf16x8*>(&lds[s][1][r * kGStr + lc]) = pw[i];
+    }
+  };
+  auto operand = [&](int s, int which, int block, int ks) {
+    return *reinterpret_cast<const bf16x8*>(&lds[s][which][((which ? wn : wm) * MB * 32 + block * 32 + n32) * kGStr + ks * 16 + hh * 8]);
+  };
+
+  f32x16 acc[MB][MB];
+#pragma unroll
+  for (int rb = 0; rb < MB; ++rb)
+#pragma unroll
+    for (int cb = 0; cb < MB; ++cb) acc[rb][cb] = f32x16{};
+
+  const __bf16* X = static_cast<const __bf16*>(a.x);
+  const __bf16* W = static_cast<const __bf16*>(a.w);
+  const int nst = (a.K + kGK - 1) / kGK;
+  auto load_stage = [&](int st) { load(X + st * kGK, a.x_stride, m0, m1, W + st * kGK, a.K, f0, f1, a.K - st * kGK); };
+  load_stage(0);
+  store(0);
+  __syncthreads();
+  for (int st = 0; st < nst; ++st) {
+    if (st + 1 < nst) load_stage(st + 1);
+#pragma unroll
+    for (int ks = 0; ks < kGK / 16; ++ks)
+#pragma unroll
+      for (int rb = 0; rb < MB; ++rb)
+#pragma unroll
+        for (int cb = 0; cb < MB; ++cb)
+          acc[rb][cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand(st & 1, 1, cb, ks), operand(st & 1, 0, rb, ks), acc[rb][cb], 0, 0, 0);
+    if (st + 1 < nst) store((st + 1) & 1);
+    __syncthreads();
+  }
+
+  // Element e of acc[rb][cb]: row (wm MB + rb) 32 + n32, feature (wn MB + cb) 32 + 8 (e / 4) + 4 hh + e % 4 of the tile.
+  const int p0 = f0 / a.split, p1 = (f1 - 1) / a.split;
+  for (int32_t s = __builtin_amdgcn_readfirstlane(first_segment(a, m0)); s < a.segments; ++s) {
+    const Segment g = segment(a, s);
+    if (g.first >= m1) break;
+    if (g.adapter < 0 || g.first >= g.end) continue;
+    for (int p = p0; p <= p1; ++p) {
+      const __bf16* u = static_cast<const __bf16*>(a.low) + p * a.low_rank;
+      const __bf16* B = static_cast<const __bf16*>(a.b) + static_cast<int64_t>(g.adapter) * a.N * a.rank;
+      const int32_t fa = p * a.split, fb = fa + a.split;
+      for (int r0 = 0; r0 < a.rank; r0 += kGK) {
+        load(u + r0, static_cast<int64_t>(a.parts) * a.low_rank, g.first, g.end, B + r0, a.rank, fa, min(fb, f1), a.rank - r0);
+        store(0);
+        __syncthreads();
+#pragma unroll
+        for (int rb = 0; rb < MB; ++rb) {
+          const int32_t row = m0 + wm * MB * 32 + rb * 32 + n32;
+          const bool mine = row >= g.first && row < g.end;
+#pragma unroll
+          for (int cb = 0; cb < MB; ++cb) {
+            f32x16 add = f32x16{};
+#pragma unroll
+            for (int ks = 0; ks < kGK / 16; ++ks)
+              add = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand(0, 1, cb, ks), operand(0, 0, rb, ks), add, 0, 0, 0);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const int32_t f = f0 + wn * MB * 32 + cb * 32 + 8 * (e >> 2) + 4 * hh + (e & 3);
+              acc[rb][cb][e] += mine && f >= fa && f < fb ? add[e] : 0.f;
+            }
+          }
+        }
+        __syncthreads();
+      }
+    }
+  }
+
+  const __bf16* bias = static_cast<const __bf16*>(a.bias);
+#pragma unroll
+  for (int rb = 0; rb < MB; ++rb) {
+    const int32_t row = m0 + wm * MB * 32 + rb * 32 + n32;
+    if (row >= m1) continue;
+#pragma unroll
+    for (int cb = 0; cb < MB; ++cb)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int32_t f = f0 + wn * MB * 32 + cb * 32 + 8 * (e >> 2) + 4 * hh + (e & 3);
+        if (f >= f1) continue;
+        const int part = f / a.split;
+        const float v = (acc[rb][cb][e] + (bias ? static_cast<float>(bias[f]) : 0.f)) * (part == 0 ? a.part0_scale : 1.f);
+        static_cast<__bf16*>(a.y[part])[static_cast<int64_t>(row) * a.split + (f - part * a.split)] = static_cast<__bf16>(v);
+      }
+  }
+}
+
+template <int RT, int kUnroll>
+void launch_few(const AdapterArgs& a, const AdapterPlan& plan, hipStream_t stream) {
+  const dim3 grid(static_cast<uint32_t>(plan.blocks)), block(kFewWaves * 64);
+  if (a.whole)
+    hipLaunchKernelGGL((few_kernel<RT, kUnroll, true>), grid, block, 0, stream, a);
+  else
+    hipLaunchKernelGGL((few_kernel<RT, kUnroll, false>), grid, block, 0, stream, a);
+}
+
 hipError_t launch_low(const AdapterArgs& a, const AdapterPlan& plan, hipStream_t stream) {
-  const uint32_t tiles = static_cast<uint32_t>(plan.low_tiles), cols = static_cast<uint32_t>(a.parts * a.low_rank + 31) / 32;
-  if (plan.kernel == AdapterKernel::kAny) {
-    hipLaunchKernelGGL((low_kernel<4, 2, 2, false>), dim3(tiles, (cols + 1) / 2), dim3(4 * 64), 0, stream, a);
-  } else if (plan.low_rows == kLowRows) {
-    hipLaunchKernelGGL((low_kernel<16, 1, 10, true>), dim3(tiles, cols), dim3(16 * 64), 0, stream, a);
+  const uint32_t tiles = static_cast<uint32_t>(plan.low_tiles), cols = static_cast<uint32_t>(a.parts * a.low_rank);
+  if (plan.low_rows == kLowRows) {
+    const dim3 grid(tiles, cols / 16), block(kLowWaves * 64);
+    if (a.whole)
+      hipLaunchKernelGGL(low_kernel<true>, grid, block, 0, stream, a);
+    else
+      hipLaunchKernelGGL(low_kernel<false>, grid, block, 0, stream, a);
   } else {
-    switch (cols) {
+    switch ((cols + 31) / 32) {
       case 1:
         hipLaunchKernelGGL((low_tile_kernel<1>), dim3(tiles), dim3(256), 0, stream, a);
         break;
@@ -698,7 +737,7 @@ hipError_t launch_low(const AdapterArgs& a, const AdapterPlan& plan, hipStream_t
         hipLaunchKernelGGL((low_tile_kernel<2>), dim3(tiles), dim3(256), 0, stream, a);
         break;
       default:
-        hipLaunchKernelGGL((low_tile_kernel<3>), dim3(tiles * ((cols + 2) / 3)), dim3(256), 0, stream, a);
+        hipLaunchKernelGGL((low_tile_kernel<3>), dim3(tiles * ((cols + 95) / 96)), dim3(256), 0, stream, a);
     }
   }
   return hipGetLastError();
@@ -714,20 +753,26 @@ hipError_t launch_adapter_project(const AdapterArgs& a, const AdapterPlan& plan,
   switch (plan.kernel) {
     case AdapterKernel::kFew:
       if (a.M <= 16)
-        hipLaunchKernelGGL((few_kernel<1, 10>), grid, dim3(kFewWaves * 64), 0, stream, a);
+        launch_few<1, 7>(a, plan, stream);
       else if (a.M <= 32)
-        hipLaunchKernelGGL((few_kernel<2, 6>), grid, dim3(kFewWaves * 64), 0, stream, a);
+        launch_few<2, 6>(a, plan, stream);
       else
-        hipLaunchKernelGGL((few_kernel<4, 4>), grid, dim3(kFewWaves * 64), 0, stream, a);
+        launch_few<4, 4>(a, plan, stream);
       break;
-    case AdapterKernel::kSmallTiles:
+    case AdapterKernel::kTiles64:
+      hipLaunchKernelGGL((tile_kernel<2, 2, 1, 1>), grid, dim3(256), 0, stream, a);
+      break;
+    case AdapterKernel::kTiles128:
       hipLaunchKernelGGL((tile_kernel<2, 2, 2, 2>), grid, dim3(256), 0, stream, a);
       break;
-    case AdapterKernel::kLargeTiles:
+    case AdapterKernel::kTiles256:
       hipLaunchKernelGGL((tile_kernel<2, 4, 4, 2>), grid, dim3(512), 0, stream, a);
       break;
-    case AdapterKernel::kAny:
-      hipLaunchKernelGGL(any_kernel, grid, dim3(kThreads), 0, stream, a);
+    case AdapterKernel::kAny64:
+      hipLaunchKernelGGL(any_kernel<1>, grid, dim3(kThreads), 0, stream, a);
+      break;
+    case AdapterKernel::kAny128:
+      hipLaunchKernelGGL(any_kernel<2>, grid, dim3(kThreads), 0, stream, a);
   }
   return hipGetLastError();
 }

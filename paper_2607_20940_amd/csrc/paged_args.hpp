@@ -177,14 +177,16 @@ struct AdapterArgs {
   int32_t parts, split;  // split: features of a part
   int32_t segments, adapters, rank, low_rank;
   float part0_scale;
+  // whole, aligned chunks of 16 bytes: the rows of x, w and a; of b; of the outputs
+  bool whole, whole_b, whole_y;
 };
 
-// Which kernel makes a product: the one for few tokens, one of two tile sizes,
-// or the one for any sizes, strides and alignments.
-enum class AdapterKernel { kFew, kSmallTiles, kLargeTiles, kAny };
+// Which kernel makes a product: the one for few tokens, one of three tile sizes
+// (tokens and features), or of two where rows may begin anywhere.
+enum class AdapterKernel { kFew, kTiles64, kTiles128, kTiles256, kAny64, kAny128 };
 constexpr int kAdapterFewTokens = 64, kAdapterFewFeatures = 32;
 
-constexpr int kLowRows = 32, kLowManyRows = 64;  // rows of a tile of the low-rank factor
+constexpr int kLowRows = 16, kLowManyRows = 64;  // rows of a tile of the low-rank factor
 struct AdapterPlan {
   AdapterKernel kernel;
   int32_t low_rows;   // of a tile of the low-rank factor's launch
@@ -193,10 +195,9 @@ struct AdapterPlan {
   int64_t workspace_bytes;
   int32_t low_rank;    // rank rounded up to whole 16 values
 };
-// aligned: rows of x, w, a, b and the outputs are whole aligned 16-byte chunks,
-// the contraction whole stages.
+// whole: as AdapterArgs has it.  The workspace is the same either way.
 hipError_t plan_adapter_project(int64_t rows, int32_t out_features, int32_t parts, int32_t segments, int32_t adapters,
-                                int32_t rank, bool aligned, AdapterPlan* plan);
+                                int32_t rank, bool whole, AdapterPlan* plan);
 hipError_t launch_adapter_project(const AdapterArgs& a, const AdapterPlan& plan, hipStream_t stream);
 
 }  // namespace mssa

@@ -26,6 +26,7 @@
 #include "paged_args.hpp"
 #include "wave_ops.hpp"
 #include "xcd.hpp"
+#include "zero_row.hpp"
 
 namespace mssa {
 namespace {
@@ -35,9 +36,6 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kTile = kPagedTile;
 constexpr uint64_t kAll = ~uint64_t{0};
-
-// What stands for a token that is not there.
-__device__ __attribute__((aligned(256))) const uint32_t zero_row[64] = {};
 
 // -------------------------------------------------------------- sharing out
 // All items stand in a row, sequence by sequence, key head by key head, item by

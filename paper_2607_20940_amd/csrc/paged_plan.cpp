@@ -35,30 +35,30 @@ hipError_t plan_paged_attention(int64_t tokens, int32_t batch, int32_t max_chunk
 }
 
 hipError_t plan_adapter_project(int64_t rows, int32_t out_features, int32_t parts, int32_t segments, int32_t adapters,
-                                int32_t rank, bool aligned, AdapterPlan* plan) {
+                                int32_t rank, bool whole, AdapterPlan* plan) {
   AdapterPlan p{};
   auto tiles = [&](int64_t m, int64_t n) { return (rows + m - 1) / m * ((out_features + n - 1) / n); };
-  p.kernel = AdapterKernel::kAny;
-  p.blocks = tiles(128, 128);
-  if (aligned) {
-    if (rows <= kAdapterFewTokens) {
-      p.kernel = AdapterKernel::kFew;
-      p.blocks = tiles(kAdapterFewTokens, kAdapterFewFeatures);
-    } else if (tiles(256, 256) >= 256) {
-      p.kernel = AdapterKernel::kLargeTiles;
-      p.blocks = tiles(256, 256);
-    } else {
-      p.kernel = AdapterKernel::kSmallTiles;
-    }
+  if (rows <= kAdapterFewTokens) {
+    p.kernel = AdapterKernel::kFew;
+    p.blocks = tiles(kAdapterFewTokens, kAdapterFewFeatures);
+  } else if (whole && tiles(256, 256) >= 256) {
+    p.kernel = AdapterKernel::kTiles256;
+    p.blocks = tiles(256, 256);
+  } else if (tiles(128, 128) >= 256) {
+    p.kernel = whole ? AdapterKernel::kTiles128 : AdapterKernel::kAny128;
+    p.blocks = tiles(128, 128);
+  } else {
+    p.kernel = whole ? AdapterKernel::kTiles64 : AdapterKernel::kAny64;
+    p.blocks = tiles(64, 64);
   }
-  if (!launchable(p.blocks, p.kernel == AdapterKernel::kLargeTiles || p.kernel == AdapterKernel::kFew ? 512 : 256)) return hipErrorInvalidValue;
+  if (!launchable(p.blocks, 512)) return hipErrorInvalidValue;
   if (segments > 0 && adapters > 0) {
     p.low_rank = (rank + 15) / 16 * 16;
     // tiles of 64 rows where each is nearly full and there are some for most CUs
-    p.low_rows = p.kernel != AdapterKernel::kAny && rows > 4096 && rows / segments >= kLowManyRows ? kLowManyRows : kLowRows;
+    p.low_rows = whole && rows > 4096 && rows / segments >= kLowManyRows ? kLowManyRows : kLowRows;
     // every segment's tiles: whole ones, and one that is not full
     p.low_tiles = std::min<int64_t>(rows, segments + rows / p.low_rows);
-    if (!launchable(p.low_tiles * ((int64_t{parts} * p.low_rank + 31) / 32), 1024)) return hipErrorInvalidValue;
+    if (!launchable(p.low_tiles, 1024)) return hipErrorInvalidValue;
     p.workspace_bytes = rows * parts * p.low_rank * 2;
   }
   *plan = p;

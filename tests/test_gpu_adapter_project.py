@@ -156,3 +156,11 @@ def test_repeatable_on_another_stream_and_in_a_graph(M):
         call(one)
         torch.cuda.synchronize()
         assert all(torch.equal(p, q) for p, q in zip(one[1], two[1]))
+
+
+@pytest.mark.parametrize("M,K,N,parts,R,S", [(4200, 72, 4104, 1, 8, 3), (4097, 136, 4608, 3, 40, 2), (5000, 64, 3700, 2, 12, 5),
+                                             (4500, 192, 3900, 3, 70, 4), (4300, 8, 4096, 1, 24, 40), (4200, 100, 2000, 1, 8, 3),
+                                             (9000, 456, 768, 3, 100, 2), (2100, 328, 2050, 1, 16, 700)])
+def test_large_tiles(M, K, N, parts, R, S):
+    rng = np.random.default_rng(M)
+    _run(M, K, N, parts, 3, R, _cuts(rng, M, S), rng.integers(-1, 3, size=S), factor=1.7)
