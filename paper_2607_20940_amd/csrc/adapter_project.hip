@@ -249,80 +249,35 @@ __global__ __launch_bounds__(256) void low_tile_kernel(AdapterArgs a) {
 
 // ------------------------------------------------------------- few tokens
 // Up to 64 tokens: bound by the weights' bytes, each read once.  A block takes
-// 32 features, its eight waves share out the contraction; W and X go from
-// memory to the matrix cores' registers as they lie, kUnroll steps of 32 values
-// on their way at once.  The adapters' share is a dot product of `rank` values
-// for each output.  kWhole: rows of whole, aligned 16-byte chunks.
-constexpr int kFewFeatures = kAdapterFewFeatures, kFewWaves = 8;
+// 32 features; its waves share out the contraction and meet in LDS at the end.
+// The adapters' share is a dot product of `rank` values for each output.
+constexpr int kFewFeatures = kAdapterFewFeatures;
 
-template <int RT, int kUnroll, bool kWhole>
-__global__ __launch_bounds__(kFewWaves * 64) void few_kernel(AdapterArgs a) {
-  constexpr int FT = kFewFeatures / 16, kRows = RT * 16, kStr = kFewFeatures + 1;
-  __shared__ float sums[kFewWaves][kRows * kStr];
-  __shared__ int32_t which[kRows];
-  const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int32_t f0 = static_cast<int32_t>(blockIdx.x) * kFewFeatures;
-  // a thread's segments write their adapter to their rows (a row is in one segment)
+// A row's adapter in its place of `which`, -1 for none: a thread's segments write
+// theirs (a row is in one segment).
+template <int kRows, int kBlock>
+__device__ inline void adapters_of_rows(const AdapterArgs& a, int32_t* which) {
+  const int tid = threadIdx.x;
   if (tid < kRows) which[tid] = -1;
   __syncthreads();
-  for (int32_t s = tid; s < a.segments; s += kFewWaves * 64) {
+  for (int32_t s = tid; s < a.segments; s += kBlock) {
     const Segment sg = segment(a, s);
     for (int32_t r = sg.first; r < sg.end; ++r) which[r] = sg.adapter;
   }
-  const __bf16 *w[FT], *x[RT];
-#pragma unroll
-  for (int f = 0; f < FT; ++f) w[f] = static_cast<const __bf16*>(a.w) + static_cast<int64_t>(min(f0 + f * 16 + n, a.N - 1)) * a.K + g * 8;
-#pragma unroll
-  for (int t = 0; t < RT; ++t) x[t] = static_cast<const __bf16*>(a.x) + min(t * 16 + n, a.M - 1) * a.x_stride + g * 8;
-  f32x4 acc[FT][RT];
-#pragma unroll
-  for (int f = 0; f < FT; ++f)
-#pragma unroll
-    for (int t = 0; t < RT; ++t) acc[f][t] = f32x4{};
-  auto get = [&](const __bf16* p, int k) -> bf16x8 {
-    if constexpr (!kWhole) return eight(p + k, a.K - k - g * 8);
-    // the last step's chunks past the row
-    return k + g * 8 < a.K ? *reinterpret_cast<const bf16x8*>(p + k) : bf16x8{};
-  };
-  const int steps = (a.K + 31) / 32, each = (steps + kFewWaves - 1) / kFewWaves;
-  const int s0 = wave * each, s1 = min(s0 + each, steps);
-#pragma unroll 1
-  for (int s = s0; s < s1; s += kUnroll) {
-    bf16x8 wv[kUnroll][FT], xv[kUnroll][RT];
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      const int k = min(s + u, s1 - 1) * 32;
-#pragma unroll
-      for (int f = 0; f < FT; ++f) wv[u][f] = get(w[f], k);
-#pragma unroll
-      for (int t = 0; t < RT; ++t) xv[u][t] = get(x[t], k);
-    }
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-#pragma unroll
-      for (int f = 0; f < FT; ++f)
-#pragma unroll
-        for (int t = 0; t < RT; ++t)
-          if (s + u < s1) acc[f][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[u][f], xv[u][t], acc[f][t], 0, 0, 0);
-    }
-  }
-  // element e of acc[f][t]: row 16 t + n, feature 16 f + 4 g + e
-#pragma unroll
-  for (int f = 0; f < FT; ++f)
-#pragma unroll
-    for (int t = 0; t < RT; ++t)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sums[wave][(t * 16 + n) * kStr + f * 16 + 4 * g + e] = acc[f][t][e];
-  __syncthreads();
+}
+
+// The block's outputs from its waves' sums [row][feature], rows kFewFeatures + 1 apart.
+template <int kRows, int kWaves>
+__device__ inline void few_outputs(const AdapterArgs& a, const float* sums, const int32_t* which, int32_t f0) {
+  constexpr int kStr = kFewFeatures + 1;
   const __bf16* bias = static_cast<const __bf16*>(a.bias);
-  for (int i = tid; i < kRows * kFewFeatures; i += kFewWaves * 64) {
+  for (int i = threadIdx.x; i < kRows * kFewFeatures; i += kWaves * 64) {
     const int r = i / kFewFeatures, f = f0 + i % kFewFeatures;
     if (r >= a.M || f >= a.N) continue;
     const int part = f / a.split, j = which[r];
     float v = 0.f;
 #pragma unroll
-    for (int k = 0; k < kFewWaves; ++k) v += sums[k][r * kStr + i % kFewFeatures];
+    for (int k = 0; k < kWaves; ++k) v += sums[k * kRows * kStr + r * kStr + i % kFewFeatures];
     if (j >= 0) {
       const __bf16* u = static_cast<const __bf16*>(a.low) + (r * a.parts + part) * a.low_rank;
       const __bf16* b = static_cast<const __bf16*>(a.b) + (static_cast<int64_t>(j) * a.N + f) * a.rank;
@@ -337,6 +292,147 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(AdapterArgs a) {
     v = (v + (bias ? static_cast<float>(bias[f]) : 0.f)) * (part == 0 ? a.part0_scale : 1.f);
     static_cast<__bf16*>(a.y[part])[static_cast<int64_t>(r) * a.split + (f - part * a.split)] = static_cast<__bf16>(v);
   }
+}
+
+// Whole rows: four waves, each with a ring of its own in LDS: 64-deep stages of
+// its share, filled by direct transfers of whole cache lines, kRing of them on
+// their way (no barriers).  Half lines a request, as the matrix cores' operands
+// lie, take 10 us more for 16 tokens of 5120 -> 15360, and streamed (nt) ones are
+// fetched twice.
+template <int RT, int kRing>
+__global__ __launch_bounds__(256) void few_ring_kernel(AdapterArgs a) {
+  constexpr int kWaves = 4, FT = kFewFeatures / 16, kRows = RT * 16, kStr = kFewFeatures + 1;
+  constexpr int kW = kFewFeatures * 128, kStage = kW + kRows * 128, kMine = kStage / 1024;  // kMine: transfers of a stage
+  __shared__ __attribute__((aligned(16))) char lds[kWaves][kRing][kStage];
+  __shared__ int32_t which[kRows];
+  static_assert(kWaves * kRows * kStr * 4 <= static_cast<int>(sizeof(lds)), "the sums fit the rings' place");
+  const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int32_t f0 = static_cast<int32_t>(blockIdx.x) * kFewFeatures;
+  const int stages = (a.K + 63) / 64, each = (stages + kWaves - 1) / kWaves, s0 = wave * each, s1 = min(s0 + each, stages);
+
+  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(&lds[wave][0][0]));
+  const uint32_t wrb = static_cast<uint32_t>(a.K) * 2, xrb = static_cast<uint32_t>(a.x_stride) * 2;
+  const __bf16* W = static_cast<const __bf16*>(a.w) + static_cast<int64_t>(f0) * a.K;
+  const uint32_t wrows = min(kFewFeatures, a.N - f0) - 1, xrows = a.M - 1;
+  // A transfer: rows 8 i + lane / 8, physical chunk lane % 8 holding logical chunk unswz128(row, lane % 8).
+  auto put = [&](int st) {
+    const int left = min(a.K - st * 64, 64);  // a multiple of 8
+    const i32x4 rw = rsrc_of(W + st * 64, wrows * wrb + left * 2);
+    const i32x4 rx = rsrc_of(static_cast<const __bf16*>(a.x) + st * 64, xrows * xrb + left * 2);
+    const uint32_t base = lds0 + (st - s0) % kRing * kStage;
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+      const bool is_x = i >= kW / 1024;
+      const int row = (is_x ? i - kW / 1024 : i) * 8 + (lane >> 3), lc = unswz128(row, lane & 7);
+      const uint32_t off = lc * 8 < left ? row * (is_x ? xrb : wrb) + lc * 16 : kPastEnd;
+      if (is_x)
+        dma16(rx, off, __builtin_amdgcn_readfirstlane(base + i * 1024));
+      else
+        dma16_nt(rw, off, __builtin_amdgcn_readfirstlane(base + i * 1024));
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < kRing; ++i)
+    if (s0 + i < s1) put(s0 + i);
+  f32x4 acc[FT][RT];
+#pragma unroll
+  for (int f = 0; f < FT; ++f)
+#pragma unroll
+    for (int t = 0; t < RT; ++t) acc[f][t] = f32x4{};
+  for (int st = s0; st < s1; ++st) {
+    // this stage's transfers are done where no more than those of the later ones are left
+    const int later = min(s1 - st, kRing) - 1;
+    if (kRing > 2 && later == 2)
+      wait_vmcnt<2 * kMine>();
+    else if (later == 1)
+      wait_vmcnt<kMine>();
+    else
+      wait_vmcnt<0>();
+    asm volatile("" ::: "memory");
+    const char* L = lds[wave][(st - s0) % kRing];
+    bf16x8 wv[2][FT], xv[2][RT];
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+#pragma unroll
+      for (int f = 0; f < FT; ++f) wv[ks][f] = *reinterpret_cast<const bf16x8*>(L + swz128(f * 16 + n, ks * 32 + g * 8) * 2);
+#pragma unroll
+      for (int t = 0; t < RT; ++t) xv[ks][t] = *reinterpret_cast<const bf16x8*>(L + kW + swz128(t * 16 + n, ks * 32 + g * 8) * 2);
+    }
+    // the buffer is filled again once it has been read
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (st + kRing < s1) put(st + kRing);
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int f = 0; f < FT; ++f)
+#pragma unroll
+        for (int t = 0; t < RT; ++t) acc[f][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[ks][f], xv[ks][t], acc[f][t], 0, 0, 0);
+  }
+  __syncthreads();
+  // element e of acc[f][t]: row 16 t + n, feature 16 f + 4 g + e
+  float* sums = reinterpret_cast<float*>(&lds[0][0][0]);
+#pragma unroll
+  for (int f = 0; f < FT; ++f)
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sums[wave * kRows * kStr + (t * 16 + n) * kStr + f * 16 + 4 * g + e] = acc[f][t][e];
+  adapters_of_rows<kRows, 256>(a, which);
+  __syncthreads();
+  few_outputs<kRows, kWaves>(a, sums, which, f0);
+}
+
+// Rows that begin anywhere: eight waves, W and X from memory to registers as the
+// matrix cores take them, kUnroll steps of 32 values on their way.
+template <int RT, int kUnroll>
+__global__ __launch_bounds__(512) void few_any_kernel(AdapterArgs a) {
+  constexpr int kWaves = 8, FT = kFewFeatures / 16, kRows = RT * 16, kStr = kFewFeatures + 1;
+  __shared__ float sums[kWaves * kRows * kStr];
+  __shared__ int32_t which[kRows];
+  const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int32_t f0 = static_cast<int32_t>(blockIdx.x) * kFewFeatures;
+  const __bf16 *w[FT], *x[RT];
+#pragma unroll
+  for (int f = 0; f < FT; ++f) w[f] = static_cast<const __bf16*>(a.w) + static_cast<int64_t>(min(f0 + f * 16 + n, a.N - 1)) * a.K + g * 8;
+#pragma unroll
+  for (int t = 0; t < RT; ++t) x[t] = static_cast<const __bf16*>(a.x) + min(t * 16 + n, a.M - 1) * a.x_stride + g * 8;
+  f32x4 acc[FT][RT];
+#pragma unroll
+  for (int f = 0; f < FT; ++f)
+#pragma unroll
+    for (int t = 0; t < RT; ++t) acc[f][t] = f32x4{};
+  const int steps = (a.K + 31) / 32, each = (steps + kWaves - 1) / kWaves, s0 = wave * each, s1 = min(s0 + each, steps);
+#pragma unroll 1
+  for (int s = s0; s < s1; s += kUnroll) {
+    bf16x8 wv[kUnroll][FT], xv[kUnroll][RT];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const int k = min(s + u, s1 - 1) * 32, left = a.K - k - g * 8;
+#pragma unroll
+      for (int f = 0; f < FT; ++f) wv[u][f] = eight(w[f] + k, left);
+#pragma unroll
+      for (int t = 0; t < RT; ++t) xv[u][t] = eight(x[t] + k, left);
+    }
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+      for (int f = 0; f < FT; ++f)
+#pragma unroll
+        for (int t = 0; t < RT; ++t)
+          if (s + u < s1) acc[f][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[u][f], xv[u][t], acc[f][t], 0, 0, 0);
+  }
+  // element e of acc[f][t]: row 16 t + n, feature 16 f + 4 g + e
+#pragma unroll
+  for (int f = 0; f < FT; ++f)
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sums[wave * kRows * kStr + (t * 16 + n) * kStr + f * 16 + 4 * g + e] = acc[f][t][e];
+  adapters_of_rows<kRows, 512>(a, which);
+  __syncthreads();
+  few_outputs<kRows, kWaves>(a, sums, which, f0);
 }
 
 // ------------------------------------------------------------ many tokens
@@ -711,13 +807,13 @@ __global__ __launch_bounds__(kThreads) void any_kernel(AdapterArgs a) {
   }
 }
 
-template <int RT, int kUnroll>
+template <int RT, int kRing, int kUnroll>
 void launch_few(const AdapterArgs& a, const AdapterPlan& plan, hipStream_t stream) {
-  const dim3 grid(static_cast<uint32_t>(plan.blocks)), block(kFewWaves * 64);
+  const dim3 grid(static_cast<uint32_t>(plan.blocks));
   if (a.whole)
-    hipLaunchKernelGGL((few_kernel<RT, kUnroll, true>), grid, block, 0, stream, a);
+    hipLaunchKernelGGL((few_ring_kernel<RT, kRing>), grid, dim3(256), 0, stream, a);
   else
-    hipLaunchKernelGGL((few_kernel<RT, kUnroll, false>), grid, block, 0, stream, a);
+    hipLaunchKernelGGL((few_any_kernel<RT, kUnroll>), grid, dim3(512), 0, stream, a);
 }
 
 hipError_t launch_low(const AdapterArgs& a, const AdapterPlan& plan, hipStream_t stream) {
@@ -753,11 +849,11 @@ hipError_t launch_adapter_project(const AdapterArgs& a, const AdapterPlan& plan,
   switch (plan.kernel) {
     case AdapterKernel::kFew:
       if (a.M <= 16)
-        launch_few<1, 7>(a, plan, stream);
+        launch_few<1, 3, 7>(a, plan, stream);
       else if (a.M <= 32)
-        launch_few<2, 6>(a, plan, stream);
+        launch_few<2, 2, 6>(a, plan, stream);
       else
-        launch_few<4, 4>(a, plan, stream);
+        launch_few<4, 3, 4>(a, plan, stream);
       break;
     case AdapterKernel::kTiles64:
       hipLaunchKernelGGL((tile_kernel<2, 2, 1, 1>), grid, dim3(256), 0, stream, a);
