@@ -92,6 +92,24 @@ __device__ inline void gdma16(const void* from, uint32_t lds_addr) {
 #pragma clang diagnostic pop
 }
 
+// As gdma16 for data read once (nt: not kept in the caches).
+__device__ inline void gdma16_nt(const void* from, uint32_t lds_addr) {
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt"
+               :: "s"(lds_addr), "v"(from) : "memory", "m0");
+#pragma clang diagnostic pop
+}
+
+// As gdma16 for 4 bytes a lane: lane i's land at lds_addr + 4 i.
+__device__ inline void gdma4(const void* from, uint32_t lds_addr) {
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
+               :: "s"(lds_addr), "v"(from) : "memory", "m0");
+#pragma clang diagnostic pop
+}
+
 // Store of lane i's 16 bytes at buffer offset voff + soff + IMM
 // (buffer_store_dwordx4, non-temporal: data that another kernel reads once);
 // lanes whose offset is past the buffer's range store nothing.  The s_nop is

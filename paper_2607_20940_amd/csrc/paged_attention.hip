@@ -15,8 +15,8 @@
 // Tokens past the sequence's last, and those whose page is none, are read from
 // a row of zeros and masked.  A token that some rows see and others do not (the
 // mask's steps) has P = 0 for the latter, which an infinity or a NaN among its
-// values would turn into a NaN: tiles with such a step look for them, and add
-// such a tile's tokens one by one.
+// values would turn into a NaN: in tiles with such a step the products take
+// zeros for them, and they are added apart, to the rows that see them.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -193,19 +193,21 @@ __device__ inline PageWalk walk_of(const PagedAttnArgs& a, int b, int len) {
 // Lane `from`'s value.
 __device__ inline int32_t of_lane(int32_t v, int from) { return __builtin_amdgcn_ds_bpermute(from * 4, v); }
 
-__device__ inline bool not_finite(bf16x8 v) {
-  const u32x4 w = __builtin_bit_cast(u32x4, v);
-  bool bad = false;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) bad = bad || (w[i] & 0x7f80u) == 0x7f80u || (w[i] & 0x7f800000u) == 0x7f800000u;
-  return bad;
+// Infinities and NaN of two bf16 values, zeros elsewhere.
+__device__ inline uint32_t wild_of(uint32_t two) {
+  return ((two & 0x7f80u) == 0x7f80u ? two & 0xffffu : 0u) | ((two & 0x7f800000u) == 0x7f800000u ? two & 0xffff0000u : 0u);
 }
 
-// v's element j, zeros elsewhere; all zeros unless `mine`.
-__device__ inline bf16x8 only(bf16x8 v, int j, bool mine) {
+// v without its infinities and NaN; `wild` collects whether it had any.
+__device__ inline bf16x8 tamed(bf16x8 v, bool* wild) {
+  u32x4 w = __builtin_bit_cast(u32x4, v);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = mine && e == j ? v[e] : static_cast<__bf16>(0.f);
-  return v;
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t x = wild_of(w[i]);
+    *wild = *wild || x != 0;
+    w[i] ^= x;
+  }
+  return __builtin_bit_cast(bf16x8, w);
 }
 
 // ------------------------------------------------------------------ many rows
@@ -285,13 +287,16 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
 
     const int r_in = wave * 32 + n, r = at.item * (NW * 32) + r_in;
     const bool ok = r < at.seq.rows;
-    const RowPlace row = row_place(a, at.seq, at.kvh, ok ? r : 0, D);
-    const int seen = ok ? row.seen : len;
+    int seen = len;
     bf16x8 qf[KS];
+    {
+      const RowPlace row = row_place(a, at.seq, at.kvh, ok ? r : 0, D);
+      if (MASK && ok) seen = row.seen;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      const bf16x8 v = *reinterpret_cast<const bf16x8*>(static_cast<const __bf16*>(a.q) + row.q + ks * 16 + hh * 8);
-      qf[ks] = ok ? v : bf16x8{};
+      for (int ks = 0; ks < KS; ++ks) {
+        const bf16x8 v = *reinterpret_cast<const bf16x8*>(static_cast<const __bf16*>(a.q) + row.q + ks * 16 + hh * 8);
+        qf[ks] = ok ? v : bf16x8{};
+      }
     }
 
     f32x16 o[DB], s[2];
@@ -306,40 +311,49 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
       const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(r0 + swz256(t_row + 8, db * 32 + t_col)));
       return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     };
-    // Tile t whose values are not all finite: its tokens one by one, each added
-    // to the rows that see it.
-    auto add_pv_one_by_one = [&](int buf, int t) {
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int cc = 0; cc < 2; ++cc)
-#pragma unroll
-          for (int db = 0; db < DB; ++db) {
-            const bf16x8 v = v_operand(buf, kb, cc, db);
+    // The infinities and NaN of tile t's values, token by token, to the rows that see them.
+    auto add_wild = [&](int buf, int t) {
 #pragma unroll 1
-            for (int i = 0; i < 16; ++i) {
-              const int j = i & 7, half = i >> 3, tok = kb * 32 + cc * 16 + 8 * (j >> 2) + 4 * half + (j & 3);
-              const f32x16 one = __builtin_amdgcn_mfma_f32_32x32x16_bf16(only(v, j, hh == half), only(pb[kb][cc], j, hh == half),
-                                                                         f32x16{}, 0, 0, 0);
-              const bool sees = static_cast<int64_t>(t) * kTile + tok < seen;
+      for (int tok = 0; tok < kTile; ++tok) {
+        const __bf16* V = lds[buf][1];
+        const uint32_t two = *reinterpret_cast<const uint32_t*>(V + swz256(tok, (lane * 2) & (D - 1)));
+        if (!__any(wild_of(two) != 0)) continue;
+        // P of the token, from the half wave that holds it
+        float p = 0.f;
 #pragma unroll
-              for (int e = 0; e < 16; ++e) o[db][e] += sees ? one[e] : 0.f;
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) p = kb * 32 + 8 * (e >> 2) + 4 * hh + (e & 3) == tok ? static_cast<float>(pb[kb][e >> 3][e & 7]) : p;
+        p = __shfl(p, n + 32 * (tok >> 2 & 1));
+        const bool sees = static_cast<int64_t>(t) * kTile + tok < seen;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const bf16x4 v = *reinterpret_cast<const bf16x4*>(V + swz256(tok, db * 32 + 8 * j + 4 * hh));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float f = static_cast<float>(v[i]);
+              const bool wild = !(__builtin_fabsf(f) < INFINITY);
+              o[db][4 * j + i] += sees && wild ? p * f : 0.f;
             }
           }
+      }
     };
     auto add_pv = [&](int buf, int t) {
       if (MASK && step) {
-        bool bad = false;
+        bool wild = false;
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
           for (int cc = 0; cc < 2; ++cc)
 #pragma unroll
-            for (int db = 0; db < DB; ++db) bad = bad || not_finite(v_operand(buf, kb, cc, db));
-        if (__any(bad)) {
-          add_pv_one_by_one(buf, t);
-          return;
-        }
+            for (int db = 0; db < DB; ++db) {
+              o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tamed(v_operand(buf, kb, cc, db), &wild), pb[kb][cc], o[db], 0, 0, 0);
+              __builtin_amdgcn_sched_barrier(0);
+            }
+        if (__any(wild)) add_wild(buf, t);
+        return;
       }
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
@@ -419,11 +433,12 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
       wait_vmcnt<0>();
       phase_end();
       if (second) phase_end();
-      for (int t = t0; t < t1; ++t) {
+      for (int t = t0;; ++t) {
         const int buf = (t - t0) & 1;
         // the wave whose turn at the matrix core it is goes first elsewhere too
         __builtin_amdgcn_s_setprio(1);
         if (t > t0) add_pv(buf ^ 1, t - 1);
+        if (t == t1) break;
         scores(buf);
         __builtin_amdgcn_s_setprio(0);
         phase_end();
@@ -436,12 +451,13 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
         wait_vmcnt<0>();
         phase_end();
       }
-      add_pv((t1 - 1 - t0) & 1, t1 - 1);
+      __builtin_amdgcn_s_setprio(0);
       if (NW == 8 && !second) phase_end();
     }
     l += other_half(l);
     // dims 32 db + 8 j + 4 hh .. + 3 of the row
     if (ok) {
+      const RowPlace row = row_place(a, at.seq, at.kvh, r, D);
       const int64_t slot = 2 * static_cast<int64_t>(worker) + (seg > 0);
       float* P = whole ? nullptr : slot_sums(a, D, slot, r_in);
       const float prior = whole && a.prior_lse ? a.prior_lse[row.lse] : 0.f;
@@ -466,16 +482,21 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
 
 // ------------------------------------------------------------------- few rows
 // Single tokens of a stream, or a few: at most RT x 16 rows share a key head.
-// Memory bound (the cache is read once), so a wave works alone on every fourth
-// tile of the block's, the next one's rows on their way to registers.  K is used
-// where it arrives: lane (n, g) of a 16x16x32 product holds 8 dims of token n.
-// V goes through a tile of the wave's own in LDS and is read transposed.
+// Memory bound (the cache is read once), so a wave works alone, without barriers,
+// on every fourth stage of 32 tokens of the block's.  K, V and the page table's
+// entries come by direct transfers into rings of the wave's own in LDS, whole
+// cache lines and streamed (nt): two stages of K and V on their way, entries two
+// stages ahead of them.  The transfers in order, stage by stage: K, V, entries of
+// the stage after the next; what a step needs is there once no more than those
+// issued after it are left.  Stages past the last are transfers of zeros.
 constexpr int kFewWaves = kPagedFewWaves;
+constexpr int kFewStage = 32;  // tokens
 
 template <int D, int RT, bool MASK>
-__global__ __launch_bounds__(kFewWaves * 64) __attribute__((amdgpu_waves_per_eu(2))) void few_rows_kernel(PagedAttnArgs a) {
-  constexpr int NS = D / 32, DT = D / 16, NU = kTile / 16, kRows = 16 * RT;
-  __shared__ __attribute__((aligned(16))) __bf16 lds[kFewWaves][32 * 128];
+__global__ __launch_bounds__(kFewWaves * 64) void few_rows_kernel(PagedAttnArgs a) {
+  constexpr int NS = D / 32, DT = D / 16, kRows = 16 * RT, kHalf = kFewStage * 256, kMoves = kFewStage / 4;
+  __shared__ __attribute__((aligned(16))) char lds[kFewWaves][2][2][kHalf];  // [wave][buffer][K | V]
+  __shared__ int32_t entries[kFewWaves][4][64];
   __shared__ float stat[2][kFewWaves][kRows];
 
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
@@ -490,8 +511,10 @@ __global__ __launch_bounds__(kFewWaves * 64) __attribute__((amdgpu_waves_per_eu(
 
   const int64_t row_bytes = static_cast<int64_t>(a.kv_heads) * D * 2;
   const float c = a.scale_log2e;
-  __bf16* V = lds[wave];
   const int t_row = 4 * g + (n >> 2), t_col = 4 * (n & 3);
+  const int t_lc = (lane & 15) ^ ((lane >> 4) << 2);
+  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(&lds[wave][0][0][0]));
+  const uint32_t ent0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(&entries[wave][0][0]));
 
   for (int seg = 0;; ++seg) {
     const int tiles = at.seq.tiles(at.item, a);
@@ -501,11 +524,43 @@ __global__ __launch_bounds__(kFewWaves * 64) __attribute__((amdgpu_waves_per_eu(
     const bool whole = take == cost;
     todo -= take;
     const int len = at.seq.len;
-    const PageWalk walk = walk_of(a, at.b, len);
+    const int32_t* const table = a.page_table + static_cast<int64_t>(at.b) * a.table_pages;
     const char* const k_base = static_cast<const char*>(a.k_pages) + static_cast<int64_t>(at.kvh) * D * 2;
     const char* const v_base = static_cast<const char*>(a.v_pages) + static_cast<int64_t>(at.kvh) * D * 2;
+    // This wave's stages: first, first + kFewWaves, .. below last (of the context's).
+    constexpr int kPer = kTile / kFewStage;
+    const int first = t0 * kPer + wave, last = t1 * kPer;
+    const int count = first < last ? (last - first + kFewWaves - 1) / kFewWaves : 0;
 
-    RowPlace place[RT];
+    // Lane i (and i + 32) looks token i of a stage up; past the last stage the
+    // sequence's last token, whose place is not used.
+    auto token = [&](int st) {
+      const uint32_t tok = static_cast<uint32_t>(first + st * kFewWaves) * kFewStage + (lane & 31);
+      return tok < static_cast<uint32_t>(len) ? tok : static_cast<uint32_t>(len) - 1;
+    };
+    auto ask = [&](int st) {
+      gdma4(table + a.page.quotient(token(st)), __builtin_amdgcn_readfirstlane(ent0 + (st & 3) * 256));
+    };
+    auto row_of = [&](int st, uint32_t* there) {
+      const int32_t found = entries[wave][st & 3][lane];
+      const uint32_t tok = token(st);
+      const bool ok = st < count && static_cast<uint32_t>(first + st * kFewWaves) * kFewStage + (lane & 31) < static_cast<uint32_t>(len) &&
+                      found >= 0 && found < a.pages;
+      *there = static_cast<uint32_t>(__ballot(ok));
+      return ok ? found * static_cast<int32_t>(a.page.d) + static_cast<int32_t>(tok - a.page.quotient(tok) * a.page.d) : -1;
+    };
+    auto bring = [&](int32_t row, int buf, int is_v) {
+#pragma unroll
+      for (int i = 0; i < kMoves; ++i) {
+        const int chunk = t_lc ^ (i & 3);
+        const int32_t r = of_lane(row, i * 4 + (lane >> 4));
+        const bool there = r >= 0 && (D == 128 || chunk < D / 8);
+        const char* p = (is_v ? v_base : k_base) + static_cast<int64_t>(r) * row_bytes + chunk * 16;
+        gdma16_nt(there ? p : reinterpret_cast<const char*>(zero_row) + chunk * 16,
+                  __builtin_amdgcn_readfirstlane(lds0 + (buf * 2 + is_v) * kHalf + i * 1024));
+      }
+    };
+
     bool ok[RT];
     int seen[RT];
     bf16x8 qf[RT][NS];
@@ -513,26 +568,14 @@ __global__ __launch_bounds__(kFewWaves * 64) __attribute__((amdgpu_waves_per_eu(
     for (int t = 0; t < RT; ++t) {
       const int r = at.item * kRows + t * 16 + n;
       ok[t] = r < at.seq.rows;
-      place[t] = row_place(a, at.seq, at.kvh, ok[t] ? r : 0, D);
-      seen[t] = ok[t] ? place[t].seen : len;
+      const RowPlace place = row_place(a, at.seq, at.kvh, ok[t] ? r : 0, D);
+      seen[t] = MASK && ok[t] ? place.seen : len;
 #pragma unroll
       for (int i = 0; i < NS; ++i) {
-        const bf16x8 v = *reinterpret_cast<const bf16x8*>(static_cast<const __bf16*>(a.q) + place[t].q + i * 32 + g * 8);
+        const bf16x8 v = *reinterpret_cast<const bf16x8*>(static_cast<const __bf16*>(a.q) + place.q + i * 32 + g * 8);
         qf[t][i] = ok[t] ? v : bf16x8{};
       }
     }
-
-    // Lane (n, g) holds dims 32 i + 8 g .. + 7 of tokens 16 u + n.
-    bf16x8 kc[NU][NS], vc[NU][NS];
-    auto fetch = [&](bf16x8 (&to)[NU][NS], const char* base, int32_t row) {
-#pragma unroll
-      for (int u = 0; u < NU; ++u) {
-        const int32_t r = of_lane(row, u * 16 + n);
-        const char* p = r >= 0 ? base + static_cast<int64_t>(r) * row_bytes : reinterpret_cast<const char*>(zero_row);
-#pragma unroll
-        for (int i = 0; i < NS; ++i) to[u][i] = *reinterpret_cast<const bf16x8*>(p + i * 64 + g * 16);
-      }
-    };
     f32x4 o[RT][DT];
     float m[RT], l[RT];
 #pragma unroll
@@ -542,50 +585,63 @@ __global__ __launch_bounds__(kFewWaves * 64) __attribute__((amdgpu_waves_per_eu(
 #pragma unroll
       for (int d = 0; d < DT; ++d) o[t][d] = f32x4{};
     }
-    uint64_t there = 0, there_next = 0;
-    int32_t row = -1, found = 0;
-    if (t0 + wave < t1) {
-      row = walk.row(t0 + wave, walk.entry(t0 + wave), &there);
-      if (t0 + wave + kFewWaves < t1) found = walk.entry(t0 + wave + kFewWaves);
-      fetch(kc, k_base, row);
-      fetch(vc, v_base, row);
-    }
-    for (int t64 = t0 + wave; t64 < t1; t64 += kFewWaves) {
-      const bool more = t64 + kFewWaves < t1;
-      f32x4 s[RT][NU];
+    uint32_t there[3];  // of this stage and the two after it
+    if (count) {
+      ask(0);
+      ask(1);
+      wait_vmcnt<0>();
+      asm volatile("" ::: "memory");
 #pragma unroll
-      for (int u = 0; u < NU; ++u) {
+      for (int st = 0; st < 2; ++st) {
+        const int32_t row = row_of(st, &there[st]);
+        bring(row, st, 0);
+        bring(row, st, 1);
+        ask(st + 2);
+      }
+    }
+    for (int st = 0; st < count; ++st) {
+      const __bf16* K = reinterpret_cast<const __bf16*>(lds[wave][st & 1][0]);
+      const __bf16* V = reinterpret_cast<const __bf16*>(lds[wave][st & 1][1]);
+      const int64_t tok0 = static_cast<int64_t>(first + st * kFewWaves) * kFewStage;
+      // K is there: after it come V, entries, K, V, entries
+      wait_vmcnt<3 * kMoves + 2>();
+      asm volatile("" ::: "memory");
+      f32x4 s[RT][2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
 #pragma unroll
         for (int t = 0; t < RT; ++t) s[t][u] = f32x4{};
 #pragma unroll
-        for (int i = 0; i < NS; ++i)
+        for (int i = 0; i < NS; ++i) {
+          const bf16x8 k = *reinterpret_cast<const bf16x8*>(K + swz256(u * 16 + n, i * 32 + g * 8));
 #pragma unroll
-          for (int t = 0; t < RT; ++t) s[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kc[u][i], qf[t][i], s[t][u], 0, 0, 0);
+          for (int t = 0; t < RT; ++t) s[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qf[t][i], s[t][u], 0, 0, 0);
+        }
       }
-      if (more) {
-        row = walk.row(t64 + kFewWaves, found, &there_next);
-        if (t64 + 2 * kFewWaves < t1) found = walk.entry(t64 + 2 * kFewWaves);
-        fetch(kc, k_base, row);
-      }
+      // V and the entries of stage st + 2 are there, K has been read: after them come K, V, entries
+      wait_vmcnt<2 * kMoves + 1>();
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      const int32_t row = row_of(st + 2, &there[2]);
+      bring(row, st & 1, 0);
       bool step = false;
-      bf16x8 pb[RT][NU / 2];
+      bf16x8 pb[RT];
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
-        // token 16 u + 4 g + i of the tile in s[t][u][i]
-        if (there != kAll) {
-          const uint64_t mine = there >> (4 * g);
+        // token 16 u + 4 g + i of the stage in s[t][u][i]
+        if (there[0] != ~0u) {
+          const uint32_t mine = there[0] >> (4 * g);
 #pragma unroll
-          for (int u = 0; u < NU; ++u)
+          for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
               if (!(mine >> (u * 16 + i) & 1)) s[t][u][i] = -INFINITY;
         }
         if constexpr (MASK) {
-          const int64_t left = static_cast<int64_t>(seen[t]) - static_cast<int64_t>(t64) * kTile;
-          if (__any(seen[t] < len && left < kTile)) {
+          const int64_t left = seen[t] - tok0;
+          if (__any(seen[t] < len && left < kFewStage)) {
             step = true;
 #pragma unroll
-            for (int u = 0; u < NU; ++u)
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
               for (int i = 0; i < 4; ++i)
                 if (u * 16 + 4 * g + i >= left) s[t][u][i] = -INFINITY;
@@ -593,7 +649,7 @@ __global__ __launch_bounds__(kFewWaves * 64) __attribute__((amdgpu_waves_per_eu(
         }
         float mx = s[t][0][0];
 #pragma unroll
-        for (int u = 0; u < NU; ++u)
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
           for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[t][u][i]);
         mx = over_row(mx, [](float x, float y) { return fmaxf(x, y); }) * c;
@@ -606,61 +662,58 @@ __global__ __launch_bounds__(kFewWaves * 64) __attribute__((amdgpu_waves_per_eu(
           for (int d = 0; d < DT; ++d) o[t][d] *= alpha;
         }
 #pragma unroll
-        for (int u = 0; u < NU; ++u)
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][u][i], c, -m[t]));
             l[t] += p;
-            pb[t][u / 2][u % 2 * 4 + i] = static_cast<__bf16>(p);
+            pb[t][u * 4 + i] = static_cast<__bf16>(p);
           }
       }
-      bool bad = false;
-      if (MASK && step) {
+      bool wild = false;
 #pragma unroll
-        for (int u = 0; u < NU; ++u)
+      for (int d = 0; d < DT; ++d) {
+        const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(V + swz256(t_row, d * 16 + t_col)));
+        const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(V + swz256(t_row + 16, d * 16 + t_col)));
+        bf16x8 vt = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        if (MASK && step) vt = tamed(vt, &wild);
 #pragma unroll
-          for (int i = 0; i < NS; ++i) bad = bad || not_finite(vc[u][i]);
+        for (int t = 0; t < RT; ++t) o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, pb[t], o[t][d], 0, 0, 0);
       }
-      const bool one_by_one = MASK && __any(bad);
-      // V in halves of 32 tokens through the wave's tile.  A wave's LDS accesses
-      // happen in their order; the fences keep the compiler to it.
-#pragma unroll
-      for (int w = 0; w < NU / 2; ++w) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int i = 0; i < NS; ++i)
-            *reinterpret_cast<bf16x8*>(V + swz256(u * 16 + n, i * 32 + g * 8)) = vc[w * 2 + u][i];
-        if (w == NU / 2 - 1 && more) fetch(vc, v_base, row);
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-#pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(V + swz256(t_row, d * 16 + t_col)));
-          const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(V + swz256(t_row + 16, d * 16 + t_col)));
-          const bf16x8 vt = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-          if (one_by_one) {
-            // the tokens one by one, each added to the rows that see it
+      if (MASK && __any(wild)) {
+        // the infinities and NaN of the values, token by token, to the rows that see them
 #pragma unroll 1
-            for (int i = 0; i < 32; ++i) {
-              const int j = i & 7, q = i >> 3, tok = w * 32 + (j >> 2) * 16 + 4 * q + (j & 3);
+        for (int tok = 0; tok < kFewStage; ++tok) {
+          const uint32_t two = *reinterpret_cast<const uint32_t*>(V + swz256(tok, (lane * 2) & (D - 1)));
+          if (!__any(wild_of(two) != 0)) continue;
 #pragma unroll
-              for (int t = 0; t < RT; ++t) {
-                const f32x4 one =
-                    __builtin_amdgcn_mfma_f32_16x16x32_bf16(only(vt, j, g == q), only(pb[t][w], j, g == q), f32x4{}, 0, 0, 0);
-                const bool sees = static_cast<int64_t>(t64) * kTile + tok < seen[t];
+          for (int t = 0; t < RT; ++t) {
+            float p = 0.f;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[t][d][e] += sees ? one[e] : 0.f;
+            for (int e = 0; e < 8; ++e) p = (e >> 2) * 16 + 4 * g + (e & 3) == tok ? static_cast<float>(pb[t][e]) : p;
+            p = __shfl(p, n + 16 * (tok >> 2 & 3));
+            const bool sees = tok0 + tok < seen[t];
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+              const bf16x4 v = *reinterpret_cast<const bf16x4*>(V + swz256(tok, d * 16 + 4 * g));
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const float f = static_cast<float>(v[e]);
+                o[t][d][e] += sees && !(__builtin_fabsf(f) < INFINITY) ? p * f : 0.f;
               }
             }
-          } else {
-#pragma unroll
-            for (int t = 0; t < RT; ++t) o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, pb[t][w], o[t][d], 0, 0, 0);
           }
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       }
-      there = there_next;
+      // V has been read
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      bring(row, st & 1, 1);
+      ask(st + 4);
+      there[0] = there[1];
+      there[1] = there[2];
     }
+    wait_vmcnt<0>();
+    asm volatile("" ::: "memory");
 
     // Join the waves: their maximum, then the scaled sums one by one.
 #pragma unroll
@@ -684,7 +737,7 @@ __global__ __launch_bounds__(kFewWaves * 64) __attribute__((amdgpu_waves_per_eu(
 #pragma unroll
       for (int d = 0; d < DT; ++d) o[t][d] *= alpha;
     }
-    f32x4* O = reinterpret_cast<f32x4*>(&lds[0][0]) + lane;
+    f32x4* O = reinterpret_cast<f32x4*>(&lds[0][0][0][0]) + lane;
     static_assert(RT * DT * 64 * 16 <= static_cast<int>(sizeof(lds)), "a wave's sums fit the V tiles' place");
     for (int w = 1; w < kFewWaves; ++w) {
       if (wave == w) {
@@ -707,6 +760,7 @@ __global__ __launch_bounds__(kFewWaves * 64) __attribute__((amdgpu_waves_per_eu(
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
         if (!ok[t]) continue;
+        const RowPlace place = row_place(a, at.seq, at.kvh, at.item * kRows + t * 16 + n, D);
         if (!whole) {
           const int64_t slot = 2 * static_cast<int64_t>(worker) + (seg > 0);
           float* P = slot_sums(a, D, slot, t * 16 + n);
@@ -714,9 +768,9 @@ __global__ __launch_bounds__(kFewWaves * 64) __attribute__((amdgpu_waves_per_eu(
           for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(P + d * 16 + 4 * g) = o[t][d];
           if (g == 0) *slot_stats(a, D, slot, t * 16 + n) = make_float2(m[t], l[t]);
         } else {
-          const float prior = a.prior_lse ? a.prior_lse[place[t].lse] : 0.f;
+          const float prior = a.prior_lse ? a.prior_lse[place.lse] : 0.f;
 #pragma unroll
-          for (int d = 0; d < DT; ++d) write_joined(a, place[t], m[t], l[t], prior, o[t][d], d * 16 + 4 * g);
+          for (int d = 0; d < DT; ++d) write_joined(a, place, m[t], l[t], prior, o[t][d], d * 16 + 4 * g);
         }
       }
     }

@@ -28,7 +28,8 @@ hipError_t plan_paged_attention(int64_t tokens, int32_t batch, int32_t max_chunk
   if (tiles > p.least) p.workers = static_cast<int32_t>(std::max<int64_t>(1, std::min(slots, items * tiles / p.least)));
   p.blocks = p.workers ? p.workers : items;
   if (!launchable(p.blocks, p.threads())) return hipErrorInvalidValue;
-  p.join_rows = p.waves ? 8 : 1;
+  // few items are in many slots each: a block takes one row of them, else eight
+  p.join_rows = p.waves || p.workers <= 16 * items ? 8 : 1;
   p.workspace_bytes = int64_t{2} * p.workers * p.slot_rows * (head_dim + 2) * 4;
   *plan = p;
   return hipSuccess;
