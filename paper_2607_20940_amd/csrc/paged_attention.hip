@@ -20,6 +20,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "attend_parts.hpp"
 #include "lds_stage.hpp"
@@ -198,13 +199,13 @@ __device__ inline uint32_t wild_of(uint32_t two) {
   return ((two & 0x7f80u) == 0x7f80u ? two & 0xffffu : 0u) | ((two & 0x7f800000u) == 0x7f800000u ? two & 0xffff0000u : 0u);
 }
 
-// v without its infinities and NaN; `wild` collects whether it had any.
-__device__ inline bf16x8 tamed(bf16x8 v, bool* wild) {
+// v without its infinities and NaN; `wild` collects their bits.
+__device__ inline bf16x8 tamed(bf16x8 v, uint32_t* wild) {
   u32x4 w = __builtin_bit_cast(u32x4, v);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const uint32_t x = wild_of(w[i]);
-    *wild = *wild || x != 0;
+    *wild |= x;
     w[i] ^= x;
   }
   return __builtin_bit_cast(bf16x8, w);
@@ -218,16 +219,26 @@ __device__ inline bf16x8 tamed(bf16x8 v, bool* wild) {
 // barrier ends each phase.  Tiles come by direct transfers, issued in the
 // softmax phase and waited for at its end: the first group brings K, the second
 // V.  Four waves (fewer rows) are one group that brings both; two such blocks
-// share a CU.
+// share a CU.  The first kLead operands of a matrix phase are read at the end of
+// the softmax phase before it, the others kLead ahead.
 //
 // With phases counted from the first group's S of tile t in 2 t: K of tile t + 1
 // is brought in 2 t + 1 and read in 2 t + 2 and 2 t + 3, V of tile t + 1 brought
-// in 2 t + 2 (four waves: 2 t + 1) and read in 2 t + 4 and 2 t + 5, each into the
+// in 2 t + 2 (four waves: 2 t + 1) and read in 2 t + 3 to 2 t + 5, each into the
 // buffer whose tile (two before) was last read in 2 t - 1 and 2 t + 1 (2 t).
+//
+// The maximum is taken only where a lane's 32 exponentials against the running
+// one pass 2^8 in sum (no single one can have stayed below): most tiles spend
+// a fused multiply-add, an exponential and an addition per score.
+constexpr int kLead = 4;
+constexpr float kRescaleSum = 256.f;  // 2^kRescaleLog2
+
 template <int D, int NW, bool MASK>
-__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) void attn_kernel(PagedAttnArgs a) {
+__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_kernel(PagedAttnArgs a) {
   constexpr int KS = D / 16, DB = D / 32, kTileElems = kTile * 128;  // 256-byte rows for both D
-  __shared__ __attribute__((aligned(16))) __bf16 lds[2][2][kTileElems];  // [buffer][K | V]
+  using T_ = std::true_type;
+  using F_ = std::false_type;
+  __shared__ __attribute__((aligned(16))) __bf16 lds[2][2][kTileElems];  // [K | V][buffer]
 
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, hh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), second = NW == 8 ? wave >> 2 : 0;
@@ -240,15 +251,21 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
   Spot at = locate(a, x0);
   if (at.b < 0) return;
 
-  // Transfers: a wave instruction fills four rows of 256 bytes, lane l bytes
-  // 16 l, i.e. row l / 16, whose chunk l % 16 holds chunk t_lc ^ i of the token.
-  const int t_lc = (lane & 15) ^ ((lane >> 4) << 2);
+  // Transfers: wave instruction i fills four rows of 256 bytes, lane l bytes 16 l,
+  // i.e. row l / 16, whose chunk l % 16 holds chunk (l % 16) ^ 4 (l / 16) ^ i.
   const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(&lds[0][0][0]));
   const int64_t row_bytes = static_cast<int64_t>(a.kv_heads) * D * 2;
   const float c = a.scale_log2e;
+  // Operands: K rows 32 kb + n, columns 16 ks + 8 hh; V rows R + t_row (+ 8 for
+  // the upper half), columns 32 db + t_col, R a multiple of 16.
   const int k_rd = swz256(n, hh * 8);
   const int t_row = 4 * (lane >> 5) + ((lane & 15) >> 2);
   const int t_col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+  int v_rd[DB][2];
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) v_rd[db][h] = swz256(t_row + 8 * h, db * 32 + t_col);
   auto phase_end = [&]() {
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
@@ -267,12 +284,16 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
     const PageWalk walk = walk_of(a, at.b, len);
     const char* const k_base = static_cast<const char*>(a.k_pages) + static_cast<int64_t>(at.kvh) * D * 2;
     const char* const v_base = static_cast<const char*>(a.v_pages) + static_cast<int64_t>(at.kvh) * D * 2;
-    // A wave brings rows 16 (wave & 3) .. + 15 of its group's tiles.
+    // A wave brings rows 16 (wave & 3) .. + 15 of its group's tiles.  What its
+    // addresses are made of is worked out anew for every tile: kept, it would
+    // cost more registers than there are.
     auto bring = [&](int32_t row, int buf) {
+      int ln = lane;
+      asm volatile("" : "+v"(ln));
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int chunk = t_lc ^ i;
-        const int32_t r = of_lane(row, (wave & 3) * 16 + i * 4 + (lane >> 4));
+        const int chunk = (ln & 15) ^ ((ln >> 4) << 2) ^ i;
+        const int32_t r = of_lane(row, (wave & 3) * 16 + i * 4 + (ln >> 4));
         const bool there = r >= 0 && (D == 128 || chunk < D / 8);
         const int64_t off = static_cast<int64_t>(r) * row_bytes + chunk * 16;
         const char* const zero = reinterpret_cast<const char*>(zero_row) + chunk * 16;
@@ -280,7 +301,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
         for (int is_v = 0; is_v < 2; ++is_v) {
           if (NW == 8 && is_v != second) continue;
           gdma16(there ? (is_v ? v_base : k_base) + off : zero,
-                 __builtin_amdgcn_readfirstlane(lds0 + ((buf * 2 + is_v) * kTile + (wave & 3) * 16 + i * 4) * 256));
+                 __builtin_amdgcn_readfirstlane(lds0 + ((is_v * 2 + buf) * kTile + (wave & 3) * 16 + i * 4) * 256));
         }
       }
     };
@@ -303,19 +324,74 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
 #pragma unroll
     for (int db = 0; db < DB; ++db) o[db] = f32x16{};
     float m = kNoMax, l = 0.f;  // running maximum (base 2), this lane's share of the sum
-    bf16x8 pb[2][2];
-    bool step = false;  // the tile of pb has a step of the mask
-    auto v_operand = [&](int buf, int kb, int cc, int db) {
-      const __bf16* r0 = lds[buf][1] + (kb * 32 + cc * 16) * 128;
-      const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(r0 + swz256(t_row, db * 32 + t_col)));
-      const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(r0 + swz256(t_row + 8, db * 32 + t_col)));
-      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    bf16x8 pb[2][2], ring[kLead];
+
+    // Operand i of a matrix phase: with pv the V^T operands of O += P V (key block
+    // kb, 16-key half cc, dims db), then the K operands of S (k-step ks, kb).
+    auto operand = [&](auto pv, int i, int vb, int kbuf) -> bf16x8 {
+      constexpr int NPV = decltype(pv)::value ? 4 * DB : 0;
+      if (i < NPV) {
+        const int db = i % DB;
+        const __bf16* r0 = &lds[1][vb][(i / DB) * 16 * 128];
+        const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(r0 + v_rd[db][0]));
+        const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(r0 + v_rd[db][1]));
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      }
+      const int j = i - NPV, ks = j / 2, kb = j % 2;
+      return *reinterpret_cast<const bf16x8*>(&lds[0][kbuf][kb * 32 * 128 + (k_rd ^ (ks * 16))]);
     };
-    // The infinities and NaN of tile t's values, token by token, to the rows that see them.
-    auto add_wild = [&](int buf, int t) {
+    auto prefill = [&](auto pv, int vb, int kbuf) {
+#pragma unroll
+      for (int i = 0; i < kLead; ++i) ring[i] = operand(pv, i, vb, kbuf);
+    };
+    auto mstep = [&](auto pv, auto sc, int vb, int kbuf) {
+      constexpr int NPV = decltype(pv)::value ? 4 * DB : 0, N = NPV + (decltype(sc)::value ? KS * 2 : 0);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const bf16x8 av = ring[i % kLead];
+        if (i < NPV) {
+          const int st = i / DB, db = i % DB;
+          o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av, pb[st >> 1][st & 1], o[db], 0, 0, 0);
+        } else {
+          const int j = i - NPV, ks = j / 2, kb = j % 2;
+          s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av, qf[ks], ks == 0 ? f32x16{} : s[kb], 0, 0, 0);
+        }
+        if (i + kLead < N) ring[i % kLead] = operand(pv, i + kLead, vb, kbuf);
+      }
+      // each read kLead instructions before its use: a V operand is two reads
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        if (i + kLead < N) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        if (i + kLead < NPV) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    // O += P V of tile t, which may have a step of the mask: without its infinities
+    // and NaN.  Those are noted, token by token, for the rows that see them: a bit
+    // for each of the lane's sums that they send up and one for down, both for a
+    // NaN.
+    uint64_t up = 0, down = 0;
+    auto add_pv_step = [&](int vb, int t) {
+      uint32_t wild = 0;
+      int at_row = t_row;
+      asm volatile("" : "+v"(at_row));  // addresses of this path's own: none is kept from outside it
+#pragma unroll
+      for (int i = 0; i < 4 * DB; ++i) {
+        const int db = i % DB, st = i / DB;
+        const __bf16* r0 = &lds[1][vb][st * 16 * 128];
+        const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(r0 + swz256(at_row, db * 32 + t_col)));
+        const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(r0 + swz256(at_row + 8, db * 32 + t_col)));
+        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tamed(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), &wild),
+                                                        pb[st >> 1][st & 1], o[db], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (!__any(wild != 0)) return;
 #pragma unroll 1
       for (int tok = 0; tok < kTile; ++tok) {
-        const __bf16* V = lds[buf][1];
+        int half = hh;
+        asm volatile("" : "+v"(half));
+        const __bf16* V = lds[1][vb];
         const uint32_t two = *reinterpret_cast<const uint32_t*>(V + swz256(tok, (lane * 2) & (D - 1)));
         if (!__any(wild_of(two) != 0)) continue;
         // P of the token, from the half wave that holds it
@@ -323,61 +399,28 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) p = kb * 32 + 8 * (e >> 2) + 4 * hh + (e & 3) == tok ? static_cast<float>(pb[kb][e >> 3][e & 7]) : p;
+          for (int e = 0; e < 16; ++e)
+            if (kb * 32 + 8 * (e >> 2) + (e & 3) == (tok & ~4)) p = static_cast<float>(pb[kb][e >> 3][e & 7]);
         p = __shfl(p, n + 32 * (tok >> 2 & 1));
-        const bool sees = static_cast<int64_t>(t) * kTile + tok < seen;
+        const bool sees = t * kTile + tok < seen, some = p > 0.f;
+#pragma unroll 1
+        for (int q = 0; q < DB * 4; ++q) {
+          const uint2 v = *reinterpret_cast<const uint2*>(V + swz256(tok, q * 8 + 4 * half));
+          uint32_t u = 0, d = 0;
 #pragma unroll
-        for (int db = 0; db < DB; ++db)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const bf16x4 v = *reinterpret_cast<const bf16x4*>(V + swz256(tok, db * 32 + 8 * j + 4 * hh));
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float f = static_cast<float>(v[i]);
-              const bool wild = !(__builtin_fabsf(f) < INFINITY);
-              o[db][4 * j + i] += sees && wild ? p * f : 0.f;
-            }
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t x = (i < 2 ? v.x : v.y) >> (16 * (i & 1)) & 0xffffu;
+            const bool is = sees && (x & 0x7f80u) == 0x7f80u, both = (x & 0x7fu) || !some;
+            u |= is && (both || !(x & 0x8000u)) ? 1u << i : 0u;
+            d |= is && (both || (x & 0x8000u)) ? 1u << i : 0u;
           }
+          up |= static_cast<uint64_t>(u) << (4 * q);
+          down |= static_cast<uint64_t>(d) << (4 * q);
+        }
       }
     };
-    auto add_pv = [&](int buf, int t) {
-      if (MASK && step) {
-        bool wild = false;
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-          for (int cc = 0; cc < 2; ++cc)
-#pragma unroll
-            for (int db = 0; db < DB; ++db) {
-              o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tamed(v_operand(buf, kb, cc, db), &wild), pb[kb][cc], o[db], 0, 0, 0);
-              __builtin_amdgcn_sched_barrier(0);
-            }
-        if (__any(wild)) add_wild(buf, t);
-        return;
-      }
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int cc = 0; cc < 2; ++cc)
-#pragma unroll
-          for (int db = 0; db < DB; ++db)
-            o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand(buf, kb, cc, db), pb[kb][cc], o[db], 0, 0, 0);
-      // operand reads a few products ahead, not all of them at once (registers)
-      interleave<DB * 4, DB * 8, DB * 3>();
-    };
-    auto scores = [&](int buf) {
-      const __bf16* Ks = lds[buf][0];
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-        s[kb] = f32x16{};
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks)
-          s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(Ks + kb * 32 * 128 + (k_rd ^ (ks * 16))),
-                                                          qf[ks], s[kb], 0, 0, 0);
-      }
-      interleave<KS * 2, KS * 2, 6>();
-    };
-    auto softmax = [&](int t, uint64_t there) {
+    // masked: the tile may have a step of the mask
+    auto softmax = [&](auto masked, int t, uint64_t there) {
       // token kb * 32 + 8 (e / 4) + 4 hh + e % 4 of the tile in s[kb][e]
       if (there != kAll) {
         const uint64_t mine = there >> (4 * hh);
@@ -387,41 +430,53 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
           for (int e = 0; e < 16; ++e)
             if (!(mine >> (kb * 32 + 8 * (e >> 2) + (e & 3)) & 1)) s[kb][e] = -INFINITY;
       }
-      if constexpr (MASK) {
-        const int64_t left = static_cast<int64_t>(seen) - static_cast<int64_t>(t) * kTile;
-        step = __any(seen < len && left < kTile);
-        if (step) {
+      if constexpr (decltype(masked)::value) {
+        const int left = seen - t * kTile - 4 * hh;
 #pragma unroll
-          for (int kb = 0; kb < 2; ++kb)
+        for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-            for (int e = 0; e < 16; ++e)
-              if (kb * 32 + 8 * (e >> 2) + 4 * hh + (e & 3) >= left) s[kb][e] = -INFINITY;
-        }
+          for (int e = 0; e < 16; ++e)
+            if (kb * 32 + 8 * (e >> 2) + (e & 3) >= left) s[kb][e] = -INFINITY;
       }
-      float mx = s[0][0];
+      auto exps = [&]() {
+        float ls[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int e = 0; e < 16; e += 2) {
+            const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][e], c, -m));
+            const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][e + 1], c, -m));
+            ls[(e >> 1) & 3] += p0 + p1;
+            pb[kb][e >> 3][e & 7] = static_cast<__bf16>(p0);
+            pb[kb][e >> 3][(e & 7) + 1] = static_cast<__bf16>(p1);
+          }
+        return (ls[0] + ls[1]) + (ls[2] + ls[3]);
+      };
+      float lt = exps();
+      if (__any(!(lt <= kRescaleSum))) {  // also true for infinite and NaN sums
+        float mx = s[0][0];
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[kb][e]);
+        mx = fmaxf(mx, other_half(mx)) * c;  // the scale is positive
+        if (__any(mx > m + kRescaleLog2)) {
+          const float mn = fmaxf(m, mx);
+          const float alpha = __builtin_amdgcn_exp2f(m - mn);
+          m = mn;
+          l *= alpha;
+#pragma unroll
+          for (int db = 0; db < DB; ++db) o[db] *= alpha;
+        }
+        lt = exps();
+      }
+      l += lt;
+      // the exponentials stay in this phase: they are not to sink into the matrix phase
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[kb][e]);
-      mx = fmaxf(mx, other_half(mx)) * c;  // the scale is positive
-      if (__any(mx > m + kRescaleLog2)) {
-        const float mn = fmaxf(m, mx);
-        const float alpha = __builtin_amdgcn_exp2f(m - mn);
-        m = mn;
-        l *= alpha;
-#pragma unroll
-        for (int db = 0; db < DB; ++db) o[db] *= alpha;
-      }
-      float ls[2] = {0.f, 0.f};
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][e], c, -m));
-          ls[e & 1] += p;
-          pb[kb][e >> 3][e & 7] = static_cast<__bf16>(p);
-        }
-      l += ls[0] + ls[1];
+        for (int h = 0; h < 2; ++h) asm volatile("" : "+v"(pb[kb][h]));
+      asm volatile("" : "+v"(l));
     };
 
     if (t0 < t1) {
@@ -433,28 +488,77 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
       wait_vmcnt<0>();
       phase_end();
       if (second) phase_end();
-      for (int t = t0;; ++t) {
-        const int buf = (t - t0) & 1;
-        // the wave whose turn at the matrix core it is goes first elsewhere too
-        __builtin_amdgcn_s_setprio(1);
-        if (t > t0) add_pv(buf ^ 1, t - 1);
-        if (t == t1) break;
-        scores(buf);
-        __builtin_amdgcn_s_setprio(0);
+      // The softmax phase of tile t in buffer buf: the next tile comes, the first
+      // operands of the next matrix phase are read.
+      auto sphase = [&](auto masked, auto next, int t, int buf) {
         phase_end();
         if (t + 1 < t1) {
           bring(walk.row(t + 1, found, &there_next), buf ^ 1);
           if (t + 2 < t1) found = walk.entry(t + 2);
         }
-        softmax(t, there);
+        softmax(masked, t, there);
         there = there_next;
+        if constexpr (decltype(next)::value) prefill(T_{}, buf, buf ^ 1);
         wait_vmcnt<0>();
         phase_end();
+      };
+      auto mphase = [&](auto pv, auto sc, int vb, int kbuf) {
+        __builtin_amdgcn_s_setprio(2);
+        mstep(pv, sc, vb, kbuf);
+        __builtin_amdgcn_s_setprio(0);
+      };
+      // Tiles before `plain` have no step of the mask, for no row of the item.
+      int plain = t1;
+      if constexpr (MASK) {
+        const int low = at.seq.seen(at.item * (NW * 32) / a.group, a.mask_block);
+        if (low < len && low / kTile < plain) plain = low / kTile > t0 ? low / kTile : t0;
       }
-      __builtin_amdgcn_s_setprio(0);
+      prefill(F_{}, 0, 0);
+      mphase(F_{}, T_{}, 0, 0);
+      // two tiles at a time: their buffers are constants
+      int t = t0, buf = 0;
+      for (; t + 2 < plain; t += 2) {
+        sphase(F_{}, T_{}, t, 0);
+        mphase(T_{}, T_{}, 0, 1);
+        sphase(F_{}, T_{}, t + 1, 1);
+        mphase(T_{}, T_{}, 1, 0);
+      }
+      if constexpr (!MASK) {
+        if (t + 1 < t1) {
+          sphase(F_{}, T_{}, t, 0);
+          mphase(T_{}, T_{}, 0, 1);
+          buf = 1;
+          ++t;
+        }
+        sphase(F_{}, T_{}, t, buf);
+        mphase(T_{}, F_{}, buf, buf ^ 1);
+      } else {
+        for (;; ++t, buf ^= 1) {
+          sphase(T_{}, F_{}, t, buf);
+          __builtin_amdgcn_s_setprio(2);
+          add_pv_step(buf, t);
+          if (t + 1 < t1) {
+            prefill(F_{}, 0, buf ^ 1);
+            mstep(F_{}, T_{}, 0, buf ^ 1);
+          }
+          __builtin_amdgcn_s_setprio(0);
+          if (t + 1 == t1) break;
+        }
+      }
       if (NW == 8 && !second) phase_end();
     }
     l += other_half(l);
+    if constexpr (MASK) {
+      if (__any((up | down) != 0)) {
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            if (up >> (db * 16 + e) & 1) o[db][e] += INFINITY;
+            if (down >> (db * 16 + e) & 1) o[db][e] -= INFINITY;
+          }
+      }
+    }
     // dims 32 db + 8 j + 4 hh .. + 3 of the row
     if (ok) {
       const RowPlace row = row_place(a, at.seq, at.kvh, r, D);
@@ -670,7 +774,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_rows_kernel(PagedAttnArgs 
             pb[t][u * 4 + i] = static_cast<__bf16>(p);
           }
       }
-      bool wild = false;
+      uint32_t wild = 0;
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
         const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(V + swz256(t_row, d * 16 + t_col)));
@@ -680,7 +784,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_rows_kernel(PagedAttnArgs 
 #pragma unroll
         for (int t = 0; t < RT; ++t) o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, pb[t], o[t][d], 0, 0, 0);
       }
-      if (MASK && __any(wild)) {
+      if (MASK && __any(wild != 0)) {
         // the infinities and NaN of the values, token by token, to the rows that see them
 #pragma unroll 1
         for (int tok = 0; tok < kFewStage; ++tok) {
