@@ -239,6 +239,9 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
   using T_ = std::true_type;
   using F_ = std::false_type;
   __shared__ __attribute__((aligned(16))) __bf16 lds[2][2][kTileElems];  // [K | V][buffer]
+  __shared__ const char* where[2][2][NW * kTile];                        // [run & 1][K | V][token]
+  __shared__ uint64_t masks[2][NW];
+  __shared__ int32_t entries[NW * kTile];
 
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, hh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), second = NW == 8 ? wave >> 2 : 0;
@@ -254,7 +257,8 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
   // Transfers: wave instruction i fills four rows of 256 bytes, lane l bytes 16 l,
   // i.e. row l / 16, whose chunk l % 16 holds chunk (l % 16) ^ 4 (l / 16) ^ i.
   const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(&lds[0][0][0]));
-  const int64_t row_bytes = static_cast<int64_t>(a.kv_heads) * D * 2;
+  const uint32_t entries0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(&entries[0]));
+  const uint32_t row_bytes = static_cast<uint32_t>(a.kv_heads) * D * 2;
   const float c = a.scale_log2e;
   // Operands: K rows 32 kb + n, columns 16 ks + 8 hh; V rows R + t_row (+ 8 for
   // the upper half), columns 32 db + t_col, R a multiple of 16.
@@ -284,26 +288,46 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
     const PageWalk walk = walk_of(a, at.b, len);
     const char* const k_base = static_cast<const char*>(a.k_pages) + static_cast<int64_t>(at.kvh) * D * 2;
     const char* const v_base = static_cast<const char*>(a.v_pages) + static_cast<int64_t>(at.kvh) * D * 2;
-    // A wave brings rows 16 (wave & 3) .. + 15 of its group's tiles.  What its
-    // addresses are made of is worked out anew for every tile: kept, it would
-    // cost more registers than there are.
-    auto bring = [&](int32_t row, int buf) {
-      int ln = lane;
+    // Where the tokens' rows lie: `where` holds the addresses of K and V for two
+    // runs of NW tiles, a thread a token and a wave a tile, of zeros for tokens
+    // that are not there; `masks` has a bit for those that are.  The page table's
+    // entries of the run after this one come by direct transfers at its first tile,
+    // and are turned into addresses at the second: the loop itself, whose vector
+    // unit the softmax fills, only reads them.
+    auto run_token = [&](int run) { return static_cast<uint32_t>(t0 + run * NW) * kTile + tid; };
+    auto ask_run = [&](int run) {
+      const uint32_t tok = min(run_token(run), walk.len - 1);
+      gdma4(walk.table + walk.page.quotient(tok), __builtin_amdgcn_readfirstlane(entries0 + wave * 256));
+    };
+    auto make_run = [&](int run) {
+      const int32_t found = entries[tid];
+      const uint32_t tok = min(run_token(run), walk.len - 1);
+      const bool is = run_token(run) < walk.len && found >= 0 && found < walk.pages;
+      const uint64_t row = static_cast<uint32_t>(found) * walk.page.d + (tok - walk.page.quotient(tok) * walk.page.d);
+      where[run & 1][0][tid] = is ? k_base + row * row_bytes : reinterpret_cast<const char*>(zero_row);
+      where[run & 1][1][tid] = is ? v_base + row * row_bytes : reinterpret_cast<const char*>(zero_row);
+      const uint64_t mask = __ballot(is);
+      if (lane == 0) masks[run & 1][wave] = mask;
+    };
+    // A wave brings rows 16 (wave & 3) .. + 15 of its group's tiles; returns the tile's mask.
+    auto bring = [&](int t, int buf) -> uint64_t {
+      const int half = (t - t0) / NW & 1, in = (t - t0) % NW;
+      int ln = lane;  // what the addresses are made of is worked out anew: kept, it would cost more registers than there are
       asm volatile("" : "+v"(ln));
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int chunk = (ln & 15) ^ ((ln >> 4) << 2) ^ i;
-        const int32_t r = of_lane(row, (wave & 3) * 16 + i * 4 + (ln >> 4));
-        const bool there = r >= 0 && (D == 128 || chunk < D / 8);
-        const int64_t off = static_cast<int64_t>(r) * row_bytes + chunk * 16;
-        const char* const zero = reinterpret_cast<const char*>(zero_row) + chunk * 16;
+      for (int is_v = 0; is_v < 2; ++is_v) {
+        if (NW == 8 && is_v) break;
+        const int what = NW == 8 ? second : is_v;
+        const char* const* const from = &where[half][what][in * kTile + (wave & 3) * 16 + (ln >> 4)];
 #pragma unroll
-        for (int is_v = 0; is_v < 2; ++is_v) {
-          if (NW == 8 && is_v != second) continue;
-          gdma16(there ? (is_v ? v_base : k_base) + off : zero,
-                 __builtin_amdgcn_readfirstlane(lds0 + ((is_v * 2 + buf) * kTile + (wave & 3) * 16 + i * 4) * 256));
+        for (int i = 0; i < 4; ++i) {
+          // 64-dim rows are half as long: their chunks fill the LDS rows' unused half too
+          const int chunk = ((ln & 15) ^ ((ln >> 4) << 2) ^ i) & (D / 8 - 1);
+          gdma16(from[i * 4] + chunk * 16, __builtin_amdgcn_readfirstlane(lds0 + ((what * 2 + buf) * kTile + (wave & 3) * 16 + i * 4) * 256));
         }
       }
+      const uint64_t mask = masks[half][in];
+      return static_cast<uint64_t>(uniform(static_cast<uint32_t>(mask >> 32))) << 32 | uniform(static_cast<uint32_t>(mask));
     };
 
     const int r_in = wave * 32 + n, r = at.item * (NW * 32) + r_in;
@@ -480,11 +504,13 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
     };
 
     if (t0 < t1) {
-      uint64_t there, there_next = 0;
-      int32_t found = walk.entry(t0);
       if (seg > 0) phase_end();  // the last item's V has been read by all
-      bring(walk.row(t0, found, &there), 0);
-      if (t0 + 1 < t1) found = walk.entry(t0 + 1);
+      ask_run(0);
+      wait_vmcnt<0>();
+      asm volatile("" ::: "memory");
+      make_run(0);
+      phase_end();
+      uint64_t there = bring(t0, 0), there_next = 0;
       wait_vmcnt<0>();
       phase_end();
       if (second) phase_end();
@@ -492,10 +518,12 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
       // operands of the next matrix phase are read.
       auto sphase = [&](auto masked, auto next, int t, int buf) {
         phase_end();
-        if (t + 1 < t1) {
-          bring(walk.row(t + 1, found, &there_next), buf ^ 1);
-          if (t + 2 < t1) found = walk.entry(t + 2);
-        }
+        if (t + 1 < t1) there_next = bring(t + 1, buf ^ 1);
+        const int in = (t - t0) % NW;
+        if (in == 0 && t + NW < t1)
+          ask_run((t - t0) / NW + 1);
+        else if (in == 1 && t + NW - 1 < t1)
+          make_run((t - t0) / NW + 1);
         softmax(masked, t, there);
         there = there_next;
         if constexpr (decltype(next)::value) prefill(T_{}, buf, buf ^ 1);
