@@ -313,11 +313,14 @@ mssa_status mssa_paged_attention(const mssa_paged_attention_desc* desc, const vo
     a.kv_heads = desc->kv_heads;
     a.group = desc->q_heads / desc->kv_heads;
     a.table_pages = desc->table_pages;
-    a.mask_block = desc->mask_block;
-    a.slot_rows = plan.slot_rows;
+    a.mask_block = std::min(desc->mask_block, int32_t{1} << 30);
+    while (a.slot_rows() < plan.slot_rows) ++a.slot_shift;
     a.workers = plan.workers;
+    a.unit_shift = plan.unit_shift;
     a.least = plan.least;
     a.page = mssa::Divisor::of(static_cast<uint32_t>(desc->page_tokens));
+    a.by_group = mssa::Divisor::of(static_cast<uint32_t>(a.group));
+    a.by_mask = mssa::Divisor::of(static_cast<uint32_t>(std::max(1, a.mask_block)));
     const double scale = desc->softmax_scale > 0.f ? static_cast<double>(desc->softmax_scale)
                                                    : 1.0 / std::sqrt(static_cast<double>(desc->head_dim));
     a.scale_log2e = static_cast<float>(scale * 1.4426950408889634);

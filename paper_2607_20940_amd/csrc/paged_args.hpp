@@ -75,47 +75,51 @@ struct PagedAttnArgs {
   int64_t q_stride, lse_stride, pages, capacity;  // capacity: tokens that a row of the table can name
   int32_t tokens, batch, each, max_chunk;
   int32_t q_heads, kv_heads, group, table_pages;
-  int32_t mask_block;
-  int32_t slot_rows;  // query rows of an item
-  int32_t workers;    // shares of all items' contexts, 0: an item a block and no joining launch
-  int32_t least;      // units of a share at least
-  Divisor page;
+  int32_t mask_block;  // at most 2^30: no chunk is longer
+  int32_t slot_shift;  // an item has 2^slot_shift query rows
+  int32_t workers;     // shares of all items' contexts, 0: an item a block and no joining launch
+  int32_t unit_shift;  // a tile weighs 2^unit_shift units
+  int32_t least;       // units of a share at least
+  Divisor page, by_group, by_mask;
   float scale_log2e;
+  MSSA_HOST_DEVICE int32_t slot_rows() const { return 1 << slot_shift; }
 };
 
 // One sequence's work.  Its query rows (chunk token, head of the group) that
 // share a key head are cut into items of slot_rows rows; an item reads the
 // tiles up to the last index that its last row sees.  Items are weighed in
-// units, linear in their number so that sums have a closed form: a tile each
-// where there is no mask, and up to the mask's steps where there is one.  Every
-// item has a unit at least, also one without keys, whose rows are written
-// all the same.
+// units of a fraction of a tile, linear in their number so that sums have a
+// closed form: their tiles where there is no mask, and where there is one, up to
+// its steps.  Every item has units, also one without keys, whose rows are
+// written all the same.
 struct PagedSeq {
   int32_t first, n;  // chunk: first row, tokens (at most max_chunk)
   int32_t len;       // cache indices in use
-  int64_t start;     // cache index of the chunk's first token (negative where the cache is shorter than the chunk)
+  int32_t start;     // cache index of the chunk's first token (negative where the cache is shorter than the chunk)
   int32_t rows, items;
   uint32_t cost0, step;  // item i weighs cost0 + i step
 
   // Cache indices below this one are seen by chunk token i.
-  MSSA_HOST_DEVICE int32_t seen(int32_t i, int32_t mask_block) const {
-    if (!mask_block) return len;
-    const int64_t end = start + (static_cast<int64_t>(i / mask_block) + 1) * mask_block;
+  MSSA_HOST_DEVICE int32_t seen(int32_t i, const PagedAttnArgs& a) const {
+    if (!a.mask_block) return len;
+    const int64_t end = static_cast<int64_t>(start) + (a.by_mask.quotient(i) + 1) * static_cast<uint32_t>(a.mask_block);
     return end < 0 ? 0 : end < len ? static_cast<int32_t>(end) : len;
   }
   MSSA_HOST_DEVICE int32_t tiles(int32_t item, const PagedAttnArgs& a) const {
-    const int64_t past = (static_cast<int64_t>(item) + 1) * a.slot_rows;
-    const int32_t last = (past < rows ? static_cast<int32_t>(past) : rows) - 1;
-    return static_cast<int32_t>((static_cast<int64_t>(seen(last / a.group, a.mask_block)) + kPagedTile - 1) / kPagedTile);
+    const int32_t past = (item + 1) << a.slot_shift, last = (past < rows ? past : rows) - 1;
+    const uint32_t end = a.mask_block ? seen(a.by_group.quotient(last), a) : len;
+    return static_cast<int32_t>((end + (kPagedTile - 1)) / kPagedTile);
   }
   MSSA_HOST_DEVICE uint32_t cost(int32_t item) const { return cost0 + static_cast<uint32_t>(item) * step; }
-  // Units of a key head's items before this one.
+  // Units of a key head's items before this one (all of a call's are fewer than
+  // 2^31, so that the items' pairs are where step is not 0).
   MSSA_HOST_DEVICE uint32_t before(int32_t item) const {
-    const uint64_t i = static_cast<uint64_t>(item);
-    return static_cast<uint32_t>(i * cost0 + (item > 0 ? i * (i - 1) / 2 * step : 0));
+    const uint32_t i = static_cast<uint32_t>(item);
+    return i * cost0 + (step ? i * (i - 1) / 2 * step : 0);
   }
   // The item that unit x of a key head belongs to.
   MSSA_HOST_DEVICE int32_t item_of(uint32_t x) const {
+    if (!step) return static_cast<int32_t>(x / cost0);
     int32_t lo = 0, hi = items - 1;
     while (lo < hi) {
       const int32_t mid = lo + (hi - lo + 1) / 2;
@@ -129,33 +133,36 @@ struct PagedSeq {
   MSSA_HOST_DEVICE static PagedSeq of(const PagedAttnArgs& a, int32_t b) {
     PagedSeq s;
     const ChunkRows c = ChunkRows::of(a.chunk_begin, b, a.each, a.tokens);
-    const int64_t all = a.kv_len[b], n = c.end - c.first;
+    const int32_t held = a.kv_len[b], all = held < 0 ? 0 : held, n = c.end - c.first;  // an empty cache is seen by none
     s.first = c.first;
     s.start = all - n;
-    s.n = n < a.max_chunk ? static_cast<int32_t>(n) : a.max_chunk;
-    s.len = all < 0 ? 0 : static_cast<int32_t>(all < a.capacity ? all : a.capacity);
+    s.n = n < a.max_chunk ? n : a.max_chunk;
+    s.len = all < a.capacity ? all : static_cast<int32_t>(a.capacity);
     s.rows = s.n * a.group;
-    s.items = (s.rows + a.slot_rows - 1) / a.slot_rows;
+    s.items = (s.rows + a.slot_rows() - 1) >> a.slot_shift;
     s.cost0 = 1;
     s.step = 0;
     if (a.workers && s.items) {
-      const uint32_t low = s.tiles(0, a), high = s.items > 1 ? s.tiles(s.items - 1, a) : low;
+      const uint32_t low = static_cast<uint32_t>(s.tiles(0, a)) << a.unit_shift;
       s.cost0 = low ? low : 1;
-      if (high > s.cost0) s.step = (high - s.cost0) / static_cast<uint32_t>(s.items - 1);
+      if (a.mask_block && s.items > 1) {
+        const uint32_t high = static_cast<uint32_t>(s.tiles(s.items - 1, a)) << a.unit_shift;
+        if (high > s.cost0) s.step = (high - s.cost0) / static_cast<uint32_t>(s.items - 1);
+      }
     }
     return s;
   }
   MSSA_HOST_DEVICE uint32_t head_units() const { return before(items); }
-  // First tile of unit u (of cost) of an item with `tiles` tiles.
+  // First tile of unit u (of cost) of an item with `tiles` tiles: u tiles / cost,
+  // rounded the same way wherever it is asked for; all of them at u = cost.
   MSSA_HOST_DEVICE static int32_t tile_at(uint32_t u, int32_t tiles, uint32_t cost) {
-    return static_cast<uint32_t>(tiles) == cost ? static_cast<int32_t>(u)
-                                                : static_cast<int32_t>(static_cast<uint64_t>(u) * static_cast<uint32_t>(tiles) / cost);
+    return static_cast<int32_t>(static_cast<double>(u) * static_cast<double>(tiles) / static_cast<double>(cost));
   }
 };
 
 struct PagedAttnPlan {
   int32_t waves;      // 32 rows each in a block; 0: the kernel for few rows
-  int32_t slot_rows, workers, least;
+  int32_t slot_rows, workers, unit_shift, least;
   int64_t blocks, workspace_bytes;
   int32_t join_rows;  // rows of a block of the joining launch
   int32_t threads() const { return (waves ? waves : kPagedFewWaves) * 64; }

@@ -46,34 +46,20 @@ constexpr uint64_t kAll = ~uint64_t{0};
 // first item of worker i and 2 i + 1 for a later one (which then is its last),
 // and a second launch joins them.
 
-__device__ inline uint32_t units_of(const PagedAttnArgs& a, int b) {
-  return b < a.batch ? PagedSeq::of(a, b).head_units() * static_cast<uint32_t>(a.kv_heads) : 0u;
+__device__ inline uint32_t units_of(const PagedAttnArgs& a, const PagedSeq& s) {
+  return s.head_units() * static_cast<uint32_t>(a.kv_heads);
 }
 
-// A sequence that the whole wave shares, in scalar registers.
-__device__ inline PagedSeq sequence(const PagedAttnArgs& a, int b) {
-  PagedSeq s = PagedSeq::of(a, b);
-  auto one = [](auto v) { return static_cast<decltype(v)>(__builtin_amdgcn_readfirstlane(static_cast<int>(v))); };
-  s.first = one(s.first);
-  s.n = one(s.n);
-  s.len = one(s.len);
-  s.start = static_cast<int64_t>(one(static_cast<uint32_t>(s.start >> 32))) << 32 | one(static_cast<uint32_t>(s.start));
-  s.rows = one(s.rows);
-  s.items = one(s.items);
-  s.cost0 = one(s.cost0);
-  s.step = one(s.step);
-  return s;
+// A value of lane i, in a scalar register.
+template <class T>
+__device__ inline T from_lane(T v, int i) {
+  return static_cast<T>(__builtin_amdgcn_readlane(static_cast<int>(v), i));
 }
-
-__device__ inline Shares shares_of(const PagedAttnArgs& a) {
-  const int lane = threadIdx.x & 63;
-  uint32_t all = 0;
-  for (int c = 0; c < a.batch; c += 64) all += __shfl(wave_prefix(units_of(a, c + lane)), 63);
-  all = uniform(all);
-  if (!a.workers) return Shares::of(all, all);  // a unit an item, an item a block
-  const uint32_t most = all / static_cast<uint32_t>(a.least), workers = static_cast<uint32_t>(a.workers);
-  return Shares::of(all, most < 1 ? 1 : most < workers ? most : workers);
+__device__ inline PagedSeq from_lane(const PagedSeq& s, int i) {
+  return {from_lane(s.first, i), from_lane(s.n, i),     from_lane(s.len, i),   from_lane(s.start, i),
+          from_lane(s.rows, i),  from_lane(s.items, i), from_lane(s.cost0, i), from_lane(s.step, i)};
 }
+__device__ inline PagedSeq sequence(const PagedAttnArgs& a, int b) { return from_lane(PagedSeq::of(a, b), 0); }
 
 // Unit x of all: its sequence, key head and item, and its place in the item.
 // Where chunk_begin decreases somewhere, chunks overlap and sums can pass 32
@@ -83,34 +69,55 @@ struct Spot {
   uint32_t unit;
   PagedSeq seq;
 };
-__device__ inline Spot locate(const PagedAttnArgs& a, uint32_t x) {
+
+// The shares of all units and the spot of the first unit of worker `w` (of no
+// share: b < 0).  Sequences are read 64 at a time, a lane each; every lane of a
+// wave calls this.
+__device__ inline Spot find_share(const PagedAttnArgs& a, uint32_t w, Shares* sh) {
   const int lane = threadIdx.x & 63;
+  uint32_t all = 0, mine = 0, pre = 0;
+  PagedSeq s{};
+  auto read = [&](int c) {
+    mine = 0;
+    if (c + lane < a.batch) {
+      s = PagedSeq::of(a, c + lane);
+      mine = units_of(a, s);
+    }
+    pre = wave_prefix(mine);
+  };
+  for (int c = 0; c < a.batch; c += 64) {
+    read(c);
+    all += from_lane(pre, 63);
+  }
+  if (!a.workers) {
+    *sh = Shares::of(all, all);  // a unit an item, an item a block
+  } else {
+    const uint32_t most = all / static_cast<uint32_t>(a.least), workers = static_cast<uint32_t>(a.workers);
+    *sh = Shares::of(all, most < 1 ? 1 : most < workers ? most : workers);
+  }
   Spot at{};
   at.b = -1;
-  uint32_t base = 0, units = 0;
+  if (w >= sh->workers) return at;
+  const uint32_t x = uniform(sh->first(w));
+  uint32_t base = 0;
   for (int c = 0; c < a.batch; c += 64) {
-    const uint32_t mine = units_of(a, c + lane), pre = wave_prefix(mine);
+    if (a.batch > 64) read(c);  // else read above
     const uint64_t past = __ballot(base + pre > x);
     if (past) {
       const int i = __builtin_ctzll(past);
+      const uint32_t units = from_lane(mine, i), y = x - (base + from_lane(pre, i) - units);
+      if (y >= units) break;
       at.b = c + i;
-      units = uniform(__shfl(mine, i));
-      base = uniform(base + __shfl(pre, i) - units);
+      at.seq = from_lane(s, i);
+      const uint32_t of_head = at.seq.head_units();
+      at.kvh = static_cast<int>(y / of_head);
+      const uint32_t z = y - static_cast<uint32_t>(at.kvh) * of_head;
+      at.item = at.seq.item_of(z);
+      at.unit = z - at.seq.before(at.item);
       break;
     }
-    base += __shfl(pre, 63);
+    base += from_lane(pre, 63);
   }
-  const uint32_t y = x - base;
-  if (at.b < 0 || y >= units) {
-    at.b = -1;
-    return at;
-  }
-  at.seq = sequence(a, at.b);
-  const uint32_t of_head = at.seq.head_units();
-  at.kvh = static_cast<int>(y / of_head);
-  const uint32_t z = y - static_cast<uint32_t>(at.kvh) * of_head;
-  at.item = at.seq.item_of(z);
-  at.unit = z - at.seq.before(at.item);
   return at;
 }
 // The item after this one; whether there is one.
@@ -130,10 +137,10 @@ __device__ inline bool next_item(const PagedAttnArgs& a, Spot* at) {
 // Row `row` of slot `slot`: its sums, and its maximum and sum of exponentials
 // (behind all slots' sums).
 __device__ inline float* slot_sums(const PagedAttnArgs& a, int D, int64_t slot, int row) {
-  return a.partial + (slot * a.slot_rows + row) * D;
+  return a.partial + (slot * a.slot_rows() + row) * D;
 }
 __device__ inline float2* slot_stats(const PagedAttnArgs& a, int D, int64_t slot, int row) {
-  return reinterpret_cast<float2*>(a.partial + 2 * static_cast<int64_t>(a.workers) * a.slot_rows * D) + slot * a.slot_rows + row;
+  return reinterpret_cast<float2*>(a.partial + 2 * static_cast<int64_t>(a.workers) * a.slot_rows() * D) + slot * a.slot_rows() + row;
 }
 
 // Where query row r of a key head lies, and which cache indices it sees.
@@ -142,10 +149,10 @@ struct RowPlace {
   int32_t seen;
 };
 __device__ inline RowPlace row_place(const PagedAttnArgs& a, const PagedSeq& s, int kvh, int r, int D) {
-  const int i = r / a.group, h = kvh * a.group + (r - i * a.group);
+  const int i = static_cast<int>(a.by_group.quotient(r)), h = kvh * a.group + (r - i * a.group);
   const int64_t row = static_cast<int64_t>(s.first) + i;
   return {row * a.q_stride + static_cast<int64_t>(h) * D, (row * a.q_heads + h) * D, h * a.lse_stride + row,
-          s.seen(i, a.mask_block)};
+          s.seen(i, a)};
 }
 
 // Four dims d .. d + 3 of a row's result from its sums v, maximum m and sum l.
@@ -247,12 +254,10 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), second = NW == 8 ? wave >> 2 : 0;
   // Workers next to one another share key heads: each XCD takes a run of them.
   const int worker = xcd_remap(blockIdx.x, gridDim.x);
-  const Shares sh = shares_of(a);
-  if (static_cast<uint32_t>(worker) >= sh.workers) return;
-  const uint32_t x0 = sh.first(worker);
-  uint32_t todo = uniform(sh.first(worker + 1) - x0);
-  Spot at = locate(a, x0);
+  Shares sh;
+  Spot at = find_share(a, worker, &sh);
   if (at.b < 0) return;
+  uint32_t todo = uniform(sh.first(worker + 1) - sh.first(worker));
 
   // Transfers: wave instruction i fills four rows of 256 bytes, lane l bytes 16 l,
   // i.e. row l / 16, whose chunk l % 16 holds chunk (l % 16) ^ 4 (l / 16) ^ i.
@@ -538,7 +543,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
       // Tiles before `plain` have no step of the mask, for no row of the item.
       int plain = t1;
       if constexpr (MASK) {
-        const int low = at.seq.seen(at.item * (NW * 32) / a.group, a.mask_block);
+        const int low = at.seq.seen(a.by_group.quotient(at.item * (NW * 32)), a);
         if (low < len && low / kTile < plain) plain = low / kTile > t0 ? low / kTile : t0;
       }
       prefill(F_{}, 0, 0);
@@ -634,12 +639,10 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_rows_kernel(PagedAttnArgs 
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int worker = xcd_remap(blockIdx.x, gridDim.x);
-  const Shares sh = shares_of(a);
-  if (static_cast<uint32_t>(worker) >= sh.workers) return;
-  const uint32_t x0 = sh.first(worker);
-  uint32_t todo = uniform(sh.first(worker + 1) - x0);
-  Spot at = locate(a, x0);
+  Shares sh;
+  Spot at = find_share(a, worker, &sh);
   if (at.b < 0) return;
+  uint32_t todo = uniform(sh.first(worker + 1) - sh.first(worker));
 
   const int64_t row_bytes = static_cast<int64_t>(a.kv_heads) * D * 2;
   const float c = a.scale_log2e;
@@ -926,18 +929,16 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(PagedAttnArgs a, int
   __shared__ float red[2][kJoinThreads / 64];
   const int tid = threadIdx.x, wave = tid >> 6, side = tid % kSide, grp = tid / kSide;
   const int j = static_cast<int>(blockIdx.x) / row_groups, r0 = (static_cast<int>(blockIdx.x) - j * row_groups) * join_rows;
-  const Shares sh = shares_of(a);
-  if (static_cast<uint32_t>(j) + 1 >= sh.workers) return;
-  const uint32_t cut = sh.first(j + 1);
-  const Spot at = locate(a, cut);
-  const uint32_t start = cut - at.unit;
+  Shares sh;
+  const Spot at = find_share(a, j + 1, &sh);
+  const uint32_t start = sh.first(j + 1) - at.unit;
   if (at.b < 0 || at.unit == 0 || sh.first(j) > start) return;
   const int w1 = static_cast<int>(min(sh.worker_of(start + at.seq.cost(at.item) - 1), sh.workers - 1));
   const int pieces = w1 - j + 1;
   const int64_t slot0 = sh.first(j) != start ? 2 * static_cast<int64_t>(j) + 1 : 2 * static_cast<int64_t>(j);
   auto slot = [&](int s) { return s == 0 ? slot0 : 2 * static_cast<int64_t>(j + s); };
-  const int rows = min(a.slot_rows, at.seq.rows - at.item * a.slot_rows), r1 = min(r0 + join_rows, rows);
-  auto place = [&](int in) { return row_place(a, at.seq, at.kvh, at.item * a.slot_rows + in, D); };
+  const int rows = min(a.slot_rows(), at.seq.rows - at.item * a.slot_rows()), r1 = min(r0 + join_rows, rows);
+  auto place = [&](int in) { return row_place(a, at.seq, at.kvh, at.item * a.slot_rows() + in, D); };
   if (pieces <= kSide && join_rows > 1) {
     for (int k = r0 + grp; k < r1; k += kGroups) {
       const RowPlace to = place(k);

@@ -24,8 +24,11 @@ hipError_t plan_paged_attention(int64_t tokens, int32_t batch, int32_t max_chunk
   const int64_t tiles = (capacity + kPagedTile - 1) / kPagedTile;
   if (items > 0x7fffffff || items * std::max<int64_t>(1, tiles) > 0x7fffffff) return hipErrorInvalidValue;
   const int64_t slots = p.waves == 8 ? 256 : 512;  // blocks resident at once
-  p.least = p.waves ? 4 : 2 * kPagedFewWaves;
-  if (tiles > p.least) p.workers = static_cast<int32_t>(std::max<int64_t>(1, std::min(slots, items * tiles / p.least)));
+  const int64_t least = p.waves ? 4 : 2 * kPagedFewWaves;  // tiles of a share at least
+  if (tiles > least) p.workers = static_cast<int32_t>(std::max<int64_t>(1, std::min(slots, items * tiles / least)));
+  // units as small as 31 bits of them allow
+  while (p.unit_shift < 4 && items * std::max<int64_t>(1, tiles) << (p.unit_shift + 1) <= 0x7fffffff) ++p.unit_shift;
+  p.least = static_cast<int32_t>(least << p.unit_shift);
   p.blocks = p.workers ? p.workers : items;
   if (!launchable(p.blocks, p.threads())) return hipErrorInvalidValue;
   // few items are in many slots each: a block takes one row of them, else eight
