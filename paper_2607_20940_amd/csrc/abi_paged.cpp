@@ -317,6 +317,7 @@ mssa_status mssa_paged_attention(const mssa_paged_attention_desc* desc, const vo
     while (a.slot_rows() < plan.slot_rows) ++a.slot_shift;
     a.workers = plan.workers;
     a.unit_shift = plan.unit_shift;
+    a.extra = plan.extra;
     a.least = plan.least;
     a.page = mssa::Divisor::of(static_cast<uint32_t>(desc->page_tokens));
     a.by_group = mssa::Divisor::of(static_cast<uint32_t>(a.group));

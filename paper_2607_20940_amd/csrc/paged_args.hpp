@@ -79,6 +79,7 @@ struct PagedAttnArgs {
   int32_t slot_shift;  // an item has 2^slot_shift query rows
   int32_t workers;     // shares of all items' contexts, 0: an item a block and no joining launch
   int32_t unit_shift;  // a tile weighs 2^unit_shift units
+  int32_t extra;       // tiles that an item weighs besides its own: what beginning and ending one takes
   int32_t least;       // units of a share at least
   Divisor page, by_group, by_mask;
   float scale_log2e;
@@ -91,7 +92,7 @@ struct PagedAttnArgs {
 // units of a fraction of a tile, linear in their number so that sums have a
 // closed form: their tiles where there is no mask, and where there is one, up to
 // its steps.  Every item has units, also one without keys, whose rows are
-// written all the same.
+// written all the same: beginning and ending an item takes as long as some tiles.
 struct PagedSeq {
   int32_t first, n;  // chunk: first row, tokens (at most max_chunk)
   int32_t len;       // cache indices in use
@@ -143,10 +144,9 @@ struct PagedSeq {
     s.cost0 = 1;
     s.step = 0;
     if (a.workers && s.items) {
-      const uint32_t low = static_cast<uint32_t>(s.tiles(0, a)) << a.unit_shift;
-      s.cost0 = low ? low : 1;
+      s.cost0 = static_cast<uint32_t>(s.tiles(0, a) + a.extra) << a.unit_shift;
       if (a.mask_block && s.items > 1) {
-        const uint32_t high = static_cast<uint32_t>(s.tiles(s.items - 1, a)) << a.unit_shift;
+        const uint32_t high = static_cast<uint32_t>(s.tiles(s.items - 1, a) + a.extra) << a.unit_shift;
         if (high > s.cost0) s.step = (high - s.cost0) / static_cast<uint32_t>(s.items - 1);
       }
     }
@@ -162,7 +162,7 @@ struct PagedSeq {
 
 struct PagedAttnPlan {
   int32_t waves;      // 32 rows each in a block; 0: the kernel for few rows
-  int32_t slot_rows, workers, unit_shift, least;
+  int32_t slot_rows, workers, unit_shift, extra, least;
   int64_t blocks, workspace_bytes;
   int32_t join_rows;  // rows of a block of the joining launch
   int32_t threads() const { return (waves ? waves : kPagedFewWaves) * 64; }

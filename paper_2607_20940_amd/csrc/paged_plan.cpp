@@ -22,12 +22,13 @@ hipError_t plan_paged_attention(int64_t tokens, int32_t batch, int32_t max_chunk
   // every sequence's items: whole ones, and one that is not full
   const int64_t items = kv_heads * std::min(batch * ((rows + p.slot_rows - 1) / p.slot_rows), batch + tokens * group / p.slot_rows);
   const int64_t tiles = (capacity + kPagedTile - 1) / kPagedTile;
-  if (items > 0x7fffffff || items * std::max<int64_t>(1, tiles) > 0x7fffffff) return hipErrorInvalidValue;
-  const int64_t slots = p.waves == 8 ? 256 : 512;  // blocks resident at once
+  p.extra = p.waves ? 8 : 6;
+  if (items > 0x7fffffff || items * (tiles + p.extra) > 0x7fffffff) return hipErrorInvalidValue;
+  const int64_t slots = p.waves == 4 ? 512 : 256;  // blocks resident at once
   const int64_t least = p.waves ? 4 : 2 * kPagedFewWaves;  // tiles of a share at least
   if (tiles > least) p.workers = static_cast<int32_t>(std::max<int64_t>(1, std::min(slots, items * tiles / least)));
   // units as small as 31 bits of them allow
-  while (p.unit_shift < 4 && items * std::max<int64_t>(1, tiles) << (p.unit_shift + 1) <= 0x7fffffff) ++p.unit_shift;
+  while (p.unit_shift < 4 && items * (tiles + p.extra) << (p.unit_shift + 1) <= 0x7fffffff) ++p.unit_shift;
   p.least = static_cast<int32_t>(least << p.unit_shift);
   p.blocks = p.workers ? p.workers : items;
   if (!launchable(p.blocks, p.threads())) return hipErrorInvalidValue;
