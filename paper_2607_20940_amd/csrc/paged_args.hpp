@@ -63,7 +63,6 @@ hipError_t launch_paged_append(const AppendArgs& a, hipStream_t stream);
 // -------------------------------------------------------------- attention
 constexpr int kPagedTile = 64;  // tokens of a tile
 constexpr int kPagedMaxWorkers = 512;
-constexpr int kPagedFewWaves = 4;  // waves of a block of the kernel for few rows
 constexpr int kPagedJoinThreads = 256;
 
 struct PagedAttnArgs {
@@ -162,10 +161,11 @@ struct PagedSeq {
 
 struct PagedAttnPlan {
   int32_t waves;      // 32 rows each in a block; 0: the kernel for few rows
+  int32_t few_waves;  // of a block of that one
   int32_t slot_rows, workers, unit_shift, extra, least;
   int64_t blocks, workspace_bytes;
   int32_t join_rows;  // rows of a block of the joining launch
-  int32_t threads() const { return (waves ? waves : kPagedFewWaves) * 64; }
+  int32_t threads() const { return (waves ? waves : few_waves) * 64; }
 };
 // Sizes whose launch would have 2^32 threads, or 2^31 units, are refused.
 hipError_t plan_paged_attention(int64_t tokens, int32_t batch, int32_t max_chunk, int32_t q_heads, int32_t kv_heads,

@@ -620,16 +620,15 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
 // ------------------------------------------------------------------- few rows
 // Single tokens of a stream, or a few: at most RT x 16 rows share a key head.
 // Memory bound (the cache is read once), so a wave works alone, without barriers,
-// on every fourth stage of 32 tokens of the block's.  K, V and the page table's
+// on every kFewWaves-th stage of 32 tokens of the block's.  K, V and the page table's
 // entries come by direct transfers into rings of the wave's own in LDS, whole
 // cache lines and streamed (nt): two stages of K and V on their way, entries two
 // stages ahead of them.  The transfers in order, stage by stage: K, V, entries of
 // the stage after the next; what a step needs is there once no more than those
 // issued after it are left.  Stages past the last are transfers of zeros.
-constexpr int kFewWaves = kPagedFewWaves;
 constexpr int kFewStage = 32;  // tokens
 
-template <int D, int RT, bool MASK>
+template <int D, int RT, bool MASK, int kFewWaves>
 __global__ __launch_bounds__(kFewWaves * 64) void few_rows_kernel(PagedAttnArgs a) {
   constexpr int NS = D / 32, DT = D / 16, kRows = 16 * RT, kHalf = kFewStage * 256, kMoves = kFewStage / 4;
   __shared__ __attribute__((aligned(16))) char lds[kFewWaves][2][2][kHalf];  // [wave][buffer][K | V]
@@ -1009,10 +1008,14 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(PagedAttnArgs a, int
 template <int D, bool MASK>
 hipError_t attend(const PagedAttnArgs& a, const PagedAttnPlan& plan, hipStream_t stream) {
   const dim3 grid(static_cast<uint32_t>(plan.blocks)), block(plan.threads());
-  if (plan.waves == 0 && plan.slot_rows == 16)
-    hipLaunchKernelGGL((few_rows_kernel<D, 1, MASK>), grid, block, 0, stream, a);
+  if (plan.waves == 0 && plan.slot_rows == 16 && plan.few_waves == 4)
+    hipLaunchKernelGGL((few_rows_kernel<D, 1, MASK, 4>), grid, block, 0, stream, a);
+  else if (plan.waves == 0 && plan.slot_rows == 16)
+    hipLaunchKernelGGL((few_rows_kernel<D, 1, MASK, 2>), grid, block, 0, stream, a);
+  else if (plan.waves == 0 && plan.few_waves == 4)
+    hipLaunchKernelGGL((few_rows_kernel<D, 2, MASK, 4>), grid, block, 0, stream, a);
   else if (plan.waves == 0)
-    hipLaunchKernelGGL((few_rows_kernel<D, 2, MASK>), grid, block, 0, stream, a);
+    hipLaunchKernelGGL((few_rows_kernel<D, 2, MASK, 2>), grid, block, 0, stream, a);
   else if (plan.waves == 4)
     hipLaunchKernelGGL((attn_kernel<D, 4, MASK>), grid, block, 0, stream, a);
   else

@@ -24,8 +24,13 @@ hipError_t plan_paged_attention(int64_t tokens, int32_t batch, int32_t max_chunk
   const int64_t tiles = (capacity + kPagedTile - 1) / kPagedTile;
   p.extra = p.waves ? 8 : 6;
   if (items > 0x7fffffff || items * (tiles + p.extra) > 0x7fffffff) return hipErrorInvalidValue;
-  const int64_t slots = p.waves == 4 ? 512 : 256;  // blocks resident at once
-  const int64_t least = p.waves ? 4 : 2 * kPagedFewWaves;  // tiles of a share at least
+  // Few rows: blocks of four waves, one on a CU; with several items a CU two of
+  // two waves, one of which begins or ends an item while the other reads (256
+  // streams of 8 key heads and 500 tokens 137 -> 87 us; one stream of 8 heads and
+  // 32760 tokens 39.5 us, 49.5 with them, whose pieces are twice as many to join).
+  p.few_waves = items >= 1024 ? 2 : 4;
+  const int64_t slots = p.waves == 8 || (!p.waves && p.few_waves == 4) ? 256 : 512;  // blocks resident at once
+  const int64_t least = p.waves ? 4 : 2 * p.few_waves;  // tiles of a share at least
   if (tiles > least) p.workers = static_cast<int32_t>(std::max<int64_t>(1, std::min(slots, items * tiles / least)));
   // units as small as 31 bits of them allow
   while (p.unit_shift < 4 && items * (tiles + p.extra) << (p.unit_shift + 1) <= 0x7fffffff) ++p.unit_shift;

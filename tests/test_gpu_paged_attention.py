@@ -96,6 +96,14 @@ def test_ragged_batches(D, mask, new, before):
     _run(new, before, 4, 2, D, 16, mask, first=3, behind=5, pad=8, lse_pad=3)
 
 
+@pytest.mark.parametrize("D,H,mask", [(64, 8, 0), (128, 8, 1), (64, 24, 1)])
+def test_many_items_of_few_rows(D, H, mask):
+    """1024 items and more: blocks of two waves."""
+    rng = np.random.default_rng(D)
+    new = rng.integers(0, 4, size=140).tolist()
+    _run(new, rng.integers(0, 500, size=140).tolist(), H, 8, D, 32, mask, first=2)
+
+
 def test_many_sequences():
     rng = np.random.default_rng(5)
     new = rng.integers(0, 3, size=150).tolist()
