@@ -314,25 +314,40 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
       const uint64_t mask = __ballot(is);
       if (lane == 0) masks[run & 1][wave] = mask;
     };
-    // A wave brings rows 16 (wave & 3) .. + 15 of its group's tiles; returns the tile's mask.
-    auto bring = [&](int t, int buf) -> uint64_t {
+    // A wave brings rows 16 (wave & 3) .. + 15 of its group's tiles.  Their addresses
+    // and the tile's mask are read before the matrix phase, which has room for
+    // it, and used in the softmax phase after it.
+    const char* place[NW == 8 ? 4 : 8];
+    uint64_t there_next = 0;
+    auto look = [&](int t) {
       const int half = (t - t0) / NW & 1, in = (t - t0) % NW;
-      int ln = lane;  // what the addresses are made of is worked out anew: kept, it would cost more registers than there are
+      int ln = lane;  // the chunks are worked out anew: kept, they would cost more registers than there are
       asm volatile("" : "+v"(ln));
 #pragma unroll
       for (int is_v = 0; is_v < 2; ++is_v) {
         if (NW == 8 && is_v) break;
-        const int what = NW == 8 ? second : is_v;
-        const char* const* const from = &where[half][what][in * kTile + (wave & 3) * 16 + (ln >> 4)];
+        const char* const* const from = &where[half][NW == 8 ? second : is_v][in * kTile + (wave & 3) * 16 + (ln >> 4)];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           // 64-dim rows are half as long: their chunks fill the LDS rows' unused half too
           const int chunk = ((ln & 15) ^ ((ln >> 4) << 2) ^ i) & (D / 8 - 1);
-          gdma16(from[i * 4] + chunk * 16, __builtin_amdgcn_readfirstlane(lds0 + ((what * 2 + buf) * kTile + (wave & 3) * 16 + i * 4) * 256));
+          place[is_v * 4 + i] = from[i * 4] + chunk * 16;
         }
       }
-      const uint64_t mask = masks[half][in];
-      return static_cast<uint64_t>(uniform(static_cast<uint32_t>(mask >> 32))) << 32 | uniform(static_cast<uint32_t>(mask));
+      there_next = masks[half][in];
+    };
+    auto bring = [&](int buf) {
+#pragma unroll
+      for (int is_v = 0; is_v < 2; ++is_v) {
+        if (NW == 8 && is_v) break;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          gdma16(place[is_v * 4 + i], __builtin_amdgcn_readfirstlane(
+              lds0 + (((NW == 8 ? second : is_v) * 2 + buf) * kTile + (wave & 3) * 16 + i * 4) * 256));
+      }
+    };
+    auto scalar_mask = [&]() {
+      return static_cast<uint64_t>(uniform(static_cast<uint32_t>(there_next >> 32))) << 32 | uniform(static_cast<uint32_t>(there_next));
     };
 
     const int r_in = wave * 32 + n, r = at.item * (NW * 32) + r_in;
@@ -515,7 +530,9 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
       asm volatile("" ::: "memory");
       make_run(0);
       phase_end();
-      uint64_t there = bring(t0, 0), there_next = 0;
+      look(t0);
+      bring(0);
+      uint64_t there = scalar_mask();
       wait_vmcnt<0>();
       phase_end();
       if (second) phase_end();
@@ -523,20 +540,22 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
       // operands of the next matrix phase are read.
       auto sphase = [&](auto masked, auto next, int t, int buf) {
         phase_end();
-        if (t + 1 < t1) there_next = bring(t + 1, buf ^ 1);
+        if (t + 1 < t1) bring(buf ^ 1);
         const int in = (t - t0) % NW;
         if (in == 0 && t + NW < t1)
           ask_run((t - t0) / NW + 1);
         else if (in == 1 && t + NW - 1 < t1)
           make_run((t - t0) / NW + 1);
         softmax(masked, t, there);
-        there = there_next;
+        there = scalar_mask();
         if constexpr (decltype(next)::value) prefill(T_{}, buf, buf ^ 1);
         wait_vmcnt<0>();
         phase_end();
       };
-      auto mphase = [&](auto pv, auto sc, int vb, int kbuf) {
+      // The matrix phase that makes tile t's scores.
+      auto mphase = [&](auto pv, auto sc, int t, int vb, int kbuf) {
         __builtin_amdgcn_s_setprio(2);
+        if (decltype(sc)::value && t + 1 < t1) look(t + 1);
         mstep(pv, sc, vb, kbuf);
         __builtin_amdgcn_s_setprio(0);
       };
@@ -547,30 +566,31 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
         if (low < len && low / kTile < plain) plain = low / kTile > t0 ? low / kTile : t0;
       }
       prefill(F_{}, 0, 0);
-      mphase(F_{}, T_{}, 0, 0);
+      mphase(F_{}, T_{}, t0, 0, 0);
       // two tiles at a time: their buffers are constants
       int t = t0, buf = 0;
       for (; t + 2 < plain; t += 2) {
         sphase(F_{}, T_{}, t, 0);
-        mphase(T_{}, T_{}, 0, 1);
+        mphase(T_{}, T_{}, t + 1, 0, 1);
         sphase(F_{}, T_{}, t + 1, 1);
-        mphase(T_{}, T_{}, 1, 0);
+        mphase(T_{}, T_{}, t + 2, 1, 0);
       }
       if constexpr (!MASK) {
         if (t + 1 < t1) {
           sphase(F_{}, T_{}, t, 0);
-          mphase(T_{}, T_{}, 0, 1);
+          mphase(T_{}, T_{}, t + 1, 0, 1);
           buf = 1;
           ++t;
         }
         sphase(F_{}, T_{}, t, buf);
-        mphase(T_{}, F_{}, buf, buf ^ 1);
+        mphase(T_{}, F_{}, t + 1, buf, buf ^ 1);
       } else {
         for (;; ++t, buf ^= 1) {
           sphase(T_{}, F_{}, t, buf);
           __builtin_amdgcn_s_setprio(2);
           add_pv_step(buf, t);
           if (t + 1 < t1) {
+            if (t + 2 < t1) look(t + 2);
             prefill(F_{}, 0, buf ^ 1);
             mstep(F_{}, T_{}, 0, buf ^ 1);
           }
