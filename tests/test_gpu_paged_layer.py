@@ -1,0 +1,157 @@
+"""Layers over a paged cache, several streams at once, against the fp64 oracle of
+the three operators one after the other.
+
+Bounds, carried along value by value.  A projected value y is off by 2^-8 |y| (its
+rounding) and 2^-8 sum_r |u_r b_r| (that of the low-rank factor u, each to 2^-8 of
+itself); 1 % more covers the fp32 sums.  Turning a pair adds up both errors, and
+rounds again.  A score is then off by e = scale (sum e_q |k| + (|q| + e_q) e_k), the
+log sum by max e, each weight by a factor of exp(2 max e) at most, and the output by
+(exp(2 max e) - 1) of the softmax mean of |v|, the mean of v's errors (exp(2 max e)
+of it), P's rounding (2^-8 of the mean of |v|) and its own (2^-8)."""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import paged
+from paper_2607_20940_amd import mssa
+from paper_2607_20940_amd.paged import PagedStreams
+
+from lowbit_common import cuda, f64
+
+pytestmark = pytest.mark.gpu
+HIDDEN, H, KH, D, PAGE = 192, 4, 2, 64, 16
+
+
+def _layer(rng, adapters, rank):
+    w = cuda(rng.normal(size=((H + 2 * KH) * D, HIDDEN)) * 0.3 * HIDDEN ** -0.5, "bf16")
+    bias = cuda(rng.normal(size=(H + 2 * KH) * D) * 0.1, "bf16")
+    a = cuda(rng.normal(size=(adapters, rank, HIDDEN)) * HIDDEN ** -0.5, "bf16")
+    b = cuda(rng.normal(size=(adapters, (H + 2 * KH) * D, rank)) * 0.1, "bf16")
+    return w, bias, a, b, torch.tensor(rng.uniform(0.5, 1.5, size=adapters), dtype=torch.float32, device="cuda")
+
+
+class _Oracle:
+    """The streams' keys and values so far, in 64 bits."""
+
+    def __init__(self, layer, freqs, mask):
+        self.layer, self.freqs, self.mask, self.kv, self.at = layer, freqs, mask, {}, {}
+
+    def run(self, chunks, x, adapters):
+        w, bias, a, b, scale = (f64(t) for t in self.layer)
+        begin = np.concatenate(([0], np.cumsum([n for _, n in chunks])))
+        y, _, _ = paged.adapter_project(x, w, bias, begin, adapters, a[:, None], b, scale, 1, 1.0)
+        low = np.zeros_like(y[0])
+        for i, j in enumerate(adapters):
+            if j >= 0:
+                r = slice(begin[i], begin[i + 1])
+                low[r] = np.abs(scale[j] * (x[r] @ a[j].T)) @ np.abs(b[j]).T
+        e = (2.0 ** -8 * 1.01 * (np.abs(y[0]) + low)).reshape(len(x), H + 2 * KH, D)
+        y = y[0].reshape(len(x), H + 2 * KH, D)
+        out, tol, lse, lse_tol = [], [], [], []
+        for i, (s, n) in enumerate(chunks):
+            r, er = y[begin[i]:begin[i + 1]], e[begin[i]:begin[i + 1]]
+            pos = self.at.get(s, 0) + np.arange(n)
+            self.at[s] = self.at.get(s, 0) + n
+            qk, _ = paged.rotate(r[:, : H + KH], pos[:, None] * self.freqs.astype(np.float64), True)
+            half = er[:, : H + KH, : D // 2] + er[:, : H + KH, D // 2:]
+            eqk = np.concatenate((half, half), -1) + 2.0 ** -8 * 1.01 * np.abs(qk)
+            new = (qk[:, H:], r[:, H + KH:], eqk[:, H:], er[:, H + KH:])
+            k, v, ek, ev = self.kv[s] = tuple(np.concatenate(t) for t in zip(self.kv.get(s, (np.zeros((0, KH, D)),) * 4), new))
+            if n == 0:
+                continue
+            held, g = len(k), H // KH
+            o, l, mag = paged.attention(qk[:, :H], k[None], v[None], None, [held], [[0]], D ** -0.5, self.mask)
+            mean_ev = paged.attention(qk[:, :H], k[None], ev[None], None, [held], [[0]], D ** -0.5, self.mask)[0]
+            es = max((eqk[:, h] @ np.abs(k[:, h // g]).T + (np.abs(qk[:, h]) + eqk[:, h]) @ ek[:, h // g].T).max() for h in range(H))
+            es *= D ** -0.5
+            f = np.exp(2 * es)
+            out.append(o)
+            lse.append(l)
+            tol.append((f - 1 + 2.0 ** -8 * f + 1e-4) * mag + f * mean_ev + 2.0 ** -8 * 1.01 * np.abs(o))
+            lse_tol.append(np.full(l.shape, es + 1e-4))
+        return np.concatenate(out), np.concatenate(tol), np.concatenate(lse, 1), np.concatenate(lse_tol, 1)
+
+    def drop(self, s, n):
+        self.kv[s] = tuple(t[n:] for t in self.kv[s])
+
+
+@pytest.mark.parametrize("mask", [0, 1, 8])
+def test_streams_come_and_go(mask):
+    rng = np.random.default_rng(mask)
+    freqs = (100.0 ** (-np.arange(D // 2) / (D // 2))).astype(np.float32)
+    p = PagedStreams(2, HIDDEN, H, KH, D, 40, PAGE, 20, 400, 5, adapters=3, rank=8, freqs=torch.from_numpy(freqs).cuda(),
+                     mask_block=mask)
+    layers = [_layer(rng, 3, 8) for _ in range(2)]
+    for i, w in enumerate(layers):
+        p.init_layer(i, *w)
+    oracles = [_Oracle(w, freqs, mask) for w in layers]
+    for s, j in (("a", 0), ("b", -1), ("c", 2)):
+        p.open(s, j)
+    adapter = {"a": 0, "b": -1, "c": 2, "d": 1}
+    steps = [[("a", 100), ("b", 7)], [("b", 1), ("a", 1), ("c", 33)], "drop", [("c", 1), ("a", 50), ("b", 0)], "close",
+             [("d", 60), ("a", 1)], [("d", 1), ("a", 1), ("c", 1)]]
+    for step in steps:
+        if step == "drop":
+            p.drop("a", 3 * PAGE)
+            for o in oracles:
+                o.drop("a", 3 * PAGE)
+        elif step == "close":
+            p.close("b")
+            p.open("d", 1)
+        else:
+            p.begin(step)
+            x = cuda(rng.normal(size=(p.tokens, HIDDEN)), "bf16")
+            for i in range(2):
+                out = torch.full((p.tokens, H, D), 7.0, dtype=torch.bfloat16, device="cuda")
+                lse = torch.empty(H, p.tokens, device="cuda")
+                p.layer_pass(i, x, out, lse)
+                ref, tol, ref_lse, lse_tol = oracles[i].run(step, f64(x), [adapter[s] for s, _ in step])
+                assert (np.abs(f64(out) - ref) <= tol).all(), (step, i)
+                assert (np.abs(f64(lse) - ref_lse) <= lse_tol).all()
+    assert len(p.free) + sum(len(s[0]) for s in p.streams.values()) == 40
+
+
+def test_joined_with_another_attention():
+    """The history in pages, the window's attention by a plan: together the attention over both."""
+    rng = np.random.default_rng(9)
+    p = PagedStreams(1, HIDDEN, H, H, D, 20, PAGE, 10, 200, 1, mask_block=0)
+    p.init_layer(0, cuda(rng.normal(size=(3 * H * D, HIDDEN)) * 0.3 * HIDDEN ** -0.5, "bf16"))
+    p.open(0)
+    p.begin([(0, 96)])
+    x = cuda(rng.normal(size=(96, HIDDEN)), "bf16")
+    alone, lse = torch.empty(96, H, D, dtype=torch.bfloat16, device="cuda"), torch.empty(H, 96, device="cuda")
+    p.layer_pass(0, x, alone, lse)
+    po, pl = cuda(rng.normal(size=(96, H, D)), "bf16"), cuda(rng.normal(size=(H, 96)) + 4, "f32")
+    out, both = po.clone(), pl.clone()
+    p.layer_pass(0, x, out, both, prior_out=out, prior_lse=both)
+    ref = np.logaddexp(f64(lse), f64(pl))
+    assert np.abs(f64(both) - ref).max() <= 1e-4
+    w, wp = np.exp(f64(lse) - ref).T[..., None], np.exp(f64(pl) - ref).T[..., None]
+    want = f64(alone) * w + f64(po) * wp
+    assert (np.abs(f64(out) - want) <= 2.0 ** -8 * (np.abs(want) + np.abs(f64(alone)) * w) * 1.01 + 1e-4).all()
+
+
+def test_a_captured_pass_repeats():
+    """Appending the same tokens again writes the same values to the same places: a pass can be replayed."""
+    rng = np.random.default_rng(3)
+    p = PagedStreams(1, HIDDEN, H, KH, D, 40, PAGE, 20, 64, 4, adapters=2, rank=16,
+                     freqs=torch.rand(D // 2, device="cuda"))
+    p.init_layer(0, *_layer(rng, 2, 16))
+    for s in range(3):
+        p.open(s, s - 1)
+    p.begin([(0, 40), (1, 3), (2, 20)])
+    x = cuda(rng.normal(size=(63, HIDDEN)), "bf16")
+    first, out = (torch.empty(63, H, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    p.layer_pass(0, x, first)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        p.layer_pass(0, x, out)
+    for scale in (1, 1, 0.5):
+        x.mul_(scale)
+        out.fill_(3)
+        g.replay()
+        p.layer_pass(0, x, first)
+        torch.cuda.synchronize()
+        assert torch.equal(out, first)
