@@ -201,13 +201,7 @@ __global__ __launch_bounds__(256) void low_tile_kernel(AdapterArgs a) {
   const int nst = (a.K + 63) / 64;
   for (int st = 0; st < kLowStages - 1 && st < nst; ++st) put(st);
   for (int st = 0; st < nst; ++st) {
-    // this stage's transfers are done where no more than those of the later ones are left
-    if (st + 2 < nst)
-      wait_vmcnt<2 * kMine>();
-    else if (st + 1 < nst)
-      wait_vmcnt<kMine>();
-    else
-      wait_vmcnt<0>();
+    wait_for_stage<kLowStages - 2, kMine>(nst - 1 - st);
     // the stage before has been read by all: its buffer is filled next
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
@@ -341,14 +335,7 @@ __global__ __launch_bounds__(256) void few_ring_kernel(AdapterArgs a) {
 #pragma unroll
     for (int t = 0; t < RT; ++t) acc[f][t] = f32x4{};
   for (int st = s0; st < s1; ++st) {
-    // this stage's transfers are done where no more than those of the later ones are left
-    const int later = min(s1 - st, kRing) - 1;
-    if (kRing > 2 && later == 2)
-      wait_vmcnt<2 * kMine>();
-    else if (later == 1)
-      wait_vmcnt<kMine>();
-    else
-      wait_vmcnt<0>();
+    wait_for_stage<kRing - 1, kMine>(s1 - 1 - st);
     asm volatile("" ::: "memory");
     const char* L = lds[wave][(st - s0) % kRing];
     bf16x8 wv[2][FT], xv[2][RT];
@@ -439,19 +426,21 @@ __global__ __launch_bounds__(512) void few_any_kernel(AdapterArgs a) {
 // Tiles of WM x MB x 32 rows and WN x NB x 32 features, WM x WN waves of
 // MB x NB matrix-core tiles each (A = W rows, B = X rows).  The contraction
 // comes in 64-deep stages of 128-byte rows (the swizzle of lds_stage.hpp)
-// through two LDS buffers, filled by direct transfers while the stage before
-// is multiplied; one barrier a stage.  The adapters follow as further stages: 64
-// ranks of one part of one segment, its rows' low-rank factors against B.
+// through kStages LDS buffers, filled by direct transfers kStages - 1 stages ahead;
+// one barrier a stage.  (Small tiles, of which there are few, wait for their
+// transfers' way: four buffers, 200 x 5120 -> 3000 takes 60 us with two, 47 with
+// four, 50 with eight.)  The adapters follow as further stages: 64 ranks
+// of one part of one segment, its rows' low-rank factors against B.
 // Tiles are taken in panels of four feature tiles, each XCD a run of them.
 // The outputs leave through LDS as whole-row 16-byte stores.
 constexpr int kBK = 64, kPanel = 4;
 
-template <int WM, int WN, int MB, int NB>
+template <int WM, int WN, int MB, int NB, int kStages>
 __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void tile_kernel(AdapterArgs a) {
   constexpr int NW = WM * WN, BM = WM * MB * 32, BN = WN * NB * 32;
   constexpr int kX = BM * 128, kW = BN * 128, kStage = kX + kW;  // bytes
   constexpr int TX = BM / 8 / NW, TW = BN / 8 / NW;              // transfers (8 rows) of a wave
-  __shared__ __attribute__((aligned(16))) char lds[2][kStage];
+  __shared__ __attribute__((aligned(16))) char lds[kStages][kStage];
   __shared__ float biases[BN];
   const int tiles_m = (a.M + BM - 1) / BM, tiles_n = (a.N + BN - 1) / BN;
   const int t = xcd_remap(blockIdx.x, tiles_m * tiles_n);
@@ -486,10 +475,13 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2,
   const uint32_t xrb = static_cast<uint32_t>(a.x_stride) * 2, wrb = static_cast<uint32_t>(a.K) * 2;
   auto put_main = [&](int st) {
     const int left = min(a.K - st * kBK, kBK);  // a multiple of 8
-    put(st & 1, X + st * kBK, xrb, static_cast<uint32_t>(m1 - m0 - 1) * xrb + left * 2, W + st * kBK, wrb,
+    put(st % kStages, X + st * kBK, xrb, static_cast<uint32_t>(m1 - m0 - 1) * xrb + left * 2, W + st * kBK, wrb,
         static_cast<uint32_t>(f1 - f0 - 1) * wrb + left * 2, left / 8);
   };
-  put_main(0);
+  const int nst = (a.K + kBK - 1) / kBK;
+#pragma unroll
+  for (int st = 0; st < kStages - 1; ++st)
+    if (st < nst) put_main(st);
 
   // The adapters' stages, found one after the other: a segment with an adapter
   // among the tile's rows, a part among its features, 64 ranks.
@@ -555,16 +547,16 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2,
 #pragma unroll
   for (int ks = 0; ks < kBK / 16; ++ks) rd[ks] = swz128(n32, ks * 16 + hh * 8) * 2;
 
-  const int nst = (a.K + kBK - 1) / kBK;
   for (int st = 0; st < nst; ++st) {
-    wait_vmcnt<0>();
-    __syncthreads();
-    if (st + 1 < nst)
-      put_main(st + 1);
-    else if (next.first < m1)
-      put_low(nst & 1);
-    const char* Xs = lds[st & 1] + wm * MB * 32 * 128;
-    const char* Ws = lds[st & 1] + kX + wn * NB * 32 * 128;
+    wait_for_stage<kStages - 2, TX + TW>(nst - 1 - st);
+    // the stage before has been read by all: its buffer is filled next
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    if (st + kStages - 1 < nst) put_main(st + kStages - 1);
+    if (st + 1 == nst && next.first < m1) put_low(nst % kStages);
+    const char* Xs = lds[st % kStages] + wm * MB * 32 * 128;
+    const char* Ws = lds[st % kStages] + kX + wn * NB * 32 * 128;
     // Operands of k step ks in register set ks & 1: the reads of step ks + 1
     // run between the matrix instructions of step ks.
     bf16x8 op[2][NB + MB];
@@ -606,9 +598,9 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2,
     wait_vmcnt<0>();
     __syncthreads();
     advance();
-    if (next.first < m1) put_low((st + 1) & 1);
-    const char* Xs = lds[st & 1] + wm * MB * 32 * 128;
-    const char* Ws = lds[st & 1] + kX + wn * NB * 32 * 128;
+    if (next.first < m1) put_low((st + 1) % kStages);
+    const char* Xs = lds[st % kStages] + wm * MB * 32 * 128;
+    const char* Ws = lds[st % kStages] + kX + wn * NB * 32 * 128;
     const bool all_f = fa <= f0 && f1 <= fb;
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) {
@@ -856,13 +848,13 @@ hipError_t launch_adapter_project(const AdapterArgs& a, const AdapterPlan& plan,
         launch_few<4, 3, 4>(a, plan, stream);
       break;
     case AdapterKernel::kTiles64:
-      hipLaunchKernelGGL((tile_kernel<2, 2, 1, 1>), grid, dim3(256), 0, stream, a);
+      hipLaunchKernelGGL((tile_kernel<2, 2, 1, 1, 4>), grid, dim3(256), 0, stream, a);
       break;
     case AdapterKernel::kTiles128:
-      hipLaunchKernelGGL((tile_kernel<2, 2, 2, 2>), grid, dim3(256), 0, stream, a);
+      hipLaunchKernelGGL((tile_kernel<2, 2, 2, 2, 2>), grid, dim3(256), 0, stream, a);
       break;
     case AdapterKernel::kTiles256:
-      hipLaunchKernelGGL((tile_kernel<2, 4, 4, 2>), grid, dim3(512), 0, stream, a);
+      hipLaunchKernelGGL((tile_kernel<2, 4, 4, 2, 2>), grid, dim3(512), 0, stream, a);
       break;
     case AdapterKernel::kAny64:
       hipLaunchKernelGGL(any_kernel<1>, grid, dim3(kThreads), 0, stream, a);

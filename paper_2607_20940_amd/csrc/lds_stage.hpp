@@ -128,6 +128,20 @@ __device__ inline void wait_vmcnt() {
   __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (0x7 << 4) | (0xF << 8));
 }
 
+// Waits until at most min(later, MOST) x EACH of the wave's transfers are left:
+// those of a stage are done once only the later stages' are.
+template <int MOST, int EACH>
+__device__ inline void wait_for_stage(int later) {
+  if constexpr (MOST == 0) {
+    wait_vmcnt<0>();
+  } else {
+    if (later >= MOST)
+      wait_vmcnt<MOST * EACH>();
+    else
+      wait_for_stage<MOST - 1, EACH>(later);
+  }
+}
+
 // Raw buffer resource (gfx9 layout) over `bytes` bytes from `base`, in SGPRs.
 __device__ inline i32x4 rsrc_of(const void* base, uint32_t bytes) {
   const uint64_t b = reinterpret_cast<uint64_t>(base);

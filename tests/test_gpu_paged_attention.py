@@ -250,3 +250,29 @@ def test_repeatable_on_another_stream_and_in_a_graph(new, before, KH):
         call(a)
         torch.cuda.synchronize()
         assert torch.equal(a[1], b[1]) and torch.equal(a[2], b[2])
+
+
+@pytest.mark.parametrize("n", [1, 300])
+def test_pools_whose_offsets_pass_32_bits(n):
+    """Pages at the far end of a pool of 5 GiB, which the append fills and the attention reads."""
+    rng = np.random.default_rng(n)
+    KH, D, page, before = 8, 128, 256, 200
+    pages = (5 << 30) // (page * KH * D * 2)
+    held = n + before
+    used = -(-held // page)
+    table = np.arange(pages - used, pages)[None]
+    x = [cuda(rng.normal(size=(held, KH * D)), "bf16") for _ in range(2)]
+    k_pages, v_pages = (torch.empty(pages, page, KH, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    d = mssa.paged_append_desc(held, 1, 0, KH, D, page, pages, used, rotate_dims=0)
+    mssa.mssa_paged_append(d, None, *x, None, ints([held]), ints(table), None, None, None, k_pages, v_pages)
+    assert torch.equal(k_pages[pages - used:].view(-1, KH * D)[:held], x[0])
+    assert torch.equal(v_pages[pages - used:].view(-1, KH * D)[:held], x[1])
+    q = cuda(rng.normal(size=(n, KH, D)), "bf16")
+    out, lse = torch.empty_like(q), torch.empty(KH, n, device="cuda")
+    d = mssa.paged_attention_desc(n, 1, n, KH, KH, D, page, pages, used, mask_block=1)
+    ws = torch.empty(mssa.mssa_paged_attention_workspace_size(d) + 16, dtype=torch.uint8, device="cuda")
+    mssa.mssa_paged_attention(d, q, k_pages, v_pages, None, ints([held]), ints(table), None, None, ws, out, lse)
+    k, v = (f64(t).reshape(1, held, KH, D) for t in x)
+    ref, ref_lse, mag = paged.attention(f64(q), k, v, None, [held], [[0]], D ** -0.5, 1)
+    assert (np.abs(f64(out) - ref) <= 2.0 ** -8 * 1.02 * (np.abs(ref) + mag) + 1e-4 * mag).all()
+    assert (np.abs(f64(lse) - ref_lse) <= 1e-4).all()
