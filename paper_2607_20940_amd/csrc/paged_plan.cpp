@@ -17,11 +17,11 @@ hipError_t plan_paged_attention(int64_t tokens, int32_t batch, int32_t max_chunk
                                 int32_t head_dim, int64_t capacity, PagedAttnPlan* plan) {
   PagedAttnPlan p{};
   const int64_t group = q_heads / kv_heads, rows = std::min<int64_t>(max_chunk, std::max<int64_t>(tokens, 1)) * group;
-  // Up to 1024 rows blocks of four waves, two on a CU: an item's rows fit better
+  // Up to 1536 rows blocks of four waves, two on a CU: an item's rows fit better
   // (391 causal tokens of 3 heads a key head, three streams: 35 us, 37 with eight
   // waves); above, eight waves share each tile (1800 tokens of 4 heads over 10800
   // tokens 70 us, 78 with four).
-  p.waves = rows <= 32 ? 0 : rows <= 1024 ? 4 : 8;
+  p.waves = rows <= 32 ? 0 : rows <= 1536 ? 4 : 8;
   p.slot_rows = p.waves ? p.waves * 32 : rows <= 16 ? 16 : 32;
   // every sequence's items: whole ones, and one that is not full
   const int64_t items = kv_heads * std::min(batch * ((rows + p.slot_rows - 1) / p.slot_rows), batch + tokens * group / p.slot_rows);
@@ -34,7 +34,7 @@ hipError_t plan_paged_attention(int64_t tokens, int32_t batch, int32_t max_chunk
   // 32760 tokens 39.5 us, 49.5 with them, whose pieces are twice as many to join).
   p.few_waves = items >= 1024 ? 2 : 4;
   const int64_t slots = p.waves == 8 || (!p.waves && p.few_waves == 4) ? 256 : 512;  // blocks resident at once
-  const int64_t least = p.waves ? 4 : 2 * p.few_waves;  // tiles of a share at least
+  const int64_t least = p.waves ? 6 : 2 * p.few_waves;  // tiles of a share at least
   if (tiles > least) p.workers = static_cast<int32_t>(std::max<int64_t>(1, std::min(slots, items * tiles / least)));
   // units as small as 31 bits of them allow
   while (p.unit_shift < 4 && items * (tiles + p.extra) << (p.unit_shift + 1) <= 0x7fffffff) ++p.unit_shift;
