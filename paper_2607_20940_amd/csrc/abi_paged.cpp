@@ -62,8 +62,9 @@ mssa_status project_check(const mssa_adapter_project_desc* d) {
   return MSSA_OK;
 }
 
-mssa_status plan_of(const mssa_adapter_project_desc* d, bool whole, mssa::AdapterPlan* plan) {
-  if (mssa::plan_adapter_project(d->rows, d->out_features, d->parts, d->segments, d->adapters, d->rank, whole, plan) != hipSuccess)
+mssa_status plan_of(const mssa_adapter_project_desc* d, mssa::AdapterPlan* plan) {
+  if (mssa::plan_adapter_project(d->rows, d->in_features, stride_or(d->x_stride, d->in_features), d->out_features, d->parts,
+                                 d->segments, d->adapters, d->rank, plan) != hipSuccess)
     return fail(MSSA_ERR_UNSUPPORTED, "too many outputs for one launch");
   return MSSA_OK;
 }
@@ -101,9 +102,8 @@ mssa_status mssa_adapter_project_workspace_size(const mssa_adapter_project_desc*
   return guarded("mssa_adapter_project_workspace_size", [&]() -> mssa_status {
     if (const mssa_status s = project_check(desc); s != MSSA_OK) return s;
     if (!bytes) return fail(MSSA_ERR_INVALID_ARG, "null argument");
-    // the same for both kinds of tensors
     mssa::AdapterPlan plan;
-    const mssa_status planned = plan_of(desc, false, &plan);
+    const mssa_status planned = plan_of(desc, &plan);
     if (planned == MSSA_OK) *bytes = plan.workspace_bytes;
     return planned;
   });
@@ -119,17 +119,17 @@ mssa_status mssa_adapter_project(const mssa_adapter_project_desc* desc, const vo
     const bool low = desc->segments > 0 && desc->adapters > 0;
     if (!x || !w || !y) return fail(MSSA_ERR_INVALID_ARG, "null argument");
     if (low && (!segment_begin || !adapter || !a || !b)) return fail(MSSA_ERR_INVALID_ARG, "null argument");
-    for (const void* t : {x, w, bias, a, b})
+    for (const void* t : {x, w, a})
+      if (!aligned16(t)) return fail(MSSA_ERR_INVALID_ARG, "x, w and a must be 16-byte aligned");
+    for (const void* t : {bias, b})
       if (!aligned_to(t, 2)) return fail(MSSA_ERR_INVALID_ARG, "a tensor is not aligned to its type");
     for (const void* t : {static_cast<const void*>(segment_begin), static_cast<const void*>(adapter), static_cast<const void*>(scale)})
       if (!aligned_to(t, 4)) return fail(MSSA_ERR_INVALID_ARG, "segments, adapters and scales must be aligned to 4 bytes");
     const int64_t x_stride = stride_or(desc->x_stride, desc->in_features);
-    // (the tiles' byte offsets have 32 bits: 256 rows of x)
-    bool whole = desc->in_features % 8 == 0 && x_stride % 8 == 0 && x_stride <= (1 << 21), whole_y = desc->out_features / desc->parts % 8 == 0;
-    for (const void* t : {x, w, a}) whole = whole && aligned16(t);
+    bool whole_y = desc->out_features / desc->parts % 8 == 0;
     for (int p = 0; p < desc->parts; ++p) whole_y = whole_y && aligned16(y[p]);
     mssa::AdapterPlan plan;
-    if (const mssa_status planned = plan_of(desc, whole, &plan); planned != MSSA_OK) return planned;
+    if (const mssa_status planned = plan_of(desc, &plan); planned != MSSA_OK) return planned;
     if (plan.workspace_bytes > 0) {
       if (!workspace || workspace_bytes < plan.workspace_bytes)
         return fail(MSSA_ERR_WORKSPACE, "workspace smaller than mssa_adapter_project_workspace_size");
@@ -163,7 +163,7 @@ mssa_status mssa_adapter_project(const mssa_adapter_project_desc* desc, const vo
     args.rank = desc->rank;
     args.low_rank = plan.low_rank;
     args.part0_scale = desc->part0_scale;
-    args.whole = whole;
+    args.whole = desc->in_features % 8 == 0 && x_stride % 8 == 0 && x_stride <= (1 << 21);
     args.whole_b = desc->rank % 8 == 0 && aligned16(b);
     args.whole_y = whole_y;
     return check_device(mssa::launch_adapter_project(args, plan, stream_of(stream)), "adapter projection launch");

@@ -678,124 +678,30 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2,
   }
 }
 
-// ------------------------------------------------------------ any alignment
-// Tiles of MB x 64 rows and as many features, a wave half by half of it, the
-// contraction in 32-deep stages through registers and LDS: rows that begin
-// anywhere.
-constexpr int kGK = 32, kGStr = kGK + 8;  // LDS row stride: conflict-free 16-byte reads
+// -------------------------------------------------------------- odd rows
+// Rows that are not whole aligned chunks, copied behind one another with zeros up
+// to whole ones: the tiles' transfers take no others.  (With 128 x 128 tiles made
+// through registers instead, 27840 x 5120 -> 15360 took 16.7 ms; the copies are 0.2.)
+struct PackArgs {
+  const __bf16* from[3];
+  __bf16* to[3];
+  int64_t stride[3], rows[3];  // stride: elements between rows
+  int32_t K, K8;
+};
 
-template <int MB>
-__global__ __launch_bounds__(kThreads) void any_kernel(AdapterArgs a) {
-  constexpr int kGM = MB * 64, kGN = kGM;
-  __shared__ __attribute__((aligned(16))) __bf16 lds[2][2][kGM * kGStr];  // [stage][X | W]
-  const int tiles_m = (a.M + kGM - 1) / kGM;
-  const int tm = blockIdx.x % tiles_m, tn = blockIdx.x / tiles_m;
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wm = wave & 1, wn = wave >> 1;
-  const int n32 = lane & 31, hh = lane >> 5;
-  const int32_t m0 = tm * kGM, m1 = min(m0 + kGM, a.M), f0 = tn * kGN, f1 = min(f0 + kGN, a.N);
-
-  // Stage loads: kGM rows x 4 pieces of 8 values per matrix, MB pieces per thread.
-  const int lr = tid >> 2, lc = (tid & 3) * 8;
-  bf16x8 px[MB], pw[MB];
-  auto load = [&](const __bf16* x, int64_t xs, int32_t xa, int32_t xb, const __bf16* w, int64_t ws, int32_t wa, int32_t wb, int left) {
+__global__ __launch_bounds__(kThreads) void pack_kernel(PackArgs a) {
+  const int32_t chunks = a.K8 / 8;
+  int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
 #pragma unroll
-    for (int i = 0; i < MB; ++i) {
-      const int32_t xr = m0 + lr + i * 64, wr = f0 + lr + i * 64;
-      px[i] = xr >= xa && xr < xb ? eight(x + xr * xs + lc, left - lc) : bf16x8{};
-      pw[i] = wr >= wa && wr < wb ? eight(w + wr * ws + lc, left - lc) : bf16x8{};
+  for (int t = 0; t < 3; ++t) {
+    const int64_t n = a.rows[t] * chunks;
+    if (i < n) {
+      const int64_t row = i / chunks;
+      const int32_t k = static_cast<int32_t>(i - row * chunks) * 8;
+      *reinterpret_cast<bf16x8*>(a.to[t] + row * a.K8 + k) = eight(a.from[t] + row * a.stride[t] + k, a.K - k);
+      return;
     }
-  };
-  auto store = [&](int s) {
-#pragma unroll
-    for (int i = 0; i < MB; ++i) {
-      const int r = lr + i * 64;
-      *reinterpret_cast<bf16x8*>(&lds[s][0][r * kGStr + lc]) = px[i];
-      *reinterpret_cast<bf16x8*>(&lds[s][1][r * kGStr + lc]) = pw[i];
-    }
-  };
-  auto operand = [&](int s, int which, int block, int ks) {
-    return *reinterpret_cast<const bf16x8*>(&lds[s][which][((which ? wn : wm) * MB * 32 + block * 32 + n32) * kGStr + ks * 16 + hh * 8]);
-  };
-
-  f32x16 acc[MB][MB];
-#pragma unroll
-  for (int rb = 0; rb < MB; ++rb)
-#pragma unroll
-    for (int cb = 0; cb < MB; ++cb) acc[rb][cb] = f32x16{};
-
-  const __bf16* X = static_cast<const __bf16*>(a.x);
-  const __bf16* W = static_cast<const __bf16*>(a.w);
-  const int nst = (a.K + kGK - 1) / kGK;
-  auto load_stage = [&](int st) { load(X + st * kGK, a.x_stride, m0, m1, W + st * kGK, a.K, f0, f1, a.K - st * kGK); };
-  load_stage(0);
-  store(0);
-  __syncthreads();
-  for (int st = 0; st < nst; ++st) {
-    if (st + 1 < nst) load_stage(st + 1);
-#pragma unroll
-    for (int ks = 0; ks < kGK / 16; ++ks)
-#pragma unroll
-      for (int rb = 0; rb < MB; ++rb)
-#pragma unroll
-        for (int cb = 0; cb < MB; ++cb)
-          acc[rb][cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand(st & 1, 1, cb, ks), operand(st & 1, 0, rb, ks), acc[rb][cb], 0, 0, 0);
-    if (st + 1 < nst) store((st + 1) & 1);
-    __syncthreads();
-  }
-
-  // Element e of acc[rb][cb]: row (wm MB + rb) 32 + n32, feature (wn MB + cb) 32 + 8 (e / 4) + 4 hh + e % 4 of the tile.
-  const int p0 = f0 / a.split, p1 = (f1 - 1) / a.split;
-  for (int32_t s = __builtin_amdgcn_readfirstlane(first_segment(a, m0)); s < a.segments; ++s) {
-    const Segment g = segment(a, s);
-    if (g.first >= m1) break;
-    if (g.adapter < 0 || g.first >= g.end) continue;
-    for (int p = p0; p <= p1; ++p) {
-      const __bf16* u = static_cast<const __bf16*>(a.low) + p * a.low_rank;
-      const __bf16* B = static_cast<const __bf16*>(a.b) + static_cast<int64_t>(g.adapter) * a.N * a.rank;
-      const int32_t fa = p * a.split, fb = fa + a.split;
-      for (int r0 = 0; r0 < a.rank; r0 += kGK) {
-        load(u + r0, static_cast<int64_t>(a.parts) * a.low_rank, g.first, g.end, B + r0, a.rank, fa, min(fb, f1), a.rank - r0);
-        store(0);
-        __syncthreads();
-#pragma unroll
-        for (int rb = 0; rb < MB; ++rb) {
-          const int32_t row = m0 + wm * MB * 32 + rb * 32 + n32;
-          const bool mine = row >= g.first && row < g.end;
-#pragma unroll
-          for (int cb = 0; cb < MB; ++cb) {
-            f32x16 add = f32x16{};
-#pragma unroll
-            for (int ks = 0; ks < kGK / 16; ++ks)
-              add = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand(0, 1, cb, ks), operand(0, 0, rb, ks), add, 0, 0, 0);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const int32_t f = f0 + wn * MB * 32 + cb * 32 + 8 * (e >> 2) + 4 * hh + (e & 3);
-              acc[rb][cb][e] += mine && f >= fa && f < fb ? add[e] : 0.f;
-            }
-          }
-        }
-        __syncthreads();
-      }
-    }
-  }
-
-  const __bf16* bias = static_cast<const __bf16*>(a.bias);
-#pragma unroll
-  for (int rb = 0; rb < MB; ++rb) {
-    const int32_t row = m0 + wm * MB * 32 + rb * 32 + n32;
-    if (row >= m1) continue;
-#pragma unroll
-    for (int cb = 0; cb < MB; ++cb)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int32_t f = f0 + wn * MB * 32 + cb * 32 + 8 * (e >> 2) + 4 * hh + (e & 3);
-        if (f >= f1) continue;
-        const int part = f / a.split;
-        const float v = (acc[rb][cb][e] + (bias ? static_cast<float>(bias[f]) : 0.f)) * (part == 0 ? a.part0_scale : 1.f);
-        static_cast<__bf16*>(a.y[part])[static_cast<int64_t>(row) * a.split + (f - part * a.split)] = static_cast<__bf16>(v);
-      }
+    i -= n;
   }
 }
 
@@ -833,7 +739,37 @@ hipError_t launch_low(const AdapterArgs& a, const AdapterPlan& plan, hipStream_t
 
 }  // namespace
 
-hipError_t launch_adapter_project(const AdapterArgs& a, const AdapterPlan& plan, hipStream_t stream) {
+hipError_t launch_adapter_project(const AdapterArgs& given, const AdapterPlan& plan, hipStream_t stream) {
+  AdapterArgs a = given;
+  if (plan.pack_x || plan.pack_w) {
+    const int32_t k8 = (a.K + 7) / 8 * 8;
+    PackArgs p{};
+    p.K = a.K;
+    p.K8 = k8;
+    char* to = static_cast<char*>(a.low) + plan.low_bytes;
+    int64_t chunks = 0;
+    auto pack = [&](int t, const void** tensor, int64_t rows, int64_t stride) {
+      p.from[t] = static_cast<const __bf16*>(*tensor);
+      p.to[t] = reinterpret_cast<__bf16*>(to);
+      p.stride[t] = stride;
+      p.rows[t] = rows;
+      *tensor = to;
+      to += rows * k8 * 2;
+      chunks += rows * (k8 / 8);
+    };
+    if (plan.pack_x) {
+      pack(0, &a.x, a.M, a.x_stride);
+      a.x_stride = k8;
+    }
+    if (plan.pack_w) {
+      pack(1, &a.w, a.N, a.K);
+      if (a.segments) pack(2, &a.a, int64_t{a.adapters} * a.parts * a.rank, a.K);
+      a.K = k8;
+    }
+    a.whole = true;
+    hipLaunchKernelGGL(pack_kernel, dim3(static_cast<uint32_t>((chunks + kThreads - 1) / kThreads)), dim3(kThreads), 0, stream, p);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
   if (plan.low_tiles) {
     if (const hipError_t e = launch_low(a, plan, stream); e != hipSuccess) return e;
   }
@@ -855,12 +791,6 @@ hipError_t launch_adapter_project(const AdapterArgs& a, const AdapterPlan& plan,
       break;
     case AdapterKernel::kTiles256:
       hipLaunchKernelGGL((tile_kernel<2, 4, 4, 2, 2>), grid, dim3(512), 0, stream, a);
-      break;
-    case AdapterKernel::kAny64:
-      hipLaunchKernelGGL(any_kernel<1>, grid, dim3(kThreads), 0, stream, a);
-      break;
-    case AdapterKernel::kAny128:
-      hipLaunchKernelGGL(any_kernel<2>, grid, dim3(kThreads), 0, stream, a);
   }
   return hipGetLastError();
 }

@@ -188,23 +188,23 @@ struct AdapterArgs {
   bool whole, whole_b, whole_y;
 };
 
-// Which kernel makes a product: the one for few tokens, one of three tile sizes
-// (tokens and features), or of two where rows may begin anywhere.
-enum class AdapterKernel { kFew, kTiles64, kTiles128, kTiles256, kAny64, kAny128 };
+// Which kernel makes a product: the one for few tokens, or one of three tile
+// sizes (tokens and features).
+enum class AdapterKernel { kFew, kTiles64, kTiles128, kTiles256 };
 constexpr int kAdapterFewTokens = 64, kAdapterFewFeatures = 32;
 
 constexpr int kLowRows = 16, kLowManyRows = 64;  // rows of a tile of the low-rank factor
 struct AdapterPlan {
   AdapterKernel kernel;
-  int32_t low_rows;   // of a tile of the low-rank factor's launch
-  int64_t low_tiles;  // its row tiles, 0: none
-  int64_t blocks;      // of the product
-  int64_t workspace_bytes;
-  int32_t low_rank;    // rank rounded up to whole 16 values
+  bool pack_x, pack_w;  // rows of x, and of w and a, are copied to whole chunks first (not for few tokens)
+  int32_t low_rows;     // of a tile of the low-rank factor's launch
+  int32_t low_rank;     // rank rounded up to whole 16 values
+  int64_t low_tiles;    // its row tiles, 0: none
+  int64_t blocks;       // of the product
+  int64_t low_bytes, workspace_bytes;  // the low-rank factors, then the copies
 };
-// whole: as AdapterArgs has it.  The workspace is the same either way.
-hipError_t plan_adapter_project(int64_t rows, int32_t out_features, int32_t parts, int32_t segments, int32_t adapters,
-                                int32_t rank, bool whole, AdapterPlan* plan);
+hipError_t plan_adapter_project(int64_t rows, int32_t in_features, int64_t x_stride, int32_t out_features, int32_t parts,
+                                int32_t segments, int32_t adapters, int32_t rank, AdapterPlan* plan);
 hipError_t launch_adapter_project(const AdapterArgs& a, const AdapterPlan& plan, hipStream_t stream);
 
 }  // namespace mssa

@@ -48,32 +48,43 @@ hipError_t plan_paged_attention(int64_t tokens, int32_t batch, int32_t max_chunk
   return hipSuccess;
 }
 
-hipError_t plan_adapter_project(int64_t rows, int32_t out_features, int32_t parts, int32_t segments, int32_t adapters,
-                                int32_t rank, bool whole, AdapterPlan* plan) {
+hipError_t plan_adapter_project(int64_t rows, int32_t in_features, int64_t x_stride, int32_t out_features, int32_t parts,
+                                int32_t segments, int32_t adapters, int32_t rank, AdapterPlan* plan) {
   AdapterPlan p{};
   auto tiles = [&](int64_t m, int64_t n) { return (rows + m - 1) / m * ((out_features + n - 1) / n); };
   if (rows <= kAdapterFewTokens) {
     p.kernel = AdapterKernel::kFew;
     p.blocks = tiles(kAdapterFewTokens, kAdapterFewFeatures);
-  } else if (whole && tiles(256, 256) >= 256) {
+  } else if (tiles(256, 256) >= 256) {
     p.kernel = AdapterKernel::kTiles256;
     p.blocks = tiles(256, 256);
   } else if (tiles(128, 128) >= 256) {
-    p.kernel = whole ? AdapterKernel::kTiles128 : AdapterKernel::kAny128;
+    p.kernel = AdapterKernel::kTiles128;
     p.blocks = tiles(128, 128);
   } else {
-    p.kernel = whole ? AdapterKernel::kTiles64 : AdapterKernel::kAny64;
+    p.kernel = AdapterKernel::kTiles64;
     p.blocks = tiles(64, 64);
   }
   if (!launchable(p.blocks, 512)) return hipErrorInvalidValue;
-  if (segments > 0 && adapters > 0) {
+  const bool low = segments > 0 && adapters > 0;
+  if (low) {
     p.low_rank = (rank + 15) / 16 * 16;
     // tiles of 64 rows where each is nearly full and there are some for most CUs
-    p.low_rows = whole && rows > 4096 && rows / segments >= kLowManyRows ? kLowManyRows : kLowRows;
+    p.low_rows = p.kernel != AdapterKernel::kFew && rows > 4096 && rows / segments >= kLowManyRows ? kLowManyRows : kLowRows;
     // every segment's tiles: whole ones, and one that is not full
     p.low_tiles = std::min<int64_t>(rows, segments + rows / p.low_rows);
     if (!launchable(p.low_tiles, 1024)) return hipErrorInvalidValue;
-    p.workspace_bytes = rows * parts * p.low_rank * 2;
+    p.low_bytes = (rows * parts * p.low_rank * 2 + 255) / 256 * 256;
+  }
+  p.workspace_bytes = p.low_bytes;
+  if (p.kernel != AdapterKernel::kFew) {
+    const int64_t k8 = (in_features + 7) / 8 * 8;
+    p.pack_w = in_features % 8 != 0;
+    // the tiles' byte offsets have 32 bits: 256 rows of x
+    p.pack_x = p.pack_w || x_stride % 8 != 0 || x_stride > (1 << 21);
+    const int64_t copied = (p.pack_x ? rows : 0) + (p.pack_w ? out_features + (low ? int64_t{adapters} * parts * rank : 0) : 0);
+    if (copied * (k8 / 8) > kLaunchThreads) return hipErrorInvalidValue;
+    p.workspace_bytes += copied * k8 * 2;
   }
   *plan = p;
   return hipSuccess;

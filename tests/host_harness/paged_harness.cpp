@@ -249,16 +249,24 @@ hipError_t launch_adapter_project(const AdapterArgs& a, const AdapterPlan& plan,
   if (a.bias) check_range(a.bias, int64_t{a.N} * 2, "bias");
   check(a.N == a.parts * a.split, "parts");
   for (int p = 0; p < a.parts; ++p) check_range(a.y[p], span(a.M, a.split, a.split), "y");
-  static const int side[][2] = {{kAdapterFewTokens, kAdapterFewFeatures}, {64, 64}, {128, 128}, {256, 256}, {64, 64}, {128, 128}};
+  static const int side[][2] = {{kAdapterFewTokens, kAdapterFewFeatures}, {64, 64}, {128, 128}, {256, 256}};
   const int* t = side[static_cast<int>(plan.kernel)];
   check(plan.blocks == (a.M + t[0] - 1) / t[0] * ((int64_t{a.N} + t[1] - 1) / t[1]), "a block a tile");
   check(plan.kernel != AdapterKernel::kFew || a.M <= kAdapterFewTokens, "few tokens");
-  if (a.whole) {
-    check(a.K % 8 == 0 && a.x_stride % 8 == 0 && (reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w)) % 16 == 0, "whole chunks");
-    check(256 * a.x_stride * 2 + 128 < 0x7ffffff0 && 256 * int64_t{a.K} * 2 + 128 < 0x7ffffff0, "offsets inside a tile");
-  } else {
-    check(plan.kernel == AdapterKernel::kFew || plan.kernel == AdapterKernel::kAny64 || plan.kernel == AdapterKernel::kAny128, "rows that begin anywhere");
+  const bool few = plan.kernel == AdapterKernel::kFew;
+  check(few ? !plan.pack_x && !plan.pack_w : a.whole || plan.pack_x, "odd rows of many are copied");
+  check(a.whole || few || plan.pack_w || a.K % 8 == 0, "odd weights are copied");
+  const int64_t k8 = (a.K + 7) / 8 * 8, stride = plan.pack_x ? k8 : a.x_stride;
+  if (!few || a.whole) {
+    check(256 * stride * 2 + 128 < 0x7ffffff0 && 256 * k8 * 2 + 128 < 0x7ffffff0, "offsets inside a tile");
+    check(stride % 8 == 0 && (reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w)) % 16 == 0, "whole chunks");
   }
+  // the copies behind the low-rank factors
+  int64_t copies = plan.pack_x ? a.M * k8 : 0;
+  if (plan.pack_w) copies += (a.N + (a.segments ? int64_t{a.adapters} * a.parts * a.rank : 0)) * k8;
+  check(copies / 8 <= kLaunchThreads, "threads of the copies");
+  if (copies) check_range(static_cast<char*>(a.low) + plan.low_bytes, copies * 2, "workspace");
+  check(plan.low_bytes % 256 == 0, "the copies' alignment");
   if (a.segments) {
     check_range(a.segment_begin, (int64_t{a.segments} + 1) * 4, "segment_begin");
     check_range(a.adapter, int64_t{a.segments} * 4, "adapter");

@@ -100,7 +100,7 @@ def test_strides_and_alignments(pad, shift, M):
     outs = []
     for f in (lambda t: t, moved):
         y = f(torch.empty(M, N, dtype=torch.bfloat16, device="cuda"))
-        mssa.mssa_adapter_project(d, f(x), f(w), f(b0), seg, which, f(a), f(b), None, ws, [y])
+        mssa.mssa_adapter_project(d, x, w, f(b0), seg, which, a, f(b), None, ws, [y])
         outs.append(f64(y))
     ref, mag, low = paged.adapter_project(f64(x), f64(w), f64(b0), [0, M // 2, M], [1, 0], f64(a), f64(b), None, 1, 1.0)
     for got in outs:
@@ -159,7 +159,7 @@ def test_repeatable_on_another_stream_and_in_a_graph(M):
 
 
 @pytest.mark.parametrize("M,K,N,parts,R,S", [(4200, 72, 4104, 1, 8, 3), (4097, 136, 4608, 3, 40, 2), (5000, 64, 3700, 2, 12, 5),
-                                             (4500, 192, 3900, 3, 70, 4), (4300, 8, 4096, 1, 24, 40), (4200, 100, 2000, 1, 8, 3),
+                                             (4500, 192, 3900, 3, 70, 4), (4300, 8, 4096, 1, 24, 40), (4200, 100, 2000, 1, 8, 3), (4500, 97, 4100, 2, 16, 3), (9000, 131, 768, 3, 40, 2),
                                              (9000, 456, 768, 3, 100, 2), (2100, 328, 2050, 1, 16, 700)])
 def test_large_tiles(M, K, N, parts, R, S):
     rng = np.random.default_rng(M)

@@ -28,8 +28,8 @@ PROJECT = dict(rows=100, in_features=64, out_features=96, segments=2, adapters=3
     (UNS, dict(rank=257), {}), (INV, dict(part0_scale=float("nan")), {}), (INV, dict(x_stride=63), {}),
     (INV, dict(x_stride=-64), {}), (INV, dict(x_stride=1 << 40), {}),
     (INV, {}, dict(x=None)), (INV, {}, dict(w=None)), (INV, {}, dict(begin=None)), (INV, {}, dict(which=None)),
-    (INV, {}, dict(a=None)), (INV, {}, dict(b=None)), (INV, {}, dict(y=[None] * 3)), (INV, {}, dict(x=P + 1)),
-    (INV, {}, dict(bias=P + 1)), (INV, {}, dict(begin=P + 2)), (INV, {}, dict(which=P + 1)), (INV, {}, dict(scale=P + 2)),
+    (INV, {}, dict(a=None)), (INV, {}, dict(b=None)), (INV, {}, dict(y=[None] * 3)), (INV, {}, dict(x=P + 8)), (INV, {}, dict(w=P + 2)),
+    (INV, {}, dict(a=P * 6 + 4)), (INV, {}, dict(b=P * 7 + 1)), (INV, {}, dict(bias=P + 1)), (INV, {}, dict(begin=P + 2)), (INV, {}, dict(which=P + 1)), (INV, {}, dict(scale=P + 2)),
     (INV, {}, dict(y=[P * 20, P * 21, P * 22 + 1])), (INV, {}, dict(y=[P * 20, P, P * 22])),
     (INV, {}, dict(y=[P * 20, P * 6, P * 22])), (WS, {}, dict(workspace=None)), (WS, {}, dict(workspace_bytes=16)),
     (INV, {}, dict(workspace=P * 9 + 4)),
@@ -130,5 +130,12 @@ def test_workspaces_are_bounded(tokens, max_chunk, table_pages):
     d = mssa.paged_attention_desc(tokens, 1, max_chunk, 12, 12, 128, 64, 1000, table_pages)
     assert 0 <= mssa.mssa_paged_attention_workspace_size(d) <= 2 * 512 * 256 * 130 * 4
     d = mssa.adapter_project_desc(tokens, 128, 384, 4, 4, 100, parts=3)
-    assert 0 < mssa.mssa_adapter_project_workspace_size(d) <= tokens * 3 * 128 * 2 + (64 << 20)
-    assert mssa.mssa_adapter_project_workspace_size(mssa.adapter_project_desc(tokens, 128, 384, 0, 4, 100)) <= 64 << 20
+    assert 0 < mssa.mssa_adapter_project_workspace_size(d) <= tokens * 3 * 112 * 2 + 256
+    assert mssa.mssa_adapter_project_workspace_size(mssa.adapter_project_desc(tokens, 128, 384, 0, 4, 100)) == 0
+
+
+def test_workspace_of_odd_rows_holds_their_copies():
+    even, odd, apart = (mssa.mssa_adapter_project_workspace_size(mssa.adapter_project_desc(300, k, 200, 2, 3, 8, x_stride=x))
+                        for k, x in ((104, 0), (97, 0), (104, 107)))
+    assert odd - even == (300 + 200 + 3 * 8) * 104 * 2 and apart - even == 300 * 104 * 2
+    assert mssa.mssa_adapter_project_workspace_size(mssa.adapter_project_desc(64, 97, 200, 2, 3, 8)) == 64 * 16 * 2
