@@ -6,10 +6,12 @@
 
 namespace mssa {
 
-// A block's threads take two pieces of 16 values each at a time; while there
-// are blocks enough for two on every CU, several tokens share a block.
+// A block's threads take four pieces of 16 values each at most; while there are
+// blocks enough for two on every CU, several tokens share a block, its sines and
+// its look-ups (4680 tokens of 12 heads: 19.1 us, 21.1 with two pieces a thread,
+// 21.4 with ten).
 int32_t append_block_tokens(int64_t tokens, int32_t units) {
-  const int64_t most = std::min<int64_t>(std::max(1, 2 * kAppendThreads / units), kAppendMaxTokens);
+  const int64_t most = std::min<int64_t>(std::max(1, 4 * kAppendThreads / units), kAppendMaxTokens);
   return static_cast<int32_t>(std::max<int64_t>(1, std::min(most, tokens / 512)));
 }
 
