@@ -654,8 +654,8 @@ mssa_status mssa_adapter_project_workspace_size(const mssa_adapter_project_desc*
  *                  out_features, rank]
  *   scale          [adapters] fp32, NULL: 1
  *   y              host array of `parts` device pointers, each [rows, N]
- * An adapter's infinities and NaN reach its own rows only.  Outputs must not
- * alias the inputs.  x, w and a are 16-byte aligned; the other tensors need the
+ * An adapter's infinities and NaN reach its own rows only.  Outputs must
+ * alias neither the inputs nor one another.  x, w and a are 16-byte aligned; the other tensors need the
  * alignment of their type only.  Rows of x, w and a that are no multiples of 8
  * values apart are copied to the workspace first (more than 64 rows). */
 mssa_status mssa_adapter_project(const mssa_adapter_project_desc* desc, const void* x, const void* w, const void* bias,

@@ -141,6 +141,8 @@ mssa_status mssa_adapter_project(const mssa_adapter_project_desc* desc, const vo
       if (!aligned_to(y[p], 2)) return fail(MSSA_ERR_INVALID_ARG, "a tensor is not aligned to its type");
       for (const void* t : {x, w, bias, a, b})
         if (t == y[p]) return fail(MSSA_ERR_INVALID_ARG, "outputs must not alias the inputs");
+      for (int o = 0; o < p; ++o)
+        if (y[o] == y[p]) return fail(MSSA_ERR_INVALID_ARG, "outputs must not alias one another");
       args.y[p] = y[p];
     }
     args.x = x;

@@ -49,6 +49,13 @@ def test_project_wants_one_output_per_part():
         mssa.mssa_adapter_project(mssa.adapter_project_desc(**PROJECT), P, P, None, P, P, P, P, None, P, [P * 6], stream=0)
 
 
+def test_project_wants_outputs_of_their_own():
+    for y in ([P * 20, P * 20, P * 22], [P * 20, P * 21, P * 20]):
+        _refused(INV, lambda: mssa.mssa_adapter_project(
+            mssa.adapter_project_desc(**PROJECT), P, P * 2, P * 3, P * 4, P * 5, P * 6, P * 7, P * 8, P * 9, y,
+            workspace_bytes=1 << 40, stream=0))
+
+
 APPEND = dict(tokens=12, batch=3, q_heads=4, kv_heads=2, head_dim=64, page_tokens=16, pages=9, table_pages=4)
 
 
