@@ -118,6 +118,15 @@ class PagedStreams:
             want.append(need - have)
         if sum(want) > len(self.free):
             raise RuntimeError(f"{sum(want)} pages are needed and {len(self.free)} are free")
+        # what the library refuses is refused before anything changes
+        b, t, m = len(chunks), sum(news), self.max_stream_pages
+        project = mssa.adapter_project_desc(t, self.hidden, self.width, b if self.adapters else 0, self.adapters, self.rank)
+        append = mssa.paged_append_desc(t, b, self.q_heads, self.kv_heads, self.head_dim, self.page_tokens, self.pages, m,
+                                        rotate_dims=self.rotate_dims, halves=self.halves, axis_pairs=self.axis_pairs,
+                                        q_stride=self.width, k_stride=self.width, v_stride=self.width)
+        attend = mssa.paged_attention_desc(t, b, max(1, *news), self.q_heads, self.kv_heads, self.head_dim, self.page_tokens,
+                                           self.pages, m, mask_block=self.mask_block, softmax_scale=self.scale)
+        size = max(mssa.mssa_adapter_project_workspace_size(project), mssa.mssa_paged_attention_workspace_size(attend))
         begin, lens, which, table, positions = [0], [], [], [], []
         for s, n, w in zip(names, news, want):
             state = self.streams[s]
@@ -130,22 +139,11 @@ class PagedStreams:
             table.extend(state[0] + [-1] * (self.max_stream_pages - len(state[0])))
         # one copy for all of it
         host = torch.tensor(begin + lens + which + table + positions, dtype=torch.int32)
-        dev = host.to(self.device)
-        b, t, m = len(chunks), begin[-1], self.max_stream_pages
+        self.places = dev = host.to(self.device)
         cut = lambda at, n: dev[at:at + n]  # noqa: E731
         self.chunk_begin, self.kv_len, self.adapter = cut(0, b + 1), cut(b + 1, b), cut(2 * b + 1, b)
         self.table, self.positions = cut(3 * b + 1, b * m), cut(3 * b + 1 + b * m, t)
-        self.tokens = t
-        self.project = mssa.adapter_project_desc(t, self.hidden, self.width, b if self.adapters else 0, self.adapters,
-                                                 self.rank)
-        self.append = mssa.paged_append_desc(t, b, self.q_heads, self.kv_heads, self.head_dim, self.page_tokens, self.pages, m,
-                                             rotate_dims=self.rotate_dims, halves=self.halves, axis_pairs=self.axis_pairs,
-                                             q_stride=self.width, k_stride=self.width, v_stride=self.width)
-        self.attend = mssa.paged_attention_desc(t, b, max(1, *news), self.q_heads, self.kv_heads, self.head_dim,
-                                                self.page_tokens, self.pages, m, mask_block=self.mask_block,
-                                                softmax_scale=self.scale)
-        size = max(mssa.mssa_adapter_project_workspace_size(self.project),
-                   mssa.mssa_paged_attention_workspace_size(self.attend))
+        self.tokens, self.project, self.append, self.attend = t, project, append, attend
         if self.workspace.numel() < size:
             self.workspace = torch.empty(size, dtype=torch.uint8, device=self.device)
         self.batch = b
@@ -153,7 +151,8 @@ class PagedStreams:
     def layer_pass(self, layer, x, out, lse=None, positions=None, prior_out=None, prior_lse=None, stream=None):
         """x [tokens, hidden], out [tokens, q_heads, head_dim] bf16, lse [q_heads, tokens] fp32 or None, of the pass that
         is open.  positions [axes, tokens] int32 (None: tokens of the stream before, one axis); prior_out and prior_lse: an
-        attention of the same queries over other keys, joined with this one (they may be out and lse)."""
+        attention of the same queries over other keys, joined with this one (they may be out and lse).  Captured into a
+        graph it serves the pass that is open, until the next begin."""
         import torch
 
         if self.batch is None:
@@ -174,6 +173,11 @@ class PagedStreams:
                 raise ValueError(f"{name} must be contiguous {dtype} {shape}, not {v.dtype} {tuple(v.shape)}")
         w, bias, a, b, scale = self.weights[layer]
         qkv = self.qkv
+        if x.is_cuda:
+            # begin replaces these, while this stream may still be reading them
+            used = torch.cuda.ExternalStream(mssa._stream(stream), device=x.device)
+            self.places.record_stream(used)
+            self.workspace.record_stream(used)
         mssa.mssa_adapter_project(self.project, x, w, bias, self.chunk_begin, self.adapter, a, b, scale, self.workspace, [qkv],
                                   stream=stream)
         q, k, v = qkv, qkv[:, self.q_width:], qkv[:, self.q_width + self.kv_width:]

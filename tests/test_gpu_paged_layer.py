@@ -155,3 +155,29 @@ def test_a_captured_pass_repeats():
         p.layer_pass(0, x, first)
         torch.cuda.synchronize()
         assert torch.equal(out, first)
+
+
+def test_passes_on_another_stream_while_the_next_ones_begin():
+    """begin replaces the tables of a pass that another stream has not come to yet: they stay as they are for it."""
+    rng = np.random.default_rng(4)
+    layer, freqs = _layer(rng, 2, 16), torch.rand(D // 2, device="cuda")
+    x = cuda(rng.normal(size=(63, HIDDEN)), "bf16")
+    want, out = (torch.zeros(63, H, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    for other, to in ((False, want), (True, out)):
+        p = PagedStreams(1, HIDDEN, H, KH, D, 40, PAGE, 20, 64, 4, adapters=2, rank=16, freqs=freqs)
+        p.init_layer(0, *layer)
+        for s in range(3):
+            p.open(s, s - 1)
+        p.begin([(0, 40), (1, 3), (2, 20)])
+        side = torch.cuda.Stream() if other else torch.cuda.current_stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            if other:
+                torch.cuda._sleep(200_000_000)
+            p.layer_pass(0, x, to)
+        if other:
+            for _ in range(6):
+                p.begin([(2, 1), (0, 2), (1, 60)])
+                p.drop(1, p.streams[1][1] // PAGE * PAGE)
+        torch.cuda.synchronize()
+    assert torch.equal(out, want)

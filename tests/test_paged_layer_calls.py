@@ -3,6 +3,7 @@
 import pytest
 import torch
 
+from paper_2607_20940_amd import mssa
 from paper_2607_20940_amd.paged import PagedStreams
 
 
@@ -50,6 +51,14 @@ def test_refused_passes_change_nothing():
     for adapter in (2, -2):
         with pytest.raises(ValueError):
             p.open("z", adapter)
+
+
+def test_passes_that_the_library_refuses_change_nothing():
+    p = _streams(rank=300)
+    p.open("a")
+    with pytest.raises(mssa.MssaError):
+        p.begin([("a", 9)])
+    assert len(p.free) == 10 and p.streams["a"][:2] == [[], 0] and p.batch is None
 
 
 def test_tensors_of_other_types_and_shapes_are_refused():
