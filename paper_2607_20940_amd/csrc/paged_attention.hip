@@ -175,24 +175,12 @@ __device__ inline void write_joined(const PagedAttnArgs& a, const RowPlace& at, 
   if (a.lse && d == 0) a.lse[at.lse] = w.lse;
 }
 
-// The pages of one sequence: lane i of a wave looks token i of a tile up.
+// The pages of one sequence.
 struct PageWalk {
   const int32_t* table;
   uint32_t len;  // at least 1 where a tile is looked up
   int64_t pages;
   Divisor page;
-  __device__ uint32_t token(int tile) const {
-    const uint32_t at = static_cast<uint32_t>(tile) * kTile + (threadIdx.x & 63);
-    return at < len ? at : len - 1;
-  }
-  __device__ int32_t entry(int tile) const { return table[page.quotient(token(tile))]; }
-  // The token's row in the pool, -1 where it has none; `there` is a bit per token.
-  __device__ int32_t row(int tile, int32_t found, uint64_t* there) const {
-    const uint32_t tok = token(tile);
-    const bool ok = static_cast<uint32_t>(tile) * kTile + (threadIdx.x & 63) < len && found >= 0 && found < pages;
-    *there = __ballot(ok);
-    return ok ? found * static_cast<int32_t>(page.d) + static_cast<int32_t>(tok - page.quotient(tok) * page.d) : -1;
-  }
 };
 __device__ inline PageWalk walk_of(const PagedAttnArgs& a, int b, int len) {
   return {a.page_table + static_cast<int64_t>(b) * a.table_pages, static_cast<uint32_t>(len), a.pages, a.page};
