@@ -35,6 +35,34 @@ __device__ inline bf16x8 eight(const __bf16* p, int n) {
   return v;
 }
 
+// Eight neighbouring values of an aligned tensor from any of them on.  Loads that are
+// no multiples of 4 bytes apart take several times as long: the 16 bytes from the even
+// place before and the last value apart, joined once both are there (16 x 577 ->
+// 1728, rank 16: 15.7 us for both kernels, 33.7 with one load at any place; 64 x
+// 2001: 34 and 59).
+struct Eight {
+  uint32_t v __attribute__((ext_vector_type(4)));
+  uint32_t last, shift;
+  __device__ static Eight at(const __bf16* p) {
+    typedef uint32_t words __attribute__((ext_vector_type(4), aligned(4)));
+    const uint32_t odd = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p) >> 1) & 1;
+    return {*reinterpret_cast<const words*>(p - odd), *reinterpret_cast<const uint16_t*>(p + 7), odd * 16};
+  }
+  __device__ bf16x8 values() const {
+    typedef uint32_t words __attribute__((ext_vector_type(4)));
+    return __builtin_bit_cast(bf16x8, words{__builtin_amdgcn_alignbit(v[1], v[0], shift), __builtin_amdgcn_alignbit(v[2], v[1], shift),
+                                            __builtin_amdgcn_alignbit(v[3], v[2], shift), __builtin_amdgcn_alignbit(last, v[3], shift)});
+  }
+};
+
+// The values of v from the (8 - n)-th on, then zeros: where a row's last eight values
+// were read because only n were left, those.
+__device__ inline bf16x8 last_of(bf16x8 v, int n) {
+  typedef unsigned __int128 u128;
+  const u128 bits = __builtin_bit_cast(u128, v);
+  return __builtin_bit_cast(bf16x8, n <= 0 ? u128{0} : n >= 8 ? bits : bits >> (16 * (8 - n)));
+}
+
 // Rows [first, end) of segment s and its adapter, -1 for none.
 struct Segment {
   int32_t first, end, adapter;
@@ -97,14 +125,16 @@ __device__ inline LowTile low_tile(const AdapterArgs& a, int32_t tile, int32_t r
 // The low-rank factors of 16 rows of one segment, 16 of the parts' rank columns,
 // which stand behind one another.  The block's 16 waves share out the
 // contraction, 320 values each on their way at once, and their sums meet in LDS,
-// in a fixed order.  kWhole: rows of whole, aligned 16-byte chunks.
+// in a fixed order.  kWhole: rows of whole, aligned 16-byte chunks; else rows of at
+// least 8 values that begin anywhere, whose last eight are read where fewer than
+// eight are left and put in place afterwards (no load waits for a branch).
 // Bound by latency: a look-up of the segment, one round of loads, a meeting.  16 rows
 // of 8 adapters, 5120 values, 48 columns: 9 us.
 constexpr int kLowWaves = 16;
 
 template <bool kWhole>
 __global__ __launch_bounds__(kLowWaves * 64) void low_kernel(AdapterArgs a) {
-  constexpr int kUnroll = 10;
+  constexpr int kUnroll = kWhole ? 10 : 7;
   __shared__ float sums[kLowWaves][16 * 17];
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, q = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -115,15 +145,23 @@ __global__ __launch_bounds__(kLowWaves * 64) void low_kernel(AdapterArgs a) {
   const int part = c0 / a.low_rank, r = min(c0 + n - part * a.low_rank, a.rank - 1);
   const __bf16* x = static_cast<const __bf16*>(a.x) + static_cast<int64_t>(row) * a.x_stride + q * 8;
   const __bf16* A = static_cast<const __bf16*>(a.a) + ((static_cast<int64_t>(g.adapter) * a.parts + part) * a.rank + r) * a.K + q * 8;
-  auto get = [&](const __bf16* p, int k) -> bf16x8 {
-    if constexpr (!kWhole) return eight(p + k, a.K - k - q * 8);
-    return k + q * 8 < a.K ? *reinterpret_cast<const bf16x8*>(p + k) : bf16x8{};
+  auto get = [&](const __bf16* p, int k) {
+    if constexpr (kWhole)
+      return k + q * 8 < a.K ? *reinterpret_cast<const bf16x8*>(p + k) : bf16x8{};
+    else
+      return Eight::at(p + min(k, a.K - 8 - q * 8));
+  };
+  auto values = [&](const auto& v, int s) -> bf16x8 {
+    if constexpr (kWhole)
+      return v;
+    else
+      return s * 32 + 32 > a.K ? last_of(v.values(), a.K - s * 32 - q * 8) : v.values();
   };
   f32x4 acc = f32x4{};
   const int steps = (a.K + 31) / 32, each = (steps + kLowWaves - 1) / kLowWaves, s0 = wave * each, s1 = min(s0 + each, steps);
 #pragma unroll 1
   for (int s = s0; s < s1; s += kUnroll) {
-    bf16x8 xv[kUnroll], av[kUnroll];
+    decltype(get(x, 0)) xv[kUnroll], av[kUnroll];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       const int k = min(s + u, s1 - 1) * 32;
@@ -132,7 +170,7 @@ __global__ __launch_bounds__(kLowWaves * 64) void low_kernel(AdapterArgs a) {
     }
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u)
-      if (s + u < s1) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[u], xv[u], acc, 0, 0, 0);
+      if (s + u < s1) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(values(av[u], s + u), values(xv[u], s + u), acc, 0, 0, 0);
   }
 #pragma unroll
   for (int e = 0; e < 4; ++e) sums[wave][n * 17 + 4 * q + e] = acc[e];
@@ -374,8 +412,9 @@ __global__ __launch_bounds__(256) void few_ring_kernel(AdapterArgs a) {
   few_outputs<kRows, kWaves>(a, sums, which, f0);
 }
 
-// Rows that begin anywhere: eight waves, W and X from memory to registers as the
-// matrix cores take them, kUnroll steps of 32 values on their way.
+// Rows of at least 8 values that begin anywhere: eight waves, W and X from memory to
+// registers as the matrix cores take them, kUnroll steps of 32 values on their way.
+// Rows' ends as in low_kernel.
 template <int RT, int kUnroll>
 __global__ __launch_bounds__(512) void few_any_kernel(AdapterArgs a) {
   constexpr int kWaves = 8, FT = kFewFeatures / 16, kRows = RT * 16, kStr = kFewFeatures + 1;
@@ -397,22 +436,29 @@ __global__ __launch_bounds__(512) void few_any_kernel(AdapterArgs a) {
   const int steps = (a.K + 31) / 32, each = (steps + kWaves - 1) / kWaves, s0 = wave * each, s1 = min(s0 + each, steps);
 #pragma unroll 1
   for (int s = s0; s < s1; s += kUnroll) {
-    bf16x8 wv[kUnroll][FT], xv[kUnroll][RT];
+    Eight wv[kUnroll][FT], xv[kUnroll][RT];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-      const int k = min(s + u, s1 - 1) * 32, left = a.K - k - g * 8;
+      const int k = min(min(s + u, s1 - 1) * 32, a.K - 8 - g * 8);
 #pragma unroll
-      for (int f = 0; f < FT; ++f) wv[u][f] = eight(w[f] + k, left);
+      for (int f = 0; f < FT; ++f) wv[u][f] = Eight::at(w[f] + k);
 #pragma unroll
-      for (int t = 0; t < RT; ++t) xv[u][t] = eight(x[t] + k, left);
+      for (int t = 0; t < RT; ++t) xv[u][t] = Eight::at(x[t] + k);
     }
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u)
+    for (int u = 0; u < kUnroll; ++u) {
+      if (s + u >= s1) continue;
+      const int left = a.K - (s + u) * 32;
+      bf16x8 xs[RT];
 #pragma unroll
-      for (int f = 0; f < FT; ++f)
+      for (int t = 0; t < RT; ++t) xs[t] = left < 32 ? last_of(xv[u][t].values(), left - g * 8) : xv[u][t].values();
 #pragma unroll
-        for (int t = 0; t < RT; ++t)
-          if (s + u < s1) acc[f][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[u][f], xv[u][t], acc[f][t], 0, 0, 0);
+      for (int f = 0; f < FT; ++f) {
+        const bf16x8 ws = left < 32 ? last_of(wv[u][f].values(), left - g * 8) : wv[u][f].values();
+#pragma unroll
+        for (int t = 0; t < RT; ++t) acc[f][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ws, xs[t], acc[f][t], 0, 0, 0);
+      }
+    }
   }
   // element e of acc[f][t]: row 16 t + n, feature 16 f + 4 g + e
 #pragma unroll
@@ -433,7 +479,8 @@ __global__ __launch_bounds__(512) void few_any_kernel(AdapterArgs a) {
 // through kStages LDS buffers, filled by direct transfers kStages - 1 stages ahead;
 // one barrier a stage.  (Small tiles, of which there are few, wait for their
 // transfers' way: four buffers, 200 x 5120 -> 3000 takes 60 us with two, 47 with
-// four, 50 with eight.)  The adapters follow as further stages: 64 ranks
+// four, 50 with eight.)  KG groups of such waves take KG stages at once, each one
+// of its own, and meet in the end.  The adapters follow as further stages: 64 ranks
 // of one part of one segment, its rows' low-rank factors against B.
 // Tiles are taken in panels of four feature tiles, each XCD a run of them.
 // The outputs leave through LDS as whole-row 16-byte stores.
@@ -443,12 +490,12 @@ __global__ __launch_bounds__(512) void few_any_kernel(AdapterArgs a) {
 // with 24 stages, a start and 118 MB / 918 of outputs.
 constexpr int kBK = 64, kPanel = 4;
 
-template <int WM, int WN, int MB, int NB, int kStages>
-__global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void tile_kernel(AdapterArgs a) {
-  constexpr int NW = WM * WN, BM = WM * MB * 32, BN = WN * NB * 32;
+template <int WM, int WN, int MB, int NB, int KG, int kStages>
+__global__ __launch_bounds__(WM * WN * KG * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void tile_kernel(AdapterArgs a) {
+  constexpr int NW = WM * WN, kThreadsAll = NW * KG * 64, BM = WM * MB * 32, BN = WN * NB * 32;
   constexpr int kX = BM * 128, kW = BN * 128, kStage = kX + kW;  // bytes
   constexpr int TX = BM / 8 / NW, TW = BN / 8 / NW;              // transfers (8 rows) of a wave
-  __shared__ __attribute__((aligned(16))) char lds[kStages][kStage];
+  __shared__ __attribute__((aligned(16))) char lds[kStages * KG][kStage];
   __shared__ float biases[BN];
   const int tiles_m = (a.M + BM - 1) / BM, tiles_n = (a.N + BN - 1) / BN;
   const int t = xcd_remap(blockIdx.x, tiles_m * tiles_n);
@@ -458,7 +505,7 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2,
   const int32_t m1 = min(m0 + BM, a.M), f1 = min(f0 + BN, a.N);
 
   const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, hh = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int kg = __builtin_amdgcn_readfirstlane((tid >> 6) / NW), wave = __builtin_amdgcn_readfirstlane((tid >> 6) % NW);
   const int wm = wave % WM, wn = wave / WM;
 
   // A transfer: rows 8 i + lane / 8, physical chunk lane % 8 holding logical
@@ -482,11 +529,11 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2,
   const __bf16* W = static_cast<const __bf16*>(a.w) + static_cast<int64_t>(f0) * a.K;
   const uint32_t xrb = static_cast<uint32_t>(a.x_stride) * 2, wrb = static_cast<uint32_t>(a.K) * 2;
   auto put_main = [&](int st) {
-    const int left = min(a.K - st * kBK, kBK);  // a multiple of 8
-    put(st % kStages, X + st * kBK, xrb, static_cast<uint32_t>(m1 - m0 - 1) * xrb + left * 2, W + st * kBK, wrb,
+    const int k = (st * KG + kg) * kBK, left = KG == 1 ? min(a.K - k, kBK) : max(min(a.K - k, kBK), 0);  // a multiple of 8
+    put(st % kStages * KG + kg, X + k, xrb, static_cast<uint32_t>(m1 - m0 - 1) * xrb + left * 2, W + k, wrb,
         static_cast<uint32_t>(f1 - f0 - 1) * wrb + left * 2, left / 8);
   };
-  const int nst = (a.K + kBK - 1) / kBK;
+  const int nst = (a.K + kBK * KG - 1) / (kBK * KG);
 #pragma unroll
   for (int st = 0; st < kStages - 1; ++st)
     if (st < nst) put_main(st);
@@ -522,17 +569,18 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2,
     const int left = min(a.rank - next.r0, kBK), chunks = (left + 7) / 8;
     const uint32_t ubytes = static_cast<uint32_t>(m1 - m0 - 1) * urb + chunks * 16;
     if (a.whole_b) {
-      put(buf, u, urb, ubytes, b, brb, static_cast<uint32_t>(f1 - f0 - 1) * brb + left * 2, chunks);
+      if (kg == 0) put(buf, u, urb, ubytes, b, brb, static_cast<uint32_t>(f1 - f0 - 1) * brb + left * 2, chunks);
     } else {
       // rows that are not whole aligned chunks: through registers
       const i32x4 ru = rsrc_of(u, ubytes);
 #pragma unroll
       for (int i = 0; i < TX; ++i) {
+        if (kg) break;
         const int row = (wave * TX + i) * 8 + (lane >> 3), lc = unswz128(row, lane & 7);
         dma16(ru, lc < chunks ? row * urb + lc * 16 : kPastEnd,
               __builtin_amdgcn_readfirstlane(lds0 + buf * kStage + (wave * TX + i) * 1024));
       }
-      for (int c = tid; c < BN * 8; c += NW * 64) {
+      for (int c = tid; c < BN * 8; c += kThreadsAll) {
         const int row = c >> 3, chunk = c & 7;
         const int n = f0 + row < f1 ? left - chunk * 8 : 0;
         *reinterpret_cast<bf16x8*>(lds[buf] + kX + swz128(row, chunk * 8) * 2) = eight(b + static_cast<int64_t>(row) * a.rank + chunk * 8, n);
@@ -562,9 +610,9 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2,
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     if (st + kStages - 1 < nst) put_main(st + kStages - 1);
-    if (st + 1 == nst && next.first < m1) put_low(nst % kStages);
-    const char* Xs = lds[st % kStages] + wm * MB * 32 * 128;
-    const char* Ws = lds[st % kStages] + kX + wn * NB * 32 * 128;
+    if (st + 1 == nst && next.first < m1) put_low(nst % kStages * KG);
+    const char* Xs = lds[st % kStages * KG + kg] + wm * MB * 32 * 128;
+    const char* Ws = lds[st % kStages * KG + kg] + kX + wn * NB * 32 * 128;
     // Operands of k step ks in register set ks & 1: the reads of step ks + 1
     // run between the matrix instructions of step ks.
     bf16x8 op[2][NB + MB];
@@ -606,9 +654,10 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2,
     wait_vmcnt<0>();
     __syncthreads();
     advance();
-    if (next.first < m1) put_low((st + 1) % kStages);
-    const char* Xs = lds[st % kStages] + wm * MB * 32 * 128;
-    const char* Ws = lds[st % kStages] + kX + wn * NB * 32 * 128;
+    if (next.first < m1) put_low((st + 1) % kStages * KG);
+    if (kg) continue;
+    const char* Xs = lds[st % kStages * KG] + wm * MB * 32 * 128;
+    const char* Ws = lds[st % kStages * KG] + kX + wn * NB * 32 * 128;
     const bool all_f = fa <= f0 && f1 <= fb;
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) {
@@ -637,6 +686,32 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2,
     }
   }
 
+  if constexpr (KG > 1) {
+    // the first group takes the others' sums, one after the other
+    static_assert(NW * MB * NB * 64 * 16 * 4 <= static_cast<int>(sizeof(lds)), "a group's sums fit the stage buffers");
+    f32x4* const S = reinterpret_cast<f32x4*>(&lds[0][0]) + wave * MB * NB * 256 + lane;
+#pragma unroll 1
+    for (int g = 1; g < KG; ++g) {
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < MB * NB * 4; ++i) {
+        f32x16& c = acc[i / 4 / NB][i / 4 % NB];
+        const int e = i % 4 * 4;
+        if (kg == g) S[i * 64] = f32x4{c[e], c[e + 1], c[e + 2], c[e + 3]};
+      }
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < MB * NB * 4; ++i) {
+        f32x16& c = acc[i / 4 / NB][i / 4 % NB];
+        if (kg == 0) {
+          const f32x4 v = S[i * 64];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) c[i % 4 * 4 + e] += v[e];
+        }
+      }
+    }
+  }
+
   // Epilogue through LDS, one wave row's rows at a time.
   constexpr int kEStr = BN + 8, kERows = MB * 32;
   static_assert(kERows * kEStr * 2 <= static_cast<int>(sizeof(lds)), "a wave row's outputs fit the stage buffers");
@@ -644,7 +719,7 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2,
 #pragma unroll 1
   for (int part_m = 0; part_m < WM; ++part_m) {
     __syncthreads();  // the stage buffers, or the rows before, are free
-    if (wm == part_m) {
+    if (wm == part_m && kg == 0) {
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -668,10 +743,10 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2,
     }
     __syncthreads();
 #pragma unroll
-    for (int p = 0; p < kERows * BN / 8 / (NW * 64); ++p) {
-      const int c = p * NW * 64 + tid, rt = c / (BN / 8), ch = c % (BN / 8);
+    for (int p = 0; p < (kERows * BN / 8 + kThreadsAll - 1) / kThreadsAll; ++p) {
+      const int c = p * kThreadsAll + tid, rt = c / (BN / 8), ch = c % (BN / 8);
       const int32_t row = m0 + part_m * kERows + rt, f = f0 + ch * 8;
-      if (row >= m1 || f >= a.N) continue;
+      if (rt >= kERows || row >= m1 || f >= a.N) continue;
       const bf16x8 v = *reinterpret_cast<const bf16x8*>(E + rt * kEStr + ch * 8);
       if (a.whole_y) {
         const int part = f / a.split;  // 8 features never straddle a part (split % 8 == 0)
@@ -688,7 +763,8 @@ __global__ __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2,
 
 // -------------------------------------------------------------- odd rows
 // Rows that are not whole aligned chunks, copied behind one another with zeros up
-// to whole ones: the tiles' transfers take no others.  (With 128 x 128 tiles made
+// to whole ones: the tiles' transfers take no others, and rows of fewer than 8 values
+// none at all.  (With 128 x 128 tiles made
 // through registers instead, 27840 x 5120 -> 15360 took 16.7 ms; the copies are 0.2.)
 struct PackArgs {
   const __bf16* from[3];
@@ -792,13 +868,16 @@ hipError_t launch_adapter_project(const AdapterArgs& given, const AdapterPlan& p
         launch_few<4, 3, 4>(a, plan, stream);
       break;
     case AdapterKernel::kTiles64:
-      hipLaunchKernelGGL((tile_kernel<2, 2, 1, 1, 4>), grid, dim3(256), 0, stream, a);
+      if (plan.groups == 2)
+        hipLaunchKernelGGL((tile_kernel<2, 2, 1, 1, 2, 4>), grid, dim3(512), 0, stream, a);
+      else
+        hipLaunchKernelGGL((tile_kernel<2, 2, 1, 1, 1, 4>), grid, dim3(256), 0, stream, a);
       break;
     case AdapterKernel::kTiles128:
-      hipLaunchKernelGGL((tile_kernel<2, 2, 2, 2, 2>), grid, dim3(256), 0, stream, a);
+      hipLaunchKernelGGL((tile_kernel<2, 2, 2, 2, 1, 2>), grid, dim3(256), 0, stream, a);
       break;
     case AdapterKernel::kTiles256:
-      hipLaunchKernelGGL((tile_kernel<2, 4, 4, 2, 2>), grid, dim3(512), 0, stream, a);
+      hipLaunchKernelGGL((tile_kernel<2, 4, 4, 2, 1, 2>), grid, dim3(512), 0, stream, a);
   }
   return hipGetLastError();
 }

@@ -66,6 +66,9 @@ hipError_t plan_adapter_project(int64_t rows, int32_t in_features, int64_t x_str
   } else {
     p.kernel = AdapterKernel::kTiles64;
     p.blocks = tiles(64, 64);
+    // Two groups need a whole CU's LDS: where there is a CU for every tile (200 x 5120
+    // -> 3000, 188 tiles: 48 us with one, 42 with two; 400 x 1536 -> 4608, 504 tiles: 30 and 36).
+    p.groups = p.blocks <= 256 ? 2 : 1;
   }
   if (!launchable(p.blocks, 512)) return hipErrorInvalidValue;
   const bool low = segments > 0 && adapters > 0;
@@ -79,7 +82,7 @@ hipError_t plan_adapter_project(int64_t rows, int32_t in_features, int64_t x_str
     p.low_bytes = (rows * parts * p.low_rank * 2 + 255) / 256 * 256;
   }
   p.workspace_bytes = p.low_bytes;
-  if (p.kernel != AdapterKernel::kFew) {
+  if (p.kernel != AdapterKernel::kFew || in_features < 8) {
     const int64_t k8 = (in_features + 7) / 8 * 8;
     p.pack_w = in_features % 8 != 0;
     // the tiles' byte offsets have 32 bits: 256 rows of x

@@ -254,7 +254,10 @@ hipError_t launch_adapter_project(const AdapterArgs& a, const AdapterPlan& plan,
   check(plan.blocks == (a.M + t[0] - 1) / t[0] * ((int64_t{a.N} + t[1] - 1) / t[1]), "a block a tile");
   check(plan.kernel != AdapterKernel::kFew || a.M <= kAdapterFewTokens, "few tokens");
   const bool few = plan.kernel == AdapterKernel::kFew;
-  check(few ? !plan.pack_x && !plan.pack_w : a.whole || plan.pack_x, "odd rows of many are copied");
+  if (few)
+    check(plan.pack_x == (a.K < 8) && plan.pack_w == plan.pack_x, "short rows of few are copied");
+  else
+    check(a.whole || plan.pack_x, "odd rows of many are copied");
   check(a.whole || few || plan.pack_w || a.K % 8 == 0, "odd weights are copied");
   const int64_t k8 = (a.K + 7) / 8 * 8, stride = plan.pack_x ? k8 : a.x_stride;
   if (!few || a.whole) {
@@ -434,6 +437,8 @@ int main(int argc, char** argv) {
             static_cast<int>(pick(0, 9)), static_cast<int>(pick(1, 256)), static_cast<int>(pick(0, 1) ? 0 : pick(1, 20)));
   }
   project(64, 1 << 20, 64, 1, 1, 1, 8, 0);
+  for (int k = 1; k < 10; ++k)
+    for (int rows : {1, 17, 64, 65}) project(rows, k, 100, 2, 3, 2, 12, k % 3);
   project(300, 64, 512, 1, 2, 1, 8, (1 << 21) - 64);
   project(300, 64, 512, 1, 2, 1, 8, 1 << 25);
   // no launch of 2^32 threads

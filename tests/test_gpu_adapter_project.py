@@ -107,6 +107,18 @@ def test_strides_and_alignments(pad, shift, M):
         assert (np.abs(got - ref[0]) <= 2.0 ** -8 * 1.01 * np.abs(ref[0]) + (K + R) * 2.0 ** -23 * (mag[0] + low[0]) + 2.0 ** -8 * low[0]).all()
 
 
+@pytest.mark.parametrize("M", [1, 20, 33, 64, 70])
+@pytest.mark.parametrize("K", [1, 3, 7, 8, 9, 15, 16, 23, 31, 33, 63, 65, 95, 577, 1537])
+@pytest.mark.parametrize("pad", [0, 1, 2, 9])
+def test_rows_of_odd_lengths(M, K, pad):
+    """Rows end anywhere and begin at any value; what stands between them is not used."""
+    def between(x, w, a, b):
+        if pad:
+            x._base[:, K:] = float("nan")
+
+    _run(M, K, 50, 2, 3, 12, [0, M // 3, M // 3, M], [2, 1, 0], pad=pad, edit=between)
+
+
 @pytest.mark.parametrize("bad", [np.inf, np.nan])
 @pytest.mark.parametrize("M,K,N,R", [(12, 128, 192, 16), (300, 128, 768, 16), (300, 100, 90, 5), (600, 128, 768, 8)])
 def test_an_adapters_infinities_stay_with_its_rows(bad, M, K, N, R):
