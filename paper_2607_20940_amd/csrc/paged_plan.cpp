@@ -57,25 +57,33 @@ hipError_t plan_adapter_project(int64_t rows, int32_t in_features, int64_t x_str
   if (rows <= kAdapterFewTokens) {
     p.kernel = AdapterKernel::kFew;
     p.blocks = tiles(kAdapterFewTokens, kAdapterFewFeatures);
-  } else if (tiles(256, 256) >= 256) {
-    p.kernel = AdapterKernel::kTiles256;
-    p.blocks = tiles(256, 256);
-  } else if (tiles(128, 128) >= 256) {
-    p.kernel = AdapterKernel::kTiles128;
-    p.blocks = tiles(128, 128);
-  } else {
+  } else if (tiles(64, 64) <= 512) {
+    // The smallest tiles that are all on the CUs at once, two of 64 or 128 on each (5120
+    // deep: 1300 x 1152, 378 tiles of 64: 51 us, 76 with 128; 1900 x 1728, 810: 86 and 77;
+    // 2500 x 3000, 480 of 128: 94 us, 124 with 256; 2500 x 4200, 660: 159 and 139).
     p.kernel = AdapterKernel::kTiles64;
     p.blocks = tiles(64, 64);
     // Two groups need a whole CU's LDS: where there is a CU for every tile (200 x 5120
     // -> 3000, 188 tiles: 48 us with one, 42 with two; 400 x 1536 -> 4608, 504 tiles: 30 and 36).
     p.groups = p.blocks <= 256 ? 2 : 1;
+  } else if (tiles(128, 128) <= 512) {
+    p.kernel = AdapterKernel::kTiles128;
+    p.blocks = tiles(128, 128);
+  } else {
+    p.kernel = AdapterKernel::kTiles256;
+    p.blocks = tiles(256, 256);
   }
   if (!launchable(p.blocks, 512)) return hipErrorInvalidValue;
   const bool low = segments > 0 && adapters > 0;
   if (low) {
     p.low_rank = (rank + 15) / 16 * 16;
-    // tiles of 64 rows where each is nearly full and there are some for most CUs
-    p.low_rows = p.kernel != AdapterKernel::kFew && rows > 4096 && rows / segments >= kLowManyRows ? kLowManyRows : kLowRows;
+    // Tiles of 64 rows where segments fill them, unless their walk through the stages
+    // takes longer than the rounds that blocks of 16 rows make, one a CU: about 5 us and
+    // a third a stage against 10 to 15 a round (both launches, rank 64, three parts: 3000 x
+    // 1536 49 us, 128 with blocks of 16 rows; 1300 x 576 26 and 45; 500 x 5120 58 and 48).
+    const int64_t small = std::min<int64_t>(rows, segments + rows / kLowRows) * (parts * p.low_rank / 16);
+    const bool walks = 45 * ((small + 255) / 256) > 17 + (in_features + 63) / 64;
+    p.low_rows = p.kernel != AdapterKernel::kFew && rows / segments >= kLowManyRows && walks ? kLowManyRows : kLowRows;
     // every segment's tiles: whole ones, and one that is not full
     p.low_tiles = std::min<int64_t>(rows, segments + rows / p.low_rows);
     if (!launchable(p.low_tiles, 1024)) return hipErrorInvalidValue;
