@@ -874,7 +874,10 @@ hipError_t launch_adapter_project(const AdapterArgs& given, const AdapterPlan& p
         hipLaunchKernelGGL((tile_kernel<2, 2, 1, 1, 1, 4>), grid, dim3(256), 0, stream, a);
       break;
     case AdapterKernel::kTiles128:
-      hipLaunchKernelGGL((tile_kernel<2, 2, 2, 2, 1, 2>), grid, dim3(256), 0, stream, a);
+      if (plan.groups == 2)
+        hipLaunchKernelGGL((tile_kernel<2, 2, 2, 2, 2, 2>), grid, dim3(512), 0, stream, a);
+      else
+        hipLaunchKernelGGL((tile_kernel<2, 2, 2, 2, 1, 2>), grid, dim3(256), 0, stream, a);
       break;
     case AdapterKernel::kTiles256:
       hipLaunchKernelGGL((tile_kernel<2, 4, 4, 2, 1, 2>), grid, dim3(512), 0, stream, a);

@@ -59,7 +59,7 @@ hipError_t plan_adapter_project(int64_t rows, int32_t in_features, int64_t x_str
     p.blocks = tiles(kAdapterFewTokens, kAdapterFewFeatures);
   } else if (tiles(64, 64) <= 512) {
     // The smallest tiles that are all on the CUs at once, two of 64 or 128 on each (5120
-    // deep: 1300 x 1152, 378 tiles of 64: 51 us, 76 with 128; 1900 x 1728, 810: 86 and 77;
+    // deep: 1300 x 1152, 378 tiles of 64: 51 us, 76 with 128; 1900 x 1728, 810: 86 and 65;
     // 2500 x 3000, 480 of 128: 94 us, 124 with 256; 2500 x 4200, 660: 159 and 139).
     p.kernel = AdapterKernel::kTiles64;
     p.blocks = tiles(64, 64);
@@ -69,6 +69,7 @@ hipError_t plan_adapter_project(int64_t rows, int32_t in_features, int64_t x_str
   } else if (tiles(128, 128) <= 512) {
     p.kernel = AdapterKernel::kTiles128;
     p.blocks = tiles(128, 128);
+    p.groups = p.blocks <= 256 ? 2 : 1;  // (2500 x 5120 -> 1536, 240 tiles: 77 us with one, 66 with two)
   } else {
     p.kernel = AdapterKernel::kTiles256;
     p.blocks = tiles(256, 256);

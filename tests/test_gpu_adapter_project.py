@@ -170,6 +170,14 @@ def test_repeatable_on_another_stream_and_in_a_graph(M):
         assert all(torch.equal(p, q) for p, q in zip(one[1], two[1]))
 
 
+@pytest.mark.parametrize("K", [8, 40, 64, 72, 128, 136, 200, 333])
+@pytest.mark.parametrize("M,N,parts,R,S", [(90, 200, 1, 8, 2), (300, 1029, 3, 20, 9), (1300, 1728, 3, 72, 3), (1290, 1730, 1, 12, 30)])
+def test_waves_that_share_out_the_contraction(M, K, N, parts, R, S):
+    """Odd and even numbers of stages, one group without any; tiles of both small sizes."""
+    rng = np.random.default_rng(K)
+    _run(M, K, N, parts, 3, R, _cuts(rng, M, S), rng.integers(-1, 3, size=S))
+
+
 @pytest.mark.parametrize("M,K,N,parts,R,S", [(4200, 72, 4104, 1, 8, 3), (4097, 136, 4608, 3, 40, 2), (5000, 64, 3700, 2, 12, 5),
                                              (4500, 192, 3900, 3, 70, 4), (4300, 8, 4096, 1, 24, 40), (4200, 100, 2000, 1, 8, 3), (4500, 97, 4100, 2, 16, 3), (9000, 131, 768, 3, 40, 2),
                                              (9000, 456, 768, 3, 100, 2), (2100, 328, 2050, 1, 16, 700)])
