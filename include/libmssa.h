@@ -657,7 +657,7 @@ mssa_status mssa_adapter_project_workspace_size(const mssa_adapter_project_desc*
  * An adapter's infinities and NaN reach its own rows only.  Outputs must
  * alias neither the inputs nor one another.  x, w and a are 16-byte aligned; the other tensors need the
  * alignment of their type only.  Rows of x, w and a that are no multiples of 8
- * values apart are copied to the workspace first (more than 64 rows, or fewer
+ * values apart are copied to the workspace first (more than 16 rows, or fewer
  * than 8 in_features). */
 mssa_status mssa_adapter_project(const mssa_adapter_project_desc* desc, const void* x, const void* w, const void* bias,
                                  const int32_t* segment_begin, const int32_t* adapter, const void* a, const void* b,

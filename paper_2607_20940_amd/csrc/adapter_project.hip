@@ -38,8 +38,7 @@ __device__ inline bf16x8 eight(const __bf16* p, int n) {
 // Eight neighbouring values of an aligned tensor from any of them on.  Loads that are
 // no multiples of 4 bytes apart take several times as long: the 16 bytes from the even
 // place before and the last value apart, joined once both are there (16 x 577 ->
-// 1728, rank 16: 15.7 us for both kernels, 33.7 with one load at any place; 64 x
-// 2001: 34 and 59).
+// 1728, rank 16: 15.7 us for both kernels, 33.7 with one load at any place).
 struct Eight {
   uint32_t v __attribute__((ext_vector_type(4)));
   uint32_t last, shift;
@@ -792,10 +791,13 @@ __global__ __launch_bounds__(kThreads) void pack_kernel(PackArgs a) {
 template <int RT, int kRing, int kUnroll>
 void launch_few(const AdapterArgs& a, const AdapterPlan& plan, hipStream_t stream) {
   const dim3 grid(static_cast<uint32_t>(plan.blocks));
-  if (a.whole)
-    hipLaunchKernelGGL((few_ring_kernel<RT, kRing>), grid, dim3(256), 0, stream, a);
-  else
-    hipLaunchKernelGGL((few_any_kernel<RT, kUnroll>), grid, dim3(512), 0, stream, a);
+  if constexpr (RT * 16 <= kAdapterFewOdd) {
+    if (!a.whole) {
+      hipLaunchKernelGGL((few_any_kernel<RT, kUnroll>), grid, dim3(512), 0, stream, a);
+      return;
+    }
+  }
+  hipLaunchKernelGGL((few_ring_kernel<RT, kRing>), grid, dim3(256), 0, stream, a);
 }
 
 hipError_t launch_low(const AdapterArgs& a, const AdapterPlan& plan, hipStream_t stream) {
@@ -863,9 +865,9 @@ hipError_t launch_adapter_project(const AdapterArgs& given, const AdapterPlan& p
       if (a.M <= 16)
         launch_few<1, 3, 7>(a, plan, stream);
       else if (a.M <= 32)
-        launch_few<2, 2, 6>(a, plan, stream);
+        launch_few<2, 2, 0>(a, plan, stream);
       else
-        launch_few<4, 3, 4>(a, plan, stream);
+        launch_few<4, 3, 0>(a, plan, stream);  // odd rows have been copied
       break;
     case AdapterKernel::kTiles64:
       if (plan.groups == 2)

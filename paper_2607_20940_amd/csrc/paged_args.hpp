@@ -192,12 +192,13 @@ struct AdapterArgs {
 // sizes (tokens and features).
 enum class AdapterKernel { kFew, kTiles64, kTiles128, kTiles256 };
 constexpr int kAdapterFewTokens = 64, kAdapterFewFeatures = 32;
+constexpr int kAdapterFewOdd = 16;  // tokens whose odd rows are read where they lie
 
 constexpr int kLowRows = 16, kLowManyRows = 64;  // rows of a tile of the low-rank factor
 struct AdapterPlan {
   AdapterKernel kernel;
   int32_t groups;       // of waves of a small tile, which share out the contraction
-  bool pack_x, pack_w;  // rows of x, and of w and a, are copied to whole chunks first (for few tokens: rows of fewer than 8 values)
+  bool pack_x, pack_w;  // rows of x, and of w and a, are copied to whole chunks first (for few tokens only rows of fewer than 8 values)
   int32_t low_rows;     // of a tile of the low-rank factor's launch
   int32_t low_rank;     // rank rounded up to whole 16 values
   int64_t low_tiles;    // its row tiles, 0: none

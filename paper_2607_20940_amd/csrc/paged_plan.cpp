@@ -91,7 +91,10 @@ hipError_t plan_adapter_project(int64_t rows, int32_t in_features, int64_t x_str
     p.low_bytes = (rows * parts * p.low_rank * 2 + 255) / 256 * 256;
   }
   p.workspace_bytes = p.low_bytes;
-  if (p.kernel != AdapterKernel::kFew || in_features < 8) {
+  // Odd rows are copied for more than 16 tokens (60 x 4733 -> 12000: 83 us, 123 read where
+  // they lie; 20 tokens: 76 and 82); for fewer the weights' bytes count, which the copy
+  // moves three times (one token: 71 and 57).
+  if (rows > kAdapterFewOdd || in_features < 8) {
     const int64_t k8 = (in_features + 7) / 8 * 8;
     p.pack_w = in_features % 8 != 0;
     // the tiles' byte offsets have 32 bits: 256 rows of x

@@ -255,12 +255,12 @@ hipError_t launch_adapter_project(const AdapterArgs& a, const AdapterPlan& plan,
   check(plan.kernel != AdapterKernel::kFew || a.M <= kAdapterFewTokens, "few tokens");
   const bool few = plan.kernel == AdapterKernel::kFew;
   if (few)
-    check(plan.pack_x == (a.K < 8) && plan.pack_w == plan.pack_x, "short rows of few are copied");
+    check(a.M > kAdapterFewOdd ? a.whole || plan.pack_x : plan.pack_x == (a.K < 8) && plan.pack_w == plan.pack_x, "odd rows of few are copied");
   else
     check(a.whole || plan.pack_x, "odd rows of many are copied");
-  check(a.whole || few || plan.pack_w || a.K % 8 == 0, "odd weights are copied");
+  check(a.whole || a.M <= kAdapterFewOdd || plan.pack_w || a.K % 8 == 0, "odd weights are copied");
   const int64_t k8 = (a.K + 7) / 8 * 8, stride = plan.pack_x ? k8 : a.x_stride;
-  if (!few || a.whole) {
+  if (a.M > kAdapterFewOdd || a.whole) {
     check(256 * stride * 2 + 128 < 0x7ffffff0 && 256 * k8 * 2 + 128 < 0x7ffffff0, "offsets inside a tile");
     check(stride % 8 == 0 && (reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w)) % 16 == 0, "whole chunks");
   }

@@ -145,4 +145,5 @@ def test_workspace_of_odd_rows_holds_their_copies():
     even, odd, apart = (mssa.mssa_adapter_project_workspace_size(mssa.adapter_project_desc(300, k, 200, 2, 3, 8, x_stride=x))
                         for k, x in ((104, 0), (97, 0), (104, 107)))
     assert odd - even == (300 + 200 + 3 * 8) * 104 * 2 and apart - even == 300 * 104 * 2
-    assert mssa.mssa_adapter_project_workspace_size(mssa.adapter_project_desc(64, 97, 200, 2, 3, 8)) == 64 * 16 * 2
+    for rows, size in ((16, 16 * 16 * 2), (17, 768 + (17 + 200 + 3 * 8) * 104 * 2)):  # few are read where they lie
+        assert mssa.mssa_adapter_project_workspace_size(mssa.adapter_project_desc(rows, 97, 200, 2, 3, 8)) == size
