@@ -8,8 +8,8 @@
 // taken in turns, position * freq / 2 pi in 64 bits, and its fraction alone
 // goes to 32 bits: a position of 2^31 leaves an angle as exact as one of 1.
 //
-// Bound by HBM: every value is read once and written once.  A piece is a thread's
-// whole work, so a block of many heads has all its loads on their way at once;
+// Bound by HBM: every value is read once and written once.  A thread takes
+// four pieces at most, so a block has all its loads on their way at once;
 // narrow tokens share a block so that its look-ups and sines, which no load of a
 // value waits for but every store does, are not its whole time.  35100 tokens of
 // 40 + 2 x 40 heads, 2.2 GB: 400 us, 5.4 TB/s (a large copy reaches 5.2); 4680 tokens of
