@@ -118,7 +118,7 @@ class PagedStreams:
             want.append(need - have)
         if sum(want) > len(self.free):
             raise RuntimeError(f"{sum(want)} pages are needed and {len(self.free)} are free")
-        # what the library refuses is refused before anything changes
+        # what can be refused or raise comes before anything changes
         b, t, m = len(chunks), sum(news), self.max_stream_pages
         project = mssa.adapter_project_desc(t, self.hidden, self.width, b if self.adapters else 0, self.adapters, self.rank)
         append = mssa.paged_append_desc(t, b, self.q_heads, self.kv_heads, self.head_dim, self.page_tokens, self.pages, m,
@@ -127,25 +127,30 @@ class PagedStreams:
         attend = mssa.paged_attention_desc(t, b, max(1, *news), self.q_heads, self.kv_heads, self.head_dim, self.page_tokens,
                                            self.pages, m, mask_block=self.mask_block, softmax_scale=self.scale)
         size = max(mssa.mssa_adapter_project_workspace_size(project), mssa.mssa_paged_attention_workspace_size(attend))
-        begin, lens, which, table, positions = [0], [], [], [], []
+        spare, begin, lens, which, table, positions, held = len(self.free), [0], [], [], [], [], []
         for s, n, w in zip(names, news, want):
-            state = self.streams[s]
-            state[0].extend(self.free.pop() for _ in range(w))
-            positions.extend(range(state[2] + state[1], state[2] + state[1] + n))
-            state[1] += n
+            pages, had, dropped, adapter = self.streams[s]
+            pages, spare = pages + self.free[spare - w:spare][::-1], spare - w
+            positions.extend(range(dropped + had, dropped + had + n))
+            held.append([pages, had + n, dropped, adapter])
             begin.append(begin[-1] + n)
-            lens.append(state[1])
-            which.append(state[3])
-            table.extend(state[0] + [-1] * (self.max_stream_pages - len(state[0])))
+            lens.append(had + n)
+            which.append(adapter)
+            table.extend(pages + [-1] * (m - len(pages)))
         # one copy for all of it
         host = torch.tensor(begin + lens + which + table + positions, dtype=torch.int32)
-        self.places = dev = host.to(self.device)
+        workspace = self.workspace
+        if workspace.numel() < size:
+            workspace = torch.empty(size, dtype=torch.uint8, device=self.device)
+        dev = host.to(self.device)
+        # nothing raises from here on: the pass is open
+        self.streams.update(zip(names, held))
+        del self.free[spare:]
         cut = lambda at, n: dev[at:at + n]  # noqa: E731
         self.chunk_begin, self.kv_len, self.adapter = cut(0, b + 1), cut(b + 1, b), cut(2 * b + 1, b)
         self.table, self.positions = cut(3 * b + 1, b * m), cut(3 * b + 1 + b * m, t)
+        self.places, self.workspace = dev, workspace
         self.tokens, self.project, self.append, self.attend = t, project, append, attend
-        if self.workspace.numel() < size:
-            self.workspace = torch.empty(size, dtype=torch.uint8, device=self.device)
         self.batch = b
 
     def layer_pass(self, layer, x, out, lse=None, positions=None, prior_out=None, prior_lse=None, stream=None):

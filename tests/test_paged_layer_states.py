@@ -1,0 +1,62 @@
+"""What a refused or failed call of the layers over a paged cache leaves behind (no GPU)."""
+
+import sys
+
+import pytest
+import torch
+
+from paper_2607_20940_amd.paged import PagedStreams
+
+
+def _streams(**kw):
+    return PagedStreams(**dict(dict(layers=1, hidden=64, q_heads=4, kv_heads=2, head_dim=64, pages=400, page_tokens=8,
+                                    max_stream_pages=200, max_tokens=600, max_batch=3, adapters=2, rank=8, device="cpu"),
+                               **kw))
+
+
+def _state(p):
+    """All that a pass changes: page accounts, streams, the open pass's sizes and tensors."""
+    places = [getattr(p, n).tolist() for n in ("chunk_begin", "kv_len", "adapter", "table", "positions") if p.batch]
+    made = [id(getattr(p, n, None)) for n in ("places", "workspace", "project", "append", "attend")]
+    return list(p.free), {s: [list(v[0]), *v[1:]] for s, v in p.streams.items()}, p.batch, getattr(p, "tokens", None), places, made
+
+
+class _Torch:
+    """torch, but for one function that raises as an allocation does that finds no memory."""
+
+    def __init__(self, name):
+        self.name = name
+
+    def __getattr__(self, name):
+        if name != self.name:
+            return getattr(torch, name)
+
+        def none(*args, **kw):
+            raise torch.OutOfMemoryError("no memory")
+
+        return none
+
+
+@pytest.mark.parametrize("opened", [False, True])
+@pytest.mark.parametrize("name", ["empty", "tensor"])
+def test_passes_that_find_no_memory_change_nothing(monkeypatch, name, opened):
+    p = _streams()
+    p.open("a")
+    p.open("b", 1)
+    if opened:
+        p.begin([("a", 1), ("b", 3)])
+    p.workspace = torch.empty(0, dtype=torch.uint8)  # any pass has to make one
+    before = _state(p)
+    with monkeypatch.context() as m:
+        m.setitem(sys.modules, "torch", _Torch(name))
+        with pytest.raises(torch.OutOfMemoryError):
+            p.begin([("b", 2), ("a", 300)])
+    assert _state(p) == before
+    # and the same pass begins where there is memory
+    p.begin([("b", 2), ("a", 300)])
+    held = {"a": 301, "b": 5} if opened else {"a": 300, "b": 2}
+    assert {s: v[1] for s, v in p.streams.items()} == held
+    assert p.kv_len.tolist() == [held["b"], held["a"]] and p.batch == 2 and p.tokens == 302
+    assert p.positions.tolist() == list(range(held["b"] - 2, held["b"])) + list(range(held["a"] - 300, held["a"]))
+    pages = [g for v in p.streams.values() for g in v[0]]
+    assert len(pages) == sum(-(-n // 8) for n in held.values()) and sorted(p.free + pages) == list(range(400))
