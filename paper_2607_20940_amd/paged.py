@@ -121,9 +121,11 @@ class PagedStreams:
         # what can be refused or raise comes before anything changes
         b, t, m = len(chunks), sum(news), self.max_stream_pages
         project = mssa.adapter_project_desc(t, self.hidden, self.width, b if self.adapters else 0, self.adapters, self.rank)
-        append = mssa.paged_append_desc(t, b, self.q_heads, self.kv_heads, self.head_dim, self.page_tokens, self.pages, m,
-                                        rotate_dims=self.rotate_dims, halves=self.halves, axis_pairs=self.axis_pairs,
-                                        q_stride=self.width, k_stride=self.width, v_stride=self.width)
+        append, check = (mssa.paged_append_desc(n, b, self.q_heads, self.kv_heads, self.head_dim, self.page_tokens, self.pages,
+                                                m, rotate_dims=self.rotate_dims, halves=self.halves,
+                                                axis_pairs=self.axis_pairs, q_stride=self.width, k_stride=self.width,
+                                                v_stride=self.width) for n in (t, 0))
+        mssa.mssa_paged_append(check, *[None] * 11, stream=0)  # checks the sizes; without tokens nothing is enqueued
         attend = mssa.paged_attention_desc(t, b, max(1, *news), self.q_heads, self.kv_heads, self.head_dim, self.page_tokens,
                                            self.pages, m, mask_block=self.mask_block, softmax_scale=self.scale)
         size = max(mssa.mssa_adapter_project_workspace_size(project), mssa.mssa_paged_attention_workspace_size(attend))

@@ -5,6 +5,7 @@ import sys
 import pytest
 import torch
 
+from paper_2607_20940_amd import mssa
 from paper_2607_20940_amd.paged import PagedStreams
 
 
@@ -60,3 +61,16 @@ def test_passes_that_find_no_memory_change_nothing(monkeypatch, name, opened):
     assert p.positions.tolist() == list(range(held["b"] - 2, held["b"])) + list(range(held["a"] - 300, held["a"]))
     pages = [g for v in p.streams.values() for g in v[0]]
     assert len(pages) == sum(-(-n // 8) for n in held.values()) and sorted(p.free + pages) == list(range(400))
+
+
+@pytest.mark.parametrize("kw", [dict(freqs=torch.zeros(12), rotate_dims=24),  # halves of 12 pairs
+                                dict(freqs=torch.zeros(32), axis_pairs=[16, 15]),
+                                dict(freqs=torch.zeros(32), axis_pairs=[33, -1])])
+def test_passes_that_the_append_refuses_change_nothing(kw):
+    p = _streams(**kw)
+    p.open("a")
+    before = _state(p)
+    for n in (0, 9):
+        with pytest.raises(mssa.MssaError):
+            p.begin([("a", n)])
+        assert _state(p) == before
