@@ -75,7 +75,7 @@ class PagedStreams:
         """A new stream without tokens; adapter: its low-rank adapter, -1 for none."""
         if stream in self.streams:
             raise ValueError(f"stream {stream!r} is open")
-        if not -1 <= adapter < max(1, self.adapters):
+        if not -1 <= adapter < self.adapters:
             raise ValueError(f"there is no adapter {adapter}")
         self.streams[stream] = [[], 0, 0, int(adapter)]
 

@@ -74,3 +74,15 @@ def test_passes_that_the_append_refuses_change_nothing(kw):
         with pytest.raises(mssa.MssaError):
             p.begin([("a", n)])
         assert _state(p) == before
+
+
+@pytest.mark.parametrize("adapters,refused", [(0, (0, 1, -2)), (1, (1, -2)), (2, (2, -2))])
+def test_adapters_that_are_not_there_are_refused(adapters, refused):
+    p = _streams(adapters=adapters)
+    for j in refused:
+        with pytest.raises(ValueError):
+            p.open("a", j)
+    assert p.streams == {}
+    for j in range(-1, adapters):
+        p.open(j, j)
+    assert [v[3] for v in p.streams.values()] == list(range(-1, adapters))
