@@ -801,24 +801,21 @@ void launch_few(const AdapterArgs& a, const AdapterPlan& plan, hipStream_t strea
 }
 
 hipError_t launch_low(const AdapterArgs& a, const AdapterPlan& plan, hipStream_t stream) {
-  const uint32_t tiles = static_cast<uint32_t>(plan.low_tiles), cols = static_cast<uint32_t>(a.parts * a.low_rank);
+  const uint32_t tiles = static_cast<uint32_t>(plan.low_tiles), across = static_cast<uint32_t>(plan.low_across);
   if (plan.low_rows == kLowRows) {
-    const dim3 grid(tiles, cols / 16), block(kLowWaves * 64);
+    const dim3 grid(tiles, across), block(kLowWaves * 64);
     if (a.whole)
       hipLaunchKernelGGL(low_kernel<true>, grid, block, 0, stream, a);
     else
       hipLaunchKernelGGL(low_kernel<false>, grid, block, 0, stream, a);
   } else {
-    switch ((cols + 31) / 32) {
-      case 1:
-        hipLaunchKernelGGL((low_tile_kernel<1>), dim3(tiles), dim3(256), 0, stream, a);
-        break;
-      case 2:
-        hipLaunchKernelGGL((low_tile_kernel<2>), dim3(tiles), dim3(256), 0, stream, a);
-        break;
-      default:
-        hipLaunchKernelGGL((low_tile_kernel<3>), dim3(tiles * ((cols + 95) / 96)), dim3(256), 0, stream, a);
-    }
+    const dim3 grid(tiles * across), block(256);
+    if (plan.low_columns == 32)
+      hipLaunchKernelGGL((low_tile_kernel<1>), grid, block, 0, stream, a);
+    else if (plan.low_columns == 64)
+      hipLaunchKernelGGL((low_tile_kernel<2>), grid, block, 0, stream, a);
+    else
+      hipLaunchKernelGGL((low_tile_kernel<3>), grid, block, 0, stream, a);
   }
   return hipGetLastError();
 }

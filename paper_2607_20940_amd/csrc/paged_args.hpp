@@ -202,6 +202,8 @@ struct AdapterPlan {
   int32_t low_rows;     // of a tile of the low-rank factor's launch
   int32_t low_rank;     // rank rounded up to whole 16 values
   int64_t low_tiles;    // its row tiles, 0: none
+  int32_t low_columns;  // rank columns of a block: 16 beside 16 rows; 32, 64 or 96 beside 64
+  int32_t low_across;   // blocks of a row tile: the grid's second axis with 16 rows, along the first with 64
   int64_t blocks;       // of the product
   int64_t low_bytes, workspace_bytes;  // the low-rank factors, then the copies
 };

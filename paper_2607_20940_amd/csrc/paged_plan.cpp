@@ -87,7 +87,10 @@ hipError_t plan_adapter_project(int64_t rows, int32_t in_features, int64_t x_str
     p.low_rows = p.kernel != AdapterKernel::kFew && rows / segments >= kLowManyRows && walks ? kLowManyRows : kLowRows;
     // every segment's tiles: whole ones, and one that is not full
     p.low_tiles = std::min<int64_t>(rows, segments + rows / p.low_rows);
-    if (!launchable(p.low_tiles, 1024)) return hipErrorInvalidValue;
+    const int32_t cols = parts * p.low_rank;
+    p.low_columns = p.low_rows == kLowRows ? 16 : cols <= 32 ? 32 : cols <= 64 ? 64 : 96;
+    p.low_across = (cols + p.low_columns - 1) / p.low_columns;
+    if (p.low_rows == kLowRows ? !launchable(p.low_tiles, 1024) : !launchable(p.low_tiles * p.low_across, 256)) return hipErrorInvalidValue;
     p.low_bytes = (rows * parts * p.low_rank * 2 + 255) / 256 * 256;
   }
   p.workspace_bytes = p.low_bytes;

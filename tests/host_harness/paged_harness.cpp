@@ -280,6 +280,11 @@ hipError_t launch_adapter_project(const AdapterArgs& a, const AdapterPlan& plan,
     check(int64_t{256} * a.parts * a.low_rank * 2 < 0x7ffffff0, "offsets inside a tile");
     // the most tiles that segments of these rows can have
     check(plan.low_tiles >= std::min<int64_t>(a.M, a.segments + (a.M - 1) / plan.low_rows), "a block a tile of the low-rank factor");
+    const int64_t cols = int64_t{a.parts} * a.low_rank;
+    check(plan.low_columns % 16 == 0 && (plan.low_rows == kLowRows ? plan.low_columns == 16 : plan.low_columns <= 96) &&
+              plan.low_across == (cols + plan.low_columns - 1) / plan.low_columns, "the low-rank factor's columns");
+    check(plan.low_rows == kLowRows ? plan.low_tiles * 1024 < int64_t{1} << 32 : plan.low_tiles * plan.low_across * 256 < int64_t{1} << 32,
+          "threads of the low-rank factor's launch");
   }
   return hipSuccess;
 }
