@@ -178,6 +178,15 @@ class PagedStreams:
         for name, v, shape, dtype in want:
             if v.dtype != dtype or not v.is_contiguous() or tuple(v.shape) != shape:
                 raise ValueError(f"{name} must be contiguous {dtype} {shape}, not {v.dtype} {tuple(v.shape)}")
+            if dtype == torch.bfloat16 and v.data_ptr() % 16:
+                raise ValueError(f"{name} must be 16-byte aligned")
+        if self.weights[layer] is None:
+            raise ValueError(f"layer {layer} has no weights")
+        # what a later one of the calls would refuse is refused before the first
+        if (prior_out is None) != (prior_lse is None):
+            raise ValueError("prior_out and prior_lse come together")
+        if any(out.data_ptr() == b.data_ptr() for b in (self.q, self.k_pages[layer], self.v_pages[layer])):
+            raise ValueError("out must not be a buffer of the layers")
         w, bias, a, b, scale = self.weights[layer]
         qkv = self.qkv
         if x.is_cuda:

@@ -86,3 +86,28 @@ def test_adapters_that_are_not_there_are_refused(adapters, refused):
     for j in range(-1, adapters):
         p.open(j, j)
     assert [v[3] for v in p.streams.values()] == list(range(-1, adapters))
+
+
+def _opened(monkeypatch, **kw):
+    """Layers with weights and an open pass of 5 tokens, and the names of the library calls that a pass makes."""
+    bf, calls = torch.bfloat16, []
+    p = _streams(adapters=0, **kw)
+    p.init_layer(0, torch.zeros(512, 64, dtype=bf))
+    p.open("a")
+    p.begin([("a", 5)])
+    for name in ("mssa_adapter_project", "mssa_paged_append", "mssa_paged_attention"):
+        monkeypatch.setattr(mssa, name, lambda *a, _name=name, **k: calls.append(_name))
+    return p, calls, torch.zeros(5, 64, dtype=bf), torch.zeros(5, 4, 64, dtype=bf), torch.zeros(4, 5)
+
+
+def test_a_refused_layer_enqueues_nothing(monkeypatch):
+    p, calls, x, out, lse = _opened(monkeypatch, layers=2)
+    shifted = torch.zeros(5 * 256 + 8, dtype=torch.bfloat16)
+    shifted = next(s for s in (shifted[i:i + 5 * 256].view(5, 4, 64) for i in (1, 2)) if s.data_ptr() % 16)
+    for args in ((0, x, out, lse, None, out, None), (0, x, out, lse, None, None, lse), (1, x, out),
+                 (0, x, shifted), (0, x, out, None, None, shifted, lse), (0, x, p.q[:5]), (0, x, p.k_pages[0].view(-1)[:1280].view(5, 4, 64))):
+        with pytest.raises(ValueError):
+            p.layer_pass(*args, stream=0)
+        assert calls == []
+    p.layer_pass(0, x, out, lse, prior_out=out, prior_lse=lse, stream=0)
+    assert calls == ["mssa_adapter_project", "mssa_paged_append", "mssa_paged_attention"]
