@@ -53,6 +53,12 @@ class PagedStreams:
         self.weights = [None] * self.layers
         self.batch = None
         self.workspace = buf(256, dtype=torch.uint8)
+        if freqs is not None:
+            self._here("freqs", freqs)
+
+    def _here(self, name, t):
+        if t.device != self.qkv.device:
+            raise ValueError(f"{name} must be on {self.qkv.device}, not on {t.device}")
 
     def init_layer(self, layer, w_qkv, b_qkv=None, a=None, b=None, scale=None):
         """w_qkv [q_width + 2 kv_width, hidden] and b_qkv bf16; a [adapters, rank, hidden], b [adapters, width, rank] bf16,
@@ -67,8 +73,11 @@ class PagedStreams:
                 continue
             if t is None or t.dtype != torch.bfloat16 or not t.is_contiguous() or tuple(t.shape) != shape:
                 raise ValueError(f"{name} must be contiguous bf16 {shape}")
+            self._here(name, t)
         if scale is not None and (scale.dtype != torch.float32 or not scale.is_contiguous() or scale.numel() != self.adapters):
             raise ValueError(f"scale must be contiguous fp32 [{self.adapters}]")
+        if scale is not None:
+            self._here("scale", scale)
         self.weights[layer] = (w_qkv, b_qkv, a, b, scale)
 
     def open(self, stream, adapter=-1):
@@ -178,6 +187,7 @@ class PagedStreams:
         for name, v, shape, dtype in want:
             if v.dtype != dtype or not v.is_contiguous() or tuple(v.shape) != shape:
                 raise ValueError(f"{name} must be contiguous {dtype} {shape}, not {v.dtype} {tuple(v.shape)}")
+            self._here(name, v)
             if dtype == torch.bfloat16 and v.data_ptr() % 16:
                 raise ValueError(f"{name} must be 16-byte aligned")
         if self.weights[layer] is None:

@@ -111,3 +111,27 @@ def test_a_refused_layer_enqueues_nothing(monkeypatch):
         assert calls == []
     p.layer_pass(0, x, out, lse, prior_out=out, prior_lse=lse, stream=0)
     assert calls == ["mssa_adapter_project", "mssa_paged_append", "mssa_paged_attention"]
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    """Their addresses are none of the device's."""
+    bf = torch.bfloat16
+    w, bias, a, b = torch.zeros(512, 64, dtype=bf), torch.zeros(512, dtype=bf), torch.zeros(2, 8, 64, dtype=bf), torch.zeros(2, 512, 8, dtype=bf)
+    scale = torch.zeros(2)
+    p = _streams()
+    for i in range(5):
+        given = [w, bias, a, b, scale]
+        given[i] = given[i].to("meta")
+        with pytest.raises(ValueError):
+            p.init_layer(0, *given)
+    assert p.weights == [None]
+    with pytest.raises(ValueError):
+        _streams(freqs=torch.zeros(32, device="meta"))
+    p, calls, x, out, lse = _opened(monkeypatch, freqs=torch.zeros(32))
+    given = (x, out, lse, torch.zeros(1, 5, dtype=torch.int32), torch.zeros_like(out), torch.zeros_like(lse))
+    for i in range(6):
+        with pytest.raises(ValueError):
+            p.layer_pass(0, *(t.to("meta") if i == j else t for j, t in enumerate(given)), stream=0)
+    assert calls == []
+    p.layer_pass(0, *given, stream=0)
+    assert len(calls) == 3
