@@ -51,6 +51,7 @@ class PagedStreams:
         self.free = list(range(self.pages))[::-1]
         self.streams = {}  # id -> [pages, tokens held, tokens dropped before them, adapter]
         self.weights = [None] * self.layers
+        self.used = set()  # (HIP stream, layer): what those passes read and write is held for the stream
         self.batch = None
         self.workspace = buf(256, dtype=torch.uint8)
         if freqs is not None:
@@ -79,6 +80,7 @@ class PagedStreams:
         if scale is not None:
             self._here("scale", scale)
         self.weights[layer] = (w_qkv, b_qkv, a, b, scale)
+        self.used = {u for u in self.used if u[1] != layer}
 
     def open(self, stream, adapter=-1):
         """A new stream without tokens; adapter: its low-rank adapter, -1 for none."""
@@ -200,10 +202,15 @@ class PagedStreams:
         w, bias, a, b, scale = self.weights[layer]
         qkv = self.qkv
         if x.is_cuda:
-            # begin replaces these, while this stream may still be reading them
-            used = torch.cuda.ExternalStream(mssa._stream(stream), device=x.device)
-            self.places.record_stream(used)
-            self.workspace.record_stream(used)
+            # begin replaces the first two, while this stream may still be reading them; the others go with the object
+            handle = mssa._stream(stream)
+            used, held = torch.cuda.ExternalStream(handle, device=x.device), [self.places, self.workspace]
+            if (handle, layer) not in self.used:
+                held += [qkv, self.q, self.freqs, self.k_pages[layer], self.v_pages[layer], w, bias, a, b, scale]
+                self.used.add((handle, layer))
+            for v in held:
+                if v is not None:
+                    v.record_stream(used)
         mssa.mssa_adapter_project(self.project, x, w, bias, self.chunk_begin, self.adapter, a, b, scale, self.workspace, [qkv],
                                   stream=stream)
         q, k, v = qkv, qkv[:, self.q_width:], qkv[:, self.q_width + self.kv_width:]
