@@ -202,6 +202,8 @@ class PagedStreams:
         w, bias, a, b, scale = self.weights[layer]
         qkv = self.qkv
         if x.is_cuda:
+            if torch.cuda.current_device() != x.device.index:
+                raise ValueError(f"the current device must be the layers', {x.device}")
             # begin replaces the first two, while this stream may still be reading them; the others go with the object
             handle = mssa._stream(stream)
             used, held = torch.cuda.ExternalStream(handle, device=x.device), [self.places, self.workspace]

@@ -83,3 +83,20 @@ def test_history_in_pages_joined_with_a_plans_sink_and_window(page):
     whole = mssa_oracle.mssa_attention(dict(desc, hist_frames=3), *(f64(t) for t in (q, ks, vs, kh, vh, kw, vw)))
     err = np.abs(f64(out) - whole)
     assert err.max() <= 2e-2 and err.mean() <= 2e-3
+
+
+def test_another_current_device_is_refused(monkeypatch):
+    """Kernels go to the current device: the layers' tensors have to be on it."""
+    p = _layers(np.random.default_rng(3))
+    p.begin([(0, 5)])
+    x, out = cuda(np.ones((5, HIDDEN)), "bf16"), torch.full((5, H, D), 7.0, dtype=torch.bfloat16, device="cuda")
+    with monkeypatch.context() as m:
+        m.setattr(torch.cuda, "current_device", lambda: 1)
+        for stream in (None, torch.cuda.default_stream(0)):
+            with pytest.raises(ValueError):
+                p.layer_pass(0, x, out, stream=stream)
+    torch.cuda.synchronize()
+    assert (out == 7).all() and all((t == 0).all() for t in (*p.k_pages, *p.v_pages))
+    p.layer_pass(0, x, out)
+    torch.cuda.synchronize()
+    assert not (out == 7).all()
