@@ -12,7 +12,10 @@
 //
 // Exit status 0 iff every check passed.  With the argument "plant" every
 // workspace is 256 bytes shorter than the size the harness passes, a mistake the
-// range checks must report.
+// range checks must report.  With the argument "odd" boundaries of chunks and
+// segments are anything (negative, past the rows, decreasing) and the stubs take the
+// kernels' look-ups step by step, with their 32-bit sums: whatever the values are, no
+// row, table entry, tile or slot lies outside and every walk ends.
 #include <hip/hip_runtime_api.h>
 
 #include <algorithm>
@@ -30,7 +33,7 @@
 namespace {
 
 int g_failures = 0, g_checks = 0, g_launches = 0;
-bool g_plant = false, g_walk = true;
+bool g_plant = false, g_walk = true, g_odd = false;
 std::string g_case, g_error;
 
 void failure(const char* what) {
@@ -82,6 +85,158 @@ int64_t pick(int64_t lo, int64_t hi) {
 extern "C" const char* hipGetErrorString(hipError_t) { return "stub"; }
 
 namespace mssa {
+namespace {
+
+// Every chunk's rows lie in the batch, whatever the boundaries are.
+void rows_inside(const int32_t* begin, int batch, int32_t tokens) {
+  for (int b = 0; b < batch; ++b) {
+    const ChunkRows c = ChunkRows::of(begin, b, 0, tokens);
+    check(0 <= c.first && c.first <= c.end && c.end <= tokens, "a chunk's rows");
+  }
+}
+
+// The look-up of a row's sequence, 64 probes at a time (append).
+void find_row(const AppendArgs& a, int32_t row) {
+  int32_t lo = 0, n = a.batch;
+  int rounds = 0;
+  while (n > 64 && ++rounds < 8) {
+    const int32_t step = (n + 63) / 64;
+    int last = 0;
+    for (int lane = 0; lane < 64; ++lane) {
+      const int32_t at = lo + lane * step;
+      if (lane * step < n && a.chunk_begin[at < a.batch ? at : a.batch] <= row) last = lane;
+    }
+    n = std::min(n - last * step, step);
+    lo += last * step;
+  }
+  check(n >= 1 && n <= 64 && lo >= 0 && lo + n <= a.batch, "a row's sequence");
+  for (int lane = n - 1; lane >= 0; --lane) {
+    const int32_t b = lo + lane;
+    if (!(a.chunk_begin[b] <= row && row < a.chunk_begin[b + 1])) continue;
+    const ChunkRows c = ChunkRows::of(a.chunk_begin, b, 0, a.tokens);
+    const int64_t index = int64_t{a.kv_len[b]} - (c.end - row);
+    if (index >= 0 && index < int64_t{a.table_pages} * a.page.d)
+      check(static_cast<int32_t>(a.page.quotient(static_cast<uint32_t>(index))) < a.table_pages, "a page table's entry");
+    return;
+  }
+}
+
+// Rows of the low-rank factor's tiles, and the first segment behind a row (projection).
+void odd_segments(const AdapterArgs& a, const AdapterPlan& plan) {
+  rows_inside(a.segment_begin, a.segments, a.M);
+  for (int32_t tile = 0; tile < plan.low_tiles; ++tile) {
+    int32_t left = tile;
+    bool found = false;
+    for (int32_t c = 0; c < a.segments && !found; c += 64) {
+      int32_t pre = 0;
+      for (int32_t s = c; s < std::min(a.segments, c + 64) && !found; ++s) {
+        const ChunkRows g = ChunkRows::of(a.segment_begin, s, 0, a.M);
+        const int32_t mine = (g.end - g.first + plan.low_rows - 1) / plan.low_rows, before = pre;
+        pre += mine;
+        if (pre <= left) continue;
+        found = true;
+        const int32_t at = left - before, first = g.first + at * plan.low_rows;
+        check(at < 0 || first >= g.end || (first >= 0 && first < a.M), "a low-rank tile's rows");
+      }
+      left -= pre;
+    }
+  }
+  for (int32_t row = 0; row < a.M; row += 16) {
+    int32_t lo = 0, n = a.segments;
+    int rounds = 0;
+    while (n > 0 && ++rounds < 64) {
+      const int32_t step = (n + 63) / 64;
+      int last = -1;
+      for (int lane = 0; lane < 64; ++lane) {
+        const int32_t at = lo + lane * step;
+        if (lane * step < n && a.segment_begin[(at < a.segments ? at : 0) + 1] <= row) last = lane;
+      }
+      if (last < 0) break;
+      const int32_t skip = last * step + 1;
+      n = std::min(n - skip, step - 1);
+      lo += skip;
+    }
+    check(rounds < 64 && lo >= 0 && lo <= a.segments, "the first segment behind a row");
+  }
+}
+
+// The shares of chunks that may overlap: sums are taken in 32 bits, as the workers take them.
+void odd_shares(const PagedAttnArgs& a, const PagedAttnPlan& plan) {
+  rows_inside(a.chunk_begin, a.batch, a.tokens);
+  std::vector<PagedSeq> seqs;
+  uint32_t all = 0;
+  for (int b = 0; b < a.batch; ++b) {
+    seqs.push_back(PagedSeq::of(a, b));
+    const PagedSeq& s = seqs.back();
+    check(s.n >= 0 && s.n <= a.max_chunk && s.first + s.n <= a.tokens && s.len >= 0 && s.len <= a.capacity, "a sequence's rows and length");
+    all += s.head_units() * static_cast<uint32_t>(a.kv_heads);
+  }
+  Shares sh = Shares::of(all, all);
+  if (a.workers) {
+    const uint32_t most = all / static_cast<uint32_t>(a.least);
+    sh = Shares::of(all, most < 1 ? 1 : std::min(most, static_cast<uint32_t>(a.workers)));
+  }
+  struct Spot {
+    int b = -1, kvh = 0, item = 0;
+    uint32_t unit = 0;
+  };
+  auto spot = [&](uint32_t w) {
+    Spot at;
+    if (w >= sh.workers) return at;
+    const uint32_t x = sh.first(w);
+    uint32_t base = 0;
+    for (int b = 0; b < a.batch; ++b) {
+      const uint32_t units = seqs[b].head_units() * static_cast<uint32_t>(a.kv_heads);
+      base += units;
+      if (base <= x) continue;
+      const uint32_t y = x - (base - units);
+      if (y >= units) return at;
+      const uint32_t head = seqs[b].head_units();
+      at.b = b;
+      at.kvh = static_cast<int>(y / head);
+      at.item = seqs[b].item_of(y - at.kvh * head);
+      at.unit = y - at.kvh * head - seqs[b].before(at.item);
+      return at;
+    }
+    return at;
+  };
+  for (uint32_t w = 0; w < plan.blocks; ++w) {
+    Spot at = spot(w);
+    if (at.b < 0) continue;
+    uint32_t todo = sh.first(w + 1) - sh.first(w);
+    int64_t pieces = 0;
+    for (int seg = 0;; ++seg) {
+      const PagedSeq& s = seqs[at.b];
+      check(at.kvh >= 0 && at.kvh < a.kv_heads && at.item >= 0 && at.item < s.items, "a worker's item");
+      const int tiles = s.tiles(at.item, a);
+      const uint32_t cost = s.cost(at.item), take = std::min(todo, cost - at.unit);
+      check(at.unit < cost && take > 0, "a worker goes on");
+      if (at.unit >= cost || !take || ++pieces > 1 << 20) break;
+      const int t0 = PagedSeq::tile_at(at.unit, tiles, cost), t1 = PagedSeq::tile_at(at.unit + take, tiles, cost);
+      check(0 <= t0 && t0 <= t1 && t1 <= (s.len + kPagedTile - 1) / kPagedTile, "a piece's tiles");
+      check(take == cost || (a.workers && 2 * w + (seg > 0) < 2 * static_cast<uint32_t>(a.workers)), "a piece's slot");
+      todo -= take;
+      at.unit = 0;
+      if (!todo) break;
+      if (++at.item < s.items) continue;
+      at.item = 0;
+      if (++at.kvh < a.kv_heads) continue;
+      at.kvh = 0;
+      do ++at.b;
+      while (at.b < a.batch && seqs[at.b].items == 0);
+      if (at.b >= a.batch) break;
+    }
+  }
+  for (uint32_t j = 0; a.workers && j + 1 < static_cast<uint32_t>(a.workers); ++j) {
+    const Spot at = spot(j + 1);
+    const uint32_t start = sh.first(j + 1) - at.unit;
+    if (at.b < 0 || at.unit == 0 || sh.first(j) > start) continue;
+    const uint32_t w1 = std::min(sh.worker_of(start + seqs[at.b].cost(at.item) - 1), sh.workers - 1);
+    check(w1 < static_cast<uint32_t>(a.workers) && at.item < seqs[at.b].items, "slots that are joined");
+  }
+}
+
+}  // namespace
 
 mssa_status fail(mssa_status s, const char* msg) noexcept {
   g_error = msg;
@@ -124,6 +279,10 @@ hipError_t launch_paged_append(const AppendArgs& a, hipStream_t) {
     if (c0 < 2 * hu && c1 < 2 * hu) ++chunks[c0], ++chunks[c1];
   }
   check(std::all_of(chunks.begin(), chunks.end(), [](int n) { return n == 1; }), "every chunk of a head once");
+  if (g_odd) {
+    rows_inside(a.chunk_begin, a.batch, a.tokens);
+    for (int32_t row = a.token0; row < a.token1; ++row) find_row(a, row);
+  }
   return hipSuccess;
 }
 
@@ -146,6 +305,10 @@ hipError_t launch_paged_attention(const PagedAttnArgs& a, const PagedAttnPlan& p
     check_range(a.partial, slots * (d + 2) * 4, "workspace");
   }
   if (!g_walk) return hipSuccess;
+  if (g_odd) {
+    odd_shares(a, plan);
+    return hipSuccess;
+  }
 
   // The shares, as find_share and next_item see them.
   std::vector<PagedSeq> seqs;
@@ -285,6 +448,7 @@ hipError_t launch_adapter_project(const AdapterArgs& a, const AdapterPlan& plan,
               plan.low_across == (cols + plan.low_columns - 1) / plan.low_columns, "the low-rank factor's columns");
     check(plan.low_rows == kLowRows ? plan.low_tiles * 1024 < int64_t{1} << 32 : plan.low_tiles * plan.low_across * 256 < int64_t{1} << 32,
           "threads of the low-rank factor's launch");
+    if (g_odd) odd_segments(a, plan);
   }
   return hipSuccess;
 }
@@ -302,6 +466,9 @@ void lengths(int batch, int64_t tokens, bool odd) {
   std::sort(g_begin.begin(), g_begin.end());
   if (odd && batch > 1) g_begin[pick(0, batch)] = static_cast<int32_t>(pick(-5, tokens + 5));  // may decrease: clamped
   g_len.assign(batch, 0);
+  if (g_odd)
+    for (int32_t& r : g_begin)
+      if (!pick(0, 3)) r = static_cast<int32_t>(pick(0, 3) ? pick(-5, tokens + 5) : pick(0, 1) ? 0x7fffffff : -0x7fffffff - 1);
 }
 
 void attend(int64_t tokens, int batch, int max_chunk, int q_heads, int kv_heads, int d, int page, int table, int mask, int most) {
@@ -402,6 +569,11 @@ void project(int64_t rows, int k, int n, int parts, int segments, int adapters, 
   void* ws = dev_alloc(bytes - (g_plant ? 256 : 0));
   void* y[8];
   for (int p = 0; p < parts; ++p) y[p] = dev_alloc(rows * (n / parts) * 2);
+  if (g_odd) {
+    lengths(segments, rows, true);
+    seg = g_begin.data();
+    g_bufs.push_back({reinterpret_cast<uintptr_t>(seg), reinterpret_cast<uintptr_t>(seg) + g_begin.size() * 4});
+  }
   check(mssa_adapter_project(&desc, x, w, bias, static_cast<int32_t*>(seg), static_cast<int32_t*>(which), a, b, nullptr, ws, bytes, y,
                              nullptr) == MSSA_OK, g_error.c_str());
 }
@@ -410,6 +582,7 @@ void project(int64_t rows, int k, int n, int parts, int segments, int adapters, 
 
 int main(int argc, char** argv) {
   g_plant = argc > 1 && !std::strcmp(argv[1], "plant");
+  g_odd = argc > 1 && !std::strcmp(argv[1], "odd");
   // quotients, at the numbers where they change and at the ends
   for (int i = 0; i < 4000; ++i) {
     const uint32_t d = static_cast<uint32_t>(i < 200 ? i + 1 : pick(1, i < 2000 ? 1 << 20 : 0x7fffffff));
@@ -435,7 +608,7 @@ int main(int argc, char** argv) {
     append(pick(1, 3000), static_cast<int>(pick(1, 100)), static_cast<int>(pick(0, 12)), static_cast<int>(pick(1, 12)), d,
            static_cast<int>(pick(1, 300)), halves ? 16 * static_cast<int>(pick(0, d / 16)) : 2 * static_cast<int>(pick(0, d / 2)), halves);
   }
-  append((int64_t{1} << 30), 3, 1, 1, 16, 16, 16, 0);  // made in slices
+  if (!g_odd) append((int64_t{1} << 30), 3, 1, 1, 16, 16, 16, 0);  // made in slices
   for (int i = 0; i < 400; ++i) {
     const int parts = static_cast<int>(pick(1, 4)), k = static_cast<int>(pick(0, 1) ? 8 * pick(1, 700) : pick(1, 3000));
     project(pick(0, 2) ? pick(1, 200) : pick(1, 30000), k, parts * static_cast<int>(pick(1, 3000)), parts, static_cast<int>(pick(0, 50)),
