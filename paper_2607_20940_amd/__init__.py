@@ -5,4 +5,4 @@
 nothing; importing ``.mssa`` loads the library and fails loudly if it is
 missing.
 """
-__all__ = ["inputs", "workloads", "mssa", "streaming", "lowbit"]
+__all__ = ["inputs", "workloads", "mssa", "streaming", "lowbit", "paged"]

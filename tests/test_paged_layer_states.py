@@ -135,3 +135,9 @@ def test_tensors_of_another_device_are_refused(monkeypatch):
     assert calls == []
     p.layer_pass(0, *given, stream=0)
     assert len(calls) == 3
+
+
+def test_the_package_names_the_module():
+    import paper_2607_20940_amd
+
+    assert "paged" in paper_2607_20940_amd.__all__
