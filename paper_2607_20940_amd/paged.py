@@ -48,6 +48,7 @@ class PagedStreams:
         self.k_pages, self.v_pages = ([torch.zeros(pool, dtype=torch.bfloat16, device=device) for _ in range(self.layers)]
                                       for _ in range(2))
         self.qkv, self.q = buf(self.max_tokens, self.width), buf(self.max_tokens, self.q_heads, self.head_dim)
+        self.new = self.qkv, self.qkv[:, self.q_width:], self.qkv[:, self.q_width + self.kv_width:]  # q, k, v of new tokens
         self.free = list(range(self.pages))[::-1]
         self.streams = {}  # id -> [pages, tokens held, tokens dropped before them, adapter]
         self.weights = [None] * self.layers
@@ -215,8 +216,7 @@ class PagedStreams:
                     v.record_stream(used)
         mssa.mssa_adapter_project(self.project, x, w, bias, self.chunk_begin, self.adapter, a, b, scale, self.workspace, [qkv],
                                   stream=stream)
-        q, k, v = qkv, qkv[:, self.q_width:], qkv[:, self.q_width + self.kv_width:]
-        mssa.mssa_paged_append(self.append, q, k, v, self.chunk_begin, self.kv_len, self.table,
+        mssa.mssa_paged_append(self.append, *self.new, self.chunk_begin, self.kv_len, self.table,
                                self.positions if positions is None else positions, self.freqs, self.q, self.k_pages[layer],
                                self.v_pages[layer], stream=stream)
         mssa.mssa_paged_attention(self.attend, self.q, self.k_pages[layer], self.v_pages[layer], self.chunk_begin, self.kv_len,
