@@ -622,9 +622,13 @@ mssa_status mssa_mx_attention(const mssa_mx_attention_desc* desc, const void* q,
  *     several tables (a shared beginning), but nothing may be appended to a
  *     cache index that two sequences share: which one stays is not defined.
  * Values on the device are not known to the host: they are clamped to what the
- * tensors hold, so that no value of them leads outside. */
+ * tensors hold, so that no value of them leads outside; what comes out for rows
+ * where boundaries decrease is not defined. */
 
-/* Shared projection with low-rank adapters. */
+/* Shared projection with low-rank adapters.  Parts are equally wide, each with
+ * a first factor of its own.  Grouped heads' q, k and v are not: they are one
+ * part, and separate first factors are stacked behind one another, the rank
+ * their sum, with zeros in b where a feature does not take a factor's columns. */
 typedef struct {
   int64_t rows;           /* tokens, 0..2^30 */
   int32_t in_features;    /* 1..2^20 */
@@ -730,7 +734,9 @@ mssa_status mssa_paged_attention_workspace_size(const mssa_paged_attention_desc*
  *   lse          [q_heads, tokens] (lse_stride) natural log of the sum of
  *                exp(scale q k) over all keys, or NULL
  * A query with no keys at all has out = 0 and lse = -inf.  What pages hold at
- * indices that a query does not see is not used, whatever it is. */
+ * indices that a query does not see is not used, whatever it is.  Scores, sums
+ * and lse are fp32; the exponentials are rounded to bf16 for their product with
+ * v (the sum that divides it is not), and out once more. */
 mssa_status mssa_paged_attention(const mssa_paged_attention_desc* desc, const void* q, const void* k_pages,
                                  const void* v_pages, const int32_t* chunk_begin, const int32_t* kv_len,
                                  const int32_t* page_table, const void* prior_out, const float* prior_lse,

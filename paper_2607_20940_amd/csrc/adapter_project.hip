@@ -2,7 +2,7 @@
 // (mssa_adapter_project): y = x W^T + bias + scale (x A^T) B^T.
 //
 // Two launches: the low-rank factor u = scale (x A^T) of every row, rounded to
-// bf16 (an operand of the second product; it adds up to 2^-9 of the adapter's
+// bf16 (an operand of the second product; it adds up to 2^-8 of the adapter's
 // share, which fp32 operands would spare at a sixteenth of the rate), then the
 // product, whose tiles add u B^T of the segments that they hold to the sums in
 // their registers before the one rounding of the output.  A tile's rows can belong
@@ -189,8 +189,8 @@ __global__ __launch_bounds__(kLowWaves * 64) void low_kernel(AdapterArgs a) {
 // block, two by two waves of 32 rows and NB x 16 columns.  The contraction comes
 // in 64-deep stages of 128-byte rows through four LDS buffers, three of them on
 // their way.  Bound by the latency of that chain and by X's bytes: 12870 rows of
-// 1536, 96 columns, 15 to 19 us; 27840 of 5120, 192 columns, 127 us: 285 MB, which
-// two blocks each read.
+// 1536, 96 columns, 20 us; 27840 of 5120, 192 columns, 130 us: 285 MB, which two
+// blocks each read.
 constexpr int kLowTileRows = kLowManyRows, kLowStages = 4;
 
 template <int NB>
@@ -484,9 +484,9 @@ __global__ __launch_bounds__(512) void few_any_kernel(AdapterArgs a) {
 // Tiles are taken in panels of four feature tiles, each XCD a run of them.
 // The outputs leave through LDS as whole-row 16-byte stores.
 // Bound by the stages' way into LDS and the outputs': 27840 x 5120 -> 15360 takes
-// 3.9 ms, 1.12 PFLOP/s (a large product reaches 1.2); 12870 x 1536 -> 4608 takes 200 us, 0.91
-// PFLOP/s, the matrix cores busy 42 % of the time: 918 tiles are 3.6 rounds, each
-// with 24 stages, a start and 118 MB / 918 of outputs.
+// 4.0 ms, 1.1 PFLOP/s (a large product reaches 1.2); 12870 x 1536 -> 4608 takes 205 to 220
+// us, 0.85 PFLOP/s, the matrix cores busy 42 % of the time: 918 tiles are 3.6 rounds,
+// each with 24 stages, a start and 118 MB / 918 of outputs.
 constexpr int kBK = 64, kPanel = 4;
 
 template <int WM, int WN, int MB, int NB, int KG, int kStages>

@@ -48,19 +48,6 @@ __device__ inline Joined join(bool has_prior, float m, float l, float prior_lse)
   return {any ? wo / (l * w) : 0.f, wp / w, (top + __builtin_amdgcn_logf(w)) * kLn2};
 }
 
-// Order of a run of NM matrix instructions and their ND LDS reads: LEAD reads
-// first, then a matrix instruction and its share of reads in turn.
-template <int NM, int ND, int LEAD>
-__device__ inline void interleave() {
-  __builtin_amdgcn_sched_group_barrier(0x100, LEAD, 0);
-#pragma unroll
-  for (int i = 0; i < (ND - LEAD) / (ND / NM); ++i) {
-    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-    __builtin_amdgcn_sched_group_barrier(0x100, ND / NM, 0);
-  }
-  __builtin_amdgcn_sched_group_barrier(0x008, NM - (ND - LEAD) / (ND / NM), 0);
-}
-
 // Combine over the four lanes that hold one query row (lane % 16).
 template <class Op>
 __device__ inline float over_row(float v, Op op) {

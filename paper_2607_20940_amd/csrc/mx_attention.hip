@@ -175,6 +175,19 @@ __device__ inline auto load_codes(__amdgpu_buffer_rsrc_t r, uint32_t off) {
     return __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0);
 }
 
+// Order of a run of NM matrix instructions and their ND LDS reads: LEAD reads
+// first, then a matrix instruction and its share of reads in turn.
+template <int NM, int ND, int LEAD>
+__device__ inline void interleave() {
+  __builtin_amdgcn_sched_group_barrier(0x100, LEAD, 0);
+#pragma unroll
+  for (int i = 0; i < (ND - LEAD) / (ND / NM); ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, ND / NM, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x008, NM - (ND - LEAD) / (ND / NM), 0);
+}
+
 // Many rows.  A wave's tile is two phases: matrix instructions (O += V^T P of
 // the tile before, then S = K Q^T), and vector work (softmax, and expanding
 // the next tile's codes).  Eight waves are two groups, one wave of each per

@@ -43,7 +43,7 @@ hipError_t plan_paged_attention(int64_t tokens, int32_t batch, int32_t max_chunk
   p.least = static_cast<int32_t>(least << p.unit_shift);
   p.blocks = p.workers ? p.workers : items;
   if (!launchable(p.blocks, p.threads())) return hipErrorInvalidValue;
-  // few items are in many slots each: a block takes one row of them, else eight
+  // few items are in many slots each: a block takes one row of them, else 16
   p.join_rows = p.waves || p.workers <= 16 * items ? 16 : 1;
   p.workspace_bytes = int64_t{2} * p.workers * p.slot_rows * (head_dim + 2) * 4;
   *plan = p;

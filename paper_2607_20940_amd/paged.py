@@ -11,6 +11,10 @@ to the device.  Then every layer runs ``layer_pass``, on the caller's stream:
    joined with an attention over other keys (a window's, a sink's).
 
 All layers share one page table: a page holds a stream's tokens in every layer.
+They also share buffers and a workspace: passes on several HIP streams have to
+wait for one another.  An adapter is one pair of factors over q, k and v together;
+where those have first factors of their own, they are stacked behind one another
+(three times the rank), with zeros in b where a feature does not take a factor.
 This module only keeps the table and sequences library calls (torch owns the
 buffers); all arithmetic runs in the library.
 """
